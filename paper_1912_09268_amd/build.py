@@ -1,5 +1,5 @@
-"""Compiles the HIP/C++ sources under csrc/ into libmgwfbp.so and the extension module _calls next to this file,
-and the benchmark's measurement aid under bench_aid/ into its own shared object there (gfx950 only)."""
+"""Compiles the HIP/C++ sources under csrc/ into libmgwfbp.so, libmgwfbp_layers.so and the extension module _calls next to this
+file, and the benchmark's measurement aid under bench_aid/ into its own shared object there (gfx950 only)."""
 from __future__ import annotations
 
 import os
@@ -13,6 +13,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB_NAME = "libmgwfbp.so"
 SOURCES = ("plan.cpp", "model.cpp", "layout.cpp", "kernels.hip")
+LAYERS_NAME = "libmgwfbp_layers.so"
+LAYERS_SOURCES = ("embed.hip", "act8.hip", "act_linear.hip")
 AID_DIR = os.path.join(ROOT, "bench_aid")
 AID_LIB = os.path.join(AID_DIR, "libmgwfbp_bench_aid.so")
 
@@ -50,6 +52,22 @@ def build_library(out: Optional[str] = None, defines: Optional[Dict[str, object]
     return out
 
 
+def build_layers(out: Optional[str] = None, verbose: bool = False) -> str:
+    """The operators that make per-layer gradients (include/mgwfbp_layers.h).  Always recompiles."""
+    hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+    out = out or os.path.join(HERE, LAYERS_NAME)
+    cmd = [hipcc] + HIPCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-x", "hip"]
+    cmd += [os.path.join(CSRC, s) for s in LAYERS_SOURCES] + ["-o", out]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{res.stdout}")
+    if verbose and res.stdout.strip():
+        print(res.stdout)
+    return out
+
+
 def build_calls() -> str:
     """The extension module with the device calls of Context: host code only, no link to the library."""
     out = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
@@ -75,5 +93,6 @@ def build_bench_aid(verbose: bool = False) -> str:
 
 if __name__ == "__main__":  # python -m paper_1912_09268_amd.build
     print(build_library(verbose=True))
+    print(build_layers(verbose=True))
     print(build_bench_aid(verbose=True))
     print(build_calls())

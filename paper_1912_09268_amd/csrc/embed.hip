@@ -1,0 +1,585 @@
+// Embedding lookup with scaling, and its gradient.
+//
+//   mgwfbp_embed        out[t,:] = sum over tables k, in order, of scale_k * table_k[id_k[t], :]
+//   mgwfbp_embed_grad   grad[r,:] = scale * sum over the tokens t with id[t] = r of dy[t,:]   (+ grad[r,:])
+//
+// Sums are binary32 and rounded once.  An id outside the table stands for no row.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "device_types.h"
+#include "mgwfbp_layers.h"
+
+namespace {
+
+using namespace ops;
+
+thread_local int g_last_hip_error = 0;
+
+constexpr int THREADS = 256;
+constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_DIM = int64_t(1) << 23;
+
+// ---------------------------------------------------------------------------------------------
+// lookup
+// ---------------------------------------------------------------------------------------------
+
+struct Table {
+    const void* rows;
+    const void* ids;
+    int64_t n_rows, stride;
+    float scale;
+    int32_t id_type;
+};
+struct EmbedArgs {
+    Table table[MGWFBP_MAX_TABLES];
+    void* out;
+    int64_t out_stride, tokens, dim;
+    uint32_t vecs;             // vectors of a row
+    uint32_t page;             // tokens per blockIdx.y, so that a page's vectors are counted in 32 bits
+};
+
+__device__ __forceinline__ int64_t id_at(const void* ids, int32_t id_type, int64_t t) {
+    return id_type == MGWFBP_I64 ? static_cast<const int64_t*>(ids)[t] : static_cast<const int32_t*>(ids)[t];
+}
+
+// One lane for eight columns of a token.  Lanes run over the vectors of a token and on into the next token, so that
+// narrow tables fill wavefronts too.
+template <typename TabT, typename OutT, int K>
+__global__ __launch_bounds__(THREADS) void embed_kernel(EmbedArgs A) {
+    const uint32_t at = blockIdx.x * THREADS + threadIdx.x;
+    const uint32_t in_page = at / A.vecs, v = at - in_page * A.vecs;
+    const int64_t t = static_cast<int64_t>(blockIdx.y) * A.page + in_page;
+    if (in_page >= A.page || t >= A.tokens) return;
+    const int64_t col = static_cast<int64_t>(v) * VEC;
+    const int n = static_cast<int>(min(A.dim - col, static_cast<int64_t>(VEC)));
+    int64_t id[K];
+    bool here[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        id[k] = id_at(A.table[k].ids, A.table[k].id_type, t);
+        here[k] = static_cast<uint64_t>(id[k]) < static_cast<uint64_t>(A.table[k].n_rows);
+    }
+    Raw8<TabT> row[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        row[k] = load8(static_cast<const TabT*>(A.table[k].rows) + (here[k] ? id[k] : 0) * A.table[k].stride + col, here[k] ? n : 0);
+    float sum[VEC] = {};
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float x = here[k] ? A.table[k].scale * get(row[k], i) : 0.f;
+            sum[i] = k == 0 ? x : sum[i] + x;
+        }
+    store8(static_cast<OutT*>(A.out) + t * A.out_stride + col, sum, n);
+}
+
+// ---------------------------------------------------------------------------------------------
+// gradient
+// ---------------------------------------------------------------------------------------------
+//
+// 1. Tokens are ordered by (row, token).  Up to RANKED_TOKENS tokens a token's place is the number of tokens before it,
+//    counted by comparing it with every other one (rank_kernel): one launch, no dependence between workgroups.  Beyond that,
+//    a radix sort by 8 bits at a time.  Tokens without a row come last.
+// 2. The ordered tokens are cut into chunks of a fixed length; lanes sum a chunk's stretches of one row each
+//    (sum_kernel).  A stretch that is all of its row's tokens is written to the gradient, any other to the workspace.
+// 3. Rows of several chunks are joined, in order (join_kernel).
+//
+// The order of every sum follows from the ids alone: the same call gives the same bits.
+
+struct GradArgs {
+    const void* ids;
+    const void* dy;
+    void* grad;
+    int64_t dy_stride, grad_stride, n_rows, dim, padding_row;
+    int64_t tokens;
+    uint32_t* order;           // [tokens] token at a place of the order
+    int32_t* row;              // [tokens] its row, n_rows if it has none
+    float* partial;            // [2 * chunks][dim_padded]: a chunk's first and its last stretch
+    uint8_t* present;          // [n_rows] rows with tokens; null where every row is cleared beforehand
+    uint32_t* other_order;     // radix sort: the other side of a pass, and the counts of every workgroup
+    int32_t* other_row;
+    uint32_t* counts;          // [blocks][256]
+    int64_t dim_padded;
+    float scale;
+    int32_t id_type, accumulate;
+    uint32_t chunk, chunks;    // tokens per chunk, number of chunks
+    uint32_t vecs, page;       // vectors of a row; chunks per blockIdx.y
+    uint32_t work_blocks;      // workgroups that rank or sum; the rest clear rows
+    uint32_t items, shift, from_ids;   // radix sort: tokens per workgroup, first bit of the digit, first pass
+};
+
+__device__ __forceinline__ int32_t row_of(const GradArgs& A, int64_t t) {
+    const int64_t id = id_at(A.ids, A.id_type, t);
+    return static_cast<uint64_t>(id) < static_cast<uint64_t>(A.n_rows) && id != A.padding_row ? static_cast<int32_t>(id)
+                                                                                              : static_cast<int32_t>(A.n_rows);
+}
+
+// Clears rows of the gradient, `count` of them at a time: workgroup `b` of `blocks`.  Only rows without tokens where
+// A.present says which these are.
+template <typename GradT> __device__ void clear_rows(const GradArgs& A, uint32_t b, uint32_t blocks) {
+    const float zeros[VEC] = {};
+    if (A.present == nullptr && A.grad_stride == A.dim) {
+        const int64_t total = A.n_rows * A.dim;
+        GradT* const g = static_cast<GradT*>(A.grad);
+        for (int64_t at = (static_cast<int64_t>(b) * THREADS + threadIdx.x) * VEC; at < total;
+             at += static_cast<int64_t>(blocks) * THREADS * VEC)
+            store8(g + at, zeros, static_cast<int>(min(total - at, static_cast<int64_t>(VEC))));
+        return;
+    }
+    // a wavefront per row
+    const int lane = threadIdx.x % 64;
+    for (int64_t r = static_cast<int64_t>(b) * (THREADS / 64) + threadIdx.x / 64; r < A.n_rows;
+         r += static_cast<int64_t>(blocks) * (THREADS / 64)) {
+        if (A.present != nullptr && A.present[r] != 0) continue;
+        GradT* const g = static_cast<GradT*>(A.grad) + r * A.grad_stride;
+        for (int64_t col = lane * VEC; col < A.dim; col += 64 * VEC)
+            store8(g + col, zeros, static_cast<int>(min(A.dim - col, static_cast<int64_t>(VEC))));
+    }
+}
+
+constexpr int RANK_EACH = 16;              // tokens that a workgroup ranks
+constexpr int64_t RANKED_TOKENS = 8192;
+
+// The place of a token is the number of pairs (row, token) below its own.  A wavefront compares 64 others at a time with
+// each of the workgroup's tokens; a comparison is one vector instruction and the count of its mask two scalar ones.
+// The workgroups behind those that rank clear the gradient.
+template <typename GradT> __global__ __launch_bounds__(THREADS) void rank_kernel(GradArgs A) {
+    if (blockIdx.x >= A.work_blocks) {
+        clear_rows<GradT>(A, blockIdx.x - A.work_blocks, gridDim.x - A.work_blocks);
+        return;
+    }
+    __shared__ uint32_t below[THREADS / 64][RANK_EACH];
+    const uint32_t n = static_cast<uint32_t>(A.tokens);
+    const uint32_t first = blockIdx.x * RANK_EACH;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    uint64_t own[RANK_EACH];
+    uint32_t count[RANK_EACH];
+#pragma unroll
+    for (int r = 0; r < RANK_EACH; ++r) {
+        const uint32_t t = min(first + r, n - 1);
+        own[r] = static_cast<uint64_t>(static_cast<uint32_t>(row_of(A, t))) << 32 | t;
+        count[r] = 0;
+    }
+    for (uint32_t s0 = wave * 64; s0 < n; s0 += THREADS) {
+        const uint32_t s = s0 + lane;
+        const uint64_t key = s < n ? static_cast<uint64_t>(static_cast<uint32_t>(row_of(A, s))) << 32 | s : ~uint64_t(0);
+#pragma unroll
+        for (int r = 0; r < RANK_EACH; ++r) count[r] += __popcll(__ballot(key < own[r]));
+    }
+    if (lane == 0)
+#pragma unroll
+        for (int r = 0; r < RANK_EACH; ++r) below[wave][r] = count[r];
+    __syncthreads();
+    const uint32_t t = first + threadIdx.x;
+    if (threadIdx.x < RANK_EACH && t < n) {
+        uint32_t place = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) place += below[w][threadIdx.x];
+        A.order[place] = t;
+        A.row[place] = row_of(A, t);
+    }
+}
+
+// ---- radix sort: a pass orders by one digit of the row and keeps the order of equal digits ----
+constexpr int DIGITS = 256;
+constexpr int WAVES = THREADS / 64;
+
+__device__ __forceinline__ int32_t sort_row(const GradArgs& A, int64_t at) { return A.from_ids ? row_of(A, at) : A.other_row[at]; }
+
+// How often each digit occurs among a workgroup's tokens.  The first pass clears the marks of rows with tokens.
+__global__ __launch_bounds__(THREADS) void digit_kernel(GradArgs A) {
+    __shared__ uint32_t count[DIGITS];
+    count[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * A.items, end = min(first + A.items, A.tokens);
+    for (int64_t at = first + threadIdx.x; at < end; at += THREADS)
+        atomicAdd(&count[(static_cast<uint32_t>(sort_row(A, at)) >> A.shift) % DIGITS], 1u);
+    if (A.from_ids && A.present != nullptr)
+        for (int64_t r = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; r < A.n_rows; r += static_cast<int64_t>(gridDim.x) * THREADS)
+            A.present[r] = 0;
+    __syncthreads();
+    A.counts[static_cast<int64_t>(blockIdx.x) * DIGITS + threadIdx.x] = count[threadIdx.x];
+}
+
+// Moves a workgroup's tokens to their places: behind every smaller digit, behind the same digit of the workgroups and
+// wavefronts before, in order within the wavefront.
+__global__ __launch_bounds__(THREADS) void move_kernel(GradArgs A) {
+    __shared__ uint32_t scan[DIGITS];
+    __shared__ uint32_t place[WAVES][DIGITS];
+    const uint32_t d = threadIdx.x, lane = d % 64, wave = d / 64;
+    uint32_t before = 0, all = 0;
+    for (uint32_t b = 0; b < gridDim.x; ++b) {
+        const uint32_t c = A.counts[static_cast<int64_t>(b) * DIGITS + d];
+        before += b < blockIdx.x ? c : 0;
+        all += c;
+    }
+    scan[d] = all;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) place[w][d] = 0;
+    __syncthreads();
+    for (uint32_t step = 1; step < DIGITS; step *= 2) {
+        const uint32_t add = d >= step ? scan[d - step] : 0;
+        __syncthreads();
+        scan[d] += add;
+        __syncthreads();
+    }
+    const int64_t part = A.items / WAVES;                    // a multiple of 64
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * A.items + wave * part, end = min(first + part, A.tokens);
+    for (int64_t at = first + lane; at < end; at += 64)
+        atomicAdd(&place[wave][(static_cast<uint32_t>(sort_row(A, at)) >> A.shift) % DIGITS], 1u);
+    __syncthreads();
+    uint32_t next = scan[d] - all + before;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const uint32_t c = place[w][d];
+        place[w][d] = next;
+        next += c;
+    }
+    __syncthreads();
+    for (int64_t at0 = first; at0 < end; at0 += 64) {        // the same number of turns for every lane of the wavefront
+        const int64_t at = at0 + lane;
+        const bool here = at < end;
+        const int32_t r = here ? sort_row(A, at) : 0;
+        const uint32_t digit = (static_cast<uint32_t>(r) >> A.shift) % DIGITS;
+        uint64_t same = __ballot(here);
+#pragma unroll
+        for (int bit = 0; bit < 8; ++bit) {
+            const bool set = (digit >> bit & 1) != 0;
+            const uint64_t mask = __ballot(set);
+            same &= set ? mask : ~mask;
+        }
+        if (here) {
+            const uint32_t ahead = __popcll(same & ((uint64_t(1) << lane) - 1));
+            const uint32_t to = place[wave][digit] + ahead;
+            A.order[to] = A.from_ids ? static_cast<uint32_t>(at) : A.other_order[at];
+            A.row[to] = r;
+            if (A.from_ids && A.present != nullptr && r < A.n_rows) A.present[r] = 1;
+        }
+        // the places are read by lanes that others have written for: no barrier between the lanes of a wavefront, but an order
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (here && (same >> lane) == 1) place[wave][digit] += __popcll(same);      // the last lane of each digit
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// ---- sums ----
+
+template <typename GradT> __device__ __forceinline__ void write_row(const GradArgs& A, int32_t r, int64_t col, int n, float (&sum)[VEC]) {
+    GradT* const g = static_cast<GradT*>(A.grad) + r * A.grad_stride + col;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sum[i] *= A.scale;
+    if (A.accumulate) {
+        const Raw8<GradT> had = load8(g, n);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum[i] += get(had, i);
+    }
+    store8(g, sum, n);
+}
+
+__device__ __forceinline__ void write_partial(const GradArgs& A, uint32_t which, int64_t col, const float (&sum)[VEC]) {
+    float* const p = A.partial + which * A.dim_padded + col;
+    *reinterpret_cast<f32x4*>(p) = f32x4{sum[0], sum[1], sum[2], sum[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+}
+
+// One lane for eight columns of a chunk.
+template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) void sum_kernel(GradArgs A) {
+    if (blockIdx.x >= A.work_blocks) {
+        if (blockIdx.y == 0) clear_rows<GradT>(A, blockIdx.x - A.work_blocks, gridDim.x - A.work_blocks);
+        return;
+    }
+    const uint32_t at = blockIdx.x * THREADS + threadIdx.x;
+    const uint32_t in_page = at / A.vecs, v = at - in_page * A.vecs;
+    const uint32_t c = blockIdx.y * A.page + in_page;
+    if (in_page >= A.page || c >= A.chunks) return;
+    const int64_t col = static_cast<int64_t>(v) * VEC;
+    const int n = static_cast<int>(min(A.dim - col, static_cast<int64_t>(VEC)));
+    const int64_t first = static_cast<int64_t>(c) * A.chunk, end = min(first + A.chunk, A.tokens);
+    const DyT* const dy = static_cast<const DyT*>(A.dy) + col;
+    const int32_t none = static_cast<int32_t>(A.n_rows);
+    const int32_t row_before = first > 0 ? A.row[first - 1] : none;
+    const int32_t row_after = end < A.tokens ? A.row[end] : none;
+    constexpr int AHEAD = 8;
+    float sum[VEC] = {};
+    int32_t current = A.row[first];
+    bool from_start = true;                                     // the current stretch began with the chunk
+    for (int64_t p0 = first; p0 < end && current != none; p0 += AHEAD) {
+        Raw8<DyT> x[AHEAD];
+        int32_t r[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int64_t p = min(p0 + j, end - 1);
+            r[j] = p0 + j < end ? A.row[p] : none;
+            x[j] = load8(dy + static_cast<int64_t>(A.order[p]) * A.dy_stride, n);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (r[j] != current) {
+                if (current != none) {                          // a stretch ends inside the chunk
+                    if (from_start && current == row_before) write_partial(A, 2 * c, col, sum);
+                    else if (p0 + j < end || current != row_after) write_row<GradT>(A, current, col, n, sum);
+                    else write_partial(A, 2 * c + 1, col, sum);
+                    from_start = false;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
+                }
+                current = r[j];
+            }
+            if (r[j] != none)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum[i] += get(x[j], i);
+        }
+    }
+    if (current != none) {                                      // it ends with the chunk
+        if (from_start && current == row_before) write_partial(A, 2 * c, col, sum);
+        else if (current != row_after) write_row<GradT>(A, current, col, n, sum);
+        else write_partial(A, 2 * c + 1, col, sum);
+    }
+}
+
+constexpr int JOIN_WAVES = 16, JOIN_COLS = 256;
+
+// A row whose tokens reach over several chunks, by the workgroup of the chunk it begins in: wavefront w adds the stretches
+// w, w + 16, ..., then the sixteen sums are added in order.
+template <typename GradT> __global__ __launch_bounds__(JOIN_WAVES * 64) void join_kernel(GradArgs A) {
+    const uint32_t c = blockIdx.x;
+    const int64_t end = static_cast<int64_t>(c + 1) * A.chunk, first = end - A.chunk;
+    if (end >= A.tokens) return;
+    const int32_t r = A.row[end - 1];
+    if (r == static_cast<int32_t>(A.n_rows) || A.row[end] != r) return;
+    if (A.row[first] == r && first > 0 && A.row[first - 1] == r) return;        // begins in an earlier chunk
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    // chunks that it covers whole, behind this one
+    uint32_t whole = 0;
+    for (;;) {
+        const uint32_t q = c + 1 + whole + lane;
+        const bool covers = q < A.chunks && static_cast<int64_t>(q + 1) * A.chunk <= A.tokens && A.row[static_cast<int64_t>(q + 1) * A.chunk - 1] == r;
+        const uint64_t mask = __ballot(covers);
+        if (~mask != 0) {
+            whole += __builtin_ctzll(~mask);
+            break;
+        }
+        whole += 64;
+    }
+    const int64_t next = static_cast<int64_t>(c + 1 + whole) * A.chunk;
+    const uint32_t pieces = 1 + whole + (next < A.tokens && A.row[next] == r ? 1 : 0);
+    __shared__ f32x4 sums[JOIN_WAVES][64];
+    const int64_t col = (static_cast<int64_t>(blockIdx.y) * 64 + lane) * 4;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (col < A.dim)
+#pragma unroll 4
+        for (uint32_t i = wave; i < pieces; i += JOIN_WAVES) {
+            const int64_t which = i == 0 ? 2 * static_cast<int64_t>(c) + 1 : 2 * static_cast<int64_t>(c + i);
+            sum += *reinterpret_cast<const f32x4*>(A.partial + which * A.dim_padded + col);
+        }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || col >= A.dim) return;
+    for (uint32_t w = 1; w < JOIN_WAVES; ++w) sum += sums[w][lane];
+    GradT* const g = static_cast<GradT*>(A.grad) + r * A.grad_stride + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (col + i < A.dim) {
+            float x = sum[i] * A.scale;
+            if (A.accumulate) x += static_cast<float>(g[i]);
+            g[i] = rounded<GradT>(x);
+        }
+}
+
+// ---- host side ----
+
+struct GradPlan {
+    bool ranked;
+    uint32_t chunk, chunks, blocks, items;
+    int64_t dim_padded;
+    int64_t order, row, partial, present, other_order, other_row, counts, bytes;     // places in the workspace
+};
+
+// What is in the workspace, and where: every part begins on 256 bytes.
+GradPlan plan_of(int64_t tokens, int64_t n_rows, int64_t dim) {
+    GradPlan p{};
+    p.ranked = tokens <= RANKED_TOKENS;
+    p.chunk = p.ranked ? 8 : 32;
+    p.chunks = static_cast<uint32_t>(ceil_div(tokens, p.chunk));
+    p.dim_padded = ceil_div(dim, VEC) * VEC;
+    // radix sort: at most 256 workgroups, since each adds up the counts of all
+    const int64_t items = std::max<int64_t>(1024, ceil_div(ceil_div(tokens, 256), THREADS) * THREADS);
+    p.items = static_cast<uint32_t>(items);
+    p.blocks = static_cast<uint32_t>(ceil_div(tokens, items));
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += ceil_div(bytes, 256) * 256;
+        return here;
+    };
+    p.order = take(tokens * 4);
+    p.row = take(tokens * 4);
+    p.partial = take(2 * static_cast<int64_t>(p.chunks) * p.dim_padded * 4);
+    if (!p.ranked) {
+        p.present = take(n_rows);
+        p.other_order = take(tokens * 4);
+        p.other_row = take(tokens * 4);
+        p.counts = take(static_cast<int64_t>(p.blocks) * DIGITS * 4);
+    }
+    p.bytes = at;
+    return p;
+}
+
+bool grad_sizes_ok(int64_t n_tokens, int64_t n_rows, int64_t dim) {
+    return n_tokens >= 0 && n_tokens <= MOST_TOKENS && n_rows >= 0 && n_rows < 0x7fffffff && dim >= 0 && dim <= MOST_DIM;
+}
+
+// Workgroups that clear: enough to fill the chip, 32 KiB each at the least.
+uint32_t clear_blocks(int64_t n_rows, int64_t dim, int64_t elem_bytes) {
+    return static_cast<uint32_t>(std::min<int64_t>(4096, std::max<int64_t>(1, n_rows * dim * elem_bytes / 32768)));
+}
+
+}  // namespace
+
+int ops::note(hipError_t e) {
+    if (e == hipSuccess) return MGWFBP_OK;
+    g_last_hip_error = static_cast<int>(e);
+    return MGWFBP_EHIP;
+}
+
+extern "C" {
+
+int mgwfbp_layers_last_hip_error(void) { return g_last_hip_error; }
+
+int mgwfbp_embed(const mgwfbp_table* tables, int32_t n_tables, int32_t table_dtype, int64_t n_tokens, int64_t dim,
+                 void* d_out, int64_t out_stride, int32_t out_dtype, void* hip_stream) {
+    if (tables == nullptr || n_tables < 1 || n_tables > MGWFBP_MAX_TABLES) return MGWFBP_EINVAL;
+    if (!is_dtype(table_dtype) || !is_dtype(out_dtype)) return MGWFBP_EINVAL;
+    if (n_tokens < 0 || n_tokens > MOST_TOKENS || dim < 0 || dim > MOST_DIM) return MGWFBP_EINVAL;
+    if (!is_matrix(n_tokens, dim, out_stride, dtype_bytes(out_dtype))) return MGWFBP_EINVAL;
+    EmbedArgs a{};
+    for (int32_t k = 0; k < n_tables; ++k) {
+        const mgwfbp_table& t = tables[k];
+        if (t.id_type != MGWFBP_I32 && t.id_type != MGWFBP_I64) return MGWFBP_EINVAL;
+        if (!is_matrix(t.n_rows, dim, t.row_stride, dtype_bytes(table_dtype))) return MGWFBP_EINVAL;
+        if (n_tokens > 0 && dim > 0) {
+            if (t.d_ids == nullptr || !is_aligned(t.d_ids, t.id_type == MGWFBP_I64 ? 8 : 4)) return MGWFBP_EINVAL;
+            if (t.n_rows > 0 && (t.d_rows == nullptr || !is_aligned(t.d_rows, dtype_bytes(table_dtype)))) return MGWFBP_EINVAL;
+        }
+        a.table[k] = {t.d_rows, t.d_ids, t.n_rows, t.row_stride, t.scale, t.id_type};
+    }
+    if (n_tokens == 0 || dim == 0) return MGWFBP_OK;
+    if (d_out == nullptr || !is_aligned(d_out, dtype_bytes(out_dtype))) return MGWFBP_EINVAL;
+    a.out = d_out;
+    a.out_stride = out_stride;
+    a.tokens = n_tokens;
+    a.dim = dim;
+    a.vecs = static_cast<uint32_t>(ceil_div(dim, VEC));
+    // pages so long that their vectors number less than 2^31, and at most 65535 of them
+    a.page = static_cast<uint32_t>(std::min<int64_t>(n_tokens, (int64_t(1) << 31) / a.vecs - 1));
+    if (ceil_div(n_tokens, a.page) > 65535) return MGWFBP_EINVAL;
+    const dim3 grid(static_cast<uint32_t>(ceil_div(static_cast<int64_t>(a.page) * a.vecs, THREADS)),
+                    static_cast<uint32_t>(ceil_div(n_tokens, a.page)));
+    return with_dtype(table_dtype, [&](auto* table_type) {
+        return with_dtype(out_dtype, [&](auto* out_type) {
+            typedef std::remove_pointer_t<decltype(table_type)> TabT;
+            typedef std::remove_pointer_t<decltype(out_type)> OutT;
+            void (*kernel)(EmbedArgs) = n_tables == 1 ? embed_kernel<TabT, OutT, 1> : n_tables == 2 ? embed_kernel<TabT, OutT, 2>
+                                      : n_tables == 3 ? embed_kernel<TabT, OutT, 3> : embed_kernel<TabT, OutT, 4>;
+            return launch(kernel, a, grid, dim3(THREADS), hip_stream);
+        });
+    });
+}
+
+int mgwfbp_embed_grad_workspace(int64_t n_tokens, int64_t n_rows, int64_t dim, uint64_t* bytes_out) {
+    if (bytes_out == nullptr || !grad_sizes_ok(n_tokens, n_rows, dim)) return MGWFBP_EINVAL;
+    *bytes_out = static_cast<uint64_t>(plan_of(n_tokens, n_rows, dim).bytes);
+    return MGWFBP_OK;
+}
+
+int mgwfbp_embed_grad(const void* d_ids, int32_t id_type, int64_t n_tokens, const void* d_dy, int64_t dy_stride,
+                      int32_t dy_dtype, float scale, int64_t padding_row, int32_t accumulate, void* d_grad, int64_t n_rows,
+                      int64_t dim, int64_t grad_stride, int32_t grad_dtype, void* d_workspace, uint64_t workspace_bytes,
+                      void* hip_stream) {
+    if (!grad_sizes_ok(n_tokens, n_rows, dim) || !is_dtype(dy_dtype) || !is_dtype(grad_dtype)) return MGWFBP_EINVAL;
+    if (id_type != MGWFBP_I32 && id_type != MGWFBP_I64) return MGWFBP_EINVAL;
+    if (!is_matrix(n_tokens, dim, dy_stride, dtype_bytes(dy_dtype))) return MGWFBP_EINVAL;
+    if (!is_matrix(n_rows, dim, grad_stride, dtype_bytes(grad_dtype))) return MGWFBP_EINVAL;
+    if (n_rows == 0 || dim == 0) return MGWFBP_OK;
+    if (d_grad == nullptr || !is_aligned(d_grad, dtype_bytes(grad_dtype))) return MGWFBP_EINVAL;
+    const GradPlan p = plan_of(n_tokens, n_rows, dim);
+    if (n_tokens > 0) {
+        if (d_ids == nullptr || !is_aligned(d_ids, id_type == MGWFBP_I64 ? 8 : 4)) return MGWFBP_EINVAL;
+        if (d_dy == nullptr || !is_aligned(d_dy, dtype_bytes(dy_dtype))) return MGWFBP_EINVAL;
+        if (d_workspace == nullptr || !is_aligned(d_workspace, 256) || workspace_bytes < static_cast<uint64_t>(p.bytes)) return MGWFBP_EINVAL;
+    } else if (accumulate) {
+        return MGWFBP_OK;
+    }
+    GradArgs a{};
+    unsigned char* const ws = static_cast<unsigned char*>(d_workspace);
+    a.ids = d_ids;
+    a.id_type = id_type;
+    a.dy = d_dy;
+    a.dy_stride = dy_stride;
+    a.grad = d_grad;
+    a.grad_stride = n_rows == 1 ? dim : grad_stride;
+    a.n_rows = n_rows;
+    a.dim = dim;
+    a.padding_row = padding_row;
+    a.tokens = n_tokens;
+    a.dim_padded = p.dim_padded;
+    a.scale = scale;
+    a.accumulate = accumulate != 0;
+    a.chunk = p.chunk;
+    a.chunks = p.chunks;
+    a.items = p.items;
+    a.vecs = static_cast<uint32_t>(ceil_div(dim, VEC));
+    a.page = static_cast<uint32_t>(std::min<int64_t>(std::max<uint32_t>(p.chunks, 1), (int64_t(1) << 30) / a.vecs));
+    if (n_tokens > 0) {
+        a.order = reinterpret_cast<uint32_t*>(ws + p.order);
+        a.row = reinterpret_cast<int32_t*>(ws + p.row);
+        a.partial = reinterpret_cast<float*>(ws + p.partial);
+    }
+    const uint32_t clearing = accumulate ? 0 : clear_blocks(n_rows, dim, dtype_bytes(grad_dtype));
+    int rc = MGWFBP_OK;
+    if (p.ranked) {
+        a.work_blocks = static_cast<uint32_t>(ceil_div(n_tokens, RANK_EACH));
+        const dim3 grid(a.work_blocks + clearing);
+        rc = with_dtype(grad_dtype, [&](auto* grad_type) {
+            return launch(rank_kernel<std::remove_pointer_t<decltype(grad_type)>>, a, grid, dim3(THREADS), hip_stream);
+        });
+        if (rc != MGWFBP_OK || n_tokens == 0) return rc;
+    } else {
+        uint32_t* const order[2] = {a.order, reinterpret_cast<uint32_t*>(ws + p.other_order)};
+        int32_t* const row[2] = {a.row, reinterpret_cast<int32_t*>(ws + p.other_row)};
+        a.counts = reinterpret_cast<uint32_t*>(ws + p.counts);
+        a.present = accumulate ? nullptr : ws + p.present;
+        int passes = 1;
+        while (passes < 4 && (static_cast<uint64_t>(n_rows) >> (8 * passes)) != 0) ++passes;
+        for (int pass = 0; pass < passes; ++pass) {             // the last one ends in order and row
+            const int to = (passes - 1 - pass) % 2;
+            a.order = order[to];
+            a.row = row[to];
+            a.other_order = order[1 - to];
+            a.other_row = row[1 - to];
+            a.shift = 8 * pass;
+            a.from_ids = pass == 0;
+            rc = launch(digit_kernel, a, dim3(p.blocks), dim3(THREADS), hip_stream);
+            if (rc == MGWFBP_OK) rc = launch(move_kernel, a, dim3(p.blocks), dim3(THREADS), hip_stream);
+            if (rc != MGWFBP_OK) return rc;
+        }
+    }
+    a.work_blocks = static_cast<uint32_t>(ceil_div(static_cast<int64_t>(a.page) * a.vecs, THREADS));
+    const dim3 grid(a.work_blocks + (p.ranked ? 0 : clearing), static_cast<uint32_t>(ceil_div(p.chunks, a.page)));
+    rc = with_dtype(dy_dtype, [&](auto* dy_type) {
+        return with_dtype(grad_dtype, [&](auto* grad_type) {
+            return launch(sum_kernel<std::remove_pointer_t<decltype(dy_type)>, std::remove_pointer_t<decltype(grad_type)>>, a, grid,
+                          dim3(THREADS), hip_stream);
+        });
+    });
+    if (rc != MGWFBP_OK || p.chunks < 2) return rc;
+    const dim3 join_grid(p.chunks - 1, static_cast<uint32_t>(ceil_div(dim, JOIN_COLS)));
+    return with_dtype(grad_dtype, [&](auto* grad_type) {
+        return launch(join_kernel<std::remove_pointer_t<decltype(grad_type)>>, a, join_grid, dim3(JOIN_WAVES * 64), hip_stream);
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,540 @@
+"""The operators that make per-layer gradients (embedding lookup and gradient, 8-bit activation checkpoints and what the
+backward pass makes of them) against plain 64-bit implementations, at the sizes and values where they can go wrong.
+
+Tolerances follow from the arithmetic the operators promise: a binary32 sum of n terms is off by at most about n * 2^-24
+times the sum of the terms' magnitudes, and a result rounded to p bits by 2^-p of itself (bfloat16 p = 8, binary16 p = 11,
+and 2^-25 near zero).  Whole numbers are compared bit for bit."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1912_09268_amd import layers_binding as M
+from paper_1912_09268_amd import layers
+
+pytestmark = pytest.mark.gpu
+
+G = 128
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+ROUND = {F32: 2.0 ** -24, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+NEAR_ZERO = {F32: 0.0, BF16: 0.0, F16: 2.0 ** -25}
+DT = {"f32": F32, "bf16": BF16, "f16": F16}
+
+
+def _say(*a):
+    print("[layers]", *a, flush=True)
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _close(got, want, slack, what=""):
+    """|got - want| <= slack + the rounding of the result's type; NaN only where wanted."""
+    torch.cuda.synchronize()
+    got64, bound = got.double(), slack + ROUND[got.dtype] * want.abs() + NEAR_ZERO[got.dtype]
+    assert torch.equal(got64.isnan(), want.isnan()), what
+    off = (got64 - want).abs()
+    bad = ~((off <= bound) | want.isnan() | (got64 == want))
+    assert not bool(bad.any()), (what, float((off / bound.clamp(min=1e-300))[~want.isnan()].max()), torch.nonzero(bad)[:4].tolist())
+
+
+def _strided(shape, dtype, how, fill=float("nan")):
+    """A matrix alone ("dense"), or a view into a larger one, shifted by an odd number of elements, whose other places hold
+    `fill`: (matrix, the memory behind it)."""
+    rows, cols = shape
+    if how == "dense":
+        t = torch.full((rows, cols), fill, dtype=dtype, device="cuda")
+        return t, t
+    whole = torch.full((rows * (cols + 5) + 9,), fill, dtype=dtype, device="cuda")
+    return torch.as_strided(whole, (rows, cols), (cols + 5, 1), 3), whole
+
+
+def _untouched(t, whole, fill):
+    """Nothing but the view has been written."""
+    if t.data_ptr() == whole.data_ptr() and t.numel() == whole.numel():
+        return True
+    mask = torch.ones_like(whole, dtype=torch.bool)
+    torch.as_strided(mask, t.shape, t.stride(), t.storage_offset()).fill_(False)
+    left = whole[mask]
+    return bool(left.isnan().all()) if math.isnan(fill) else bool((left == fill).all())
+
+
+# ---- embedding lookup ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("how", ["dense", "strided"])
+@pytest.mark.parametrize("table,out", [("f32", "bf16"), ("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32"), ("f16", "bf16")])
+@pytest.mark.parametrize("tokens,dim,rows,tables", [(1, 1024, 50, 3), (1, 1, 1, 1), (7, 7, 3, 2), (513, 8, 40, 4), (300, 1027, 1000, 1),
+                                                   (65, 64, 5, 3), (2, 4097, 9, 2)])
+def test_embed(tokens, dim, rows, tables, table, out, how):
+    _say("embed", tokens, dim, rows, tables, table, out, how)
+    g = _gen(tokens * 31 + dim)
+    tabs, ids, scales, want, terms = [], [], [], 0.0, 0.0
+    for k in range(tables):
+        n = rows + k
+        t, _ = _strided((n, dim), DT[table], how)
+        t.copy_(torch.randn(n, dim, generator=g, device="cuda"))
+        i = torch.randint(-2, n + 2, (tokens,), generator=g, device="cuda")         # some outside the table
+        i[torch.rand(tokens, generator=g, device="cuda") < 0.1] = 2 ** 31 - 1
+        i = i.to(torch.int32) if k % 2 else i
+        if k == 0 and tokens > 3:
+            i[1], i[2] = -2 ** 63, 2 ** 40
+        here = (i >= 0) & (i < n)
+        s = (32.0, 1.0, -0.3, 1.7)[k]
+        picked = torch.where(here[:, None], t.double()[i.long().clamp(0, n - 1)] * float(np.float32(s)), 0.0)
+        want, terms = want + picked, terms + picked.abs()
+        tabs.append(t), ids.append(i), scales.append(s)
+    o, whole = _strided((tokens, dim), DT[out], how)
+    got = layers.embed(tabs, ids, scales=scales, out=o)
+    assert got is o
+    _close(o, want, 2 * tables * 2.0 ** -24 * terms, "embed")
+    assert _untouched(o, whole, float("nan"))
+
+
+def test_embed_makes_its_output_and_takes_any_shape_of_ids():
+    table = torch.randn(10, 24, device="cuda")
+    ids = torch.arange(12, device="cuda").view(3, 4) % 10
+    out = layers.embed(table, ids, dtype=F32)
+    assert out.shape == (3, 4, 24) and torch.equal(out, table[ids])
+    assert layers.embed(table, ids).dtype == BF16
+    assert layers.embed(table, ids[:0]).shape == (0, 4, 24)
+    empty = torch.empty(0, 24, device="cuda")                            # a table without rows: every id is outside
+    assert torch.equal(layers.embed(empty, ids, dtype=F32), torch.zeros(3, 4, 24, device="cuda"))
+
+
+def test_rows_of_a_table_beyond_32_bits_of_offset():
+    _say("embed, embed_grad: offsets beyond 2^32 elements")
+    rows, stride, dim = 530000, 8192, 40
+    memory = torch.empty(rows * stride, dtype=BF16, device="cuda")       # 4.3e9 elements
+    table = torch.as_strided(memory, (rows, dim), (stride, 1))
+    ids = torch.tensor([0, rows - 1, 524287, 524288, 262144, rows - 1], device="cuda")
+    for i in set(ids.tolist()):
+        table[i] = i % 251
+    out = layers.embed(table, ids, dtype=F32)
+    assert torch.equal(out, (ids % 251).float()[:, None].expand(-1, dim))
+    dy = torch.ones(ids.numel(), dim, dtype=BF16, device="cuda")
+    layers.embed_grad(dy, ids, table, accumulate=True)
+    for i in set(ids.tolist()):
+        assert bool((table[i].float() == i % 251 + ids.tolist().count(i)).all()), i
+
+
+# ---- its gradient ----------------------------------------------------------------------------------------------------
+
+def _embed_grad_reference(dy, ids, rows, scale, padding_row):
+    """(sum, sum of magnitudes, terms of a row) in 64 bits."""
+    ids = ids.reshape(-1).long()
+    fine = torch.nonzero((ids >= 0) & (ids < rows) & (ids != padding_row)).squeeze(1)
+    at = ids[fine].cpu()
+    d = dy[fine].double().cpu()
+    total = torch.zeros(rows, dy.shape[1], dtype=torch.float64).index_add_(0, at, d)
+    terms = torch.zeros(rows, dy.shape[1], dtype=torch.float64).index_add_(0, at, d.abs())
+    count = torch.zeros(rows, 1, dtype=torch.float64).index_add_(0, at, torch.ones(len(at), 1, dtype=torch.float64))
+    return (total * scale).cuda(), (terms * abs(scale)).cuda(), count.cuda()
+
+
+def _spread(tokens, rows, spread, g):
+    if spread == "one":
+        return torch.full((tokens,), rows // 2, device="cuda")
+    if spread == "none":
+        return torch.full((tokens,), -1, device="cuda")
+    u = torch.rand(tokens, generator=g, device="cuda", dtype=torch.float64)
+    ids = (torch.exp(u * math.log(rows + 1.0)) - 1.0 if spread == "words" else u * rows).long().clamp(0, rows - 1)
+    if spread == "holes":
+        ids[torch.rand(tokens, generator=g, device="cuda") < 0.4] = -7
+        ids[torch.rand(tokens, generator=g, device="cuda") < 0.1] = rows
+    return ids
+
+
+@pytest.mark.parametrize("spread", ["words", "even", "one", "holes", "none"])
+@pytest.mark.parametrize("tokens,rows,dim", [(1, 1, 1), (1, 5, 1024), (2, 3, 9), (9, 2, 64), (64, 300, 33), (65, 1, 520), (1000, 7, 130),
+                                            (4096, 2, 256), (4096, 3001, 72), (8192, 900, 24), (8193, 900, 24), (20011, 257, 40),
+                                            (30000, 70001, 9), (70000, 2, 8)])
+def test_embed_grad(tokens, rows, dim, spread):
+    kinds = [(F32, F32), (BF16, BF16), (F16, F16), (BF16, F32), (F32, F16)]
+    dy_t, grad_t = kinds[(tokens + rows + len(spread)) % len(kinds)]
+    how = "strided" if (tokens + dim) % 2 else "dense"
+    _say("embed_grad", tokens, rows, dim, spread, dy_t, grad_t, how)
+    g = _gen(tokens + rows)
+    ids = _spread(tokens, rows, spread, g)
+    ids = ids.to(torch.int32) if tokens % 3 == 0 else ids
+    dy, _ = _strided((tokens, dim), dy_t, how)
+    dy.copy_(torch.randn(tokens, dim, generator=g, device="cuda"))
+    dy[(ids < 0) | (ids >= rows)] = float("nan")                          # places that stand for no row are not looked at
+    grad, whole = _strided((rows, dim), grad_t, how)
+    scale = 0.37
+    layers.embed_grad(dy, ids, grad, scale=scale)
+    want, terms, count = _embed_grad_reference(dy, ids, rows, float(np.float32(scale)), -1)
+    _close(grad, want, (count + 2) * 2.0 ** -24 * terms, "embed_grad")
+    assert _untouched(grad, whole, float("nan"))
+    again = torch.empty_like(grad).copy_(grad)
+    layers.embed_grad(dy, ids, grad, scale=scale)
+    assert torch.equal(again, grad)                                      # the same call gives the same bits
+    # added to what is there, without the most frequent row
+    had = torch.randn(rows, dim, generator=g, device="cuda").to(grad_t)
+    grad.copy_(had)
+    pad = int(ids[0])
+    layers.embed_grad(dy, ids, grad, scale=scale, padding_row=pad, accumulate=True)
+    want, terms, count = _embed_grad_reference(dy, ids, rows, float(np.float32(scale)), pad)
+    _close(grad, want + had.double(), (count + 3) * 2.0 ** -24 * (terms + had.double().abs()), "accumulated")
+    rest = count.squeeze(1) == 0
+    assert torch.equal(grad[rest], had[rest])
+
+
+def test_embed_grad_of_padding_rows_and_of_no_tokens():
+    grad = torch.full((6, 10), 5.0, device="cuda")
+    ids = torch.tensor([[4, 0], [4, 3]], device="cuda")
+    dy = torch.ones(2, 2, 10, device="cuda")
+    layers.embed_grad(dy, ids, grad, padding_row=4)
+    want = torch.zeros(6, 10, device="cuda")
+    want[0] = want[3] = 1.0
+    assert torch.equal(grad, want)
+    grad.fill_(5.0)
+    layers.embed_grad(dy[:0].view(0, 10), ids[:0], grad, accumulate=True)
+    assert bool((grad == 5.0).all())
+    layers.embed_grad(dy[:0].view(0, 10), ids[:0], grad)
+    assert bool((grad == 0.0).all())
+
+
+def test_embed_grad_infinities_stay_in_their_rows():
+    for tokens in (100, 9000):
+        ids = torch.arange(tokens, device="cuda") % 50
+        dy = torch.ones(tokens, 16, device="cuda")
+        dy[7, 3], dy[8, 2] = float("inf"), float("nan")
+        grad = torch.empty(50, 16, device="cuda")
+        layers.embed_grad(dy, ids, grad)
+        torch.cuda.synchronize()
+        assert float(grad[7, 3]) == math.inf and math.isnan(float(grad[8, 2]))
+        grad[7, 3] = grad[8, 2] = tokens // 50
+        assert bool((grad == tokens // 50).all())
+
+
+def test_embedding_gradient_against_differences():
+    """sum(weight * embed(table)) is linear in the table: a difference over any step is its slope."""
+    g = _gen(5)
+    table, ids = torch.randn(9, 12, generator=g, device="cuda"), torch.randint(-1, 9, (40,), generator=g, device="cuda")
+    weight = torch.randn(40, 12, generator=g, device="cuda")
+    grad = layers.embed_grad(weight, ids, torch.empty(9, 12, device="cuda"), scale=3.0)
+
+    def loss(t):
+        return float((layers.embed(t, ids, scales=[3.0], dtype=F32).double() * weight.double()).sum())
+
+    for r, c in ((0, 0), (3, 11), (8, 5)):
+        up, down = table.clone(), table.clone()
+        up[r, c] += 1.0
+        down[r, c] -= 1.0
+        # values up to about 4 * 3 with one rounding each, 40 of them; the step itself is rounded, too
+        assert abs((loss(up) - loss(down)) / 2 - float(grad[r, c])) < 40 * 12 * 2.0 ** -22
+
+
+# ---- 8-bit checkpoints -----------------------------------------------------------------------------------------------
+
+def _codes(x):
+    """q and scale by their definition, in numpy's binary32, which rounds every operation once."""
+    x = x.float().cpu().numpy()
+    tokens, channels = x.shape
+    groups = -(-tokens // G)
+    q, scale = np.zeros((tokens, channels), np.int8), np.zeros((groups, channels), np.float32)
+    with np.errstate(all="ignore"):
+        for g in range(groups):
+            part = x[g * G:(g + 1) * G]
+            most = np.abs(part).max(0)
+            s = np.maximum(most, np.float32(2.0 ** -100)) * (np.float32(1) / np.float32(127))
+            fine = np.isfinite(most)
+            inv = np.where(fine, np.float32(1) / s, np.float32(0)).astype(np.float32)
+            scale[g] = np.where(fine, s, np.nan)
+            q[g * G:(g + 1) * G] = np.where(fine, np.clip(np.rint(np.where(fine, part, 0) * inv), -127, 127), 0)
+    return q, scale
+
+
+def _f64(kind, x):
+    """(f, f') in 64 bits."""
+    if kind == "identity":
+        return x, torch.ones_like(x)
+    if kind == "gelu":
+        below = 0.5 * torch.erfc(-x / math.sqrt(2.0))
+        return x * below, below + x * torch.exp(-x * x / 2) / math.sqrt(2 * math.pi)
+    if kind == "gelu_tanh":
+        s = torch.sigmoid(2 * math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3))
+        return x * s, s + x * s * (1 - s) * 2 * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * x * x)
+    s = torch.sigmoid(x)
+    return x * s, s + x * s * (1 - s)
+
+
+# The functions' own error: the tail's fit and roundings 5.1e-7 of at most 1/2, the exponential's argument, and a few units of
+# v_exp_f32 and v_rcp_f32, relative to x for the value and absolute for the slope.
+OWN = 2e-6
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("tokens,channels", [(1, 1), (1, 1024), (2, 17), (127, 8), (128, 15), (129, 16), (300, 130), (77, 1001), (513, 257)])
+def test_act_store(tokens, channels, dtype):
+    kind = ("identity", "gelu", "gelu_tanh", "silu")[(tokens + channels) % 4]
+    how = "strided" if tokens % 2 else "dense"
+    _say("act_store", tokens, channels, dtype, kind, how)
+    g = _gen(tokens * 7 + channels)
+    x, _ = _strided((tokens, channels), DT[dtype], how)
+    size = torch.exp(2 * torch.randn(channels, generator=g, device="cuda"))
+    size[::5] = 0.0                                                       # channels of zeros
+    x.copy_(torch.randn(tokens, channels, generator=g, device="cuda") * size)
+    y, whole = _strided((tokens, channels), DT[dtype], how)
+    act = layers.act_store(x, kind=kind, y=y)
+    torch.cuda.synchronize()
+    q, scale = _codes(x)
+    assert np.array_equal(act.q[:, :channels].cpu().numpy(), q)
+    assert np.array_equal(act.scale[:, :channels].cpu().numpy().view(np.uint32), scale.view(np.uint32))
+    assert not bool(act.q[:, channels:].any())
+    assert act.q.shape[1] % 16 == 0 and act.q.shape[1] - channels < 16
+    want, _ = _f64(kind, x.double())
+    _close(y, want, OWN * x.double().abs(), "y")
+    assert _untouched(y, whole, float("nan"))
+    alone = layers.act_store(x)                                           # without y
+    assert torch.equal(alone.q, act.q) and torch.equal(alone.scale, act.scale)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_act_store_of_extreme_values(dtype):
+    tiny, huge = {"f32": (1e-38, 3e38), "bf16": (1e-38, 3e38), "f16": (6e-8, 65504.0)}[dtype]
+    x = torch.zeros(140, 24, device="cuda", dtype=DT[dtype])
+    x[3, 0], x[130, 0] = math.inf, 1.0                                    # poisons its own group and channel only
+    x[4, 1] = -math.inf
+    x[5, 2] = math.nan
+    x[:, 3] = tiny
+    x[:, 4] = huge
+    x[::2, 5] = -huge
+    x[:, 6] = torch.linspace(-1, 1, 140).to(DT[dtype])
+    x[:, 7] = torch.arange(140, device="cuda") - 63.5                     # ties
+    x[127, 8], x[128, 8] = 2.0, 3.0
+    act = layers.act_store(x, kind="gelu", y=torch.empty_like(x))
+    torch.cuda.synchronize()
+    q, scale = _codes(x)
+    assert np.array_equal(act.q[:, :24].cpu().numpy(), q)
+    got = act.scale[:, :24].cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(scale)) and np.isnan(got).sum() == 3
+    assert np.array_equal(got[~np.isnan(got)], scale[~np.isnan(scale)])
+    back = layers.act_backward(act, y=torch.empty(140, 24, device="cuda"))
+    assert bool(back[:128, :3].isnan().all()) and not bool(back[128:].isnan().any()) and not bool(back[:, 3:].isnan().any())
+    assert float(back[130, 0]) == 1.0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind", ["identity", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("tokens,channels", [(1, 1), (3, 1024), (9, 17), (128, 8), (129, 100), (250, 1001), (1030, 264)])
+def test_act_backward(tokens, channels, kind, dtype):
+    how = "strided" if channels % 2 else "dense"
+    _say("act_backward", tokens, channels, kind, dtype, how)
+    g = _gen(tokens + channels)
+    x = torch.randn(tokens, channels, generator=g, device="cuda") * 3
+    x[:, ::7] *= 4                                                        # into the tails
+    act = layers.act_store(x)
+    held = act.q[:, :channels].double() * act.scale.double().repeat_interleave(G, 0)[:tokens, :channels]
+    dy, _ = _strided((tokens, channels), DT[dtype], how)
+    dy.copy_(torch.randn(tokens, channels, generator=g, device="cuda"))
+    dx, dx_whole = _strided((tokens, channels), DT[dtype], how)
+    y, y_whole = _strided((tokens, channels), DT[dtype], how)
+    value, slope = _f64(kind, held)
+    layers.act_backward(act, dy, kind=kind, dx=dx, y=y)
+    _close(dx, dy.double() * slope, OWN * dy.double().abs(), "dx")
+    _close(y, value, OWN * held.abs(), "y")
+    assert _untouched(dx, dx_whole, float("nan")) and _untouched(y, y_whole, float("nan"))
+    assert torch.equal(layers.act_backward(act, dy, kind=kind), dx)
+    assert torch.equal(layers.act_backward(act, kind=kind, y=torch.empty_like(dx)), y)
+
+
+@pytest.mark.parametrize("kind", ["gelu", "gelu_tanh", "silu"])
+def test_activation_slopes_against_differences(kind):
+    """The slope from the checkpoint against a central difference of the function that act_store computes."""
+    x = torch.linspace(-6, 6, 128 * 48, device="cuda").view(128, 48)
+    act = layers.act_store(x)
+    at = layers.act_backward(act, y=torch.empty(128, 48, device="cuda"))
+    slope = layers.act_backward(act, torch.ones(128, 48, device="cuda"), kind=kind)
+    h = 2.0 ** -5
+    up, down = torch.empty_like(at), torch.empty_like(at)
+    layers.act_store(at + h, kind=kind, y=up)
+    layers.act_store(at - h, kind=kind, y=down)
+    # third derivatives are below 1.7: h^2 / 6 of it; values up to 6 with OWN of themselves, over 2 h
+    assert float(((up - down) / (2 * h) - slope).abs().max()) < h * h / 6 * 1.7 + 2 * OWN * 6 / (2 * h)
+
+
+def _checkpoint(tokens, channels, g):
+    """(act, the values it stands for in 64 bits): numbers as they are held, without act_store."""
+    act = layers.act_empty(tokens, channels)
+    act.q.copy_(torch.randint(-127, 128, act.q.shape, generator=g, device="cuda"))
+    act.scale.copy_(torch.exp(torch.randn(act.scale.shape, generator=g, device="cuda")))
+    if channels > 2:
+        act.scale[:, 1] = 2.0 ** -100 / 127
+    act.q[:, channels:] = 127                                              # behind the last channel: not looked at
+    act.scale[:, channels:] = float("nan")
+    return act, act.q[:, :channels].double() * act.scale.double().repeat_interleave(G, 0)[:tokens, :channels]
+
+
+def _linear_slack(tokens, terms, had):
+    """A group's sum and the groups' sum, in binary32, with whatever joins them."""
+    return (min(tokens, G) + -(-tokens // G) + 8) * 2.0 ** -24 * (terms + had)
+
+
+SIZES = [(1, 1, 1), (1, 1024, 1024), (8, 129, 127), (15, 128, 128), (16, 64, 200), (17, 33, 9), (63, 16, 130), (65, 250, 31), (127, 8, 8),
+         (128, 40, 257), (129, 385, 100), (300, 1000, 129), (1000, 70, 77), (2049, 300, 260), (5000, 17, 5)]
+
+
+@pytest.mark.parametrize("dy_t,grad_t", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("bf16", "f32"), ("f16", "bf16")])
+@pytest.mark.parametrize("tokens,channels,outputs", SIZES)
+def test_act_linear_grad(tokens, channels, outputs, dy_t, grad_t):
+    how = "strided" if (tokens + channels) % 2 else "dense"
+    _say("act_linear_grad", tokens, channels, outputs, dy_t, grad_t, how)
+    g = _gen(tokens + 3 * channels + outputs)
+    act, x = _checkpoint(tokens, channels, g)
+    dy, _ = _strided((tokens, outputs), DT[dy_t], how)
+    dy.copy_(torch.randn(tokens, outputs, generator=g, device="cuda"))
+    dw, whole = _strided((outputs, channels), DT[grad_t], how)
+    db = torch.full((outputs,), float("nan"), dtype=DT[grad_t], device="cuda")
+    d64 = dy.double().cpu()
+    x = x.cpu()
+    want, terms = (d64.t() @ x).cuda(), (d64.abs().t() @ x.abs()).cuda()
+    limit = 65504.0 / max(1.0, float(want.abs().max())) if DT[grad_t] == F16 else 1.0
+    if limit < 1.0:                                                       # binary16 results in range
+        act.scale.mul_(2.0 ** math.floor(math.log2(limit)))
+        want, terms = want * 2.0 ** math.floor(math.log2(limit)), terms * 2.0 ** math.floor(math.log2(limit))
+    layers.act_linear_grad(dy, act, dw, db=db)
+    _close(dw, want, _linear_slack(tokens, terms, 0.0), "dw")
+    _close(db, d64.sum(0).cuda(), (tokens + 8) * 2.0 ** -24 * d64.abs().sum(0).cuda(), "db")
+    assert _untouched(dw, whole, float("nan"))
+    first = dw.clone()
+    layers.act_linear_grad(dy, act, dw)                                   # without a bias; the same bits
+    assert torch.equal(first, dw)
+    had, had_b = torch.randn(outputs, channels, generator=g, device="cuda").to(dw.dtype), torch.randn(outputs, generator=g, device="cuda").to(dw.dtype)
+    dw.copy_(had), db.copy_(had_b)
+    layers.act_linear_grad(dy, act, dw, db=db, accumulate=True)
+    _close(dw, want + had.double(), _linear_slack(tokens, terms, had.double().abs()), "accumulated dw")
+    _close(db, d64.sum(0).cuda() + had_b.double(), (tokens + 9) * 2.0 ** -24 * (d64.abs().sum(0).cuda() + had_b.double().abs()), "accumulated db")
+
+
+def test_act_linear_grad_of_no_tokens_and_of_no_channels():
+    act = layers.act_empty(0, 40)
+    dw, db = torch.full((9, 40), 3.0, device="cuda"), torch.full((9,), 3.0, device="cuda")
+    dy = torch.empty(0, 9, device="cuda", dtype=BF16)
+    layers.act_linear_grad(dy, act, dw, db=db, accumulate=True)
+    assert bool((dw == 3.0).all()) and bool((db == 3.0).all())
+    layers.act_linear_grad(dy, act, dw, db=db)
+    assert not bool(dw.any()) and not bool(db.any())
+    none = layers.act_empty(20, 0)
+    layers.act_linear_grad(torch.ones(20, 9, device="cuda"), none, torch.empty(9, 0, device="cuda"), db=db)
+    assert bool((db == 20.0).all())
+
+
+@pytest.mark.parametrize("dy_t", ["bf16", "f16", "f32"])
+def test_values_that_are_not_finite_stay_where_they_belong(dy_t):
+    tokens, channels, outputs = 300, 150, 140
+    act, _ = _checkpoint(tokens, channels, _gen(1))
+    act.scale[:, :channels] = 1.0
+    act.q.fill_(1)
+    act.scale[1, 5] = float("nan")                                        # an overflow of the forward pass
+    dy = torch.ones(tokens, outputs, device="cuda", dtype=DT[dy_t])
+    dy[299, 7], dy[0, 9] = math.inf, math.nan
+    dw, db = torch.empty(outputs, channels, device="cuda"), torch.empty(outputs, device="cuda")
+    layers.act_linear_grad(dy, act, dw, db=db)
+    torch.cuda.synchronize()
+    assert bool(dw[:, 5].isnan().all()) and bool(dw[9].isnan().all()) and math.isnan(float(db[9]))
+    assert float(db[7]) == math.inf and bool((dw[7, :5] == math.inf).all()) and bool((dw[7, 6:] == math.inf).all())
+    fine = torch.ones(outputs, channels, dtype=torch.bool, device="cuda")
+    fine[:, 5] = fine[7] = fine[9] = False
+    assert bool((dw[fine] == 300.0).all())
+
+
+def test_binary32_gradients_keep_their_digits():
+    """dy and q so that the result is dy itself: all 24 bits arrive, over the whole range of exponents."""
+    tokens, outputs = 128, 64
+    g = _gen(3)
+    act = layers.act_empty(tokens, 128)
+    act.q.zero_()
+    act.q.fill_diagonal_(1)
+    act.scale.fill_(1.0)
+    dy = torch.randn(tokens, outputs, generator=g, device="cuda") * torch.exp2(torch.randint(-80, 80, (tokens, outputs), generator=g, device="cuda").float())
+    dw = torch.empty(outputs, 128, device="cuda")
+    layers.act_linear_grad(dy, act, dw)
+    assert torch.equal(dw, dy.t())
+
+
+def test_weight_gradient_against_differences():
+    """sum(upstream * linear(x)) is linear in the weights: a difference over any step is its slope."""
+    g = _gen(8)
+    act, x = _checkpoint(37, 20, g)
+    dy = torch.randn(37, 6, generator=g, device="cuda")
+    dw, db = torch.empty(6, 20, device="cuda"), torch.empty(6, device="cuda")
+    layers.act_linear_grad(dy, act, dw, db=db)
+    w, b = torch.randn(6, 20, generator=g, device="cuda").double(), torch.zeros(6, device="cuda").double()
+
+    def loss(w, b):
+        return float(((x @ w.t().contiguous() + b) * dy.double()).sum())
+
+    slack = 64 * 2.0 ** -24 * float((dy.double().abs().t().contiguous() @ x.abs()).max())
+    for o, c in ((0, 0), (5, 19), (2, 7)):
+        up = w.clone()
+        up[o, c] += 1.0
+        assert abs(loss(up, b) - loss(w, b) - float(dw[o, c])) < slack + 1e-9
+        up = b.clone()
+        up[o] += 1.0
+        assert abs(loss(w, up) - loss(w, b) - float(db[o])) < slack + 1e-9
+
+
+# ---- streams, graphs, workspaces -------------------------------------------------------------------------------------
+
+def _pass(table, ids, x, dy, grad, dw, db, y, dx, act, out, spaces):
+    layers.embed([table], [ids], out=out)
+    layers.act_store(x, act, kind="gelu", y=y)
+    layers.act_backward(act, dy, kind="gelu", dx=dx)
+    layers.act_linear_grad(dx, act, dw, db=db, workspace=spaces[0])
+    layers.embed_grad(dx, ids, grad, workspace=spaces[1])
+
+
+@pytest.mark.parametrize("tokens", [700, 9000])
+def test_a_graph_of_all_operators_replays(tokens):
+    """All of them recorded once, on a stream of their own, replayed with eager work in between and new inputs each time."""
+    _say("graph", tokens)
+    g = _gen(tokens)
+    rows, n = 500, 200
+    table, ids = torch.randn(rows, n, generator=g, device="cuda"), torch.randint(0, rows, (tokens,), generator=g, device="cuda")
+    x, dy = torch.randn(tokens, n, generator=g, device="cuda").to(BF16), torch.randn(tokens, n, generator=g, device="cuda").to(BF16)
+    act = layers.act_empty(tokens, n)
+    mem = [torch.empty(rows, n, device="cuda"), torch.empty(n, n, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(x), torch.empty_like(x), act,
+           torch.empty(tokens, n, dtype=BF16, device="cuda")]
+    spaces = [torch.empty(M.act_linear_grad_workspace(tokens, n, n), dtype=torch.uint8, device="cuda"),
+              torch.empty(M.embed_grad_workspace(tokens, rows, n), dtype=torch.uint8, device="cuda")]
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        _pass(table, ids, x, dy, *mem, spaces)
+    for replay in range(4):
+        ids.copy_(torch.randint(0, rows, (tokens,), generator=g, device="cuda"))
+        x.copy_(torch.randn(tokens, n, generator=g, device="cuda"))
+        dy.copy_(torch.randn(tokens, n, generator=g, device="cuda"))
+        for t in spaces:
+            t.fill_(255)                                                   # nothing is carried over in a workspace
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = [torch.empty_like(t) if isinstance(t, torch.Tensor) else layers.act_empty(tokens, n) for t in mem]
+        _pass(table, ids, x, dy, *eager, [None, None])
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(mem, eager)):
+            if i == 5:
+                assert torch.equal(a.q, b.q) and torch.equal(a.scale[:, :n], b.scale[:, :n]), replay
+            else:
+                assert torch.equal(a, b), (replay, i)
+
+
+def test_operators_run_on_the_current_stream():
+    """Behind other work of a stream that is not the default one."""
+    stream = torch.cuda.Stream()
+    table, ids = torch.zeros(64, 256, device="cuda"), torch.arange(64, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        busy = torch.ones(4096, 4096, device="cuda")
+        for _ in range(20):
+            busy = busy @ busy * 2.0 ** -12
+        table.copy_(busy[:64, :256])
+        out = layers.embed(table, ids, dtype=F32)
+        grad = layers.embed_grad(out, ids, torch.empty(64, 256, device="cuda"))
+    stream.synchronize()
+    assert torch.equal(out, table) and torch.equal(grad, table) and bool((table == 1.0).all())
