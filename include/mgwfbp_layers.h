@@ -94,7 +94,7 @@ int mgwfbp_act_backward(const int8_t* d_q, const float* d_scale, int64_t ld, int
  * output [n_tokens][n_outputs] and the checkpoint of its input:
  *   dw[o,c] = sum over t of dy[t,o] * x^[t,c];  db[o] = sum over t of dy[t,o]        (d_db NULL: left out)
  * accumulate != 0 adds to what is in dw and db.  The products are exact; the sums binary32.
- *   n_tokens 0..2^23, n_outputs 0..2^23; ceil(n_outputs/128) * ceil(n_channels/128) <= 2^23 */
+ *   n_tokens 0..2^23, n_outputs 0..2^23; ceil(n_outputs/128) * ceil(n_channels/128) <= 2^22 */
 int mgwfbp_act_linear_grad_workspace(int64_t n_tokens, int64_t n_channels, int64_t n_outputs, uint64_t* bytes_out);
 int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, int64_t n_tokens, int64_t n_channels,
                            const void* d_dy, int64_t dy_stride, int32_t dy_dtype, int64_t n_outputs, int32_t accumulate,

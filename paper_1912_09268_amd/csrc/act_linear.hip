@@ -20,12 +20,10 @@ namespace {
 using namespace ops;
 
 constexpr int GROUP = MGWFBP_ACT_GROUP;
-constexpr int THREADS = 256;
-constexpr int TILE_O = 128, TILE_C = 128, STEP = 64;          // outputs, channels and tokens that a workgroup takes at a time
 constexpr int MAX_SPLITS = 64;
+constexpr int BIAS_SHARES = 8;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 struct LinearArgs {
@@ -35,10 +33,10 @@ struct LinearArgs {
     void* dw;
     void* db;
     float* partial;                    // [splits][outputs][channels_padded], and the bias parts behind it
-    float* bias_partial;               // [bias_parts][outputs]
-    int64_t dy_stride, ld, dw_stride;
-    int64_t tokens, channels, outputs, channels_padded;
-    uint32_t tiles_c, tiles, splits, groups, groups_per_split, bias_parts;
+    float* bias_partial;               // [splits * bias_shares][outputs]
+    int64_t dy_stride, ld, dw_stride, channels_padded;
+    int32_t tokens, channels, outputs;
+    uint32_t tiles_c, tiles, splits, groups, groups_per_split, bias_shares;
     int32_t accumulate;
 };
 
@@ -54,20 +52,21 @@ template <> struct Mma<_Float16> {
     static __device__ __forceinline__ f32x16 mul(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
-// LDS: tiles of STEP rows (tokens) by 128 columns of 2 bytes.  A fragment of the matrix instruction has eight tokens of one
+// LDS: tiles of STEP rows (tokens) by COLS columns of 2 bytes.  A fragment of the matrix instruction has eight tokens of one
 // column in a lane, so it is read transposed (ds_read_b64_tr_b16: sixteen lanes read four rows of 16 columns and get four
-// tokens of a column each).  The four rows begin on the same bank, so the 64-byte pieces of a row are exchanged by the
-// row's two lowest bits.
-constexpr int ROW_BYTES = 256;
-__device__ __forceinline__ uint32_t lds_at(uint32_t row, uint32_t col) {
-    return row * ROW_BYTES + ((col / 32 ^ (row & 3)) * 64) + (col % 32) * 2;
+// tokens of a column each).  Rows begin on the same bank, so the 32-byte pieces of a row are exchanged by a pattern of the
+// row's two lowest bits: 0, 2, 5, 7 puts the pieces of four rows on different banks, and those of the next sixteen lanes, which
+// read the neighbouring 16 columns, on others again.
+template <int COLS> __device__ __forceinline__ uint32_t lds_at(uint32_t row, uint32_t col) {
+    const uint32_t r = row & 3;
+    return row * (COLS * 2) + ((col / 16 ^ (2 * r + (r >> 1))) * 32) + (col % 16) * 2;
 }
 
-template <typename Frag> __device__ __forceinline__ Frag read_fragment(const char* tile, uint32_t at) {
+template <int COLS, typename Frag> __device__ __forceinline__ Frag read_fragment(const char* tile, uint32_t at) {
     typedef __attribute__((address_space(3))) s16x4* lds;
     union { s16x4 half[2]; Frag whole; } u;
     u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at));
-    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at + 4 * ROW_BYTES));
+    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at + 4 * (COLS * 2)));
     return u.whole;
 }
 
@@ -93,59 +92,97 @@ template <typename T> __device__ __forceinline__ void split(const Raw8<T>& x, ty
     }
 }
 
-template <typename DyT, typename GradT>
-__global__ __launch_bounds__(THREADS) void linear_kernel(LinearArgs A) {
+// A workgroup's tile of dw and how it is taken: WAVES_O x WAVES_C wavefronts of 64 outputs by 64 channels each, STEP tokens at a
+// time through one of two buffers in LDS.
+template <typename DyT, int WAVES_O_, int WAVES_C_, int STEP_> struct Shape {
+    static constexpr int WAVES_O = WAVES_O_, WAVES_C = WAVES_C_, STEP = STEP_;
+    static constexpr int THREADS = WAVES_O * WAVES_C * 64;
+    static constexpr int TILE_O = WAVES_O * 64, TILE_C = WAVES_C * 64;
+    static constexpr int PARTS = Parts<DyT>::n;
+    static constexpr int DY_BYTES = STEP * TILE_O * 2, X_BYTES = STEP * TILE_C * 2;
+    static constexpr int BUFFER = PARTS * DY_BYTES + X_BYTES;
+    static constexpr int DY_VECS = STEP * TILE_O / VEC / THREADS;            // vectors that a thread brings
+    static constexpr int DY_ROWS = THREADS / (TILE_O / VEC);                 // rows that all threads bring at once
+    static constexpr int X_VECS = STEP * TILE_C / VEC / THREADS;
+    static constexpr int X_ROWS = THREADS / (TILE_C / VEC);
+    static constexpr int STEPS = GROUP / STEP;
+};
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <typename DyT, typename S> struct Staged { Raw8<DyT> dy[S::DY_VECS]; u32x2 q[S::X_VECS]; };
+
+// Tokens move from memory to registers, from there (binary32 cut into its parts, q widened) to LDS, and from LDS to the
+// matrix cores.  Two steps are on their way in registers and one in the other buffer while a step is multiplied; one
+// barrier a step.
+template <typename DyT, typename GradT, typename S>
+__global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     typedef typename Mma<DyT>::elem E;
     typedef typename Mma<DyT>::frag Frag;
-    constexpr int PARTS = Parts<DyT>::n;
-    constexpr int TILE_BYTES = STEP * ROW_BYTES;
-    __shared__ __align__(256) char lds[(PARTS + 1) * TILE_BYTES];
-    char* const lds_x = lds + PARTS * TILE_BYTES;
+    __shared__ __align__(256) char lds[2 * S::BUFFER];
 
-    const uint32_t split_no = blockIdx.x / A.tiles, tile = blockIdx.x - split_no * A.tiles;
+    // Consecutive workgroups go to the eight dies in turn; each die gets consecutive tiles, so that the tiles that share dy or q
+    // share its L2.
+    const uint32_t per_die = gridDim.x / 8;
+    const uint32_t id = blockIdx.x < per_die * 8 ? blockIdx.x % 8 * per_die + blockIdx.x / 8 : blockIdx.x;
+    const uint32_t split_no = id / A.tiles, tile = id - split_no * A.tiles;
     const uint32_t tile_o = tile / A.tiles_c, tile_c = tile - tile_o * A.tiles_c;
-    const int64_t o0 = static_cast<int64_t>(tile_o) * TILE_O, c0 = static_cast<int64_t>(tile_c) * TILE_C;
+    const int32_t o0 = tile_o * S::TILE_O, c0 = tile_c * S::TILE_C;
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint32_t wave_o = wave / 2 * 64, wave_c = wave % 2 * 64;
+    const uint32_t wave_o = wave / S::WAVES_C * 64, wave_c = wave % S::WAVES_C * 64;
 
-    // what a thread brings: of dy four vectors of 8 columns, of q two of 16
-    const uint32_t dy_col = threadIdx.x % 16 * 8, dy_row = threadIdx.x / 16;       // rows dy_row + 16 j
-    const uint32_t q_col = threadIdx.x % 8 * 16, q_row = threadIdx.x / 8;          // rows q_row + 32 j
-    const int dy_n = static_cast<int>(max(int64_t(0), min(A.outputs - o0 - dy_col, int64_t(VEC))));
-    const bool q_here = c0 + q_col < A.ld;
-    Raw8<DyT> dy[4];
-    u32x4 q[2];
-    auto fetch = [&](int64_t t0) {
+    const uint32_t dy_col = threadIdx.x % (S::TILE_O / VEC) * VEC, dy_row = threadIdx.x / (S::TILE_O / VEC);
+    const uint32_t q_col = threadIdx.x % (S::TILE_C / VEC) * VEC, q_row = threadIdx.x / (S::TILE_C / VEC);
+    const bool whole_tile = o0 + S::TILE_O <= A.outputs && c0 + S::TILE_C <= A.ld;
+    const int dy_n = max(0, min(A.outputs - o0 - static_cast<int32_t>(dy_col), VEC));
+    const bool q_here = c0 + static_cast<int64_t>(q_col) < A.ld;
+    const DyT* const dy_at = static_cast<const DyT*>(A.dy) + o0 + dy_col;
+    const int8_t* const q_at = A.q + c0 + q_col;
+
+    auto fetch = [&](Staged<DyT, S>& to, int32_t t0) {
+        if (whole_tile && t0 + S::STEP <= A.tokens) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t t = t0 + dy_row + 16 * j;
-            dy[j] = load8(static_cast<const DyT*>(A.dy) + t * A.dy_stride + o0 + dy_col, t < A.tokens ? dy_n : 0);
-        }
+            for (int j = 0; j < S::DY_VECS; ++j) to.dy[j] = load8(dy_at + static_cast<int64_t>(t0 + static_cast<int32_t>(dy_row) + S::DY_ROWS * j) * A.dy_stride);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t t = t0 + q_row + 32 * j;
-            q[j] = u32x4{0, 0, 0, 0};
-            if (q_here && t < A.tokens) q[j] = *reinterpret_cast<const u32x4*>(A.q + t * A.ld + c0 + q_col);
+            for (int j = 0; j < S::X_VECS; ++j)
+                to.q[j] = *reinterpret_cast<const u32x2*>(q_at + static_cast<int64_t>(t0 + static_cast<int32_t>(q_row) + S::X_ROWS * j) * A.ld);
+        } else {
+#pragma unroll
+            for (int j = 0; j < S::DY_VECS; ++j) {
+                const int32_t t = t0 + dy_row + S::DY_ROWS * j;
+                to.dy[j] = load8(dy_at + static_cast<int64_t>(t) * A.dy_stride, t < A.tokens ? dy_n : 0);
+            }
+#pragma unroll
+            for (int j = 0; j < S::X_VECS; ++j) {
+                const int32_t t = t0 + q_row + S::X_ROWS * j;
+                to.q[j] = u32x2{0, 0};
+                if (q_here && t < A.tokens) to.q[j] = *reinterpret_cast<const u32x2*>(q_at + static_cast<int64_t>(t) * A.ld);
+            }
         }
     };
-    auto put = [&] {
+    float bias[VEC] = {};
+    auto put = [&](const Staged<DyT, S>& from, char* buffer, bool add_bias) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            Frag part[PARTS];
-            split<DyT>(dy[j], part);
+        for (int j = 0; j < S::DY_VECS; ++j) {
+            Frag part[S::PARTS];
+            split<DyT>(from.dy[j], part);
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) *reinterpret_cast<Frag*>(lds + p * TILE_BYTES + lds_at(dy_row + 16 * j, dy_col)) = part[p];
+            for (int p = 0; p < S::PARTS; ++p)
+                *reinterpret_cast<Frag*>(buffer + p * S::DY_BYTES + lds_at<S::TILE_O>(dy_row + S::DY_ROWS * j, dy_col)) = part[p];
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < S::X_VECS; ++j) {
+            Frag x;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                Frag x;
+            for (int i = 0; i < VEC; ++i)
+                x[i] = static_cast<E>(static_cast<float>(static_cast<int32_t>(from.q[j][i / 4]) << (24 - 8 * (i % 4)) >> 24));
+            *reinterpret_cast<Frag*>(buffer + S::PARTS * S::DY_BYTES + lds_at<S::TILE_C>(q_row + S::X_ROWS * j, q_col)) = x;
+        }
+        if (add_bias)
 #pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    x[i] = static_cast<E>(static_cast<float>(static_cast<int32_t>(q[j][2 * h + i / 4]) << (24 - 8 * (i % 4)) >> 24));
-                *reinterpret_cast<Frag*>(lds_x + lds_at(q_row + 32 * j, q_col + 8 * h)) = x;
-            }
+            for (int j = 0; j < S::DY_VECS; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) bias[i] += get(from.dy[j], i);
     };
 
     // where a lane reads: rows 8 (lane / 32) + (lane % 16) / 4, columns 16 (lane / 16 % 2) + 4 (lane % 4) of a 32-column piece
@@ -153,45 +190,63 @@ __global__ __launch_bounds__(THREADS) void linear_kernel(LinearArgs A) {
     uint32_t at_o[2], at_c[2];
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
-        at_o[f] = lds_at(r, wave_o + f * 32 + cc);
-        at_c[f] = lds_at(r, wave_c + f * 32 + cc);
+        at_o[f] = lds_at<S::TILE_O>(r, wave_o + f * 32 + cc);
+        at_c[f] = lds_at<S::TILE_C>(r, wave_c + f * 32 + cc) + S::PARTS * S::DY_BYTES;
     }
+    f32x16 sum[2][2];
+    auto multiply = [&](const char* buffer, bool first) {
+#pragma unroll
+        for (int k = 0; k < S::STEP / 16; ++k) {
+            Frag x[2];
+#pragma unroll
+            for (int f = 0; f < 2; ++f) x[f] = read_fragment<S::TILE_C, Frag>(buffer, at_c[f] + k * 16 * (S::TILE_C * 2));
+#pragma unroll
+            for (int p = S::PARTS - 1; p >= 0; --p) {
+                Frag y[2];
+#pragma unroll
+                for (int f = 0; f < 2; ++f) y[f] = read_fragment<S::TILE_O, Frag>(buffer, at_o[f] + p * S::DY_BYTES + k * 16 * (S::TILE_O * 2));
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) sum[i][j] = Mma<DyT>::mul(y[i], x[j], first && k == 0 && p == S::PARTS - 1 ? f32x16{} : sum[i][j]);
+            }
+        }
+    };
 
     f32x16 total[2][2] = {};
-    const uint32_t g_first = split_no * A.groups_per_split, g_end = min(g_first + A.groups_per_split, A.groups);
-    if (g_first < g_end) fetch(static_cast<int64_t>(g_first) * GROUP);
-    for (uint32_t g = g_first; g < g_end; ++g) {
+    const int32_t t_first = split_no * A.groups_per_split * GROUP;
+    const int32_t t_end = min(A.tokens, static_cast<int32_t>((split_no + 1) * A.groups_per_split * GROUP));
+    const uint32_t share = A.db != nullptr && tile_c < A.bias_shares ? tile_c : ~0u;       // the steps whose bias this workgroup adds
+    uint32_t step = 0;
+    auto bias_due = [&] {
+        const bool due = step == share;
+        step = step + 1 == A.bias_shares ? 0 : step + 1;
+        return due;
+    };
+    Staged<DyT, S> staged[2];
+    if (t_first < t_end) {
+        fetch(staged[0], t_first);
+        if (t_first + S::STEP < t_end) fetch(staged[1], t_first + S::STEP);
+        put(staged[0], lds, bias_due());
+        if (t_first + 2 * S::STEP < t_end) fetch(staged[0], t_first + 2 * S::STEP);
+        __syncthreads();
+    }
+    for (int32_t t0 = t_first; t0 < t_end; t0 += GROUP) {
         float scale[2];
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-            const int64_t c = c0 + wave_c + f * 32 + lane % 32;
-            scale[f] = c < A.channels ? A.scale[g * A.ld + c] : 0.f;
+            const int32_t c = c0 + wave_c + f * 32 + lane % 32;
+            scale[f] = c < A.channels ? A.scale[t0 / GROUP * A.ld + c] : 0.f;
         }
-        f32x16 sum[2][2] = {};
-        for (int s = 0; s < GROUP / STEP; ++s) {
-            const int64_t t0 = static_cast<int64_t>(g) * GROUP + s * STEP;
-            if (t0 >= A.tokens) break;
-            __syncthreads();
-            put();
-            __syncthreads();
-            if (t0 + STEP < A.tokens && (s + 1 < GROUP / STEP || g + 1 < g_end)) fetch(t0 + STEP);
-            const int turns = static_cast<int>(min(int64_t(STEP / 16), (A.tokens - t0 + 15) / 16));
 #pragma unroll
-            for (int k = 0; k < STEP / 16; ++k) {
-                if (k >= turns) break;
-                Frag x[2];
-#pragma unroll
-                for (int f = 0; f < 2; ++f) x[f] = read_fragment<Frag>(lds_x, at_c[f] + k * 16 * ROW_BYTES);
-#pragma unroll
-                for (int p = PARTS - 1; p >= 0; --p) {
-                    Frag y[2];
-#pragma unroll
-                    for (int f = 0; f < 2; ++f) y[f] = read_fragment<Frag>(lds + p * TILE_BYTES, at_o[f] + k * 16 * ROW_BYTES);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) sum[i][j] = Mma<DyT>::mul(y[i], x[j], sum[i][j]);
-                }
+        for (int s = 0; s < S::STEPS; ++s) {
+            const int32_t t = t0 + s * S::STEP;
+            if (t < t_end) {
+                Staged<DyT, S>& next = staged[(s + 1) % 2];
+                if (t + S::STEP < t_end) put(next, lds + (s + 1) % 2 * S::BUFFER, bias_due());
+                if (t + 3 * S::STEP < t_end) fetch(next, t + 3 * S::STEP);
+                multiply(lds + s % 2 * S::BUFFER, s == 0);
+                __syncthreads();
             }
         }
 #pragma unroll
@@ -203,32 +258,70 @@ __global__ __launch_bounds__(THREADS) void linear_kernel(LinearArgs A) {
     }
 
     // element e of a lane: row 8 (e / 4) + 4 (lane / 32) + e % 4, column lane % 32
+    const bool direct = A.splits == 1;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j) {
+        const int32_t c = c0 + wave_c + j * 32 + lane % 32;
+        if (c >= A.channels) continue;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t c = c0 + wave_c + j * 32 + lane % 32;
-            if (c >= A.channels) continue;
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int64_t o = o0 + wave_o + i * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4;
-                if (o >= A.outputs) continue;
-                if (A.splits > 1) {
-                    A.partial[(static_cast<int64_t>(split_no) * A.outputs + o) * A.channels_padded + c] = total[i][j][e];
-                } else {
-                    GradT* const w = static_cast<GradT*>(A.dw) + o * A.dw_stride + c;
-                    const float had = A.accumulate ? static_cast<float>(*w) : 0.f;
-                    *w = rounded<GradT>(total[i][j][e] + had);
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const int32_t o = o0 + wave_o + i * 32 + e4 * 8 + lane / 32 * 4;
+                float* p = A.partial + (static_cast<int64_t>(split_no) * A.outputs + o) * A.channels_padded + c;
+                GradT* w = static_cast<GradT*>(A.dw) + o * A.dw_stride + c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (o + e < A.outputs) {
+                        const float x = total[i][j][e4 * 4 + e];
+                        if (!direct) *p = x;
+                        else if (A.accumulate) *w = rounded<GradT>(x + static_cast<float>(*w));
+                        else *w = rounded<GradT>(x);
+                    }
+                    p += A.channels_padded;
+                    w += A.dw_stride;
                 }
             }
+    }
+    if (share != ~0u) {                                  // the rows' sums of the bias, in order
+        float* const sums = reinterpret_cast<float*>(lds);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sums[dy_row * S::TILE_O + dy_col + i] = bias[i];
+        __syncthreads();
+        const int32_t o = o0 + threadIdx.x;
+        if (threadIdx.x < S::TILE_O && o < A.outputs) {
+            float all = 0.f;
+            for (int w = 0; w < S::DY_ROWS; ++w) all += sums[w * S::TILE_O + threadIdx.x];
+            if (A.splits * A.bias_shares > 1) {
+                A.bias_partial[static_cast<int64_t>(split_no * A.bias_shares + share) * A.outputs + o] = all;
+            } else {
+                GradT* const b = static_cast<GradT*>(A.db) + o;
+                *b = rounded<GradT>(all + (A.accumulate ? static_cast<float>(*b) : 0.f));
+            }
         }
+    }
 }
 
-// The splits' sums, in order.
-template <typename GradT> __global__ __launch_bounds__(THREADS) void linear_join_kernel(LinearArgs A) {
-    const int64_t c = (static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x) * 4;
+constexpr int JOIN_THREADS = 256;
+
+// The splits' sums, in order; the first rows of workgroups join the bias, too.
+template <typename GradT> __global__ __launch_bounds__(JOIN_THREADS) void linear_join_kernel(LinearArgs A) {
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * JOIN_THREADS + threadIdx.x;
+    if (A.db != nullptr && blockIdx.y == gridDim.y - 1) {
+        for (int64_t o = at; o < A.outputs; o += static_cast<int64_t>(gridDim.x) * JOIN_THREADS) {
+            float sum = 0.f;
+#pragma unroll 8
+            for (uint32_t s = 0; s < A.splits * A.bias_shares; ++s) sum += A.bias_partial[static_cast<int64_t>(s) * A.outputs + o];
+            GradT* const b = static_cast<GradT*>(A.db) + o;
+            *b = rounded<GradT>(sum + (A.accumulate ? static_cast<float>(*b) : 0.f));
+        }
+        return;
+    }
+    const int64_t c = at * 4;
     if (c >= A.channels) return;
-    for (int64_t o = blockIdx.y; o < A.outputs; o += gridDim.y) {
+    const uint32_t rows = gridDim.y - (A.db != nullptr ? 1 : 0);
+    for (int64_t o = blockIdx.y; o < A.outputs; o += rows) {
         f32x4 sum = *reinterpret_cast<const f32x4*>(A.partial + o * A.channels_padded + c);
 #pragma unroll 4
         for (uint32_t s = 1; s < A.splits; ++s)
@@ -240,70 +333,37 @@ template <typename GradT> __global__ __launch_bounds__(THREADS) void linear_join
     }
 }
 
-constexpr int BIAS_TOKENS = 256;       // tokens of a part
-
-// Column sums of dy: 128 columns of 256 tokens by a workgroup.
-template <typename DyT> __global__ __launch_bounds__(THREADS) void bias_kernel(LinearArgs A) {
-    const uint32_t lane = threadIdx.x % 16, row = threadIdx.x / 16;
-    const int64_t o = (static_cast<int64_t>(blockIdx.x) * 16 + lane) * VEC;
-    const int n = static_cast<int>(max(int64_t(0), min(A.outputs - o, int64_t(VEC))));
-    float sum[VEC] = {};
-#pragma unroll 8
-    for (int s = 0; s < BIAS_TOKENS / 16; ++s) {
-        const int64_t t = static_cast<int64_t>(blockIdx.y) * BIAS_TOKENS + s * 16 + row;
-        const Raw8<DyT> x = load8(static_cast<const DyT*>(A.dy) + t * A.dy_stride + o, t < A.tokens ? n : 0);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) sum[i] += get(x, i);
-    }
-    __shared__ float sums[16][16 * VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) sums[row][lane * VEC + i] = sum[i];
-    __syncthreads();
-    const int64_t out = static_cast<int64_t>(blockIdx.x) * 16 * VEC + threadIdx.x;
-    if (threadIdx.x < 16 * VEC && out < A.outputs) {
-        float all = 0.f;
-        for (int w = 0; w < 16; ++w) all += sums[w][threadIdx.x];
-        A.bias_partial[static_cast<int64_t>(blockIdx.y) * A.outputs + out] = all;
-    }
-}
-
-template <typename GradT> __global__ __launch_bounds__(THREADS) void bias_join_kernel(LinearArgs A) {
-    const int64_t o = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x;
-    if (o >= A.outputs) return;
-    float sum = 0.f;
-#pragma unroll 8
-    for (uint32_t s = 0; s < A.bias_parts; ++s) sum += A.bias_partial[static_cast<int64_t>(s) * A.outputs + o];
-    GradT* const b = static_cast<GradT*>(A.db) + o;
-    *b = rounded<GradT>(sum + (A.accumulate ? static_cast<float>(*b) : 0.f));
-}
+// The tiles: 256 outputs by 128 channels, 64 tokens a step; half of that where dy takes three parts.
+template <typename DyT> using Wide = Shape<DyT, 4, 2, sizeof(DyT) == 4 ? 32 : 64>;
+constexpr int TILE_O = 256, TILE_C = 128;
 
 struct LinearPlan {
-    uint32_t tiles_o, tiles_c, groups, splits, groups_per_split, bias_parts;
+    uint32_t tiles_o, tiles_c, groups, splits, groups_per_split, bias_shares;
     int64_t channels_padded, bias_at, bytes;
 };
 
 LinearPlan plan_of(int64_t tokens, int64_t channels, int64_t outputs) {
     LinearPlan p{};
     p.tiles_o = static_cast<uint32_t>(ceil_div(outputs, TILE_O));
-    p.tiles_c = static_cast<uint32_t>(ceil_div(channels, TILE_C));
+    p.tiles_c = static_cast<uint32_t>(std::max<int64_t>(ceil_div(channels, TILE_C), 1));       // the bias is made with some tile
     p.groups = static_cast<uint32_t>(ceil_div(tokens, GROUP));
     const int64_t tiles = static_cast<int64_t>(p.tiles_o) * p.tiles_c;
-    // enough workgroups for two on each of the 256 compute units, and two groups at the least for each of them
-    int64_t splits = std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), std::max<uint32_t>(p.groups / 2, 1), MAX_SPLITS});
+    // enough workgroups for each of the 256 compute units, and two groups at the least for each of them
+    int64_t splits = std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), std::max<uint32_t>(p.groups / 2, 1), MAX_SPLITS});
     splits = std::max<int64_t>(splits, 1);
     p.groups_per_split = static_cast<uint32_t>(ceil_div(std::max<uint32_t>(p.groups, 1), splits));
     p.splits = static_cast<uint32_t>(ceil_div(std::max<uint32_t>(p.groups, 1), p.groups_per_split));
+    p.bias_shares = p.splits > 1 ? std::min<uint32_t>(p.tiles_c, BIAS_SHARES) : 1;
     p.channels_padded = ceil_div(channels, 4) * 4;
-    p.bias_parts = static_cast<uint32_t>(ceil_div(std::max<int64_t>(tokens, 1), BIAS_TOKENS));
     const int64_t sums = p.splits > 1 ? p.splits * outputs * p.channels_padded * 4 : 0;
     p.bias_at = ceil_div(sums, 256) * 256;
-    p.bytes = p.bias_at + p.bias_parts * outputs * 4;
+    p.bytes = p.splits > 1 ? p.bias_at + static_cast<int64_t>(p.splits) * p.bias_shares * outputs * 4 : 0;
     return p;
 }
 
 bool sizes_ok(int64_t tokens, int64_t channels, int64_t outputs) {
     return tokens >= 0 && tokens <= (int64_t(1) << 23) && channels >= 0 && channels <= (int64_t(1) << 23) && outputs >= 0 &&
-           outputs <= (int64_t(1) << 23) && ceil_div(channels, TILE_C) * ceil_div(outputs, TILE_O) <= (int64_t(1) << 23);
+           outputs <= (int64_t(1) << 23) && ceil_div(channels, 128) * ceil_div(outputs, 128) <= (int64_t(1) << 22);
 }
 
 }  // namespace
@@ -347,32 +407,27 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
     a.dy_stride = dy_stride;
     a.ld = ld;
     a.dw_stride = dw_stride;
-    a.tokens = n_tokens;
-    a.channels = n_channels;
-    a.outputs = n_outputs;
+    a.tokens = static_cast<int32_t>(n_tokens);
+    a.channels = static_cast<int32_t>(n_channels);
+    a.outputs = static_cast<int32_t>(n_outputs);
     a.channels_padded = p.channels_padded;
     a.tiles_c = p.tiles_c;
     a.tiles = p.tiles_o * p.tiles_c;
     a.splits = p.splits;
     a.groups = p.groups;
     a.groups_per_split = p.groups_per_split;
-    a.bias_parts = p.bias_parts;
+    a.bias_shares = p.bias_shares;
     a.accumulate = accumulate != 0;
+    if (n_channels == 0) a.ld = 0;
+    const uint32_t rows = static_cast<uint32_t>(std::min<int64_t>(n_outputs, 32767)) + (d_db != nullptr ? 1 : 0);
+    const dim3 join_grid(static_cast<uint32_t>(std::max<int64_t>(ceil_div(n_channels, 4 * JOIN_THREADS), 1)), rows);
     return with_dtype(dy_dtype, [&](auto* dy_type) {
         return with_dtype(grad_dtype, [&](auto* grad_type) {
             typedef std::remove_pointer_t<decltype(dy_type)> DyT;
             typedef std::remove_pointer_t<decltype(grad_type)> GradT;
-            int rc = MGWFBP_OK;
-            if (n_channels > 0) rc = launch(linear_kernel<DyT, GradT>, a, dim3(a.tiles * a.splits), dim3(THREADS), hip_stream);
-            if (rc == MGWFBP_OK && n_channels > 0 && a.splits > 1)
-                rc = launch(linear_join_kernel<GradT>, a,
-                            dim3(static_cast<uint32_t>(ceil_div(n_channels, 4 * THREADS)), static_cast<uint32_t>(std::min<int64_t>(n_outputs, 65535))),
-                            dim3(THREADS), hip_stream);
-            if (rc == MGWFBP_OK && d_db != nullptr)
-                rc = launch(bias_kernel<DyT>, a, dim3(static_cast<uint32_t>(ceil_div(n_outputs, 16 * VEC)), a.bias_parts), dim3(THREADS), hip_stream);
-            if (rc == MGWFBP_OK && d_db != nullptr)
-                rc = launch(bias_join_kernel<GradT>, a, dim3(static_cast<uint32_t>(ceil_div(n_outputs, THREADS))), dim3(THREADS), hip_stream);
-            return rc;
+            const int rc = launch(linear_kernel<DyT, GradT, Wide<DyT>>, a, dim3(a.tiles * a.splits), dim3(Wide<DyT>::THREADS), hip_stream);
+            if (rc != MGWFBP_OK || a.splits == 1) return rc;
+            return launch(linear_join_kernel<GradT>, a, join_grid, dim3(JOIN_THREADS), hip_stream);
         });
     });
 }
