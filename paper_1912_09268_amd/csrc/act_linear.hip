@@ -36,7 +36,7 @@ struct LinearArgs {
     float* bias_partial;               // [splits * bias_shares][outputs]
     int64_t dy_stride, ld, dw_stride, channels_padded;
     int32_t tokens, channels, outputs;
-    uint32_t tiles_c, tiles, splits, groups, groups_per_split, bias_shares;
+    uint32_t tiles_c, tiles, splits, groups, groups_per_split, bias_shares, bias_blocks;
     int32_t accumulate;
 };
 
@@ -305,32 +305,33 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
 
 constexpr int JOIN_THREADS = 256;
 
-// The splits' sums, in order; the first rows of workgroups join the bias, too.
+// The splits' sums, in order: a thread takes four channels of an output.  The first bias_blocks workgroups join the bias.
 template <typename GradT> __global__ __launch_bounds__(JOIN_THREADS) void linear_join_kernel(LinearArgs A) {
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * JOIN_THREADS + threadIdx.x;
-    if (A.db != nullptr && blockIdx.y == gridDim.y - 1) {
-        for (int64_t o = at; o < A.outputs; o += static_cast<int64_t>(gridDim.x) * JOIN_THREADS) {
-            float sum = 0.f;
+    if (blockIdx.x < A.bias_blocks) {
+        const int32_t o = blockIdx.x * JOIN_THREADS + threadIdx.x;
+        if (o >= A.outputs) return;
+        float sum = 0.f;
 #pragma unroll 8
-            for (uint32_t s = 0; s < A.splits * A.bias_shares; ++s) sum += A.bias_partial[static_cast<int64_t>(s) * A.outputs + o];
-            GradT* const b = static_cast<GradT*>(A.db) + o;
-            *b = rounded<GradT>(sum + (A.accumulate ? static_cast<float>(*b) : 0.f));
-        }
+        for (uint32_t s = 0; s < A.splits * A.bias_shares; ++s) sum += A.bias_partial[static_cast<int64_t>(s) * A.outputs + o];
+        GradT* const b = static_cast<GradT*>(A.db) + o;
+        *b = rounded<GradT>(sum + (A.accumulate ? static_cast<float>(*b) : 0.f));
         return;
     }
-    const int64_t c = at * 4;
-    if (c >= A.channels) return;
-    const uint32_t rows = gridDim.y - (A.db != nullptr ? 1 : 0);
-    for (int64_t o = blockIdx.y; o < A.outputs; o += rows) {
-        f32x4 sum = *reinterpret_cast<const f32x4*>(A.partial + o * A.channels_padded + c);
+    const uint32_t at = (blockIdx.x - A.bias_blocks) * JOIN_THREADS + threadIdx.x;
+    const uint32_t vecs = static_cast<uint32_t>(A.channels_padded / 4);
+    const uint32_t o = at / vecs, c = (at - o * vecs) * 4;
+    if (o >= static_cast<uint32_t>(A.outputs)) return;
+    const float* p = A.partial + static_cast<int64_t>(o) * A.channels_padded + c;
+    const int64_t next = A.outputs * A.channels_padded;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll 4
-        for (uint32_t s = 1; s < A.splits; ++s)
-            sum += *reinterpret_cast<const f32x4*>(A.partial + (static_cast<int64_t>(s) * A.outputs + o) * A.channels_padded + c);
-        GradT* const w = static_cast<GradT*>(A.dw) + o * A.dw_stride + c;
+    for (uint32_t s = 1; s < A.splits; ++s) sum += *reinterpret_cast<const f32x4*>(p += next);
+    GradT* const w = static_cast<GradT*>(A.dw) + static_cast<int64_t>(o) * A.dw_stride + c;
+    if (A.accumulate)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (c + i < A.channels) w[i] = rounded<GradT>(sum[i] + (A.accumulate ? static_cast<float>(w[i]) : 0.f));
-    }
+            if (c + i < static_cast<uint32_t>(A.channels)) sum[i] += static_cast<float>(w[i]);
+    store4(w, sum, A.channels - static_cast<int32_t>(c));
 }
 
 // The tiles: 256 outputs by 128 channels, 64 tokens a step; half of that where dy takes three parts.
@@ -419,8 +420,9 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
     a.bias_shares = p.bias_shares;
     a.accumulate = accumulate != 0;
     if (n_channels == 0) a.ld = 0;
-    const uint32_t rows = static_cast<uint32_t>(std::min<int64_t>(n_outputs, 32767)) + (d_db != nullptr ? 1 : 0);
-    const dim3 join_grid(static_cast<uint32_t>(std::max<int64_t>(ceil_div(n_channels, 4 * JOIN_THREADS), 1)), rows);
+    // Split launches have at most 256 tiles of 256 x 128, so that the join's threads number less than 2^22.
+    a.bias_blocks = d_db != nullptr ? static_cast<uint32_t>(ceil_div(n_outputs, JOIN_THREADS)) : 0;
+    const dim3 join_grid(a.bias_blocks + static_cast<uint32_t>(p.splits > 1 ? ceil_div(n_outputs * (p.channels_padded / 4), JOIN_THREADS) : 0));
     return with_dtype(dy_dtype, [&](auto* dy_type) {
         return with_dtype(grad_dtype, [&](auto* grad_type) {
             typedef std::remove_pointer_t<decltype(dy_type)> DyT;

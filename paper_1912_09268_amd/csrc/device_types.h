@@ -89,6 +89,18 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
         if (i < n) p[i] = rounded<T>(x[i]);
 }
 
+// The first n of four results.
+template <typename T> __device__ __forceinline__ void store4(T* p, f32x4 x, int n) {
+    typedef T vec __attribute__((ext_vector_type(4), aligned(alignof(T))));
+    if (n >= 4) {
+        *reinterpret_cast<vec*>(p) = vec{rounded<T>(x[0]), rounded<T>(x[1]), rounded<T>(x[2]), rounded<T>(x[3])};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) p[i] = rounded<T>(x[i]);
+}
+
 // ---- host side -------------------------------------------------------------------------------
 
 inline bool is_dtype(int32_t t) { return t == MGWFBP_F32 || t == MGWFBP_BF16 || t == MGWFBP_F16; }
