@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "device_types.h"
 #include "mgwfbp_layers.h"
@@ -114,8 +115,10 @@ template <typename DyT, typename S> struct Staged { Raw8<DyT> dy[S::DY_VECS]; u3
 
 // Tokens move from memory to registers, from there (binary32 cut into its parts, q widened) to LDS, and from LDS to the
 // matrix cores.  Two steps are on their way in registers and one in the other buffer while a step is multiplied; one
-// barrier a step.
-template <typename DyT, typename GradT, typename S>
+// barrier a step.  RAGGED: the outputs are no multiple of eight, and the vector that holds the last ones is read element
+// by element (or there are no channels).  Other vectors behind the last output or channel are read from the last ones that exist: what they make
+// belongs to no element of dw.
+template <typename DyT, typename GradT, typename S, bool RAGGED>
 __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     typedef typename Mma<DyT>::elem E;
     typedef typename Mma<DyT>::frag Frag;
@@ -130,59 +133,76 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     const int32_t o0 = tile_o * S::TILE_O, c0 = tile_c * S::TILE_C;
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const uint32_t wave_o = wave / S::WAVES_C * 64, wave_c = wave % S::WAVES_C * 64;
+    const int32_t t_first = split_no * A.groups_per_split * GROUP;
+    const int32_t t_end = min(A.tokens, static_cast<int32_t>((split_no + 1) * A.groups_per_split * GROUP));
 
     const uint32_t dy_col = threadIdx.x % (S::TILE_O / VEC) * VEC, dy_row = threadIdx.x / (S::TILE_O / VEC);
     const uint32_t q_col = threadIdx.x % (S::TILE_C / VEC) * VEC, q_row = threadIdx.x / (S::TILE_C / VEC);
-    const bool whole_tile = o0 + S::TILE_O <= A.outputs && c0 + S::TILE_C <= A.ld;
-    const int dy_n = max(0, min(A.outputs - o0 - static_cast<int32_t>(dy_col), VEC));
-    const bool q_here = c0 + static_cast<int64_t>(q_col) < A.ld;
-    const DyT* const dy_at = static_cast<const DyT*>(A.dy) + o0 + dy_col;
-    const int8_t* const q_at = A.q + c0 + q_col;
+    const int32_t o_in = o0 + static_cast<int32_t>(dy_col);
+    const int dy_n = RAGGED ? max(0, min(A.outputs - o_in, VEC)) : VEC;
+    const DyT* const dy_at = static_cast<const DyT*>(A.dy) + (RAGGED ? o_in : min(o_in, A.outputs - VEC));
+    const int8_t* const q_at = A.q + min(static_cast<int64_t>(c0 + q_col), A.ld - VEC);
 
-    auto fetch = [&](Staged<DyT, S>& to, int32_t t0) {
-        if (whole_tile && t0 + S::STEP <= A.tokens) {
+    const DyT* dy_next = dy_at + (t_first + static_cast<int64_t>(dy_row)) * A.dy_stride;      // the rows that are fetched next
+    const int8_t* q_next = q_at + (t_first + static_cast<int64_t>(q_row)) * A.ld;
+    int32_t t_next = t_first;
+
+    // The next STEP rows; rows behind the last token are zeros.
+    auto fetch = [&](Staged<DyT, S>& to, auto steady) {
+        if (decltype(steady)::value || t_next + S::STEP <= A.tokens) {
 #pragma unroll
-            for (int j = 0; j < S::DY_VECS; ++j) to.dy[j] = load8(dy_at + static_cast<int64_t>(t0 + static_cast<int32_t>(dy_row) + S::DY_ROWS * j) * A.dy_stride);
+            for (int j = 0; j < S::DY_VECS; ++j) to.dy[j] = load8(dy_next + j * (S::DY_ROWS * A.dy_stride), dy_n);
 #pragma unroll
             for (int j = 0; j < S::X_VECS; ++j)
-                to.q[j] = *reinterpret_cast<const u32x2*>(q_at + static_cast<int64_t>(t0 + static_cast<int32_t>(q_row) + S::X_ROWS * j) * A.ld);
+                if (!RAGGED || A.ld > 0) to.q[j] = *reinterpret_cast<const u32x2*>(q_next + j * (S::X_ROWS * A.ld));
         } else {
+            const int32_t dy_rows = A.tokens - t_next - static_cast<int32_t>(dy_row), q_rows = A.tokens - t_next - static_cast<int32_t>(q_row);
 #pragma unroll
-            for (int j = 0; j < S::DY_VECS; ++j) {
-                const int32_t t = t0 + dy_row + S::DY_ROWS * j;
-                to.dy[j] = load8(dy_at + static_cast<int64_t>(t) * A.dy_stride, t < A.tokens ? dy_n : 0);
-            }
+            for (int j = 0; j < S::DY_VECS; ++j) to.dy[j] = load8(dy_next + j * (S::DY_ROWS * A.dy_stride), S::DY_ROWS * j < dy_rows ? dy_n : 0);
 #pragma unroll
             for (int j = 0; j < S::X_VECS; ++j) {
-                const int32_t t = t0 + q_row + S::X_ROWS * j;
                 to.q[j] = u32x2{0, 0};
-                if (q_here && t < A.tokens) to.q[j] = *reinterpret_cast<const u32x2*>(q_at + static_cast<int64_t>(t) * A.ld);
+                if ((!RAGGED || A.ld > 0) && S::X_ROWS * j < q_rows) to.q[j] = *reinterpret_cast<const u32x2*>(q_next + j * (S::X_ROWS * A.ld));
             }
         }
+        t_next += S::STEP;
+        dy_next += S::STEP * A.dy_stride;
+        q_next += S::STEP * A.ld;
+    };
+    // The pieces of a step on the way to LDS: a vector of dy, or of q.
+    auto put_dy = [&](const Staged<DyT, S>& from, char* buffer, int j) {
+        Frag part[S::PARTS];
+        split<DyT>(from.dy[j], part);
+#pragma unroll
+        for (int p = 0; p < S::PARTS; ++p)
+            *reinterpret_cast<Frag*>(buffer + p * S::DY_BYTES + lds_at<S::TILE_O>(dy_row + S::DY_ROWS * j, dy_col)) = part[p];
+    };
+    auto put_q = [&](const Staged<DyT, S>& from, char* buffer, int j) {
+        Frag x;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            x[i] = static_cast<E>(static_cast<float>(static_cast<int32_t>(from.q[j][i / 4]) << (24 - 8 * (i % 4)) >> 24));
+        *reinterpret_cast<Frag*>(buffer + S::PARTS * S::DY_BYTES + lds_at<S::TILE_C>(q_row + S::X_ROWS * j, q_col)) = x;
+    };
+    constexpr int TURNS = S::STEP / 16;
+    auto put_some = [&](const Staged<DyT, S>& from, char* buffer, int turn) {          // a step in TURNS parts
+#pragma unroll
+        for (int j = 0; j < S::DY_VECS; ++j)
+            if (j * TURNS / S::DY_VECS == turn) put_dy(from, buffer, j);
+#pragma unroll
+        for (int j = 0; j < S::X_VECS; ++j)
+            if (j * TURNS / S::X_VECS == turn) put_q(from, buffer, j);
     };
     float bias[VEC] = {};
-    auto put = [&](const Staged<DyT, S>& from, char* buffer, bool add_bias) {
-#pragma unroll
-        for (int j = 0; j < S::DY_VECS; ++j) {
-            Frag part[S::PARTS];
-            split<DyT>(from.dy[j], part);
-#pragma unroll
-            for (int p = 0; p < S::PARTS; ++p)
-                *reinterpret_cast<Frag*>(buffer + p * S::DY_BYTES + lds_at<S::TILE_O>(dy_row + S::DY_ROWS * j, dy_col)) = part[p];
-        }
-#pragma unroll
-        for (int j = 0; j < S::X_VECS; ++j) {
-            Frag x;
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                x[i] = static_cast<E>(static_cast<float>(static_cast<int32_t>(from.q[j][i / 4]) << (24 - 8 * (i % 4)) >> 24));
-            *reinterpret_cast<Frag*>(buffer + S::PARTS * S::DY_BYTES + lds_at<S::TILE_C>(q_row + S::X_ROWS * j, q_col)) = x;
-        }
-        if (add_bias)
+    const uint32_t share = A.db != nullptr && tile_c < A.bias_shares ? tile_c : ~0u;       // the steps whose bias this workgroup adds
+    uint32_t step = 0;
+    auto add_bias = [&](const Staged<DyT, S>& from) {
+        if (step == share)
 #pragma unroll
             for (int j = 0; j < S::DY_VECS; ++j)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) bias[i] += get(from.dy[j], i);
+        step = step + 1 == A.bias_shares ? 0 : step + 1;
     };
 
     // where a lane reads: rows 8 (lane / 32) + (lane % 16) / 4, columns 16 (lane / 16 % 2) + 4 (lane % 4) of a 32-column piece
@@ -194,44 +214,44 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
         at_c[f] = lds_at<S::TILE_C>(r, wave_c + f * 32 + cc) + S::PARTS * S::DY_BYTES;
     }
     f32x16 sum[2][2];
-    auto multiply = [&](const char* buffer, bool first) {
+    // One step, in TURNS * PARTS turns of four products; the fragments of a turn are read during the one before.  Between them, the
+    // next step is put into the other buffer.  (The turns are kept apart: moved into each other they take more registers
+    // than there are.)
+    auto multiply = [&](const char* buffer, bool first, auto&& between) {
+        Frag x[2][2], y[2][2];
+        auto read = [&](int u) {
+            const int k = u / S::PARTS, p = S::PARTS - 1 - u % S::PARTS;
 #pragma unroll
-        for (int k = 0; k < S::STEP / 16; ++k) {
-            Frag x[2];
-#pragma unroll
-            for (int f = 0; f < 2; ++f) x[f] = read_fragment<S::TILE_C, Frag>(buffer, at_c[f] + k * 16 * (S::TILE_C * 2));
-#pragma unroll
-            for (int p = S::PARTS - 1; p >= 0; --p) {
-                Frag y[2];
-#pragma unroll
-                for (int f = 0; f < 2; ++f) y[f] = read_fragment<S::TILE_O, Frag>(buffer, at_o[f] + p * S::DY_BYTES + k * 16 * (S::TILE_O * 2));
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) sum[i][j] = Mma<DyT>::mul(y[i], x[j], first && k == 0 && p == S::PARTS - 1 ? f32x16{} : sum[i][j]);
+            for (int f = 0; f < 2; ++f) {
+                if (u % S::PARTS == 0) x[k % 2][f] = read_fragment<S::TILE_C, Frag>(buffer, at_c[f] + k * 16 * (S::TILE_C * 2));
+                y[u % 2][f] = read_fragment<S::TILE_O, Frag>(buffer, at_o[f] + p * S::DY_BYTES + k * 16 * (S::TILE_O * 2));
             }
+        };
+        read(0);
+#pragma unroll
+        for (int u = 0; u < TURNS * S::PARTS; ++u) {
+            if (u + 1 < TURNS * S::PARTS) read(u + 1);
+            if (u % S::PARTS == 0) between(u / S::PARTS);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) sum[i][j] = Mma<DyT>::mul(y[u % 2][i], x[u / S::PARTS % 2][j], first && u == 0 ? f32x16{} : sum[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
     f32x16 total[2][2] = {};
-    const int32_t t_first = split_no * A.groups_per_split * GROUP;
-    const int32_t t_end = min(A.tokens, static_cast<int32_t>((split_no + 1) * A.groups_per_split * GROUP));
-    const uint32_t share = A.db != nullptr && tile_c < A.bias_shares ? tile_c : ~0u;       // the steps whose bias this workgroup adds
-    uint32_t step = 0;
-    auto bias_due = [&] {
-        const bool due = step == share;
-        step = step + 1 == A.bias_shares ? 0 : step + 1;
-        return due;
-    };
     Staged<DyT, S> staged[2];
     if (t_first < t_end) {
-        fetch(staged[0], t_first);
-        if (t_first + S::STEP < t_end) fetch(staged[1], t_first + S::STEP);
-        put(staged[0], lds, bias_due());
-        if (t_first + 2 * S::STEP < t_end) fetch(staged[0], t_first + 2 * S::STEP);
+        fetch(staged[0], std::false_type());
+        if (t_first + S::STEP < t_end) fetch(staged[1], std::false_type());
+        add_bias(staged[0]);
+#pragma unroll
+        for (int k = 0; k < TURNS; ++k) put_some(staged[0], lds, k);
+        if (t_first + 2 * S::STEP < t_end) fetch(staged[0], std::false_type());
         __syncthreads();
     }
-    for (int32_t t0 = t_first; t0 < t_end; t0 += GROUP) {
+    auto group = [&](int32_t t0, auto steady) {
         float scale[2];
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
@@ -241,11 +261,23 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
 #pragma unroll
         for (int s = 0; s < S::STEPS; ++s) {
             const int32_t t = t0 + s * S::STEP;
-            if (t < t_end) {
-                Staged<DyT, S>& next = staged[(s + 1) % 2];
-                if (t + S::STEP < t_end) put(next, lds + (s + 1) % 2 * S::BUFFER, bias_due());
-                if (t + 3 * S::STEP < t_end) fetch(next, t + 3 * S::STEP);
-                multiply(lds + s % 2 * S::BUFFER, s == 0);
+            Staged<DyT, S>& next = staged[(s + 1) % 2];
+            char* const other = lds + (s + 1) % 2 * S::BUFFER;
+            const char* const own = lds + s % 2 * S::BUFFER;
+            if constexpr (decltype(steady)::value) {
+                add_bias(next);
+                multiply(own, s == 0, [&](int k) { put_some(next, other, k); });
+                fetch(next, steady);
+                __syncthreads();
+            } else if (t < t_end) {
+                const bool more = t + S::STEP < t_end;
+                if (more) {
+                    add_bias(next);
+#pragma unroll
+                    for (int k = 0; k < TURNS; ++k) put_some(next, other, k);
+                }
+                if (t + 3 * S::STEP < t_end) fetch(next, steady);
+                multiply(own, s == 0, [](int) {});
                 __syncthreads();
             }
         }
@@ -255,7 +287,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) total[i][j][e] = __builtin_fmaf(scale[j], sum[i][j][e], total[i][j][e]);
-    }
+    };
+    int32_t t0 = t_first;
+    for (; t0 + GROUP + 3 * S::STEP <= t_end; t0 += GROUP) group(t0, std::true_type());     // every step of it has three behind it
+    for (; t0 < t_end; t0 += GROUP) group(t0, std::false_type());
 
     // element e of a lane: row 8 (e / 4) + 4 (lane / 32) + e % 4, column lane % 32
     const bool direct = A.splits == 1;
@@ -419,7 +454,7 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
     a.groups_per_split = p.groups_per_split;
     a.bias_shares = p.bias_shares;
     a.accumulate = accumulate != 0;
-    if (n_channels == 0) a.ld = 0;
+    if (n_channels == 0) a.ld = 0;                       // no q: the bias alone
     // Split launches have at most 256 tiles of 256 x 128, so that the join's threads number less than 2^22.
     a.bias_blocks = d_db != nullptr ? static_cast<uint32_t>(ceil_div(n_outputs, JOIN_THREADS)) : 0;
     const dim3 join_grid(a.bias_blocks + static_cast<uint32_t>(p.splits > 1 ? ceil_div(n_outputs * (p.channels_padded / 4), JOIN_THREADS) : 0));
@@ -427,7 +462,8 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
         return with_dtype(grad_dtype, [&](auto* grad_type) {
             typedef std::remove_pointer_t<decltype(dy_type)> DyT;
             typedef std::remove_pointer_t<decltype(grad_type)> GradT;
-            const int rc = launch(linear_kernel<DyT, GradT, Wide<DyT>>, a, dim3(a.tiles * a.splits), dim3(Wide<DyT>::THREADS), hip_stream);
+            void (*kernel)(LinearArgs) = n_outputs % VEC != 0 || a.ld == 0 ? linear_kernel<DyT, GradT, Wide<DyT>, true> : linear_kernel<DyT, GradT, Wide<DyT>, false>;
+            const int rc = launch(kernel, a, dim3(a.tiles * a.splits), dim3(Wide<DyT>::THREADS), hip_stream);
             if (rc != MGWFBP_OK || a.splits == 1) return rc;
             return launch(linear_join_kernel<GradT>, a, join_grid, dim3(JOIN_THREADS), hip_stream);
         });
