@@ -94,9 +94,10 @@ template <typename T> __device__ __forceinline__ void split(const Raw8<T>& x, ty
 }
 
 // A workgroup's tile of dw and how it is taken: WAVES_O x WAVES_C wavefronts of 64 outputs by 64 channels each, STEP tokens at a
-// time through one of two buffers in LDS.
-template <typename DyT, int WAVES_O_, int WAVES_C_, int STEP_> struct Shape {
-    static constexpr int WAVES_O = WAVES_O_, WAVES_C = WAVES_C_, STEP = STEP_;
+// time through one of BUFFERS buffers in LDS.
+template <typename DyT, int WAVES_O_, int WAVES_C_, int STEP_, int BUFFERS_> struct Shape {
+    static constexpr int WAVES_O = WAVES_O_, WAVES_C = WAVES_C_, STEP = STEP_, BUFFERS = BUFFERS_;
+    static constexpr int AHEAD = BUFFERS - 1;                                // steps between LDS and the matrix cores
     static constexpr int THREADS = WAVES_O * WAVES_C * 64;
     static constexpr int TILE_O = WAVES_O * 64, TILE_C = WAVES_C * 64;
     static constexpr int PARTS = Parts<DyT>::n;
@@ -114,15 +115,16 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 template <typename DyT, typename S> struct Staged { Raw8<DyT> dy[S::DY_VECS]; u32x2 q[S::X_VECS]; };
 
 // Tokens move from memory to registers, from there (binary32 cut into its parts, q widened) to LDS, and from LDS to the
-// matrix cores.  Two steps are on their way in registers and one in the other buffer while a step is multiplied; one
-// barrier a step.  RAGGED: the outputs are no multiple of eight, and the vector that holds the last ones is read element
+// matrix cores.  Two steps are on their way in registers and AHEAD in the other buffers while a step is multiplied; one
+// barrier a step.  With three buffers a step's first fragments are read before the barrier that ends the step before, so that
+// the matrix cores go on right behind it.  RAGGED: the outputs are no multiple of eight, and the vector that holds the last ones is read element
 // by element (or there are no channels).  Other vectors behind the last output or channel are read from the last ones that exist: what they make
 // belongs to no element of dw.
 template <typename DyT, typename GradT, typename S, bool RAGGED>
 __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     typedef typename Mma<DyT>::elem E;
     typedef typename Mma<DyT>::frag Frag;
-    __shared__ __align__(256) char lds[2 * S::BUFFER];
+    __shared__ __align__(256) char lds[S::BUFFERS * S::BUFFER];
 
     // Consecutive workgroups go to the eight dies in turn; each die gets consecutive tiles, so that the tiles that share dy or q
     // share its L2.
@@ -214,23 +216,25 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
         at_c[f] = lds_at<S::TILE_C>(r, wave_c + f * 32 + cc) + S::PARTS * S::DY_BYTES;
     }
     f32x16 sum[2][2];
-    // One step, in TURNS * PARTS turns of four products; the fragments of a turn are read during the one before.  Between them, the
-    // next step is put into the other buffer.  (The turns are kept apart: moved into each other they take more registers
-    // than there are.)
-    auto multiply = [&](const char* buffer, bool first, auto&& between) {
-        Frag x[2][2], y[2][2];
-        auto read = [&](int u) {
-            const int k = u / S::PARTS, p = S::PARTS - 1 - u % S::PARTS;
+    // One step, in UNITS turns of four products; the fragments of a turn are read during the one before.  Between them, a later
+    // step is put into its buffer.  (The turns are kept apart: moved into each other they take more registers than there
+    // are.)
+    constexpr int UNITS = TURNS * S::PARTS;
+    Frag x[2][2], y[2][2];
+    auto read = [&](uint32_t buffer, int u) {
+        const int k = u / S::PARTS, p = S::PARTS - 1 - u % S::PARTS;
 #pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                if (u % S::PARTS == 0) x[k % 2][f] = read_fragment<S::TILE_C, Frag>(buffer, at_c[f] + k * 16 * (S::TILE_C * 2));
-                y[u % 2][f] = read_fragment<S::TILE_O, Frag>(buffer, at_o[f] + p * S::DY_BYTES + k * 16 * (S::TILE_O * 2));
-            }
-        };
-        read(0);
+        for (int f = 0; f < 2; ++f) {
+            if (u % S::PARTS == 0) x[k % 2][f] = read_fragment<S::TILE_C, Frag>(lds + buffer, at_c[f] + k * 16 * (S::TILE_C * 2));
+            y[u % 2][f] = read_fragment<S::TILE_O, Frag>(lds + buffer, at_o[f] + p * S::DY_BYTES + k * 16 * (S::TILE_O * 2));
+        }
+    };
+    auto multiply = [&](uint32_t buffer, uint32_t after, bool first, auto&& between) {
+        if constexpr (S::AHEAD == 1) read(buffer, 0);
 #pragma unroll
-        for (int u = 0; u < TURNS * S::PARTS; ++u) {
-            if (u + 1 < TURNS * S::PARTS) read(u + 1);
+        for (int u = 0; u < UNITS; ++u) {
+            if (u + 1 < UNITS) read(buffer, u + 1);
+            else if constexpr (S::AHEAD > 1) read(after, 0);
             if (u % S::PARTS == 0) between(u / S::PARTS);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -239,47 +243,56 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    static_assert(S::AHEAD == 1 || (UNITS % 2 == 0 && TURNS % 2 == 0), "a step's first fragments go where its first turn looks for them");
 
     f32x16 total[2][2] = {};
     Staged<DyT, S> staged[2];
-    if (t_first < t_end) {
-        fetch(staged[0], std::false_type());
-        if (t_first + S::STEP < t_end) fetch(staged[1], std::false_type());
-        add_bias(staged[0]);
+    uint32_t buffer = 0;                                      // that of the present step
+    auto behind = [&](int n) {                                // that of the n-th step after it
+        const uint32_t at = buffer + n * S::BUFFER;
+        return at < S::BUFFERS * S::BUFFER ? at : at - S::BUFFERS * S::BUFFER;
+    };
+    const int32_t steps = (t_end - t_first + S::STEP - 1) / S::STEP;
+    if (steps > 0) {
 #pragma unroll
-        for (int k = 0; k < TURNS; ++k) put_some(staged[0], lds, k);
-        if (t_first + 2 * S::STEP < t_end) fetch(staged[0], std::false_type());
+        for (int n = 0; n < S::AHEAD + 2; ++n) {
+            if (n >= 2 && n - 2 < steps) {
+                add_bias(staged[n % 2]);
+#pragma unroll
+                for (int k = 0; k < TURNS; ++k) put_some(staged[n % 2], lds + (n - 2) * S::BUFFER, k);
+            }
+            if (n < steps) fetch(staged[n % 2], std::false_type());
+        }
         __syncthreads();
+        if constexpr (S::AHEAD > 1) read(0, 0);
     }
-    auto group = [&](int32_t t0, auto steady) {
+    auto group = [&](int32_t at, auto steady) {               // the steps from `at`, a group's first
         float scale[2];
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
             const int32_t c = c0 + wave_c + f * 32 + lane % 32;
-            scale[f] = c < A.channels ? A.scale[t0 / GROUP * A.ld + c] : 0.f;
+            scale[f] = c < A.channels ? A.scale[(t_first / GROUP + at / S::STEPS) * A.ld + c] : 0.f;
         }
 #pragma unroll
         for (int s = 0; s < S::STEPS; ++s) {
-            const int32_t t = t0 + s * S::STEP;
-            Staged<DyT, S>& next = staged[(s + 1) % 2];
-            char* const other = lds + (s + 1) % 2 * S::BUFFER;
-            const char* const own = lds + s % 2 * S::BUFFER;
+            Staged<DyT, S>& later = staged[(s + S::AHEAD) % 2];
+            const uint32_t to = behind(S::AHEAD), after = behind(1);
             if constexpr (decltype(steady)::value) {
-                add_bias(next);
-                multiply(own, s == 0, [&](int k) { put_some(next, other, k); });
-                fetch(next, steady);
+                add_bias(later);
+                multiply(buffer, after, s == 0, [&](int k) { put_some(later, lds + to, k); });
+                fetch(later, steady);
                 __syncthreads();
-            } else if (t < t_end) {
-                const bool more = t + S::STEP < t_end;
-                if (more) {
-                    add_bias(next);
+            } else if (at + s < steps) {
+                if (at + s + S::AHEAD < steps) {
+                    add_bias(later);
 #pragma unroll
-                    for (int k = 0; k < TURNS; ++k) put_some(next, other, k);
+                    for (int k = 0; k < TURNS; ++k) put_some(later, lds + to, k);
                 }
-                if (t + 3 * S::STEP < t_end) fetch(next, steady);
-                multiply(own, s == 0, [](int) {});
+                if (at + s + S::AHEAD + 2 < steps) fetch(later, steady);
+                multiply(buffer, after, s == 0, [](int) {});             // behind the last step: fragments that nothing uses
                 __syncthreads();
             }
+            buffer = after;
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -288,9 +301,10 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) total[i][j][e] = __builtin_fmaf(scale[j], sum[i][j][e], total[i][j][e]);
     };
-    int32_t t0 = t_first;
-    for (; t0 + GROUP + 3 * S::STEP <= t_end; t0 += GROUP) group(t0, std::true_type());     // every step of it has three behind it
-    for (; t0 < t_end; t0 += GROUP) group(t0, std::false_type());
+    int32_t at = 0;
+    // as long as every step of a group has AHEAD + 2 whole ones behind it
+    for (; (at + S::STEPS + S::AHEAD + 2) * S::STEP <= t_end - t_first; at += S::STEPS) group(at, std::true_type());
+    for (; at < steps; at += S::STEPS) group(at, std::false_type());
 
     // element e of a lane: row 8 (e / 4) + 4 (lane / 32) + e % 4, column lane % 32
     const bool direct = A.splits == 1;
@@ -369,8 +383,8 @@ template <typename GradT> __global__ __launch_bounds__(JOIN_THREADS) void linear
     store4(w, sum, A.channels - static_cast<int32_t>(c));
 }
 
-// The tiles: 256 outputs by 128 channels, 64 tokens a step; half of that where dy takes three parts.
-template <typename DyT> using Wide = Shape<DyT, 4, 2, sizeof(DyT) == 4 ? 32 : 64>;
+// The tiles: 256 outputs by 128 channels, 64 tokens a step, 144 KiB of LDS; where dy takes three parts 32 tokens and 112 KiB.
+template <typename DyT> using Wide = Shape<DyT, 4, 2, sizeof(DyT) == 4 ? 32 : 64, sizeof(DyT) == 4 ? 2 : 3>;
 constexpr int TILE_O = 256, TILE_C = 128;
 
 struct LinearPlan {
