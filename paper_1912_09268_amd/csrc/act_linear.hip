@@ -114,6 +114,49 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 template <typename DyT, typename S> struct Staged { Raw8<DyT> dy[S::DY_VECS]; u32x2 q[S::X_VECS]; };
 
+// The pieces of a step on the way to LDS: a vector of dy, or of q.
+template <typename DyT, typename S> __device__ __forceinline__ void put_dy(const Staged<DyT, S>& from, char* buffer, int j, uint32_t row, uint32_t col) {
+    typename Mma<DyT>::frag part[S::PARTS];
+    split<DyT>(from.dy[j], part);
+#pragma unroll
+    for (int p = 0; p < S::PARTS; ++p)
+        *reinterpret_cast<typename Mma<DyT>::frag*>(buffer + p * S::DY_BYTES + lds_at<S::TILE_O>(row + S::DY_ROWS * j, col)) = part[p];
+}
+template <typename DyT, typename S> __device__ __forceinline__ void put_q(const Staged<DyT, S>& from, char* buffer, int j, uint32_t row, uint32_t col) {
+    typename Mma<DyT>::frag x;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+        x[i] = static_cast<typename Mma<DyT>::elem>(static_cast<float>(static_cast<int32_t>(from.q[j][i / 4]) << (24 - 8 * (i % 4)) >> 24));
+    *reinterpret_cast<typename Mma<DyT>::frag*>(buffer + S::PARTS * S::DY_BYTES + lds_at<S::TILE_C>(row + S::X_ROWS * j, col)) = x;
+}
+template <typename DyT, typename S>
+__device__ __forceinline__ void put_step(const Staged<DyT, S>& from, char* buffer, uint32_t dy_row, uint32_t dy_col, uint32_t q_row, uint32_t q_col) {
+#pragma unroll
+    for (int j = 0; j < S::DY_VECS; ++j) put_dy<DyT, S>(from, buffer, j, dy_row, dy_col);
+#pragma unroll
+    for (int j = 0; j < S::X_VECS; ++j) put_q<DyT, S>(from, buffer, j, q_row, q_col);
+}
+
+// The threads' sums of a tile's outputs, added in the order of their rows: to db, or as a part of the bias.
+template <typename GradT, typename S>
+__device__ __forceinline__ void write_bias(const LinearArgs& A, float* sums, const float (&bias)[VEC], int32_t o0, uint32_t row, uint32_t col, void* db,
+                                           uint32_t part) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sums[row * S::TILE_O + col + i] = bias[i];
+    __syncthreads();
+    const int32_t o = o0 + threadIdx.x;
+    if (threadIdx.x >= S::TILE_O || o >= A.outputs) return;
+    float all = 0.f;
+    for (int w = 0; w < S::DY_ROWS; ++w) all += sums[w * S::TILE_O + threadIdx.x];
+    if (db == nullptr) {
+        A.bias_partial[static_cast<int64_t>(part) * A.outputs + o] = all;
+    } else {
+        GradT* const b = static_cast<GradT*>(db) + o;
+        *b = rounded<GradT>(all + (A.accumulate ? static_cast<float>(*b) : 0.f));
+    }
+}
+
 // Tokens move from memory to registers, from there (binary32 cut into its parts, q widened) to LDS, and from LDS to the
 // matrix cores.  Two steps are on their way in registers and AHEAD in the other buffers while a step is multiplied; one
 // barrier a step.  With three buffers a step's first fragments are read before the barrier that ends the step before, so that
@@ -122,7 +165,6 @@ template <typename DyT, typename S> struct Staged { Raw8<DyT> dy[S::DY_VECS]; u3
 // belongs to no element of dw.
 template <typename DyT, typename GradT, typename S, bool RAGGED>
 __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
-    typedef typename Mma<DyT>::elem E;
     typedef typename Mma<DyT>::frag Frag;
     __shared__ __align__(256) char lds[S::BUFFERS * S::BUFFER];
 
@@ -171,29 +213,14 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
         dy_next += S::STEP * A.dy_stride;
         q_next += S::STEP * A.ld;
     };
-    // The pieces of a step on the way to LDS: a vector of dy, or of q.
-    auto put_dy = [&](const Staged<DyT, S>& from, char* buffer, int j) {
-        Frag part[S::PARTS];
-        split<DyT>(from.dy[j], part);
-#pragma unroll
-        for (int p = 0; p < S::PARTS; ++p)
-            *reinterpret_cast<Frag*>(buffer + p * S::DY_BYTES + lds_at<S::TILE_O>(dy_row + S::DY_ROWS * j, dy_col)) = part[p];
-    };
-    auto put_q = [&](const Staged<DyT, S>& from, char* buffer, int j) {
-        Frag x;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i)
-            x[i] = static_cast<E>(static_cast<float>(static_cast<int32_t>(from.q[j][i / 4]) << (24 - 8 * (i % 4)) >> 24));
-        *reinterpret_cast<Frag*>(buffer + S::PARTS * S::DY_BYTES + lds_at<S::TILE_C>(q_row + S::X_ROWS * j, q_col)) = x;
-    };
     constexpr int TURNS = S::STEP / 16;
     auto put_some = [&](const Staged<DyT, S>& from, char* buffer, int turn) {          // a step in TURNS parts
 #pragma unroll
         for (int j = 0; j < S::DY_VECS; ++j)
-            if (j * TURNS / S::DY_VECS == turn) put_dy(from, buffer, j);
+            if (j * TURNS / S::DY_VECS == turn) put_dy<DyT, S>(from, buffer, j, dy_row, dy_col);
 #pragma unroll
         for (int j = 0; j < S::X_VECS; ++j)
-            if (j * TURNS / S::X_VECS == turn) put_q(from, buffer, j);
+            if (j * TURNS / S::X_VECS == turn) put_q<DyT, S>(from, buffer, j, q_row, q_col);
     };
     float bias[VEC] = {};
     const uint32_t share = A.db != nullptr && tile_c < A.bias_shares ? tile_c : ~0u;       // the steps whose bias this workgroup adds
@@ -258,8 +285,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
         for (int n = 0; n < S::AHEAD + 2; ++n) {
             if (n >= 2 && n - 2 < steps) {
                 add_bias(staged[n % 2]);
-#pragma unroll
-                for (int k = 0; k < TURNS; ++k) put_some(staged[n % 2], lds + (n - 2) * S::BUFFER, k);
+                put_step<DyT, S>(staged[n % 2], lds + (n - 2) * S::BUFFER, dy_row, dy_col, q_row, q_col);
             }
             if (n < steps) fetch(staged[n % 2], std::false_type());
         }
@@ -285,8 +311,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
             } else if (at + s < steps) {
                 if (at + s + S::AHEAD < steps) {
                     add_bias(later);
-#pragma unroll
-                    for (int k = 0; k < TURNS; ++k) put_some(later, lds + to, k);
+                    put_step<DyT, S>(later, lds + to, dy_row, dy_col, q_row, q_col);
                 }
                 if (at + s + S::AHEAD + 2 < steps) fetch(later, steady);
                 multiply(buffer, after, s == 0, [](int) {});             // behind the last step: fragments that nothing uses
@@ -332,24 +357,100 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
                 }
             }
     }
-    if (share != ~0u) {                                  // the rows' sums of the bias, in order
-        float* const sums = reinterpret_cast<float*>(lds);
-        __syncthreads();
+    if (share != ~0u)
+        write_bias<GradT, S>(A, reinterpret_cast<float*>(lds), bias, o0, dy_row, dy_col, A.splits * A.bias_shares > 1 ? nullptr : A.db,
+                             split_no * A.bias_shares + share);
+}
+
+// Few tokens, one group of them: what counts is dw, which is written once, so the tiles are small and four workgroups share a
+// compute unit: while one writes its tile, others read and multiply theirs.  A scale belongs to one sum; there is nothing to
+// join.
+template <typename DyT> using Short = Shape<DyT, 2, 2, 32, 1>;
+
+template <typename DyT, typename GradT, bool RAGGED>
+__global__ __launch_bounds__(Short<DyT>::THREADS, 4) void linear_short_kernel(LinearArgs A) {
+    typedef Short<DyT> S;
+    typedef typename Mma<DyT>::frag Frag;
+    __shared__ __align__(256) char lds[S::BUFFER];
+    const uint32_t tile_o = blockIdx.x / A.tiles_c, tile_c = blockIdx.x - tile_o * A.tiles_c;
+    const int32_t o0 = tile_o * S::TILE_O, c0 = tile_c * S::TILE_C;
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const uint32_t wave_o = wave / S::WAVES_C * 64, wave_c = wave % S::WAVES_C * 64;
+    const uint32_t dy_col = threadIdx.x % (S::TILE_O / VEC) * VEC, dy_row = threadIdx.x / (S::TILE_O / VEC);
+    const uint32_t q_col = threadIdx.x % (S::TILE_C / VEC) * VEC, q_row = threadIdx.x / (S::TILE_C / VEC);
+    const int32_t o_in = o0 + static_cast<int32_t>(dy_col);
+    const int dy_n = RAGGED ? max(0, min(A.outputs - o_in, VEC)) : VEC;
+    const DyT* const dy_at = static_cast<const DyT*>(A.dy) + (RAGGED ? o_in : min(o_in, A.outputs - VEC));
+    const int8_t* const q_at = A.q + min(static_cast<int64_t>(c0 + q_col), A.ld - VEC);
+    const uint32_t r = lane / 32 * 8 + lane % 16 / 4, cc = lane / 16 % 2 * 16 + lane % 4 * 4;
+    float scale[2];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) sums[dy_row * S::TILE_O + dy_col + i] = bias[i];
+    for (int f = 0; f < 2; ++f) {
+        const int32_t c = c0 + wave_c + f * 32 + lane % 32;
+        scale[f] = A.tokens > 0 && c < A.channels ? A.scale[c] : 0.f;      // without tokens there is no scale
+    }
+    float bias[VEC] = {};
+    f32x16 sum[2][2] = {};
+    for (int32_t t0 = 0; t0 < A.tokens; t0 += S::STEP) {
+        Staged<DyT, S> staged;
+#pragma unroll
+        for (int j = 0; j < S::DY_VECS; ++j) {
+            const int32_t t = t0 + dy_row + S::DY_ROWS * j;
+            staged.dy[j] = load8(dy_at + t * A.dy_stride, t < A.tokens ? dy_n : 0);
+        }
+#pragma unroll
+        for (int j = 0; j < S::X_VECS; ++j) {
+            const int32_t t = t0 + q_row + S::X_ROWS * j;
+            staged.q[j] = u32x2{0, 0};
+            if (t < A.tokens && (!RAGGED || A.ld > 0)) staged.q[j] = *reinterpret_cast<const u32x2*>(q_at + t * A.ld);
+        }
+        if (t0 > 0) __syncthreads();
+        put_step<DyT, S>(staged, lds, dy_row, dy_col, q_row, q_col);
+        if (A.db != nullptr && tile_c == 0)
+#pragma unroll
+            for (int j = 0; j < S::DY_VECS; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) bias[i] += get(staged.dy[j], i);
         __syncthreads();
-        const int32_t o = o0 + threadIdx.x;
-        if (threadIdx.x < S::TILE_O && o < A.outputs) {
-            float all = 0.f;
-            for (int w = 0; w < S::DY_ROWS; ++w) all += sums[w * S::TILE_O + threadIdx.x];
-            if (A.splits * A.bias_shares > 1) {
-                A.bias_partial[static_cast<int64_t>(split_no * A.bias_shares + share) * A.outputs + o] = all;
-            } else {
-                GradT* const b = static_cast<GradT*>(A.db) + o;
-                *b = rounded<GradT>(all + (A.accumulate ? static_cast<float>(*b) : 0.f));
-            }
+        const int turns = min(S::STEP, A.tokens - t0 + 15) / 16;
+#pragma unroll
+        for (int k = 0; k < S::STEP / 16; ++k) {
+            if (k >= turns) break;
+            Frag x[2];
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+                x[f] = read_fragment<S::TILE_C, Frag>(lds + S::PARTS * S::DY_BYTES, lds_at<S::TILE_C>(r, wave_c + f * 32 + cc) + k * 16 * (S::TILE_C * 2));
+#pragma unroll
+            for (int p = S::PARTS - 1; p >= 0; --p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const Frag y = read_fragment<S::TILE_O, Frag>(lds + p * S::DY_BYTES, lds_at<S::TILE_O>(r, wave_o + i * 32 + cc) + k * 16 * (S::TILE_O * 2));
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) sum[i][j] = Mma<DyT>::mul(y, x[j], sum[i][j]);
+                }
         }
     }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int32_t c = c0 + wave_c + j * 32 + lane % 32;
+        if (c >= A.channels) continue;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+                const int32_t o = o0 + wave_o + i * 32 + e4 * 8 + lane / 32 * 4;
+                GradT* w = static_cast<GradT*>(A.dw) + o * A.dw_stride + c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (o + e < A.outputs) {
+                        const float x = scale[j] * sum[i][j][e4 * 4 + e];
+                        *w = rounded<GradT>(A.accumulate ? x + static_cast<float>(*w) : x);
+                    }
+                    w += A.dw_stride;
+                }
+            }
+    }
+    if (A.db != nullptr && tile_c == 0) write_bias<GradT, S>(A, reinterpret_cast<float*>(lds), bias, o0, dy_row, dy_col, A.db, 0);
 }
 
 constexpr int JOIN_THREADS = 256;
@@ -388,15 +489,17 @@ template <typename DyT> using Wide = Shape<DyT, 4, 2, sizeof(DyT) == 4 ? 32 : 64
 constexpr int TILE_O = 256, TILE_C = 128;
 
 struct LinearPlan {
+    bool few;                          // tokens: of one group
     uint32_t tiles_o, tiles_c, groups, splits, groups_per_split, bias_shares;
     int64_t channels_padded, bias_at, bytes;
 };
 
 LinearPlan plan_of(int64_t tokens, int64_t channels, int64_t outputs) {
     LinearPlan p{};
-    p.tiles_o = static_cast<uint32_t>(ceil_div(outputs, TILE_O));
-    p.tiles_c = static_cast<uint32_t>(std::max<int64_t>(ceil_div(channels, TILE_C), 1));       // the bias is made with some tile
     p.groups = static_cast<uint32_t>(ceil_div(tokens, GROUP));
+    p.few = p.groups <= 1;
+    p.tiles_o = static_cast<uint32_t>(ceil_div(outputs, p.few ? 128 : TILE_O));
+    p.tiles_c = static_cast<uint32_t>(std::max<int64_t>(ceil_div(channels, TILE_C), 1));       // the bias is made with some tile
     const int64_t tiles = static_cast<int64_t>(p.tiles_o) * p.tiles_c;
     // enough workgroups for each of the 256 compute units, and two groups at the least for each of them
     int64_t splits = std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), std::max<uint32_t>(p.groups / 2, 1), MAX_SPLITS});
@@ -477,6 +580,8 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
             typedef std::remove_pointer_t<decltype(dy_type)> DyT;
             typedef std::remove_pointer_t<decltype(grad_type)> GradT;
             void (*kernel)(LinearArgs) = n_outputs % VEC != 0 || a.ld == 0 ? linear_kernel<DyT, GradT, Wide<DyT>, true> : linear_kernel<DyT, GradT, Wide<DyT>, false>;
+            void (*few)(LinearArgs) = n_outputs % VEC != 0 || a.ld == 0 ? linear_short_kernel<DyT, GradT, true> : linear_short_kernel<DyT, GradT, false>;
+            if (p.few) return launch(few, a, dim3(a.tiles), dim3(Short<DyT>::THREADS), hip_stream);
             const int rc = launch(kernel, a, dim3(a.tiles * a.splits), dim3(Wide<DyT>::THREADS), hip_stream);
             if (rc != MGWFBP_OK || a.splits == 1) return rc;
             return launch(linear_join_kernel<GradT>, a, join_grid, dim3(JOIN_THREADS), hip_stream);
