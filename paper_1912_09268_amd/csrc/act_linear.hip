@@ -57,10 +57,10 @@ template <> struct Mma<_Float16> {
 // column in a lane, so it is read transposed (ds_read_b64_tr_b16: sixteen lanes read four rows of 16 columns and get four
 // tokens of a column each).  Rows begin on the same bank, so the 32-byte pieces of a row are exchanged by a pattern of the
 // row's two lowest bits: 0, 2, 5, 7 puts the pieces of four rows on different banks, and those of the next sixteen lanes, which
-// read the neighbouring 16 columns, on others again.
+// read the neighbouring 16 columns, on others again (rows of 64 columns begin on two banks in turn: 0, 0, 2, 2).
 template <int COLS> __device__ __forceinline__ uint32_t lds_at(uint32_t row, uint32_t col) {
-    const uint32_t r = row & 3;
-    return row * (COLS * 2) + ((col / 16 ^ (2 * r + (r >> 1))) * 32) + (col % 16) * 2;
+    const uint32_t r = row & 3, pattern = COLS == 64 ? r & 2 : 2 * r + (r >> 1);
+    return row * (COLS * 2) + ((col / 16 ^ pattern) * 32) + (col % 16) * 2;
 }
 
 template <int COLS, typename Frag> __device__ __forceinline__ Frag read_fragment(const char* tile, uint32_t at) {
@@ -93,13 +93,13 @@ template <typename T> __device__ __forceinline__ void split(const Raw8<T>& x, ty
     }
 }
 
-// A workgroup's tile of dw and how it is taken: WAVES_O x WAVES_C wavefronts of 64 outputs by 64 channels each, STEP tokens at a
-// time through one of BUFFERS buffers in LDS.
-template <typename DyT, int WAVES_O_, int WAVES_C_, int STEP_, int BUFFERS_> struct Shape {
-    static constexpr int WAVES_O = WAVES_O_, WAVES_C = WAVES_C_, STEP = STEP_, BUFFERS = BUFFERS_;
+// A workgroup's tile of dw and how it is taken: WAVES_O x WAVES_C wavefronts of FRAGS 32 outputs by 64 channels each, STEP tokens
+// at a time through one of BUFFERS buffers in LDS.
+template <typename DyT, int FRAGS_, int WAVES_O_, int WAVES_C_, int STEP_, int BUFFERS_> struct Shape {
+    static constexpr int FRAGS = FRAGS_, WAVES_O = WAVES_O_, WAVES_C = WAVES_C_, STEP = STEP_, BUFFERS = BUFFERS_;
     static constexpr int AHEAD = BUFFERS - 1;                                // steps between LDS and the matrix cores
     static constexpr int THREADS = WAVES_O * WAVES_C * 64;
-    static constexpr int TILE_O = WAVES_O * 64, TILE_C = WAVES_C * 64;
+    static constexpr int TILE_O = WAVES_O * FRAGS * 32, TILE_C = WAVES_C * 64;
     static constexpr int PARTS = Parts<DyT>::n;
     static constexpr int DY_BYTES = STEP * TILE_O * 2, X_BYTES = STEP * TILE_C * 2;
     static constexpr int BUFFER = PARTS * DY_BYTES + X_BYTES;
@@ -108,6 +108,7 @@ template <typename DyT, int WAVES_O_, int WAVES_C_, int STEP_, int BUFFERS_> str
     static constexpr int X_VECS = STEP * TILE_C / VEC / THREADS;
     static constexpr int X_ROWS = THREADS / (TILE_C / VEC);
     static constexpr int STEPS = GROUP / STEP;
+    static constexpr int LDS = BUFFERS * BUFFER > TILE_O * TILE_C * 4 ? BUFFERS * BUFFER : TILE_O * TILE_C * 4;     // buffers, then the tile
 };
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -157,6 +158,46 @@ __device__ __forceinline__ void write_bias(const LinearArgs& A, float* sums, con
     }
 }
 
+// A workgroup's tile to memory: `rows` rows of `cols` elements, `stride` apart, are there.  It goes through LDS, so that it is
+// written in pieces of 16 bytes a lane.  Element e of a lane is in row 8 (e / 4) + 4 (lane / 32) + e % 4 and column lane % 32;
+// the halves of a wavefront would meet on the same banks, so rows with bit 2 have neighbouring pieces of 32 columns exchanged.
+template <typename S, bool STREAM, typename T>
+__device__ __forceinline__ void write_tile(float* tile, const f32x16 (&value)[S::FRAGS][2], uint32_t wave_o, uint32_t wave_c, uint32_t lane, T* out,
+                                           int64_t stride, int32_t rows, int32_t cols, bool accumulate) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < S::FRAGS; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t row = wave_o + i * 32 + e / 4 * 8 + lane / 32 * 4 + e % 4, col = wave_c + j * 32 + lane % 32;
+                tile[row * S::TILE_C + (col ^ (row & 4) * 8)] = value[i][j][e];
+            }
+    __syncthreads();
+    constexpr int W = 16 / sizeof(T), ROW_VECS = S::TILE_C / W;
+    const uint32_t col = threadIdx.x % ROW_VECS * W;
+    const int n = cols - static_cast<int32_t>(col);
+    if (n <= 0) return;
+    T* w = out + threadIdx.x / ROW_VECS * stride + col;
+#pragma unroll 4
+    for (int32_t row = threadIdx.x / ROW_VECS; row < min(rows, S::TILE_O); row += S::THREADS / ROW_VECS) {
+        float x[W];
+#pragma unroll
+        for (int i = 0; i < W; i += 4) {
+            const f32x4 four = *reinterpret_cast<const f32x4*>(tile + row * S::TILE_C + ((col + i) ^ (row & 4) * 8));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i + e] = four[e];
+        }
+        if (accumulate)
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                if (i < n) x[i] += static_cast<float>(w[i]);
+        store_some<STREAM>(w, x, n);
+        w += S::THREADS / ROW_VECS * stride;
+    }
+}
+
 // Tokens move from memory to registers, from there (binary32 cut into its parts, q widened) to LDS, and from LDS to the
 // matrix cores.  Two steps are on their way in registers and AHEAD in the other buffers while a step is multiplied; one
 // barrier a step.  With three buffers a step's first fragments are read before the barrier that ends the step before, so that
@@ -166,7 +207,7 @@ __device__ __forceinline__ void write_bias(const LinearArgs& A, float* sums, con
 template <typename DyT, typename GradT, typename S, bool RAGGED>
 __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     typedef typename Mma<DyT>::frag Frag;
-    __shared__ __align__(256) char lds[S::BUFFERS * S::BUFFER];
+    __shared__ __align__(256) char lds[S::LDS];
 
     // Consecutive workgroups go to the eight dies in turn; each die gets consecutive tiles, so that the tiles that share dy or q
     // share its L2.
@@ -331,51 +372,37 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     for (; (at + S::STEPS + S::AHEAD + 2) * S::STEP <= t_end - t_first; at += S::STEPS) group(at, std::true_type());
     for (; at < steps; at += S::STEPS) group(at, std::false_type());
 
-    // element e of a lane: row 8 (e / 4) + 4 (lane / 32) + e % 4, column lane % 32
-    const bool direct = A.splits == 1;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int32_t c = c0 + wave_c + j * 32 + lane % 32;
-        if (c >= A.channels) continue;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                const int32_t o = o0 + wave_o + i * 32 + e4 * 8 + lane / 32 * 4;
-                float* p = A.partial + (static_cast<int64_t>(split_no) * A.outputs + o) * A.channels_padded + c;
-                GradT* w = static_cast<GradT*>(A.dw) + o * A.dw_stride + c;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (o + e < A.outputs) {
-                        const float x = total[i][j][e4 * 4 + e];
-                        if (!direct) *p = x;
-                        else if (A.accumulate) *w = rounded<GradT>(x + static_cast<float>(*w));
-                        else *w = rounded<GradT>(x);
-                    }
-                    p += A.channels_padded;
-                    w += A.dw_stride;
-                }
-            }
-    }
     if (share != ~0u)
         write_bias<GradT, S>(A, reinterpret_cast<float*>(lds), bias, o0, dy_row, dy_col, A.splits * A.bias_shares > 1 ? nullptr : A.db,
                              split_no * A.bias_shares + share);
+    float* const whole = reinterpret_cast<float*>(lds);
+    if (A.splits > 1)
+        write_tile<S, false>(whole, total, wave_o, wave_c, lane, A.partial + (static_cast<int64_t>(split_no) * A.outputs + o0) * A.channels_padded + c0,
+                             A.channels_padded, A.outputs - o0, static_cast<int32_t>(A.channels_padded) - c0, false);
+    else
+        write_tile<S, false>(whole, total, wave_o, wave_c, lane, static_cast<GradT*>(A.dw) + o0 * A.dw_stride + c0, A.dw_stride, A.outputs - o0,
+                             A.channels - c0, A.accumulate);
 }
 
-// Few tokens, one group of them: what counts is dw, which is written once, so the tiles are small and four workgroups share a
-// compute unit: while one writes its tile, others read and multiply theirs.  A scale belongs to one sum; there is nothing to
+// Few tokens, one group of them: what counts is dw, which is written once, so the tiles are small and many workgroups share a
+// compute unit: while some write their tiles, others read and multiply theirs.  A scale belongs to one sum; there is nothing to
 // join.
-template <typename DyT> using Short = Shape<DyT, 2, 2, 32, 1>;
+template <typename DyT> using Short = Shape<DyT, 1, 2, 2, 32, 1>;
+// A dw larger than the 256 MB memory-side cache is written past it.  32 tokens, 25088 channels, binary32, with a reader behind (a
+// maximum over dw): 392 MB 183 us streamed and 209 kept, 196 MB 99 and 91, 98 MB 57 and 47; the kernel alone is 1 to 7 %
+// faster streamed at every size.
+constexpr int64_t STREAM_BYTES = 256 << 20;
+constexpr int SHORT_TILE_O = 64, SHORT_PER_CU = 4;
 
-template <typename DyT, typename GradT, bool RAGGED>
-__global__ __launch_bounds__(Short<DyT>::THREADS, 4) void linear_short_kernel(LinearArgs A) {
+template <typename DyT, typename GradT, bool RAGGED, bool STREAM>
+__global__ __launch_bounds__(Short<DyT>::THREADS, SHORT_PER_CU) void linear_short_kernel(LinearArgs A) {
     typedef Short<DyT> S;
     typedef typename Mma<DyT>::frag Frag;
-    __shared__ __align__(256) char lds[S::BUFFER];
+    __shared__ __align__(256) char lds[S::LDS];
     const uint32_t tile_o = blockIdx.x / A.tiles_c, tile_c = blockIdx.x - tile_o * A.tiles_c;
     const int32_t o0 = tile_o * S::TILE_O, c0 = tile_c * S::TILE_C;
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint32_t wave_o = wave / S::WAVES_C * 64, wave_c = wave % S::WAVES_C * 64;
+    const uint32_t wave_o = wave / S::WAVES_C * (S::FRAGS * 32), wave_c = wave % S::WAVES_C * 64;
     const uint32_t dy_col = threadIdx.x % (S::TILE_O / VEC) * VEC, dy_row = threadIdx.x / (S::TILE_O / VEC);
     const uint32_t q_col = threadIdx.x % (S::TILE_C / VEC) * VEC, q_row = threadIdx.x / (S::TILE_C / VEC);
     const int32_t o_in = o0 + static_cast<int32_t>(dy_col);
@@ -390,7 +417,7 @@ __global__ __launch_bounds__(Short<DyT>::THREADS, 4) void linear_short_kernel(Li
         scale[f] = A.tokens > 0 && c < A.channels ? A.scale[c] : 0.f;      // without tokens there is no scale
     }
     float bias[VEC] = {};
-    f32x16 sum[2][2] = {};
+    f32x16 sum[S::FRAGS][2] = {};
     for (int32_t t0 = 0; t0 < A.tokens; t0 += S::STEP) {
         Staged<DyT, S> staged;
 #pragma unroll
@@ -423,34 +450,22 @@ __global__ __launch_bounds__(Short<DyT>::THREADS, 4) void linear_short_kernel(Li
 #pragma unroll
             for (int p = S::PARTS - 1; p >= 0; --p)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < S::FRAGS; ++i) {
                     const Frag y = read_fragment<S::TILE_O, Frag>(lds + p * S::DY_BYTES, lds_at<S::TILE_O>(r, wave_o + i * 32 + cc) + k * 16 * (S::TILE_O * 2));
 #pragma unroll
                     for (int j = 0; j < 2; ++j) sum[i][j] = Mma<DyT>::mul(y, x[j], sum[i][j]);
                 }
         }
     }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int32_t c = c0 + wave_c + j * 32 + lane % 32;
-        if (c >= A.channels) continue;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                const int32_t o = o0 + wave_o + i * 32 + e4 * 8 + lane / 32 * 4;
-                GradT* w = static_cast<GradT*>(A.dw) + o * A.dw_stride + c;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (o + e < A.outputs) {
-                        const float x = scale[j] * sum[i][j][e4 * 4 + e];
-                        *w = rounded<GradT>(A.accumulate ? x + static_cast<float>(*w) : x);
-                    }
-                    w += A.dw_stride;
-                }
-            }
-    }
     if (A.db != nullptr && tile_c == 0) write_bias<GradT, S>(A, reinterpret_cast<float*>(lds), bias, o0, dy_row, dy_col, A.db, 0);
+#pragma unroll
+    for (int i = 0; i < S::FRAGS; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[i][j][e] *= scale[j];
+    write_tile<S, STREAM>(reinterpret_cast<float*>(lds), sum, wave_o, wave_c, lane, static_cast<GradT*>(A.dw) + o0 * A.dw_stride + c0, A.dw_stride,
+                          A.outputs - o0, A.channels - c0, A.accumulate);
 }
 
 constexpr int JOIN_THREADS = 256;
@@ -473,19 +488,20 @@ template <typename GradT> __global__ __launch_bounds__(JOIN_THREADS) void linear
     if (o >= static_cast<uint32_t>(A.outputs)) return;
     const float* p = A.partial + static_cast<int64_t>(o) * A.channels_padded + c;
     const int64_t next = A.outputs * A.channels_padded;
-    f32x4 sum = *reinterpret_cast<const f32x4*>(p);
+    f32x4 all = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll 4
-    for (uint32_t s = 1; s < A.splits; ++s) sum += *reinterpret_cast<const f32x4*>(p += next);
+    for (uint32_t s = 1; s < A.splits; ++s) all += *reinterpret_cast<const f32x4*>(p += next);
     GradT* const w = static_cast<GradT*>(A.dw) + static_cast<int64_t>(o) * A.dw_stride + c;
+    float sum[4] = {all[0], all[1], all[2], all[3]};
     if (A.accumulate)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (c + i < static_cast<uint32_t>(A.channels)) sum[i] += static_cast<float>(w[i]);
-    store4(w, sum, A.channels - static_cast<int32_t>(c));
+    store_some(w, sum, A.channels - static_cast<int32_t>(c));
 }
 
-// The tiles: 256 outputs by 128 channels, 64 tokens a step, 144 KiB of LDS; where dy takes three parts 32 tokens and 112 KiB.
-template <typename DyT> using Wide = Shape<DyT, 4, 2, sizeof(DyT) == 4 ? 32 : 64, sizeof(DyT) == 4 ? 2 : 3>;
+// The tiles: 256 outputs by 128 channels, 64 tokens a step, 144 KiB of LDS; where dy takes three parts 32 tokens and 128 KiB.
+template <typename DyT> using Wide = Shape<DyT, 2, 4, 2, sizeof(DyT) == 4 ? 32 : 64, sizeof(DyT) == 4 ? 2 : 3>;
 constexpr int TILE_O = 256, TILE_C = 128;
 
 struct LinearPlan {
@@ -498,7 +514,7 @@ LinearPlan plan_of(int64_t tokens, int64_t channels, int64_t outputs) {
     LinearPlan p{};
     p.groups = static_cast<uint32_t>(ceil_div(tokens, GROUP));
     p.few = p.groups <= 1;
-    p.tiles_o = static_cast<uint32_t>(ceil_div(outputs, p.few ? 128 : TILE_O));
+    p.tiles_o = static_cast<uint32_t>(ceil_div(outputs, p.few ? SHORT_TILE_O : TILE_O));
     p.tiles_c = static_cast<uint32_t>(std::max<int64_t>(ceil_div(channels, TILE_C), 1));       // the bias is made with some tile
     const int64_t tiles = static_cast<int64_t>(p.tiles_o) * p.tiles_c;
     // enough workgroups for each of the 256 compute units, and two groups at the least for each of them
@@ -579,9 +595,12 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
         return with_dtype(grad_dtype, [&](auto* grad_type) {
             typedef std::remove_pointer_t<decltype(dy_type)> DyT;
             typedef std::remove_pointer_t<decltype(grad_type)> GradT;
-            void (*kernel)(LinearArgs) = n_outputs % VEC != 0 || a.ld == 0 ? linear_kernel<DyT, GradT, Wide<DyT>, true> : linear_kernel<DyT, GradT, Wide<DyT>, false>;
-            void (*few)(LinearArgs) = n_outputs % VEC != 0 || a.ld == 0 ? linear_short_kernel<DyT, GradT, true> : linear_short_kernel<DyT, GradT, false>;
+            const bool ragged = n_outputs % VEC != 0 || a.ld == 0;
+            const bool stream = n_outputs * n_channels * static_cast<int64_t>(sizeof(GradT)) >= STREAM_BYTES;
+            void (*few)(LinearArgs) = ragged ? (stream ? linear_short_kernel<DyT, GradT, true, true> : linear_short_kernel<DyT, GradT, true, false>)
+                                             : (stream ? linear_short_kernel<DyT, GradT, false, true> : linear_short_kernel<DyT, GradT, false, false>);
             if (p.few) return launch(few, a, dim3(a.tiles), dim3(Short<DyT>::THREADS), hip_stream);
+            void (*kernel)(LinearArgs) = ragged ? linear_kernel<DyT, GradT, Wide<DyT>, true> : linear_kernel<DyT, GradT, Wide<DyT>, false>;
             const int rc = launch(kernel, a, dim3(a.tiles * a.splits), dim3(Wide<DyT>::THREADS), hip_stream);
             if (rc != MGWFBP_OK || a.splits == 1) return rc;
             return launch(linear_join_kernel<GradT>, a, join_grid, dim3(JOIN_THREADS), hip_stream);

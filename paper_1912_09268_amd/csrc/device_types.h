@@ -89,15 +89,19 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
         if (i < n) p[i] = rounded<T>(x[i]);
 }
 
-// The first n of four results.
-template <typename T> __device__ __forceinline__ void store4(T* p, f32x4 x, int n) {
-    typedef T vec __attribute__((ext_vector_type(4), aligned(alignof(T))));
-    if (n >= 4) {
-        *reinterpret_cast<vec*>(p) = vec{rounded<T>(x[0]), rounded<T>(x[1]), rounded<T>(x[2]), rounded<T>(x[3])};
+// The first n of W results, W elements of T being 16 bytes or fewer; STREAM: past the caches.
+template <bool STREAM = false, typename T, int W> __device__ __forceinline__ void store_some(T* p, const float (&x)[W], int n) {
+    if (n >= W) {
+        typedef T vec __attribute__((ext_vector_type(W), aligned(alignof(T))));
+        vec v;
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = rounded<T>(x[i]);
+        if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<vec*>(p));
+        else *reinterpret_cast<vec*>(p) = v;
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < W; ++i)
         if (i < n) p[i] = rounded<T>(x[i]);
 }
 
