@@ -217,7 +217,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     const uint32_t tile_o = tile / A.tiles_c, tile_c = tile - tile_o * A.tiles_c;
     const int32_t o0 = tile_o * S::TILE_O, c0 = tile_c * S::TILE_C;
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint32_t wave_o = wave / S::WAVES_C * 64, wave_c = wave % S::WAVES_C * 64;
+    const uint32_t wave_o = wave / S::WAVES_C * (S::FRAGS * 32), wave_c = wave % S::WAVES_C * 64;
     const int32_t t_first = split_no * A.groups_per_split * GROUP;
     const int32_t t_end = min(A.tokens, static_cast<int32_t>((split_no + 1) * A.groups_per_split * GROUP));
 
@@ -277,25 +277,25 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
 
     // where a lane reads: rows 8 (lane / 32) + (lane % 16) / 4, columns 16 (lane / 16 % 2) + 4 (lane % 4) of a 32-column piece
     const uint32_t r = lane / 32 * 8 + lane % 16 / 4, cc = lane / 16 % 2 * 16 + lane % 4 * 4;
-    uint32_t at_o[2], at_c[2];
+    uint32_t at_o[S::FRAGS], at_c[2];
 #pragma unroll
-    for (int f = 0; f < 2; ++f) {
-        at_o[f] = lds_at<S::TILE_O>(r, wave_o + f * 32 + cc);
-        at_c[f] = lds_at<S::TILE_C>(r, wave_c + f * 32 + cc) + S::PARTS * S::DY_BYTES;
-    }
-    f32x16 sum[2][2];
-    // One step, in UNITS turns of four products; the fragments of a turn are read during the one before.  Between them, a later
+    for (int f = 0; f < S::FRAGS; ++f) at_o[f] = lds_at<S::TILE_O>(r, wave_o + f * 32 + cc);
+#pragma unroll
+    for (int f = 0; f < 2; ++f) at_c[f] = lds_at<S::TILE_C>(r, wave_c + f * 32 + cc) + S::PARTS * S::DY_BYTES;
+    f32x16 sum[S::FRAGS][2];
+    // One step, in UNITS turns of a few products; the fragments of a turn are read during the one before.  Between them, a later
     // step is put into its buffer.  (The turns are kept apart: moved into each other they take more registers than there
     // are.)
     constexpr int UNITS = TURNS * S::PARTS;
-    Frag x[2][2], y[2][2];
+    Frag x[2][2], y[2][S::FRAGS];
     auto read = [&](uint32_t buffer, int u) {
         const int k = u / S::PARTS, p = S::PARTS - 1 - u % S::PARTS;
+        if (u % S::PARTS == 0)
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            if (u % S::PARTS == 0) x[k % 2][f] = read_fragment<S::TILE_C, Frag>(lds + buffer, at_c[f] + k * 16 * (S::TILE_C * 2));
+            for (int f = 0; f < 2; ++f) x[k % 2][f] = read_fragment<S::TILE_C, Frag>(lds + buffer, at_c[f] + k * 16 * (S::TILE_C * 2));
+#pragma unroll
+        for (int f = 0; f < S::FRAGS; ++f)
             y[u % 2][f] = read_fragment<S::TILE_O, Frag>(lds + buffer, at_o[f] + p * S::DY_BYTES + k * 16 * (S::TILE_O * 2));
-        }
     };
     auto multiply = [&](uint32_t buffer, uint32_t after, bool first, auto&& between) {
         if constexpr (S::AHEAD == 1) read(buffer, 0);
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
             else if constexpr (S::AHEAD > 1) read(after, 0);
             if (u % S::PARTS == 0) between(u / S::PARTS);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < S::FRAGS; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) sum[i][j] = Mma<DyT>::mul(y[u % 2][i], x[u / S::PARTS % 2][j], first && u == 0 ? f32x16{} : sum[i][j]);
             __builtin_amdgcn_sched_barrier(0);
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     };
     static_assert(S::AHEAD == 1 || (UNITS % 2 == 0 && TURNS % 2 == 0), "a step's first fragments go where its first turn looks for them");
 
-    f32x16 total[2][2] = {};
+    f32x16 total[S::FRAGS][2] = {};
     Staged<DyT, S> staged[2];
     uint32_t buffer = 0;                                      // that of the present step
     auto behind = [&](int n) {                                // that of the n-th step after it
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
             buffer = after;
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < S::FRAGS; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -502,20 +502,30 @@ template <typename GradT> __global__ __launch_bounds__(JOIN_THREADS) void linear
 
 // The tiles: 256 outputs by 128 channels, 64 tokens a step, 144 KiB of LDS; where dy takes three parts 32 tokens and 128 KiB.
 template <typename DyT> using Wide = Shape<DyT, 2, 4, 2, sizeof(DyT) == 4 ? 32 : 64, sizeof(DyT) == 4 ? 2 : 3>;
-constexpr int TILE_O = 256, TILE_C = 128;
+// Square ones: 128 outputs by 128 channels, half as many registers for sums.
+template <typename DyT> using Square = Shape<DyT, 1, 4, 2, sizeof(DyT) == 4 ? 32 : 64, sizeof(DyT) == 4 ? 2 : 3>;
+constexpr int TILE_C = 128;
+enum { SHORT, SQUARE, WIDE };
+constexpr int TILE_O[] = {SHORT_TILE_O, 128, 256};
 
 struct LinearPlan {
-    bool few;                          // tokens: of one group
+    int form;
     uint32_t tiles_o, tiles_c, groups, splits, groups_per_split, bias_shares;
     int64_t channels_padded, bias_at, bytes;
 };
 
+// Which tiles.  Wide ones read least (binary16, 4096 channels and outputs, 8192 tokens: 333 us, square 423).  But where they are
+// fewer than the compute units they are split over the tokens and joined, and with few tokens that costs more than it
+// gives: 1024 channels, 4096 outputs, 1024 tokens 31 us, square 17; 4096 tokens 55 and 54; 1024 outputs and 16384 tokens
+// 55 and 60; binary32 with 256 tokens, 1024 channels and outputs 18 and 13.
+constexpr int64_t SQUARE_GROUPS = 16;
+
 LinearPlan plan_of(int64_t tokens, int64_t channels, int64_t outputs) {
     LinearPlan p{};
     p.groups = static_cast<uint32_t>(ceil_div(tokens, GROUP));
-    p.few = p.groups <= 1;
-    p.tiles_o = static_cast<uint32_t>(ceil_div(outputs, p.few ? SHORT_TILE_O : TILE_O));
     p.tiles_c = static_cast<uint32_t>(std::max<int64_t>(ceil_div(channels, TILE_C), 1));       // the bias is made with some tile
+    p.form = p.groups <= 1 ? SHORT : p.groups <= SQUARE_GROUPS && ceil_div(outputs, TILE_O[WIDE]) * p.tiles_c < 256 ? SQUARE : WIDE;
+    p.tiles_o = static_cast<uint32_t>(ceil_div(outputs, TILE_O[p.form]));
     const int64_t tiles = static_cast<int64_t>(p.tiles_o) * p.tiles_c;
     // enough workgroups for each of the 256 compute units, and two groups at the least for each of them
     int64_t splits = std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), std::max<uint32_t>(p.groups / 2, 1), MAX_SPLITS});
@@ -599,9 +609,10 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
             const bool stream = n_outputs * n_channels * static_cast<int64_t>(sizeof(GradT)) >= STREAM_BYTES;
             void (*few)(LinearArgs) = ragged ? (stream ? linear_short_kernel<DyT, GradT, true, true> : linear_short_kernel<DyT, GradT, true, false>)
                                              : (stream ? linear_short_kernel<DyT, GradT, false, true> : linear_short_kernel<DyT, GradT, false, false>);
-            if (p.few) return launch(few, a, dim3(a.tiles), dim3(Short<DyT>::THREADS), hip_stream);
-            void (*kernel)(LinearArgs) = ragged ? linear_kernel<DyT, GradT, Wide<DyT>, true> : linear_kernel<DyT, GradT, Wide<DyT>, false>;
-            const int rc = launch(kernel, a, dim3(a.tiles * a.splits), dim3(Wide<DyT>::THREADS), hip_stream);
+            void (*square)(LinearArgs) = ragged ? linear_kernel<DyT, GradT, Square<DyT>, true> : linear_kernel<DyT, GradT, Square<DyT>, false>;
+            void (*wide)(LinearArgs) = ragged ? linear_kernel<DyT, GradT, Wide<DyT>, true> : linear_kernel<DyT, GradT, Wide<DyT>, false>;
+            const int rc = launch(p.form == SHORT ? few : p.form == SQUARE ? square : wide, a, dim3(a.tiles * a.splits),
+                                  dim3(p.form == SHORT ? Short<DyT>::THREADS : p.form == SQUARE ? Square<DyT>::THREADS : Wide<DyT>::THREADS), hip_stream);
             if (rc != MGWFBP_OK || a.splits == 1) return rc;
             return launch(linear_join_kernel<GradT>, a, join_grid, dim3(JOIN_THREADS), hip_stream);
         });
