@@ -18,6 +18,10 @@ using namespace ops;
 
 thread_local int g_last_hip_error = 0;
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int THREADS = 256;
 constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_DIM = int64_t(1) << 23;
 
@@ -84,10 +88,11 @@ __global__ __launch_bounds__(THREADS) void embed_kernel(EmbedArgs A) {
 //    counted by comparing it with every other one (rank_kernel): one launch, no dependence between workgroups.  Beyond that,
 //    a radix sort by 8 bits at a time.  Tokens without a row come last.
 // 2. The ordered tokens are cut into chunks of a fixed length; lanes sum a chunk's stretches of one row each
-//    (sum_kernel).  A stretch that is all of its row's tokens is written to the gradient, any other to the workspace.
-// 3. Rows of several chunks are joined, in order (join_kernel).
+//    (sum_kernel).  Rows of one or two chunks are written to the gradient, longer ones in stretches to the workspace.  In the
+//    same launch, rows that are not among the ordered tokens are cleared.
+// 3. The stretches of longer rows are joined, in order (join_kernel).
 //
-// The order of every sum follows from the ids alone: the same call gives the same bits.
+// The order of every sum follows from the sizes and ids alone: the same call gives the same bits.
 
 struct GradArgs {
     const void* ids;
@@ -98,7 +103,7 @@ struct GradArgs {
     uint32_t* order;           // [tokens] token at a place of the order
     int32_t* row;              // [tokens] its row, n_rows if it has none
     float* partial;            // [2 * chunks][dim_padded]: a chunk's first and its last stretch
-    uint8_t* present;          // [n_rows] rows with tokens; null where every row is cleared beforehand
+    u32x2* joins;              // [1 + chunks] how many rows have to be joined; the chunks they begin in and the rows, in any order
     uint32_t* other_order;     // radix sort: the other side of a pass, and the counts of every workgroup
     int32_t* other_row;
     uint32_t* counts;          // [blocks][256]
@@ -107,7 +112,10 @@ struct GradArgs {
     int32_t id_type, accumulate;
     uint32_t chunk, chunks;    // tokens per chunk, number of chunks
     uint32_t vecs, page;       // vectors of a row; chunks per blockIdx.y
-    uint32_t work_blocks;      // workgroups that rank or sum; the rest clear rows
+    int64_t early_rows;        // rows that are cleared with the ranking, whether they have tokens or not
+    uint32_t rank_blocks, sum_blocks;  // workgroups that rank, that sum; the rest clear clear_rows rows each
+    uint32_t clear_rows;
+    uint32_t join_width;       // lanes side by side that join a row
     uint32_t items, shift, from_ids;   // radix sort: tokens per workgroup, first bit of the digit, first pass
 };
 
@@ -117,57 +125,78 @@ __device__ __forceinline__ int32_t row_of(const GradArgs& A, int64_t t) {
                                                                                               : static_cast<int32_t>(A.n_rows);
 }
 
-// Clears rows of the gradient, `count` of them at a time: workgroup `b` of `blocks`.  Only rows without tokens where
-// A.present says which these are.
-template <typename GradT> __device__ void clear_rows(const GradArgs& A, uint32_t b, uint32_t blocks) {
-    const float zeros[VEC] = {};
-    if (A.present == nullptr && A.grad_stride == A.dim) {
-        const int64_t total = A.n_rows * A.dim;
-        GradT* const g = static_cast<GradT*>(A.grad);
-        for (int64_t at = (static_cast<int64_t>(b) * THREADS + threadIdx.x) * VEC; at < total;
-             at += static_cast<int64_t>(blocks) * THREADS * VEC)
-            store8(g + at, zeros, static_cast<int>(min(total - at, static_cast<int64_t>(VEC))));
-        return;
+// Clears the rows from first on, at most A.clear_rows and below end; with `all` not set, only those that are not among the ordered
+// tokens.
+template <typename GradT> __device__ void clear_some_rows(const GradArgs& A, int64_t first, int64_t end, bool all) {
+    __shared__ uint8_t absent[THREADS];
+    const int rows = static_cast<int>(min(end - first, static_cast<int64_t>(A.clear_rows)));
+    if (!all) {
+        if (static_cast<int>(threadIdx.x) < rows) {
+            const int32_t r = static_cast<int32_t>(first) + threadIdx.x;
+            uint32_t lo = 0, hi = static_cast<uint32_t>(A.tokens);       // the first place with a row of r or more
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (A.row[mid] < r) lo = mid + 1; else hi = mid;
+            }
+            absent[threadIdx.x] = lo >= static_cast<uint32_t>(A.tokens) || A.row[lo] != r;
+        }
+        __syncthreads();
     }
-    // a wavefront per row
-    const int lane = threadIdx.x % 64;
-    for (int64_t r = static_cast<int64_t>(b) * (THREADS / 64) + threadIdx.x / 64; r < A.n_rows;
-         r += static_cast<int64_t>(blocks) * (THREADS / 64)) {
-        if (A.present != nullptr && A.present[r] != 0) continue;
-        GradT* const g = static_cast<GradT*>(A.grad) + r * A.grad_stride;
-        for (int64_t col = lane * VEC; col < A.dim; col += 64 * VEC)
-            store8(g + col, zeros, static_cast<int>(min(A.dim - col, static_cast<int64_t>(VEC))));
+    const float zeros[VEC] = {};
+    const uint32_t at_once = min(A.vecs, static_cast<uint32_t>(THREADS)), beside = THREADS / at_once;
+    const uint32_t beside_no = threadIdx.x / at_once;
+    if (beside_no >= beside) return;
+    for (int i = beside_no; i < rows; i += beside) {
+        if (!all && !absent[i]) continue;
+        GradT* const g = static_cast<GradT*>(A.grad) + (first + i) * A.grad_stride;
+        for (uint32_t v = threadIdx.x - beside_no * at_once; v < A.vecs; v += at_once)
+            store8(g + static_cast<int64_t>(v) * VEC, zeros, static_cast<int>(min(A.dim - static_cast<int64_t>(v) * VEC, static_cast<int64_t>(VEC))));
     }
 }
 
-constexpr int RANK_EACH = 16;              // tokens that a workgroup ranks
+constexpr int RANK_EACH = 8;               // tokens that a workgroup ranks
+constexpr int RANK_AHEAD = 16;             // ids that a lane has on their way
 constexpr int64_t RANKED_TOKENS = 8192;
+constexpr int64_t NARROW_ROWS = (int64_t(1) << 18) - 1;      // (row, token) of so many rows fits 31 bits
 
 // The place of a token is the number of pairs (row, token) below its own.  A wavefront compares 64 others at a time with
-// each of the workgroup's tokens; a comparison is one vector instruction and the count of its mask two scalar ones.
-// The workgroups behind those that rank clear the gradient.
-template <typename GradT> __global__ __launch_bounds__(THREADS) void rank_kernel(GradArgs A) {
-    if (blockIdx.x >= A.work_blocks) {
-        clear_rows<GradT>(A, blockIdx.x - A.work_blocks, gridDim.x - A.work_blocks);
+// each of the workgroup's tokens; a comparison is one vector instruction and the count of its mask two scalar ones.  4096
+// tokens are 16 M comparisons, 260 thousand instructions: a microsecond of the chip.  What takes its time is that ids come
+// from memory, so the workgroups behind the first rank_blocks clear the first early_rows rows meanwhile.
+template <typename Key, typename GradT> __global__ __launch_bounds__(THREADS) void rank_kernel(GradArgs A) {
+    if (blockIdx.x >= A.rank_blocks) {
+        clear_some_rows<GradT>(A, static_cast<int64_t>(blockIdx.x - A.rank_blocks) * A.clear_rows, A.early_rows, true);
         return;
     }
+    constexpr int TOKEN_BITS = sizeof(Key) == 4 ? 13 : 32;
+    static_assert(RANKED_TOKENS <= 1 << 13, "tokens of narrow keys");
+    if (blockIdx.x == 0 && threadIdx.x == 0) A.joins[0] = u32x2{0, 0};
     __shared__ uint32_t below[THREADS / 64][RANK_EACH];
+    __shared__ int32_t own_row[RANK_EACH];
     const uint32_t n = static_cast<uint32_t>(A.tokens);
     const uint32_t first = blockIdx.x * RANK_EACH;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    uint64_t own[RANK_EACH];
+    auto key_of = [&](uint32_t t) { return static_cast<Key>(static_cast<uint32_t>(row_of(A, t))) << TOKEN_BITS | t; };
+    Key own[RANK_EACH];
     uint32_t count[RANK_EACH];
 #pragma unroll
     for (int r = 0; r < RANK_EACH; ++r) {
-        const uint32_t t = min(first + r, n - 1);
-        own[r] = static_cast<uint64_t>(static_cast<uint32_t>(row_of(A, t))) << 32 | t;
+        own[r] = key_of(min(first + r, n - 1));
         count[r] = 0;
+        if (threadIdx.x == 0) own_row[r] = static_cast<int32_t>(own[r] >> TOKEN_BITS);
     }
-    for (uint32_t s0 = wave * 64; s0 < n; s0 += THREADS) {
-        const uint32_t s = s0 + lane;
-        const uint64_t key = s < n ? static_cast<uint64_t>(static_cast<uint32_t>(row_of(A, s))) << 32 | s : ~uint64_t(0);
+    for (uint32_t s0 = wave * 64; s0 < n; s0 += RANK_AHEAD * THREADS) {
+        Key key[RANK_AHEAD];
 #pragma unroll
-        for (int r = 0; r < RANK_EACH; ++r) count[r] += __popcll(__ballot(key < own[r]));
+        for (int j = 0; j < RANK_AHEAD; ++j) {
+            const uint32_t s = s0 + j * THREADS + lane;
+            const Key k = key_of(min(s, n - 1));
+            key[j] = s < n ? k : ~Key(0);
+        }
+#pragma unroll
+        for (int j = 0; j < RANK_AHEAD; ++j)
+#pragma unroll
+            for (int r = 0; r < RANK_EACH; ++r) count[r] += __popcll(__ballot(key[j] < own[r]));
     }
     if (lane == 0)
 #pragma unroll
@@ -179,7 +208,7 @@ template <typename GradT> __global__ __launch_bounds__(THREADS) void rank_kernel
 #pragma unroll
         for (int w = 0; w < THREADS / 64; ++w) place += below[w][threadIdx.x];
         A.order[place] = t;
-        A.row[place] = row_of(A, t);
+        A.row[place] = own_row[threadIdx.x];
     }
 }
 
@@ -189,17 +218,16 @@ constexpr int WAVES = THREADS / 64;
 
 __device__ __forceinline__ int32_t sort_row(const GradArgs& A, int64_t at) { return A.from_ids ? row_of(A, at) : A.other_row[at]; }
 
-// How often each digit occurs among a workgroup's tokens.  The first pass clears the marks of rows with tokens.
+// How often each digit occurs among a workgroup's tokens.
 __global__ __launch_bounds__(THREADS) void digit_kernel(GradArgs A) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) A.joins[0] = u32x2{0, 0};
     __shared__ uint32_t count[DIGITS];
     count[threadIdx.x] = 0;
     __syncthreads();
     const int64_t first = static_cast<int64_t>(blockIdx.x) * A.items, end = min(first + A.items, A.tokens);
+#pragma unroll 4
     for (int64_t at = first + threadIdx.x; at < end; at += THREADS)
         atomicAdd(&count[(static_cast<uint32_t>(sort_row(A, at)) >> A.shift) % DIGITS], 1u);
-    if (A.from_ids && A.present != nullptr)
-        for (int64_t r = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; r < A.n_rows; r += static_cast<int64_t>(gridDim.x) * THREADS)
-            A.present[r] = 0;
     __syncthreads();
     A.counts[static_cast<int64_t>(blockIdx.x) * DIGITS + threadIdx.x] = count[threadIdx.x];
 }
@@ -211,6 +239,7 @@ __global__ __launch_bounds__(THREADS) void move_kernel(GradArgs A) {
     __shared__ uint32_t place[WAVES][DIGITS];
     const uint32_t d = threadIdx.x, lane = d % 64, wave = d / 64;
     uint32_t before = 0, all = 0;
+#pragma unroll 16
     for (uint32_t b = 0; b < gridDim.x; ++b) {
         const uint32_t c = A.counts[static_cast<int64_t>(b) * DIGITS + d];
         before += b < blockIdx.x ? c : 0;
@@ -256,7 +285,6 @@ __global__ __launch_bounds__(THREADS) void move_kernel(GradArgs A) {
             const uint32_t to = place[wave][digit] + ahead;
             A.order[to] = A.from_ids ? static_cast<uint32_t>(at) : A.other_order[at];
             A.row[to] = r;
-            if (A.from_ids && A.present != nullptr && r < A.n_rows) A.present[r] = 1;
         }
         // the places are read by lanes that others have written for: no barrier between the lanes of a wavefront, but an order
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -285,10 +313,12 @@ __device__ __forceinline__ void write_partial(const GradArgs& A, uint32_t which,
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
 }
 
-// One lane for eight columns of a chunk.
+// One lane for eight columns of a chunk.  A row that begins in a chunk and ends in the next one is summed by the lanes of the
+// first alone; only rows that reach further are joined.
 template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) void sum_kernel(GradArgs A) {
-    if (blockIdx.x >= A.work_blocks) {
-        if (blockIdx.y == 0) clear_rows<GradT>(A, blockIdx.x - A.work_blocks, gridDim.x - A.work_blocks);
+    if (blockIdx.x >= A.sum_blocks) {
+        if (blockIdx.y == 0)
+            clear_some_rows<GradT>(A, A.early_rows + static_cast<int64_t>(blockIdx.x - A.sum_blocks) * A.clear_rows, A.n_rows, false);
         return;
     }
     const uint32_t at = blockIdx.x * THREADS + threadIdx.x;
@@ -297,32 +327,47 @@ template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) vo
     if (in_page >= A.page || c >= A.chunks) return;
     const int64_t col = static_cast<int64_t>(v) * VEC;
     const int n = static_cast<int>(min(A.dim - col, static_cast<int64_t>(VEC)));
-    const int64_t first = static_cast<int64_t>(c) * A.chunk, end = min(first + A.chunk, A.tokens);
+    const int64_t first = static_cast<int64_t>(c) * A.chunk, end = min(first + A.chunk, A.tokens), further = min(end + A.chunk, A.tokens);
     const DyT* const dy = static_cast<const DyT*>(A.dy) + col;
     const int32_t none = static_cast<int32_t>(A.n_rows);
-    const int32_t row_before = first > 0 ? A.row[first - 1] : none;
-    const int32_t row_after = end < A.tokens ? A.row[end] : none;
-    constexpr int AHEAD = 8;
+    const int32_t front = A.row[first], back = A.row[end - 1];
+    const int32_t before = first > 0 ? A.row[first - 1] : none, long_before = first > A.chunk ? A.row[first - A.chunk - 1] : none;
+    const int32_t after = end < A.tokens ? A.row[end] : none, long_after = further < A.tokens ? A.row[further] : none;
+    if (front == none) return;
+    const bool goes_on = back != none && after == back;         // the last stretch, behind the chunk
+    const bool came = before == front;                          // the first stretch, from before the chunk
+    const bool through = came && goes_on && front == back;
+    const bool skips = came && !through && long_before != front;            // the chunk before has summed it
+    const bool extends = goes_on && !through && long_after != back;
+    const int64_t stop = extends ? further : end;
+    constexpr int AHEAD = sizeof(DyT) == 4 ? 8 : 16;             // 64 registers of dy on their way
     float sum[VEC] = {};
-    int32_t current = A.row[first];
-    bool from_start = true;                                     // the current stretch began with the chunk
-    for (int64_t p0 = first; p0 < end && current != none; p0 += AHEAD) {
+    int32_t current = none;
+    for (int64_t p0 = first; p0 < stop; p0 += AHEAD) {
         Raw8<DyT> x[AHEAD];
         int32_t r[AHEAD];
+        uint32_t token[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const int64_t p = min(p0 + j, end - 1);
-            r[j] = p0 + j < end ? A.row[p] : none;
-            x[j] = load8(dy + static_cast<int64_t>(A.order[p]) * A.dy_stride, n);
+        for (int j = 0; j < AHEAD; j += 4) {                     // whole fours: order and row are padded to 256 bytes
+            const u32x4 four = *reinterpret_cast<const u32x4*>(A.order + p0 + j);
+            const i32x4 rows = *reinterpret_cast<const i32x4*>(A.row + p0 + j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t p = p0 + j + i;
+                const bool counts = p < end ? !(skips && rows[i] == front) : p < stop && rows[i] == back;
+                r[j + i] = counts ? rows[i] : none;
+                token[j + i] = r[j + i] != none ? four[i] : 0;
+            }
         }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) x[j] = load8(dy + static_cast<int64_t>(token[j]) * A.dy_stride, n);
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             if (r[j] != current) {
-                if (current != none) {                          // a stretch ends inside the chunk
-                    if (from_start && current == row_before) write_partial(A, 2 * c, col, sum);
-                    else if (p0 + j < end || current != row_after) write_row<GradT>(A, current, col, n, sum);
-                    else write_partial(A, 2 * c + 1, col, sum);
-                    from_start = false;
+                if (current != none) {                          // a stretch has ended
+                    if (came && current == front) write_partial(A, 2 * c, col, sum);
+                    else if (goes_on && !extends && current == back) write_partial(A, 2 * c + 1, col, sum);
+                    else write_row<GradT>(A, current, col, n, sum);
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
                 }
@@ -333,60 +378,69 @@ template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) vo
                 for (int i = 0; i < VEC; ++i) sum[i] += get(x[j], i);
         }
     }
-    if (current != none) {                                      // it ends with the chunk
-        if (from_start && current == row_before) write_partial(A, 2 * c, col, sum);
-        else if (current != row_after) write_row<GradT>(A, current, col, n, sum);
-        else write_partial(A, 2 * c + 1, col, sum);
+    if (current != none) {
+        if (came && current == front) write_partial(A, 2 * c, col, sum);
+        else if (goes_on && !extends && current == back) write_partial(A, 2 * c + 1, col, sum);
+        else write_row<GradT>(A, current, col, n, sum);
     }
+    if (v == 0 && goes_on && !through && !extends)              // begins here: to be joined
+        A.joins[1 + atomicAdd(reinterpret_cast<uint32_t*>(A.joins), 1u)] = u32x2{c, static_cast<uint32_t>(back)};
 }
 
-constexpr int JOIN_WAVES = 16, JOIN_COLS = 256;
-
-// A row whose tokens reach over several chunks, by the workgroup of the chunk it begins in: wavefront w adds the stretches
-// w, w + 16, ..., then the sixteen sums are added in order.
-template <typename GradT> __global__ __launch_bounds__(JOIN_WAVES * 64) void join_kernel(GradArgs A) {
-    const uint32_t c = blockIdx.x;
-    const int64_t end = static_cast<int64_t>(c + 1) * A.chunk, first = end - A.chunk;
-    if (end >= A.tokens) return;
-    const int32_t r = A.row[end - 1];
-    if (r == static_cast<int32_t>(A.n_rows) || A.row[end] != r) return;
-    if (A.row[first] == r && first > 0 && A.row[first - 1] == r) return;        // begins in an earlier chunk
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    // chunks that it covers whole, behind this one
-    uint32_t whole = 0;
-    for (;;) {
-        const uint32_t q = c + 1 + whole + lane;
-        const bool covers = q < A.chunks && static_cast<int64_t>(q + 1) * A.chunk <= A.tokens && A.row[static_cast<int64_t>(q + 1) * A.chunk - 1] == r;
-        const uint64_t mask = __ballot(covers);
-        if (~mask != 0) {
-            whole += __builtin_ctzll(~mask);
-            break;
-        }
-        whole += 64;
-    }
-    const int64_t next = static_cast<int64_t>(c + 1 + whole) * A.chunk;
-    const uint32_t pieces = 1 + whole + (next < A.tokens && A.row[next] == r ? 1 : 0);
-    __shared__ f32x4 sums[JOIN_WAVES][64];
-    const int64_t col = (static_cast<int64_t>(blockIdx.y) * 64 + lane) * 4;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (col < A.dim)
-#pragma unroll 4
-        for (uint32_t i = wave; i < pieces; i += JOIN_WAVES) {
-            const int64_t which = i == 0 ? 2 * static_cast<int64_t>(c) + 1 : 2 * static_cast<int64_t>(c + i);
-            sum += *reinterpret_cast<const f32x4*>(A.partial + which * A.dim_padded + col);
-        }
-    sums[wave][lane] = sum;
-    __syncthreads();
-    if (wave != 0 || col >= A.dim) return;
-    for (uint32_t w = 1; w < JOIN_WAVES; ++w) sum += sums[w][lane];
-    GradT* const g = static_cast<GradT*>(A.grad) + r * A.grad_stride + col;
+// Rows whose tokens reach over several chunks, one at a time by a workgroup.  A lane has four columns, join_width lanes a row's
+// stretch; slot i of the workgroup's adds the stretches i, i + slots, ..., then the slots' sums are added in order.  All of it
+// is waiting for memory, so what can be asked for at once is: the first row of the list before its length is known, and the
+// beginnings of four chunks a lane to find the row's last one.
+template <typename GradT> __global__ __launch_bounds__(THREADS) void join_kernel(GradArgs A) {
+    __shared__ f32x4 sums[THREADS];
+    const uint32_t lane = threadIdx.x % 64;
+    const uint32_t slot = threadIdx.x / A.join_width, slots = THREADS / A.join_width, place = threadIdx.x % A.join_width;
+    const int64_t col = (static_cast<int64_t>(blockIdx.y) * A.join_width + place) * 4;
+    const uint32_t rows_to_join = A.joins[0].x;
+    u32x2 join = A.joins[1 + blockIdx.x];                                        // within the list, whatever its length
+    for (uint32_t no = blockIdx.x; no < rows_to_join;) {
+        const uint32_t c = join.x;
+        const int32_t r = static_cast<int32_t>(join.y);
+        uint32_t pieces = 1;                                                     // chunks behind c that begin with the row have one, too
+        for (;;) {
+            uint64_t begins[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (col + i < A.dim) {
-            float x = sum[i] * A.scale;
-            if (A.accumulate) x += static_cast<float>(g[i]);
-            g[i] = rounded<GradT>(x);
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t q = c + pieces + j * 64 + lane;
+                begins[j] = __ballot(q < A.chunks && A.row[static_cast<int64_t>(min(q, A.chunks - 1)) * A.chunk] == r);
+            }
+            uint32_t more = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (more == j * 64u) more += ~begins[j] != 0 ? __builtin_ctzll(~begins[j]) : 64;
+            pieces += more;
+            if (more < 256) break;
         }
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        if (col < A.dim) {
+            if (slot == 0) sum = *reinterpret_cast<const f32x4*>(A.partial + (2 * static_cast<int64_t>(c) + 1) * A.dim_padded + col);
+#pragma unroll 16
+            for (uint32_t i = slot == 0 ? slots : slot; i < pieces; i += slots)
+                sum += *reinterpret_cast<const f32x4*>(A.partial + 2 * static_cast<int64_t>(c + i) * A.dim_padded + col);
+        }
+        no += gridDim.x;
+        if (no < rows_to_join) join = A.joins[1 + no];
+        sums[threadIdx.x] = sum;
+        __syncthreads();
+        if (slot == 0 && col < A.dim) {
+            for (uint32_t w = 1; w < min(slots, pieces); ++w) sum += sums[w * A.join_width + place];
+            GradT* const g = static_cast<GradT*>(A.grad) + r * A.grad_stride + col;
+            const int n = static_cast<int>(min(A.dim - col, int64_t(4)));
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[i] = sum[i] * A.scale;
+                if (A.accumulate && i < n) x[i] += static_cast<float>(g[i]);
+            }
+            store_some(g, x, n);
+        }
+        __syncthreads();
+    }
 }
 
 // ---- host side ----
@@ -395,14 +449,16 @@ struct GradPlan {
     bool ranked;
     uint32_t chunk, chunks, blocks, items;
     int64_t dim_padded;
-    int64_t order, row, partial, present, other_order, other_row, counts, bytes;     // places in the workspace
+    int64_t order, row, partial, joins, other_order, other_row, counts, bytes;     // places in the workspace
 };
 
 // What is in the workspace, and where: every part begins on 256 bytes.
 GradPlan plan_of(int64_t tokens, int64_t n_rows, int64_t dim) {
     GradPlan p{};
     p.ranked = tokens <= RANKED_TOKENS;
-    p.chunk = p.ranked ? 8 : 32;
+    // Chunks of 16 to 64 tokens: longer ones leave less to join, shorter ones more lanes that sum, of which a chip full is wanted.
+    const int64_t lanes = tokens * ceil_div(std::max<int64_t>(dim, 1), VEC);
+    p.chunk = lanes / 64 >= 131072 ? 64 : lanes / 32 >= 65536 ? 32 : 16;
     p.chunks = static_cast<uint32_t>(ceil_div(tokens, p.chunk));
     p.dim_padded = ceil_div(dim, VEC) * VEC;
     // radix sort: at most 256 workgroups, since each adds up the counts of all
@@ -418,8 +474,8 @@ GradPlan plan_of(int64_t tokens, int64_t n_rows, int64_t dim) {
     p.order = take(tokens * 4);
     p.row = take(tokens * 4);
     p.partial = take(2 * static_cast<int64_t>(p.chunks) * p.dim_padded * 4);
+    p.joins = take((1 + static_cast<int64_t>(p.chunks)) * 8);
     if (!p.ranked) {
-        p.present = take(n_rows);
         p.other_order = take(tokens * 4);
         p.other_row = take(tokens * 4);
         p.counts = take(static_cast<int64_t>(p.blocks) * DIGITS * 4);
@@ -430,11 +486,6 @@ GradPlan plan_of(int64_t tokens, int64_t n_rows, int64_t dim) {
 
 bool grad_sizes_ok(int64_t n_tokens, int64_t n_rows, int64_t dim) {
     return n_tokens >= 0 && n_tokens <= MOST_TOKENS && n_rows >= 0 && n_rows < 0x7fffffff && dim >= 0 && dim <= MOST_DIM;
-}
-
-// Workgroups that clear: enough to fill the chip, 32 KiB each at the least.
-uint32_t clear_blocks(int64_t n_rows, int64_t dim, int64_t elem_bytes) {
-    return static_cast<uint32_t>(std::min<int64_t>(4096, std::max<int64_t>(1, n_rows * dim * elem_bytes / 32768)));
 }
 
 }  // namespace
@@ -537,21 +588,25 @@ int mgwfbp_embed_grad(const void* d_ids, int32_t id_type, int64_t n_tokens, cons
         a.order = reinterpret_cast<uint32_t*>(ws + p.order);
         a.row = reinterpret_cast<int32_t*>(ws + p.row);
         a.partial = reinterpret_cast<float*>(ws + p.partial);
+        a.joins = reinterpret_cast<u32x2*>(ws + p.joins);
     }
-    const uint32_t clearing = accumulate ? 0 : clear_blocks(n_rows, dim, dtype_bytes(grad_dtype));
+    // A workgroup clears about 32 KiB, at most one row a thread.
+    a.clear_rows = static_cast<uint32_t>(std::min<int64_t>(THREADS, std::max<int64_t>(1, 32768 / (dim * dtype_bytes(grad_dtype)))));
     int rc = MGWFBP_OK;
-    if (p.ranked) {
-        a.work_blocks = static_cast<uint32_t>(ceil_div(n_tokens, RANK_EACH));
-        const dim3 grid(a.work_blocks + clearing);
+    if (p.ranked && n_tokens > 0) {
+        // Where most rows have no tokens, half of them are cleared beside the ranking.
+        a.early_rows = !accumulate && n_rows >= 4 * n_tokens ? n_rows / 2 : 0;
+        a.rank_blocks = static_cast<uint32_t>(ceil_div(n_tokens, RANK_EACH));
+        const dim3 grid(a.rank_blocks + static_cast<uint32_t>(ceil_div(a.early_rows, a.clear_rows)));
         rc = with_dtype(grad_dtype, [&](auto* grad_type) {
-            return launch(rank_kernel<std::remove_pointer_t<decltype(grad_type)>>, a, grid, dim3(THREADS), hip_stream);
+            typedef std::remove_pointer_t<decltype(grad_type)> GradT;
+            return launch(n_rows <= NARROW_ROWS ? rank_kernel<uint32_t, GradT> : rank_kernel<uint64_t, GradT>, a, grid, dim3(THREADS), hip_stream);
         });
-        if (rc != MGWFBP_OK || n_tokens == 0) return rc;
-    } else {
+        if (rc != MGWFBP_OK) return rc;
+    } else if (n_tokens > 0) {
         uint32_t* const order[2] = {a.order, reinterpret_cast<uint32_t*>(ws + p.other_order)};
         int32_t* const row[2] = {a.row, reinterpret_cast<int32_t*>(ws + p.other_row)};
         a.counts = reinterpret_cast<uint32_t*>(ws + p.counts);
-        a.present = accumulate ? nullptr : ws + p.present;
         int passes = 1;
         while (passes < 4 && (static_cast<uint64_t>(n_rows) >> (8 * passes)) != 0) ++passes;
         for (int pass = 0; pass < passes; ++pass) {             // the last one ends in order and row
@@ -567,8 +622,9 @@ int mgwfbp_embed_grad(const void* d_ids, int32_t id_type, int64_t n_tokens, cons
             if (rc != MGWFBP_OK) return rc;
         }
     }
-    a.work_blocks = static_cast<uint32_t>(ceil_div(static_cast<int64_t>(a.page) * a.vecs, THREADS));
-    const dim3 grid(a.work_blocks + (p.ranked ? 0 : clearing), static_cast<uint32_t>(ceil_div(p.chunks, a.page)));
+    const uint32_t clearing = accumulate ? 0 : static_cast<uint32_t>(ceil_div(n_rows - a.early_rows, a.clear_rows));
+    a.sum_blocks = n_tokens > 0 ? static_cast<uint32_t>(ceil_div(static_cast<int64_t>(a.page) * a.vecs, THREADS)) : 0;
+    const dim3 grid(a.sum_blocks + clearing, std::max<uint32_t>(static_cast<uint32_t>(ceil_div(p.chunks, a.page)), 1));
     rc = with_dtype(dy_dtype, [&](auto* dy_type) {
         return with_dtype(grad_dtype, [&](auto* grad_type) {
             return launch(sum_kernel<std::remove_pointer_t<decltype(dy_type)>, std::remove_pointer_t<decltype(grad_type)>>, a, grid,
@@ -576,9 +632,13 @@ int mgwfbp_embed_grad(const void* d_ids, int32_t id_type, int64_t n_tokens, cons
         });
     });
     if (rc != MGWFBP_OK || p.chunks < 2) return rc;
-    const dim3 join_grid(p.chunks - 1, static_cast<uint32_t>(ceil_div(dim, JOIN_COLS)));
+    // 64 columns a workgroup: a compute unit takes in about 25 GB/s, so a long row wants many of them.
+    a.join_width = 1;
+    while (a.join_width < 16 && a.join_width * 4 < dim) a.join_width *= 2;
+    const int64_t join_slices = ceil_div(dim, 4 * static_cast<int64_t>(a.join_width));
+    const dim3 join_grid(std::min<uint32_t>(p.chunks - 1, static_cast<uint32_t>(std::max<int64_t>(1024 / join_slices, 1))), static_cast<uint32_t>(join_slices));
     return with_dtype(grad_dtype, [&](auto* grad_type) {
-        return launch(join_kernel<std::remove_pointer_t<decltype(grad_type)>>, a, join_grid, dim3(JOIN_WAVES * 64), hip_stream);
+        return launch(join_kernel<std::remove_pointer_t<decltype(grad_type)>>, a, join_grid, dim3(THREADS), hip_stream);
     });
 }
 
