@@ -1,5 +1,5 @@
-"""Compiles the HIP/C++ sources under csrc/ into libmgwfbp.so, libmgwfbp_layers.so and the extension module _calls next to this
-file, and the benchmark's measurement aid under bench_aid/ into its own shared object there (gfx950 only)."""
+"""Compiles the HIP/C++ sources under csrc/ into libmgwfbp.so, libmgwfbp_layers.so and the extension modules _calls and
+_layers_calls next to this file, and the benchmark's measurement aid under bench_aid/ into its own shared object there (gfx950 only)."""
 from __future__ import annotations
 
 import os
@@ -79,6 +79,24 @@ def build_calls() -> str:
     return out
 
 
+def build_layers_calls() -> str:
+    """The extension module that takes the tensors of layers.py apart: host code against torch's headers, no link to the
+    library."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    out = os.path.join(HERE, "_layers_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", sysconfig.get_paths()["include"],
+           "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(root, "include"),
+           "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-isystem", "/opt/rocm/include",
+           os.path.join(CSRC, "layers_calls.cpp"), "-L", os.path.join(root, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch",
+           "-ltorch_python", "-o", out]
+    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"g++ failed ({res.returncode}):\n{res.stdout}")
+    return out
+
+
 def build_bench_aid(verbose: bool = False) -> str:
     """The stream probe and cache scrub that bench.py uses; kept out of libmgwfbp.so on purpose."""
     hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
@@ -96,3 +114,4 @@ if __name__ == "__main__":  # python -m paper_1912_09268_amd.build
     print(build_layers(verbose=True))
     print(build_bench_aid(verbose=True))
     print(build_calls())
+    print(build_layers_calls())

@@ -456,6 +456,7 @@ struct GradPlan {
 GradPlan plan_of(int64_t tokens, int64_t n_rows, int64_t dim) {
     GradPlan p{};
     p.ranked = tokens <= RANKED_TOKENS;
+    if (tokens == 0) return p;                               // nothing to order
     // Chunks of 16 to 64 tokens: longer ones leave less to join, shorter ones more lanes that sum, of which a chip full is wanted.
     const int64_t lanes = tokens * ceil_div(std::max<int64_t>(dim, 1), VEC);
     p.chunk = lanes / 64 >= 131072 ? 64 : lanes / 32 >= 65536 ? 32 : 16;

@@ -1,7 +1,7 @@
 """The operators that make per-layer gradients, on torch tensors: embedding lookup and its gradient, and activation
 checkpoints in 8 bits with what the backward pass makes of them.
 
-Arguments are checked here (ValueError) and handed to the binding; memory and streams are torch's.  Every call runs on
+Arguments are checked (ValueError) and handed to the library, in native code where the extension module is there; memory and streams are torch's.  Every call runs on
 the tensors' device and on torch's current stream there, and does not wait for it.  A tensor made on another stream
 needs that stream's work to be waited for, and Tensor.record_stream where it is freed early, as with any other call.
 
@@ -22,6 +22,14 @@ from typing import NamedTuple, Optional, Sequence, Union
 import torch
 
 from . import layers_binding as B
+
+try:
+    from . import _layers_calls as _native
+    B._native = _native
+    B._announce()
+except ImportError:             # not built for this Python and torch: every call goes the plain way
+    class _native:
+        embed = embed_grad = act_store = act_backward = act_linear_grad = staticmethod(lambda *args: NotImplemented)
 
 _DTYPES = {torch.float32: B.F32, torch.bfloat16: B.BF16, torch.float16: B.F16}
 _ID_TYPES = {torch.int32: B.I32, torch.int64: B.I64}
@@ -106,6 +114,8 @@ def embed(tables: Tensors, ids: Tensors, scales: Optional[Sequence[float]] = Non
     tables = [tables] if isinstance(tables, torch.Tensor) else tables
     ids = [ids] if isinstance(ids, torch.Tensor) else ids
     scales = [1.0] * len(tables) if scales is None else scales
+    if out is not None and _native.embed(tables, ids, scales, out) is None:
+        return out
     if not 1 <= len(tables) <= B.MAX_TABLES or len(ids) != len(tables) or len(scales) != len(tables):
         _fail(f"one to {B.MAX_TABLES} tables with ids and a scale each")
     device = _device(*tables, *ids, out)
@@ -135,6 +145,8 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, scale: f
     """grad[r] = scale * sum of dy[t] over the tokens with ids[t] == r, for every row of grad [rows, dim]; added to grad where
     `accumulate`.  dy [tokens, dim]; tokens of `padding_row` and ids outside the table count for nothing.
     `workspace`: device memory of layers_binding.embed_grad_workspace(tokens, rows, dim) bytes to use; None takes torch's."""
+    if _native.embed_grad(dy, ids, grad, scale, padding_row, accumulate, workspace) is None:
+        return grad
     device = _device(dy, ids, grad, workspace)
     if ids.dtype not in _ID_TYPES or not ids.is_contiguous():
         _fail("ids must be a contiguous int32 or int64 tensor")
@@ -174,6 +186,8 @@ def _address(t: Optional[torch.Tensor]) -> int:
 def act_store(x: torch.Tensor, act: Optional[Act8] = None, kind: str = "identity", y: Optional[torch.Tensor] = None) -> Act8:
     """x [tokens, channels] in 8 bits, into `act` (or new memory), which is returned; and y = f(x) in the same pass where `y` is
     given (x's type).  A group with an infinity or NaN is held as NaN."""
+    if act is not None and _native.act_store(x, act.q, act.scale, act.channels, KINDS.get(kind), y) is None:
+        return act
     x_stride = _matrix(x, "x", None, None)
     tokens, channels = x.shape
     if act is None:
@@ -195,6 +209,8 @@ def act_backward(act: Act8, dy: Optional[torch.Tensor] = None, kind: str = "iden
                  y: Optional[torch.Tensor] = None):
     """dx = dy * f'(x) and, where `y` is given, y = f(x), for the x that `act` holds.  dy, dx and y are [tokens, channels] of one
     type.  With dy and without dx, dx is a new tensor.  Without dy, only y.  Returns dx, or y without dy."""
+    if _native.act_backward(act.q, act.scale, act.channels, dy, KINDS.get(kind), dx, y) is None:
+        return y if dy is None else dx
     tokens, ld = _act(act)
     if dy is None and (dx is not None or y is None):
         _fail("dx takes a dy, and without dy there must be a y")
@@ -216,6 +232,8 @@ def act_linear_grad(dy: torch.Tensor, act: Act8, dw: torch.Tensor, db: Optional[
     """dw [outputs, channels] = dy^T x and, where `db` [outputs] is given, db = dy's column sums, for the x that `act` holds and
     dy [tokens, outputs]; added to what is there where `accumulate`.  dw and db are of one type.
     `workspace`: device memory of layers_binding.act_linear_grad_workspace(tokens, channels, outputs) bytes; None takes torch's."""
+    if _native.act_linear_grad(dy, act.q, act.scale, act.channels, dw, db, accumulate, workspace) is None:
+        return dw
     tokens, ld = _act(act)
     device = _device(dy, act.q, act.scale, dw, db, workspace)
     dy_stride = _matrix(dy, "dy", tokens, None)

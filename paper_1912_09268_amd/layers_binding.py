@@ -56,7 +56,17 @@ def lib() -> C.CDLL:
             fn.restype = res
             fn.argtypes = args
         _LIB = handle
+        _announce()
     return _LIB
+
+
+_native = None      # the extension module of layers.py, once that is imported
+
+
+def _announce() -> None:
+    """Hands the loaded library's entry points to the extension module that takes the tensors of layers.py apart."""
+    if _native is not None and _LIB is not None:
+        _native.set_functions(_check, {name: C.cast(getattr(_LIB, name), _vp).value for name in _SIGNATURES})
 
 
 def _check(fn: str, status: int) -> None:

@@ -538,3 +538,37 @@ def test_operators_run_on_the_current_stream():
         grad = layers.embed_grad(out, ids, torch.empty(64, 256, device="cuda"))
     stream.synchronize()
     assert torch.equal(out, table) and torch.equal(grad, table) and bool((table == 1.0).all())
+
+
+def test_both_ways_of_taking_tensors_apart_agree(monkeypatch):
+    """The extension module takes well-formed calls (and is built); what it leaves goes the plain way, with the same result."""
+    assert layers._native.__name__.endswith("_layers_calls")
+    g = _gen(21)
+    table, ids, x = torch.randn(30, 48, generator=g, device="cuda"), torch.randint(0, 30, (5, 40), generator=g, device="cuda"), torch.randn(200, 48, generator=g, device="cuda")
+
+    def once():
+        out = layers.embed([table, table], [ids, ids], scales=[1, 2.5], out=torch.empty(5, 40, 48, dtype=BF16, device="cuda"))
+        act = layers.act_store(x, layers.act_empty(200, 48), kind="silu", y=torch.empty_like(x))
+        dx = layers.act_backward(act, x, kind="silu", dx=torch.empty_like(x))
+        dw, db = torch.empty(48, 48, device="cuda"), torch.empty(48, device="cuda")
+        layers.act_linear_grad(dx, act, dw, db=db)
+        return [out, act.q, act.scale, dx, dw, db, layers.embed_grad(dx, ids, torch.empty(30, 48, device="cuda"))]
+
+    native = once()
+    taken = []
+    for name in ("embed", "embed_grad", "act_store", "act_backward", "act_linear_grad"):
+        real = getattr(layers._native, name)
+        monkeypatch.setattr(layers._native, name, lambda *a, name=name, real=real: taken.append(name if real(*a) is None else "") or NotImplemented)
+    plain = once()
+    assert sorted(set(taken)) == ["act_backward", "act_linear_grad", "act_store", "embed", "embed_grad"]
+    torch.cuda.synchronize()
+    for a, b in zip(native, plain):
+        assert torch.equal(a, b)
+    with pytest.raises(ValueError):
+        layers.embed([table], [ids], out=torch.empty(5, 40, 47, dtype=BF16, device="cuda"))
+    with pytest.raises(ValueError):
+        layers.act_store(x, layers.act_empty(199, 48))
+    with pytest.raises(ValueError):
+        layers.embed_grad(x, ids, torch.empty(30, 48, device="cuda", dtype=torch.float64))
+    with pytest.raises(ValueError):
+        layers.act_linear_grad(x, layers.act_store(x), torch.empty(48, 48, device="cuda"), workspace=torch.empty(16, device="cuda")[1:])

@@ -91,8 +91,8 @@ def test_act_calls_refuse():
                 d_db=P, grad_dtype=B.F32, d_workspace=P, workspace_bytes=1 << 30)
     for bad in (dict(d_q=0), dict(d_scale=P + 4), dict(ld=16), dict(ld=33), dict(n_tokens=-1), dict(n_tokens=2 ** 23 + 1), dict(n_channels=-1), dict(d_dy=0), dict(d_dy=P + 2),
                 dict(dy_stride=6), dict(dy_dtype=3), dict(n_outputs=-1), dict(d_dw=0), dict(d_dw=P + 2), dict(dw_stride=19), dict(d_db=P + 1), dict(grad_dtype=4),
-                dict(d_workspace=0), dict(d_workspace=P + 64), dict(workspace_bytes=B.act_linear_grad_workspace(9, 20, 7) - 1),
-                dict(n_channels=2 ** 23, n_outputs=2 ** 23, ld=2 ** 23)):
+                dict(n_tokens=4096, d_workspace=0), dict(n_tokens=4096, d_workspace=P + 64),          # split over the tokens: it takes one
+                dict(n_tokens=4096, workspace_bytes=B.act_linear_grad_workspace(4096, 20, 7) - 1), dict(n_channels=2 ** 23, n_outputs=2 ** 23, ld=2 ** 23)):
         _refused(B.act_linear_grad, *{**grad, **bad}.values())
     B.act_linear_grad(*{**grad, "n_outputs": 0, "d_dy": 0, "d_dw": 0, "d_db": 0}.values())
     _refused(B.act_dims, -1, 4)
