@@ -112,42 +112,52 @@ struct GradArgs {
     int32_t id_type, accumulate;
     uint32_t chunk, chunks;    // tokens per chunk, number of chunks
     uint32_t vecs, page;       // vectors of a row; chunks per blockIdx.y
-    int64_t early_rows;        // rows that are cleared with the ranking, whether they have tokens or not
-    uint32_t rank_blocks, sum_blocks;  // workgroups that rank, that sum; the rest clear clear_rows rows each
+    uint32_t sum_blocks;       // workgroups that sum; the rest clear clear_rows rows each
     uint32_t clear_rows;
     uint32_t join_width;       // lanes side by side that join a row
     uint32_t items, shift, from_ids;   // radix sort: tokens per workgroup, first bit of the digit, first pass
 };
 
-__device__ __forceinline__ int32_t row_of(const GradArgs& A, int64_t t) {
-    const int64_t id = id_at(A.ids, A.id_type, t);
+__device__ __forceinline__ int32_t row_of(const GradArgs& A, int64_t id) {
     return static_cast<uint64_t>(id) < static_cast<uint64_t>(A.n_rows) && id != A.padding_row ? static_cast<int32_t>(id)
                                                                                               : static_cast<int32_t>(A.n_rows);
 }
 
-// Clears the rows from first on, at most A.clear_rows and below end; with `all` not set, only those that are not among the ordered
-// tokens.
-template <typename GradT> __device__ void clear_some_rows(const GradArgs& A, int64_t first, int64_t end, bool all) {
-    __shared__ uint8_t absent[THREADS];
-    const int rows = static_cast<int>(min(end - first, static_cast<int64_t>(A.clear_rows)));
-    if (!all) {
-        if (static_cast<int>(threadIdx.x) < rows) {
-            const int32_t r = static_cast<int32_t>(first) + threadIdx.x;
-            uint32_t lo = 0, hi = static_cast<uint32_t>(A.tokens);       // the first place with a row of r or more
-            while (lo < hi) {
-                const uint32_t mid = (lo + hi) / 2;
-                if (A.row[mid] < r) lo = mid + 1; else hi = mid;
-            }
-            absent[threadIdx.x] = lo >= static_cast<uint32_t>(A.tokens) || A.row[lo] != r;
-        }
-        __syncthreads();
+// The first place of the order with a row of r or more, by a wavefront: 64 places looked at in a turn, so that two turns find
+// one of 4096 and three one of 260 thousand.
+__device__ __forceinline__ uint32_t first_place(const GradArgs& A, int32_t r) {
+    const uint32_t lane = threadIdx.x % 64;
+    uint32_t lo = 0, hi = static_cast<uint32_t>(A.tokens);               // it is one of lo .. hi
+    while (lo < hi) {
+        const uint32_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const uint32_t below = __popcll(__ballot(at < hi && A.row[min(at, hi - 1)] < r));
+        if (below == 0) break;
+        hi = min(lo + below * step, hi);
+        lo += (below - 1) * step + 1;
     }
+    return lo;
+}
+
+// Clears those rows from first on, at most A.clear_rows, that are not among the ordered tokens.
+template <typename GradT> __device__ void clear_absent_rows(const GradArgs& A, int64_t first) {
+    __shared__ uint8_t absent[THREADS];
+    __shared__ uint32_t place[2];
+    const int rows = static_cast<int>(min(A.n_rows - first, static_cast<int64_t>(A.clear_rows)));
+    absent[threadIdx.x] = 1;
+    const uint32_t wave = threadIdx.x / 64;
+    if (wave < 2) {                                                  // the places of the first row and of the first row behind
+        const uint32_t at = first_place(A, static_cast<int32_t>(first) + (wave == 0 ? 0 : rows));
+        if (threadIdx.x % 64 == 0) place[wave] = at;
+    }
+    __syncthreads();
+    for (uint32_t at = place[0] + threadIdx.x; at < place[1]; at += THREADS) absent[A.row[at] - first] = 0;
+    __syncthreads();
     const float zeros[VEC] = {};
     const uint32_t at_once = min(A.vecs, static_cast<uint32_t>(THREADS)), beside = THREADS / at_once;
     const uint32_t beside_no = threadIdx.x / at_once;
     if (beside_no >= beside) return;
     for (int i = beside_no; i < rows; i += beside) {
-        if (!all && !absent[i]) continue;
+        if (!absent[i]) continue;
         GradT* const g = static_cast<GradT*>(A.grad) + (first + i) * A.grad_stride;
         for (uint32_t v = threadIdx.x - beside_no * at_once; v < A.vecs; v += at_once)
             store8(g + static_cast<int64_t>(v) * VEC, zeros, static_cast<int>(min(A.dim - static_cast<int64_t>(v) * VEC, static_cast<int64_t>(VEC))));
@@ -162,12 +172,8 @@ constexpr int64_t NARROW_ROWS = (int64_t(1) << 18) - 1;      // (row, token) of 
 // The place of a token is the number of pairs (row, token) below its own.  A wavefront compares 64 others at a time with
 // each of the workgroup's tokens; a comparison is one vector instruction and the count of its mask two scalar ones.  4096
 // tokens are 16 M comparisons, 260 thousand instructions: a microsecond of the chip.  What takes its time is that ids come
-// from memory, so the workgroups behind the first rank_blocks clear the first early_rows rows meanwhile.
-template <typename Key, typename GradT> __global__ __launch_bounds__(THREADS) void rank_kernel(GradArgs A) {
-    if (blockIdx.x >= A.rank_blocks) {
-        clear_some_rows<GradT>(A, static_cast<int64_t>(blockIdx.x - A.rank_blocks) * A.clear_rows, A.early_rows, true);
-        return;
-    }
+// from memory, all at once.
+template <typename Key, typename IdT> __global__ __launch_bounds__(THREADS) void rank_kernel(GradArgs A) {
     constexpr int TOKEN_BITS = sizeof(Key) == 4 ? 13 : 32;
     static_assert(RANKED_TOKENS <= 1 << 13, "tokens of narrow keys");
     if (blockIdx.x == 0 && threadIdx.x == 0) A.joins[0] = u32x2{0, 0};
@@ -176,7 +182,7 @@ template <typename Key, typename GradT> __global__ __launch_bounds__(THREADS) vo
     const uint32_t n = static_cast<uint32_t>(A.tokens);
     const uint32_t first = blockIdx.x * RANK_EACH;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    auto key_of = [&](uint32_t t) { return static_cast<Key>(static_cast<uint32_t>(row_of(A, t))) << TOKEN_BITS | t; };
+    auto key_of = [&](uint32_t t) { return static_cast<Key>(static_cast<uint32_t>(row_of(A, static_cast<const IdT*>(A.ids)[t]))) << TOKEN_BITS | t; };
     Key own[RANK_EACH];
     uint32_t count[RANK_EACH];
 #pragma unroll
@@ -216,7 +222,7 @@ template <typename Key, typename GradT> __global__ __launch_bounds__(THREADS) vo
 constexpr int DIGITS = 256;
 constexpr int WAVES = THREADS / 64;
 
-__device__ __forceinline__ int32_t sort_row(const GradArgs& A, int64_t at) { return A.from_ids ? row_of(A, at) : A.other_row[at]; }
+__device__ __forceinline__ int32_t sort_row(const GradArgs& A, int64_t at) { return A.from_ids ? row_of(A, id_at(A.ids, A.id_type, at)) : A.other_row[at]; }
 
 // How often each digit occurs among a workgroup's tokens.
 __global__ __launch_bounds__(THREADS) void digit_kernel(GradArgs A) {
@@ -317,8 +323,7 @@ __device__ __forceinline__ void write_partial(const GradArgs& A, uint32_t which,
 // first alone; only rows that reach further are joined.
 template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) void sum_kernel(GradArgs A) {
     if (blockIdx.x >= A.sum_blocks) {
-        if (blockIdx.y == 0)
-            clear_some_rows<GradT>(A, A.early_rows + static_cast<int64_t>(blockIdx.x - A.sum_blocks) * A.clear_rows, A.n_rows, false);
+        if (blockIdx.y == 0) clear_absent_rows<GradT>(A, static_cast<int64_t>(blockIdx.x - A.sum_blocks) * A.clear_rows);
         return;
     }
     const uint32_t at = blockIdx.x * THREADS + threadIdx.x;
@@ -595,14 +600,9 @@ int mgwfbp_embed_grad(const void* d_ids, int32_t id_type, int64_t n_tokens, cons
     a.clear_rows = static_cast<uint32_t>(std::min<int64_t>(THREADS, std::max<int64_t>(1, 32768 / (dim * dtype_bytes(grad_dtype)))));
     int rc = MGWFBP_OK;
     if (p.ranked && n_tokens > 0) {
-        // Where most rows have no tokens, half of them are cleared beside the ranking.
-        a.early_rows = !accumulate && n_rows >= 4 * n_tokens ? n_rows / 2 : 0;
-        a.rank_blocks = static_cast<uint32_t>(ceil_div(n_tokens, RANK_EACH));
-        const dim3 grid(a.rank_blocks + static_cast<uint32_t>(ceil_div(a.early_rows, a.clear_rows)));
-        rc = with_dtype(grad_dtype, [&](auto* grad_type) {
-            typedef std::remove_pointer_t<decltype(grad_type)> GradT;
-            return launch(n_rows <= NARROW_ROWS ? rank_kernel<uint32_t, GradT> : rank_kernel<uint64_t, GradT>, a, grid, dim3(THREADS), hip_stream);
-        });
+        void (*narrow)(GradArgs) = id_type == MGWFBP_I64 ? rank_kernel<uint32_t, int64_t> : rank_kernel<uint32_t, int32_t>;
+        void (*wide)(GradArgs) = id_type == MGWFBP_I64 ? rank_kernel<uint64_t, int64_t> : rank_kernel<uint64_t, int32_t>;
+        rc = launch(n_rows <= NARROW_ROWS ? narrow : wide, a, dim3(static_cast<uint32_t>(ceil_div(n_tokens, RANK_EACH))), dim3(THREADS), hip_stream);
         if (rc != MGWFBP_OK) return rc;
     } else if (n_tokens > 0) {
         uint32_t* const order[2] = {a.order, reinterpret_cast<uint32_t*>(ws + p.other_order)};
@@ -623,7 +623,7 @@ int mgwfbp_embed_grad(const void* d_ids, int32_t id_type, int64_t n_tokens, cons
             if (rc != MGWFBP_OK) return rc;
         }
     }
-    const uint32_t clearing = accumulate ? 0 : static_cast<uint32_t>(ceil_div(n_rows - a.early_rows, a.clear_rows));
+    const uint32_t clearing = accumulate ? 0 : static_cast<uint32_t>(ceil_div(n_rows, a.clear_rows));
     a.sum_blocks = n_tokens > 0 ? static_cast<uint32_t>(ceil_div(static_cast<int64_t>(a.page) * a.vecs, THREADS)) : 0;
     const dim3 grid(a.sum_blocks + clearing, std::max<uint32_t>(static_cast<uint32_t>(ceil_div(p.chunks, a.page)), 1));
     rc = with_dtype(dy_dtype, [&](auto* dy_type) {
