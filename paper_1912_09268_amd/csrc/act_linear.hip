@@ -105,15 +105,15 @@ template <typename DyT, int FRAGS_, int WAVES_O_, int WAVES_C_, int STEP_, int B
     static constexpr int BUFFER = PARTS * DY_BYTES + X_BYTES;
     static constexpr int DY_VECS = STEP * TILE_O / VEC / THREADS;            // vectors that a thread brings
     static constexpr int DY_ROWS = THREADS / (TILE_O / VEC);                 // rows that all threads bring at once
-    static constexpr int X_VECS = STEP * TILE_C / VEC / THREADS;
-    static constexpr int X_ROWS = THREADS / (TILE_C / VEC);
+    static constexpr int XW = STEP * TILE_C / 16 >= THREADS ? 16 : 8;         // channels of q that a thread brings at once
+    static constexpr int X_VECS = STEP * TILE_C / XW / THREADS;
+    static constexpr int X_ROWS = THREADS / (TILE_C / XW);
+    typedef uint32_t X __attribute__((ext_vector_type(XW / 4)));
     static constexpr int STEPS = GROUP / STEP;
     static constexpr int LDS = BUFFERS * BUFFER > TILE_O * TILE_C * 4 ? BUFFERS * BUFFER : TILE_O * TILE_C * 4;     // buffers, then the tile
 };
 
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-template <typename DyT, typename S> struct Staged { Raw8<DyT> dy[S::DY_VECS]; u32x2 q[S::X_VECS]; };
+template <typename DyT, typename S> struct Staged { Raw8<DyT> dy[S::DY_VECS]; typename S::X q[S::X_VECS]; };
 
 // The pieces of a step on the way to LDS: a vector of dy, or of q.
 template <typename DyT, typename S> __device__ __forceinline__ void put_dy(const Staged<DyT, S>& from, char* buffer, int j, uint32_t row, uint32_t col) {
@@ -124,11 +124,14 @@ template <typename DyT, typename S> __device__ __forceinline__ void put_dy(const
         *reinterpret_cast<typename Mma<DyT>::frag*>(buffer + p * S::DY_BYTES + lds_at<S::TILE_O>(row + S::DY_ROWS * j, col)) = part[p];
 }
 template <typename DyT, typename S> __device__ __forceinline__ void put_q(const Staged<DyT, S>& from, char* buffer, int j, uint32_t row, uint32_t col) {
-    typename Mma<DyT>::frag x;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i)
-        x[i] = static_cast<typename Mma<DyT>::elem>(static_cast<float>(static_cast<int32_t>(from.q[j][i / 4]) << (24 - 8 * (i % 4)) >> 24));
-    *reinterpret_cast<typename Mma<DyT>::frag*>(buffer + S::PARTS * S::DY_BYTES + lds_at<S::TILE_C>(row + S::X_ROWS * j, col)) = x;
+    for (int h = 0; h < S::XW / VEC; ++h) {
+        typename Mma<DyT>::frag x;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            x[i] = static_cast<typename Mma<DyT>::elem>(static_cast<float>(static_cast<int32_t>(from.q[j][2 * h + i / 4]) << (24 - 8 * (i % 4)) >> 24));
+        *reinterpret_cast<typename Mma<DyT>::frag*>(buffer + S::PARTS * S::DY_BYTES + lds_at<S::TILE_C>(row + S::X_ROWS * j, col + h * VEC)) = x;
+    }
 }
 template <typename DyT, typename S>
 __device__ __forceinline__ void put_step(const Staged<DyT, S>& from, char* buffer, uint32_t dy_row, uint32_t dy_col, uint32_t q_row, uint32_t q_col) {
@@ -222,11 +225,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     const int32_t t_end = min(A.tokens, static_cast<int32_t>((split_no + 1) * A.groups_per_split * GROUP));
 
     const uint32_t dy_col = threadIdx.x % (S::TILE_O / VEC) * VEC, dy_row = threadIdx.x / (S::TILE_O / VEC);
-    const uint32_t q_col = threadIdx.x % (S::TILE_C / VEC) * VEC, q_row = threadIdx.x / (S::TILE_C / VEC);
+    const uint32_t q_col = threadIdx.x % (S::TILE_C / S::XW) * S::XW, q_row = threadIdx.x / (S::TILE_C / S::XW);
     const int32_t o_in = o0 + static_cast<int32_t>(dy_col);
     const int dy_n = RAGGED ? max(0, min(A.outputs - o_in, VEC)) : VEC;
     const DyT* const dy_at = static_cast<const DyT*>(A.dy) + (RAGGED ? o_in : min(o_in, A.outputs - VEC));
-    const int8_t* const q_at = A.q + min(static_cast<int64_t>(c0 + q_col), A.ld - VEC);
+    const int8_t* const q_at = A.q + min(static_cast<int64_t>(c0 + q_col), A.ld - S::XW);
 
     const DyT* dy_next = dy_at + (t_first + static_cast<int64_t>(dy_row)) * A.dy_stride;      // the rows that are fetched next
     const int8_t* q_next = q_at + (t_first + static_cast<int64_t>(q_row)) * A.ld;
@@ -239,15 +242,15 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
             for (int j = 0; j < S::DY_VECS; ++j) to.dy[j] = load8(dy_next + j * (S::DY_ROWS * A.dy_stride), dy_n);
 #pragma unroll
             for (int j = 0; j < S::X_VECS; ++j)
-                if (!RAGGED || A.ld > 0) to.q[j] = *reinterpret_cast<const u32x2*>(q_next + j * (S::X_ROWS * A.ld));
+                if (!RAGGED || A.ld > 0) to.q[j] = *reinterpret_cast<const typename S::X*>(q_next + j * (S::X_ROWS * A.ld));
         } else {
             const int32_t dy_rows = A.tokens - t_next - static_cast<int32_t>(dy_row), q_rows = A.tokens - t_next - static_cast<int32_t>(q_row);
 #pragma unroll
             for (int j = 0; j < S::DY_VECS; ++j) to.dy[j] = load8(dy_next + j * (S::DY_ROWS * A.dy_stride), S::DY_ROWS * j < dy_rows ? dy_n : 0);
 #pragma unroll
             for (int j = 0; j < S::X_VECS; ++j) {
-                to.q[j] = u32x2{0, 0};
-                if ((!RAGGED || A.ld > 0) && S::X_ROWS * j < q_rows) to.q[j] = *reinterpret_cast<const u32x2*>(q_next + j * (S::X_ROWS * A.ld));
+                to.q[j] = typename S::X(0);
+                if ((!RAGGED || A.ld > 0) && S::X_ROWS * j < q_rows) to.q[j] = *reinterpret_cast<const typename S::X*>(q_next + j * (S::X_ROWS * A.ld));
             }
         }
         t_next += S::STEP;
@@ -404,11 +407,11 @@ __global__ __launch_bounds__(Short<DyT>::THREADS, SHORT_PER_CU) void linear_shor
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const uint32_t wave_o = wave / S::WAVES_C * (S::FRAGS * 32), wave_c = wave % S::WAVES_C * 64;
     const uint32_t dy_col = threadIdx.x % (S::TILE_O / VEC) * VEC, dy_row = threadIdx.x / (S::TILE_O / VEC);
-    const uint32_t q_col = threadIdx.x % (S::TILE_C / VEC) * VEC, q_row = threadIdx.x / (S::TILE_C / VEC);
+    const uint32_t q_col = threadIdx.x % (S::TILE_C / S::XW) * S::XW, q_row = threadIdx.x / (S::TILE_C / S::XW);
     const int32_t o_in = o0 + static_cast<int32_t>(dy_col);
     const int dy_n = RAGGED ? max(0, min(A.outputs - o_in, VEC)) : VEC;
     const DyT* const dy_at = static_cast<const DyT*>(A.dy) + (RAGGED ? o_in : min(o_in, A.outputs - VEC));
-    const int8_t* const q_at = A.q + min(static_cast<int64_t>(c0 + q_col), A.ld - VEC);
+    const int8_t* const q_at = A.q + min(static_cast<int64_t>(c0 + q_col), A.ld - S::XW);
     const uint32_t r = lane / 32 * 8 + lane % 16 / 4, cc = lane / 16 % 2 * 16 + lane % 4 * 4;
     float scale[2];
 #pragma unroll
@@ -428,8 +431,8 @@ __global__ __launch_bounds__(Short<DyT>::THREADS, SHORT_PER_CU) void linear_shor
 #pragma unroll
         for (int j = 0; j < S::X_VECS; ++j) {
             const int32_t t = t0 + q_row + S::X_ROWS * j;
-            staged.q[j] = u32x2{0, 0};
-            if (t < A.tokens && (!RAGGED || A.ld > 0)) staged.q[j] = *reinterpret_cast<const u32x2*>(q_at + t * A.ld);
+            staged.q[j] = typename S::X(0);
+            if (t < A.tokens && (!RAGGED || A.ld > 0)) staged.q[j] = *reinterpret_cast<const typename S::X*>(q_at + t * A.ld);
         }
         if (t0 > 0) __syncthreads();
         put_step<DyT, S>(staged, lds, dy_row, dy_col, q_row, q_col);
@@ -500,13 +503,15 @@ template <typename GradT> __global__ __launch_bounds__(JOIN_THREADS) void linear
     store_some(w, sum, A.channels - static_cast<int32_t>(c));
 }
 
-// The tiles: 256 outputs by 128 channels, 64 tokens a step, 144 KiB of LDS; where dy takes three parts 32 tokens and 128 KiB.
-template <typename DyT> using Wide = Shape<DyT, 2, 4, 2, sizeof(DyT) == 4 ? 32 : 64, sizeof(DyT) == 4 ? 2 : 3>;
+// The tiles: 256 outputs by 128 channels, 64 tokens a step, 144 KiB of LDS.  Where dy takes three parts, 128 outputs by 256 channels,
+// 32 tokens and 128 KiB: q's bytes are the cheaper ones there (1024 channels, 4096 outputs, 32768 tokens 753 us, the other
+// way round 830; level in 16 bits).
+template <typename DyT> using Wide = Shape<DyT, 2, sizeof(DyT) == 4 ? 2 : 4, sizeof(DyT) == 4 ? 4 : 2, sizeof(DyT) == 4 ? 32 : 64, sizeof(DyT) == 4 ? 2 : 3>;
 // Square ones: 128 outputs by 128 channels, half as many registers for sums.
 template <typename DyT> using Square = Shape<DyT, 1, 4, 2, sizeof(DyT) == 4 ? 32 : 64, sizeof(DyT) == 4 ? 2 : 3>;
-constexpr int TILE_C = 128;
-enum { SHORT, SQUARE, WIDE };
-constexpr int TILE_O[] = {SHORT_TILE_O, 128, 256};
+enum { SHORT, SQUARE, WIDE, WIDE_PARTS };
+constexpr int TILE_O[] = {SHORT_TILE_O, 128, 256, 128}, TILE_C[] = {128, 128, 128, 256};
+static_assert(Wide<float>::TILE_O == TILE_O[WIDE_PARTS] && Wide<__bf16>::TILE_O == TILE_O[WIDE] && Square<float>::TILE_O == TILE_O[SQUARE], "tiles");
 
 struct LinearPlan {
     int form;
@@ -520,11 +525,12 @@ struct LinearPlan {
 // 55 and 60; binary32 with 256 tokens, 1024 channels and outputs 18 and 13.
 constexpr int64_t SQUARE_GROUPS = 16;
 
-LinearPlan plan_of(int64_t tokens, int64_t channels, int64_t outputs) {
+LinearPlan plan_of(int64_t tokens, int64_t channels, int64_t outputs, bool parts) {
     LinearPlan p{};
     p.groups = static_cast<uint32_t>(ceil_div(tokens, GROUP));
-    p.tiles_c = static_cast<uint32_t>(std::max<int64_t>(ceil_div(channels, TILE_C), 1));       // the bias is made with some tile
-    p.form = p.groups <= 1 ? SHORT : p.groups <= SQUARE_GROUPS && ceil_div(outputs, TILE_O[WIDE]) * p.tiles_c < 256 ? SQUARE : WIDE;
+    const int wide = parts ? WIDE_PARTS : WIDE;
+    p.form = p.groups <= 1 ? SHORT : p.groups <= SQUARE_GROUPS && ceil_div(outputs, TILE_O[wide]) * ceil_div(channels, TILE_C[wide]) < 256 ? SQUARE : wide;
+    p.tiles_c = static_cast<uint32_t>(std::max<int64_t>(ceil_div(channels, TILE_C[p.form]), 1));       // the bias is made with some tile
     p.tiles_o = static_cast<uint32_t>(ceil_div(outputs, TILE_O[p.form]));
     const int64_t tiles = static_cast<int64_t>(p.tiles_o) * p.tiles_c;
     // enough workgroups for each of the 256 compute units, and two groups at the least for each of them
@@ -551,7 +557,7 @@ extern "C" {
 
 int mgwfbp_act_linear_grad_workspace(int64_t n_tokens, int64_t n_channels, int64_t n_outputs, uint64_t* bytes_out) {
     if (bytes_out == nullptr || !sizes_ok(n_tokens, n_channels, n_outputs)) return MGWFBP_EINVAL;
-    *bytes_out = static_cast<uint64_t>(plan_of(n_tokens, n_channels, n_outputs).bytes);
+    *bytes_out = static_cast<uint64_t>(std::max(plan_of(n_tokens, n_channels, n_outputs, false).bytes, plan_of(n_tokens, n_channels, n_outputs, true).bytes));
     return MGWFBP_OK;
 }
 
@@ -572,7 +578,7 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
     }
     if (d_db != nullptr && !is_aligned(d_db, dtype_bytes(grad_dtype))) return MGWFBP_EINVAL;
     if (n_tokens > 0 && (d_dy == nullptr || !is_aligned(d_dy, dtype_bytes(dy_dtype)))) return MGWFBP_EINVAL;
-    const LinearPlan p = plan_of(n_tokens, n_channels, n_outputs);
+    const LinearPlan p = plan_of(n_tokens, n_channels, n_outputs, dy_dtype == MGWFBP_F32);
     if (p.bytes > 0 && (d_workspace == nullptr || !is_aligned(d_workspace, 256) || workspace_bytes < static_cast<uint64_t>(p.bytes)))
         return MGWFBP_EINVAL;
     LinearArgs a{};
@@ -598,7 +604,7 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
     a.bias_shares = p.bias_shares;
     a.accumulate = accumulate != 0;
     if (n_channels == 0) a.ld = 0;                       // no q: the bias alone
-    // Split launches have at most 256 tiles of 256 x 128, so that the join's threads number less than 2^22.
+    // Split launches have at most 256 tiles, so that the join's threads number less than 2^22.
     a.bias_blocks = d_db != nullptr ? static_cast<uint32_t>(ceil_div(n_outputs, JOIN_THREADS)) : 0;
     const dim3 join_grid(a.bias_blocks + static_cast<uint32_t>(p.splits > 1 ? ceil_div(n_outputs * (p.channels_padded / 4), JOIN_THREADS) : 0));
     return with_dtype(dy_dtype, [&](auto* dy_type) {

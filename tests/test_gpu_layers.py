@@ -409,6 +409,21 @@ def test_act_linear_grad(tokens, channels, outputs, dy_t, grad_t):
     _close(db, d64.sum(0).cuda() + had_b.double(), (tokens + 9) * 2.0 ** -24 * (d64.abs().sum(0).cuda() + had_b.double().abs()), "accumulated db")
 
 
+@pytest.mark.parametrize("dy_t", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tokens,channels,outputs", [(700, 4100, 2304), (3000, 1030, 520), (6000, 520, 1100), (8200, 260, 96)])
+def test_act_linear_grad_of_many_tiles_and_tokens(tokens, channels, outputs, dy_t):
+    """Long enough for every stage of the pipeline through LDS, split over the tokens and not."""
+    _say("act_linear_grad, large", tokens, channels, outputs, dy_t)
+    g = _gen(tokens)
+    act, x = _checkpoint(tokens, channels, g)
+    dy = torch.randn(tokens, outputs, generator=g, device="cuda").to(DT[dy_t])
+    dw, db = torch.empty(outputs, channels, device="cuda"), torch.empty(outputs, device="cuda")
+    layers.act_linear_grad(dy, act, dw, db=db)
+    d64 = dy.double().t().contiguous()
+    _close(dw, d64 @ x, _linear_slack(tokens, d64.abs() @ x.abs(), 0.0), "dw")
+    _close(db, d64.sum(1), (tokens + 8) * 2.0 ** -24 * d64.abs().sum(1), "db")
+
+
 def test_act_linear_grad_of_no_tokens_and_of_no_channels():
     act = layers.act_empty(0, 40)
     dw, db = torch.full((9, 40), 3.0, device="cuda"), torch.full((9,), 3.0, device="cuda")
