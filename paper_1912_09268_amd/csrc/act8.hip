@@ -24,6 +24,7 @@ constexpr int THREADS = 256;
 constexpr int GROUP = MGWFBP_ACT_GROUP;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // ---------------------------------------------------------------------------------------------
 // store
@@ -44,82 +45,99 @@ constexpr int BLOCK_COLS = LANES * VEC;
 constexpr int ROWS = THREADS / LANES;                        // rows of a step
 constexpr int STEPS = GROUP / ROWS;
 
+// Magnitudes of eight elements as bit patterns without sign, in which infinities and NaN are above all finite ones; 16-bit types
+// are kept in pairs.
+template <typename T> struct Magnitudes {
+    static constexpr int N = VEC * sizeof(T) / 4;
+    uint32_t m[N] = {};
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        if constexpr (sizeof(T) == 4) return max(a, b);
+        else return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    }
+    __device__ __forceinline__ void take(const Raw8<T>& x) {
+        typedef uint32_t words __attribute__((ext_vector_type(N)));
+        const words w = __builtin_bit_cast(words, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) m[i] = larger(m[i], w[i] & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu));
+    }
+    __device__ __forceinline__ void take(int i, uint32_t other) { m[i] = larger(m[i], other); }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, m[i]);
+        else return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(m[i / 2] >> (16 * (i % 2)))));
+    }
+};
+
+// Four whole numbers of -127 .. 127 to bytes: added to 1.5 * 2^23 a number's last eight bits are those of the sum, which rounds to
+// nearest even on the way.  (NaN gives 0.)
+__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d) {
+    auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x + 12582912.f); };
+    const uint32_t low = __builtin_amdgcn_perm(bits(b), bits(a), 0x0c0c0400), high = __builtin_amdgcn_perm(bits(d), bits(c), 0x04000c0c);
+    return low | high;
+}
+
 // A workgroup takes 128 channels of a group: the whole of it stays in registers between the search for the largest magnitude
-// and the rounding, so x is read once.
-template <typename T, int KIND> __global__ __launch_bounds__(THREADS) void store_kernel(StoreArgs A) {
+// and the rounding, so x is read once.  y does not wait for that: it is made and written as rows arrive.
+template <typename T, int KIND, bool Y> __global__ __launch_bounds__(THREADS) void store_kernel(StoreArgs A) {
     const uint32_t g = blockIdx.x / A.col_blocks, cb = blockIdx.x - g * A.col_blocks;
     const uint32_t lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
     const int64_t col = static_cast<int64_t>(cb) * BLOCK_COLS + lane * VEC;
     const int n = static_cast<int>(max(static_cast<int64_t>(0), min(A.channels - col, static_cast<int64_t>(VEC))));
     const int64_t t0 = static_cast<int64_t>(g) * GROUP + row;
+    const T* const from = static_cast<const T*>(A.x) + t0 * A.x_stride + col;
+    T* const to = static_cast<T*>(A.y) + t0 * A.y_stride + col;
     Raw8<T> x[STEPS];
 #pragma unroll
+    for (int s = 0; s < STEPS; ++s) x[s] = load8(from + s * (ROWS * A.x_stride), t0 + s * ROWS < A.tokens ? n : 0);
+    Magnitudes<T> most;
+#pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        const int64_t t = t0 + s * ROWS;
-        x[s] = load8(static_cast<const T*>(A.x) + t * A.x_stride + col, t < A.tokens ? n : 0);
+        most.take(x[s]);
+        if constexpr (Y)
+            if (t0 + s * ROWS < A.tokens && n > 0) {
+                float out[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    float slope;
+                    activate<KIND>(get(x[s], i), out[i], slope);
+                }
+                store8(to + s * (ROWS * A.y_stride), out, n);
+            }
     }
-    // Largest magnitudes, as bit patterns: those of infinities and NaN are above all finite ones'.
-    uint32_t most[VEC] = {};
+    constexpr int N = Magnitudes<T>::N;
+    __shared__ uint32_t of_wave[THREADS / 64][LANES * N];
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) most[i] = max(most[i], __builtin_bit_cast(uint32_t, get(x[s], i)) & 0x7fffffffu);
-    __shared__ uint32_t of_wave[THREADS / 64][BLOCK_COLS];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        most[i] = max(most[i], __shfl_xor(most[i], 16));
-        most[i] = max(most[i], __shfl_xor(most[i], 32));
+    for (int i = 0; i < N; ++i) {
+        most.take(i, __shfl_xor(most.m[i], 16));
+        most.take(i, __shfl_xor(most.m[i], 32));
+        if (threadIdx.x % 64 < LANES) of_wave[threadIdx.x / 64][lane * N + i] = most.m[i];
     }
-    if (threadIdx.x % 64 < LANES)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) of_wave[threadIdx.x / 64][lane * VEC + i] = most[i];
     __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) most.take(i, of_wave[w][lane * N + i]);
+    if (col >= A.ld) return;
     float scale[VEC], inv[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-#pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) most[i] = max(most[i], of_wave[w][lane * VEC + i]);
-        const bool finite = most[i] < 0x7f800000u;
-        // The bound keeps scale and its inverse normal numbers.
-        scale[i] = max(__builtin_bit_cast(float, most[i]), 0x1p-100f) * (1.f / 127.f);
+        // The bound keeps scale and its inverse normal numbers.  A group that is not finite has codes of 0: its elements times 0
+        // are 0 or NaN.
+        const float largest = most.get(i);
+        const bool finite = __builtin_bit_cast(uint32_t, largest) < 0x7f800000u;
+        scale[i] = max(largest, 0x1p-100f) * (1.f / 127.f);
         inv[i] = finite ? 1.f / scale[i] : 0.f;
-        if (!finite) scale[i] = __builtin_nanf("");
+        scale[i] = i >= n ? 0.f : finite ? scale[i] : __builtin_nanf("");
     }
-    if (col < A.ld) {
-        if (row == 0) {
-            float out[VEC];
+    if (row == 0) store8(A.scale + g * A.ld + col, scale);
+    int8_t* const q = A.q + t0 * A.ld + col;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) out[i] = i < n ? scale[i] : 0.f;
-            store8(A.scale + g * A.ld + col, out);
-        }
+    for (int s = 0; s < STEPS; ++s) {
+        if (t0 + s * ROWS >= A.tokens) break;
+        float r[VEC];
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int64_t t = t0 + s * ROWS;
-            if (t >= A.tokens) break;
-            u32x2 packed = {0, 0};
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                // Times 0 in a group that is not finite: 0, or NaN, which the comparisons of the clamp turn into -127.
-                const float r = __builtin_rintf(get(x[s], i) * inv[i]);
-                const int32_t code = inv[i] != 0.f ? static_cast<int32_t>(__builtin_amdgcn_fmed3f(r, -127.f, 127.f)) : 0;
-                packed[i / 4] |= (static_cast<uint32_t>(code) & 0xffu) << (8 * (i % 4));
-            }
-            *reinterpret_cast<u32x2*>(A.q + t * A.ld + col) = packed;
-        }
+        for (int i = 0; i < VEC; ++i) r[i] = get(x[s], i) * inv[i];
+        *reinterpret_cast<u32x2*>(q + s * (ROWS * A.ld)) = u32x2{four_codes(r[0], r[1], r[2], r[3]), four_codes(r[4], r[5], r[6], r[7])};
     }
-    if (A.y != nullptr && n > 0)
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int64_t t = t0 + s * ROWS;
-            if (t >= A.tokens) break;
-            float out[VEC];
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                float slope;
-                activate<KIND>(get(x[s], i), out[i], slope);
-            }
-            store8(static_cast<T*>(A.y) + t * A.y_stride + col, out, n);
-        }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -220,9 +238,10 @@ int mgwfbp_act_store(const void* d_x, int64_t x_stride, int32_t dtype, int64_t n
     const int64_t blocks = a.col_blocks * ceil_div(n_tokens, GROUP);
     if (blocks >= (int64_t(1) << 24)) return MGWFBP_EINVAL;
     return with_dtype(dtype, [&](auto* type) {
-        return with_kind(d_y == nullptr ? MGWFBP_IDENTITY : kind, [&](auto k) {
-            return launch(store_kernel<std::remove_pointer_t<decltype(type)>, decltype(k)::value>, a, dim3(static_cast<uint32_t>(blocks)),
-                          dim3(THREADS), hip_stream);
+        return with_kind(kind, [&](auto k) {
+            typedef std::remove_pointer_t<decltype(type)> T;
+            void (*kernel)(StoreArgs) = d_y == nullptr ? store_kernel<T, MGWFBP_IDENTITY, false> : store_kernel<T, decltype(k)::value, true>;
+            return launch(kernel, a, dim3(static_cast<uint32_t>(blocks)), dim3(THREADS), hip_stream);
         });
     });
 }

@@ -36,8 +36,8 @@ template <int KIND> __device__ __forceinline__ void activate(float x, float& val
         p = __builtin_fmaf(p, t, 0.09147620121370333f);
         p = __builtin_fmaf(p, t, 0.09317902474729383f);
         const float tail = p * t * e;
+        value = __builtin_fmaf(-__builtin_fabsf(x), tail, __builtin_fmaxf(x, 0.f));
         const float below = x >= 0.f ? 1.f - tail : tail;      // Phi(x)
-        value = x * below;
         slope = __builtin_fmaf(x * 0.3989422804014327f, e, below);
     } else if constexpr (KIND == MGWFBP_GELU_TANH) {
         // (1 + tanh u) / 2 is the logistic function of 2u
