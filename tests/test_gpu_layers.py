@@ -587,3 +587,36 @@ def test_both_ways_of_taking_tensors_apart_agree(monkeypatch):
         layers.embed_grad(x, ids, torch.empty(30, 48, device="cuda", dtype=torch.float64))
     with pytest.raises(ValueError):
         layers.act_linear_grad(x, layers.act_store(x), torch.empty(48, 48, device="cuda"), workspace=torch.empty(16, device="cuda")[1:])
+
+
+@pytest.mark.parametrize("spread", ["words", "one", "holes"])
+@pytest.mark.parametrize("tokens,rows,dim", [(131, 3, 200), (300, 4, 1025), (129, 4, 7), (40000, 4, 24), (5000, 1, 2056), (9001, 100, 17),
+                                            (8200, 6, 520), (12000, 200000, 16), (6000, 300000, 8), (257, 30000, 48)])
+def test_embed_grad_in_every_form(tokens, rows, dim, spread):
+    """Few rows in one and in several chunks of tokens; one, two and three passes of the sort; ranking with narrow and wide keys."""
+    test_embed_grad(tokens, rows, dim, spread)
+
+
+def test_rows_of_activations_beyond_32_bits_of_offset():
+    """Views whose last rows begin more than 2^32 elements behind the first."""
+    _say("act_*: offsets beyond 2^32 elements")
+    tokens, stride, channels = 530001, 8192, 24
+    memory = torch.empty(tokens * stride, dtype=BF16, device="cuda")         # 4.3e9 elements
+    x = torch.as_strided(memory, (tokens, channels), (stride, 1))
+    want = (torch.arange(tokens, device="cuda") % 127 + 1).to(BF16)[:, None] * torch.tensor([1.0, -1.0], device="cuda", dtype=BF16).repeat(channels // 2)
+    x.copy_(want)
+    act = layers.act_store(x)
+    back = layers.act_backward(act, y=torch.empty(tokens, channels, device="cuda"))
+    # half a step of 1/127 of the group's largest, 127, and the roundings of a product and a quotient
+    assert float((back - want.float()).abs().max()) < 0.5 * 127 / 127 * 1.001
+    dw, db = torch.empty(channels, channels, device="cuda"), torch.empty(channels, device="cuda")
+    layers.act_linear_grad(x, act, dw, db=db)                                  # dy is the view
+    exact = want.double().t().contiguous() @ back.double()
+    assert float((dw.double() - exact).abs().max()) < 2e-5 * float(exact.abs().max())
+    assert float((db.double() - want.double().sum(0)).abs().max()) < 2e-5 * float(want.double().abs().sum(0).max())
+    grad = layers.embed_grad(x, torch.arange(tokens, device="cuda") // 3, torch.empty((tokens + 2) // 3, channels, device="cuda"))
+    last = (tokens - 1) // 3 * 3
+    assert torch.equal(grad[-1], want[last:].float().sum(0)) and torch.equal(grad[1000], want[3000:3003].float().sum(0))
+    memory[(tokens - 1) * stride:].fill_(7.0)
+    dx = layers.act_backward(act, x, kind="identity", dx=torch.as_strided(torch.empty_like(memory), (tokens, channels), (stride, 1)))
+    assert torch.equal(dx[-1], x[-1]) and torch.equal(dx[524287:524290], x[524287:524290])
