@@ -305,16 +305,18 @@ __global__ __launch_bounds__(THREADS) void move_kernel(GradArgs A) {
 
 // ---- sums ----
 
-template <typename GradT> __device__ __forceinline__ void write_row(const GradArgs& A, int32_t r, int64_t col, int n, float (&sum)[VEC]) {
+template <typename GradT, bool ACCUMULATE>
+__device__ __forceinline__ void write_row(const GradArgs& A, int32_t r, int64_t col, int n, const float (&sum)[VEC]) {
     GradT* const g = static_cast<GradT*>(A.grad) + r * A.grad_stride + col;
+    float x[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) sum[i] *= A.scale;
-    if (A.accumulate) {
+    for (int i = 0; i < VEC; ++i) x[i] = sum[i] * A.scale;
+    if constexpr (ACCUMULATE) {
         const Raw8<GradT> had = load8(g, n);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) sum[i] += get(had, i);
+        for (int i = 0; i < VEC; ++i) x[i] += get(had, i);
     }
-    store8(g, sum, n);
+    store8(g, x, n);
 }
 
 __device__ __forceinline__ void write_partial(const GradArgs& A, uint32_t which, int64_t col, const float (&sum)[VEC]) {
@@ -324,8 +326,10 @@ __device__ __forceinline__ void write_partial(const GradArgs& A, uint32_t which,
 }
 
 // One lane for eight columns of a chunk.  A row that begins in a chunk and ends in the next one is summed by the lanes of the
-// first alone; only rows that reach further are joined.
-template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) void sum_kernel(GradArgs A) {
+// first alone; only rows that reach further are joined.  What stands once for every token in the code is kept small (the
+// stretch from before the chunk and the one that goes on behind it are written at the end): with everything in place, the
+// instructions of a short launch came from memory for longer than its data.
+template <typename DyT, typename GradT, bool ACCUMULATE> __global__ __launch_bounds__(THREADS) void sum_kernel(GradArgs A) {
     if (blockIdx.x >= A.sum_blocks) {
         if (blockIdx.y == 0) clear_absent_rows<GradT>(A, static_cast<int64_t>(blockIdx.x - A.sum_blocks) * A.clear_rows);
         return;
@@ -339,6 +343,17 @@ template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) vo
     const int64_t first = static_cast<int64_t>(c) * A.chunk, end = min(first + A.chunk, A.tokens), further = min(end + A.chunk, A.tokens);
     const DyT* const dy = static_cast<const DyT*>(A.dy) + col;
     const int32_t none = static_cast<int32_t>(A.n_rows);
+    constexpr int AHEAD = sizeof(DyT) == 4 ? 8 : 16;             // 64 registers of dy on their way
+    u32x4 order[AHEAD / 4];                                      // the next places, asked for early: whole fours, padded to 256 bytes
+    i32x4 rows[AHEAD / 4];
+    auto look = [&](int64_t p) {
+#pragma unroll
+        for (int j = 0; j < AHEAD / 4; ++j) {
+            order[j] = *reinterpret_cast<const u32x4*>(A.order + p + 4 * j);
+            rows[j] = *reinterpret_cast<const i32x4*>(A.row + p + 4 * j);
+        }
+    };
+    look(first);
     const int32_t front = A.row[first], back = A.row[end - 1];
     const int32_t before = first > 0 ? A.row[first - 1] : none, long_before = first > A.chunk ? A.row[first - A.chunk - 1] : none;
     const int32_t after = end < A.tokens ? A.row[end] : none, long_after = further < A.tokens ? A.row[further] : none;
@@ -349,37 +364,38 @@ template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) vo
     const bool skips = came && !through && long_before != front;            // the chunk before has summed it
     const bool extends = goes_on && !through && long_after != back;
     const int64_t stop = extends ? further : end;
-    constexpr int AHEAD = sizeof(DyT) == 4 ? 8 : 16;             // 64 registers of dy on their way
-    float sum[VEC] = {};
+    float sum[VEC] = {}, head[VEC] = {};
     int32_t current = none;
     for (int64_t p0 = first; p0 < stop; p0 += AHEAD) {
         Raw8<DyT> x[AHEAD];
         int32_t r[AHEAD];
         uint32_t token[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; j += 4) {                     // whole fours: order and row are padded to 256 bytes
-            const u32x4 four = *reinterpret_cast<const u32x4*>(A.order + p0 + j);
-            const i32x4 rows = *reinterpret_cast<const i32x4*>(A.row + p0 + j);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t p = p0 + j + i;
-                const bool counts = p < end ? !(skips && rows[i] == front) : p < stop && rows[i] == back;
-                r[j + i] = counts ? rows[i] : none;
-                token[j + i] = r[j + i] != none ? four[i] : 0;
-            }
+        for (int j = 0; j < AHEAD; ++j) {
+            const int64_t p = p0 + j;
+            const int32_t row = rows[j / 4][j % 4];
+            const bool counts = p < end ? !(skips && row == front) : p < stop && row == back;
+            r[j] = counts ? row : none;
+            token[j] = r[j] != none ? order[j / 4][j % 4] : 0;
         }
+        if (n == VEC) {
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) x[j] = load8(dy + static_cast<int64_t>(token[j]) * A.dy_stride, n);
+            for (int j = 0; j < AHEAD; ++j) x[j] = load8(dy + static_cast<int64_t>(token[j]) * A.dy_stride);
+        } else {
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) x[j] = load8(dy + static_cast<int64_t>(token[j]) * A.dy_stride, n);
+        }
+        if (p0 + AHEAD < stop) look(p0 + AHEAD);
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            if (r[j] != current) {
-                if (current != none) {                          // a stretch has ended
-                    if (came && current == front) write_partial(A, 2 * c, col, sum);
-                    else if (goes_on && !extends && current == back) write_partial(A, 2 * c + 1, col, sum);
-                    else write_row<GradT>(A, current, col, n, sum);
+            if (r[j] != current) {                              // a stretch has ended
+                if (came && current == front)
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
-                }
+                    for (int i = 0; i < VEC; ++i) head[i] = sum[i];
+                else if (current != none)
+                    write_row<GradT, ACCUMULATE>(A, current, col, n, sum);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
                 current = r[j];
             }
             if (r[j] != none)
@@ -387,10 +403,12 @@ template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) vo
                 for (int i = 0; i < VEC; ++i) sum[i] += get(x[j], i);
         }
     }
-    if (current != none) {
-        if (came && current == front) write_partial(A, 2 * c, col, sum);
-        else if (goes_on && !extends && current == back) write_partial(A, 2 * c + 1, col, sum);
-        else write_row<GradT>(A, current, col, n, sum);
+    // The last stretch is still in sum if it reaches the end; one that ends in tokens without a row has been written.
+    const bool front_last = came && current == front;
+    if (came && !skips) write_partial(A, 2 * c, col, front_last ? sum : head);
+    if (current != none && !front_last) {
+        if (goes_on && !extends && current == back) write_partial(A, 2 * c + 1, col, sum);
+        else write_row<GradT, ACCUMULATE>(A, current, col, n, sum);
     }
     if (v == 0 && goes_on && !through && !extends)              // begins here: to be joined
         A.joins[1 + atomicAdd(reinterpret_cast<uint32_t*>(A.joins), 1u)] = u32x2{c, static_cast<uint32_t>(back)};
@@ -746,8 +764,9 @@ int mgwfbp_embed_grad(const void* d_ids, int32_t id_type, int64_t n_tokens, cons
     const dim3 grid(a.sum_blocks + clearing, std::max<uint32_t>(static_cast<uint32_t>(ceil_div(p.chunks, a.page)), 1));
     rc = with_dtype(dy_dtype, [&](auto* dy_type) {
         return with_dtype(grad_dtype, [&](auto* grad_type) {
-            return launch(sum_kernel<std::remove_pointer_t<decltype(dy_type)>, std::remove_pointer_t<decltype(grad_type)>>, a, grid,
-                          dim3(THREADS), hip_stream);
+            typedef std::remove_pointer_t<decltype(dy_type)> DyT;
+            typedef std::remove_pointer_t<decltype(grad_type)> GradT;
+            return launch(accumulate ? sum_kernel<DyT, GradT, true> : sum_kernel<DyT, GradT, false>, a, grid, dim3(THREADS), hip_stream);
         });
     });
     if (rc != MGWFBP_OK || p.chunks < 2) return rc;
