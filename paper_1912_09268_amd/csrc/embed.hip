@@ -185,12 +185,22 @@ template <typename Key, typename IdT> __global__ __launch_bounds__(THREADS) void
     const uint32_t n = static_cast<uint32_t>(A.tokens);
     const uint32_t first = blockIdx.x * RANK_EACH;
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    auto key_of = [&](uint32_t t) { return static_cast<Key>(static_cast<uint32_t>(row_of(A, static_cast<const IdT*>(A.ids)[t]))) << TOKEN_BITS | t; };
+    const IdT* const ids = static_cast<const IdT*>(A.ids);
+    auto key_of = [&](IdT id, uint32_t t) { return static_cast<Key>(static_cast<uint32_t>(row_of(A, id))) << TOKEN_BITS | t; };
+    IdT other[RANK_AHEAD];                                   // ids of the next turn
+    auto look = [&](uint32_t s0) {
+#pragma unroll
+        for (int j = 0; j < RANK_AHEAD; ++j) other[j] = ids[min(s0 + j * THREADS + lane, n - 1)];
+    };
+    look(wave * 64);
+    IdT mine[RANK_EACH];
+#pragma unroll
+    for (int r = 0; r < RANK_EACH; ++r) mine[r] = ids[min(first + r, n - 1)];
     Key own[RANK_EACH];
     uint32_t count[RANK_EACH];
 #pragma unroll
     for (int r = 0; r < RANK_EACH; ++r) {
-        own[r] = key_of(min(first + r, n - 1));
+        own[r] = key_of(mine[r], min(first + r, n - 1));
         count[r] = 0;
         if (threadIdx.x == 0) own_row[r] = static_cast<int32_t>(own[r] >> TOKEN_BITS);
     }
@@ -199,9 +209,10 @@ template <typename Key, typename IdT> __global__ __launch_bounds__(THREADS) void
 #pragma unroll
         for (int j = 0; j < RANK_AHEAD; ++j) {
             const uint32_t s = s0 + j * THREADS + lane;
-            const Key k = key_of(min(s, n - 1));
+            const Key k = key_of(other[j], min(s, n - 1));
             key[j] = s < n ? k : ~Key(0);
         }
+        if (s0 + RANK_AHEAD * THREADS < n) look(s0 + RANK_AHEAD * THREADS);
 #pragma unroll
         for (int j = 0; j < RANK_AHEAD; ++j)
 #pragma unroll
