@@ -84,7 +84,8 @@ __global__ __launch_bounds__(THREADS) void embed_kernel(EmbedArgs A) {
 // gradient
 // ---------------------------------------------------------------------------------------------
 //
-// A table of up to FEW_ROWS rows (token types) needs no order: every lane keeps a sum for each row (few_rows_kernel, and
+// Up to FEW_TOKENS_MOST tokens need no order: every row looks for its own (direct_kernel; one launch).
+// A table of up to FEW_ROWS rows (token types) needs none either: every lane keeps a sum for each row (few_rows_kernel, and
 // few_join_kernel where there are several chunks of tokens).  4096 tokens of 1024 bfloat16 columns and 2 rows: 8 us, and 21
 // the other way.  For the rest:
 // 1. Tokens are ordered by (row, token).  Up to RANKED_TOKENS tokens a token's place is the number of tokens before it,
@@ -481,6 +482,67 @@ template <typename GradT> __global__ __launch_bounds__(THREADS) void join_kernel
     }
 }
 
+// ---- few tokens: no order, every row looks for its own ----
+
+constexpr int64_t FEW_TOKENS_MOST = 256;
+constexpr int DIRECT_WAVES = THREADS / 64;
+
+// Lanes hold the ids, LANE_IDS each; a row's tokens are the bits of as many comparisons.  A wavefront takes one row after the other,
+// and 512 columns: zeros where there are no tokens, else their sum in order, AHEAD of them on their way at a time.
+template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) void direct_kernel(GradArgs A) {
+    constexpr int LANE_IDS = FEW_TOKENS_MOST / 64;
+    constexpr int AHEAD = sizeof(DyT) == 4 ? 8 : 16;
+    const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t n = static_cast<uint32_t>(A.tokens);
+    int32_t row[LANE_IDS];
+#pragma unroll
+    for (int k = 0; k < LANE_IDS; ++k) {
+        const uint32_t t = k * 64 + lane;
+        row[k] = row_of(A, id_at(A.ids, A.id_type, min(t, n - 1)));
+        if (t >= n) row[k] = static_cast<int32_t>(A.n_rows);
+    }
+    const int64_t col = (static_cast<int64_t>(blockIdx.y) * 64 + lane) * VEC;
+    const int width = static_cast<int>(max(int64_t(0), min(A.dim - col, static_cast<int64_t>(VEC))));
+    const DyT* const dy = static_cast<const DyT*>(A.dy) + col;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * A.clear_rows, end = min(first + A.clear_rows, A.n_rows);
+    for (int64_t r = first + wave; r < end; r += DIRECT_WAVES) {
+        uint64_t mine[LANE_IDS];
+#pragma unroll
+        for (int k = 0; k < LANE_IDS; ++k) mine[k] = __ballot(row[k] == static_cast<int32_t>(r));
+        uint32_t count = 0;
+#pragma unroll
+        for (int k = 0; k < LANE_IDS; ++k) count += __popcll(mine[k]);
+        if (count == 0 && A.accumulate) continue;
+        float sum[VEC] = {};
+        for (uint32_t done = 0; done < count; done += AHEAD) {
+            Raw8<DyT> x[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {                    // the next token: the lowest bit that is left
+                uint32_t t = 0;
+                bool found = false;
+#pragma unroll
+                for (int k = 0; k < LANE_IDS; ++k)
+                    if (!found && mine[k] != 0) {
+                        t = k * 64 + __builtin_ctzll(mine[k]);
+                        mine[k] &= mine[k] - 1;
+                        found = true;
+                    }
+                x[j] = load8(dy + static_cast<int64_t>(t) * A.dy_stride, done + j < count ? width : 0);
+            }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+                if (done + j < count)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) sum[i] += get(x[j], i);
+        }
+        if (width > 0) {
+            if (count == 0) store8(static_cast<GradT*>(A.grad) + r * A.grad_stride + col, sum, width);
+            else if (A.accumulate) write_row<GradT, true>(A, static_cast<int32_t>(r), col, width, sum);
+            else write_row<GradT, false>(A, static_cast<int32_t>(r), col, width, sum);
+        }
+    }
+}
+
 // ---- few rows: no order, a sum for each row in every lane ----
 
 constexpr int FEW_ROWS = 4;
@@ -573,7 +635,7 @@ int passes_of(int64_t n_rows) {          // of eight bits, for the numbers 0 .. 
 }
 
 struct GradPlan {
-    bool few, ranked;
+    bool direct, few, ranked;          // the forms that need no order; how the others order
     uint32_t chunk, chunks, blocks, items;
     int64_t dim_padded;
     int64_t order, row, partial, joins, other_order, other_row, counts, bytes;     // places in the workspace
@@ -582,9 +644,10 @@ struct GradPlan {
 // What is in the workspace, and where: every part begins on 256 bytes.
 GradPlan plan_of(int64_t tokens, int64_t n_rows, int64_t dim) {
     GradPlan p{};
-    p.few = n_rows <= FEW_ROWS;
+    p.direct = tokens <= FEW_TOKENS_MOST;
+    p.few = !p.direct && n_rows <= FEW_ROWS;
     p.ranked = tokens <= RANKED_TOKENS;
-    if (tokens == 0) return p;                               // nothing to order
+    if (p.direct) return p;                                  // no workspace
     // Chunks of 16 to 64 tokens: longer ones leave less to join, shorter ones more lanes that sum, of which a chip full is wanted.
     const int64_t lanes = tokens * ceil_div(std::max<int64_t>(dim, 1), VEC);
     p.chunk = lanes / 64 >= 131072 ? 64 : lanes / 32 >= 65536 ? 32 : 16;
@@ -729,7 +792,19 @@ int mgwfbp_embed_grad(const void* d_ids, int32_t id_type, int64_t n_tokens, cons
         a.partial = reinterpret_cast<float*>(ws + p.partial);
         a.joins = reinterpret_cast<u32x2*>(ws + p.joins);
     }
-    if (p.few && n_tokens > 0) {
+    if (p.direct && n_tokens > 0) {
+        // Rows of a workgroup: about 32 KiB of the gradient, but no fewer than its wavefronts, and so few that the chip is full.
+        const int64_t slices = ceil_div(dim, 64 * VEC), share = std::max<int64_t>(DIRECT_WAVES, 32768 / (std::min<int64_t>(dim, 64 * VEC) * dtype_bytes(grad_dtype)));
+        a.clear_rows = static_cast<uint32_t>(std::max<int64_t>(DIRECT_WAVES, std::min(share, ceil_div(n_rows * slices, 1024))));
+        const dim3 direct_grid(static_cast<uint32_t>(ceil_div(n_rows, a.clear_rows)), static_cast<uint32_t>(slices));
+        return with_dtype(dy_dtype, [&](auto* dy_type) {
+            return with_dtype(grad_dtype, [&](auto* grad_type) {
+                return launch(direct_kernel<std::remove_pointer_t<decltype(dy_type)>, std::remove_pointer_t<decltype(grad_type)>>, a, direct_grid, dim3(THREADS),
+                              hip_stream);
+            });
+        });
+    }
+    if (p.few) {
         const dim3 few_grid(static_cast<uint32_t>(ceil_div(dim, FEW_LANES * VEC)), p.chunks);
         const int status = with_dtype(dy_dtype, [&](auto* dy_type) {
             return with_dtype(grad_dtype, [&](auto* grad_type) {
@@ -747,7 +822,7 @@ int mgwfbp_embed_grad(const void* d_ids, int32_t id_type, int64_t n_tokens, cons
     // A workgroup clears about 32 KiB, at most one row a thread.
     a.clear_rows = static_cast<uint32_t>(std::min<int64_t>(THREADS, std::max<int64_t>(1, 32768 / (dim * dtype_bytes(grad_dtype)))));
     int rc = MGWFBP_OK;
-    if (p.ranked && n_tokens > 0) {
+    if (n_tokens > 0 && p.ranked) {
         void (*narrow)(GradArgs) = id_type == MGWFBP_I64 ? rank_kernel<uint32_t, int64_t> : rank_kernel<uint32_t, int32_t>;
         void (*wide)(GradArgs) = id_type == MGWFBP_I64 ? rank_kernel<uint64_t, int64_t> : rank_kernel<uint64_t, int32_t>;
         rc = launch(n_rows <= NARROW_ROWS ? narrow : wide, a, dim3(static_cast<uint32_t>(ceil_div(n_tokens, RANK_EACH))), dim3(THREADS), hip_stream);

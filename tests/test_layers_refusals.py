@@ -57,7 +57,7 @@ def test_embed_refuses():
 
 
 def test_embed_grad_refuses():
-    good = dict(d_ids=P, id_type=B.I64, n_tokens=100, d_dy=P, dy_stride=64, dy_dtype=B.BF16, scale=1.0, padding_row=-1, accumulate=False,
+    good = dict(d_ids=P, id_type=B.I64, n_tokens=1000, d_dy=P, dy_stride=64, dy_dtype=B.BF16, scale=1.0, padding_row=-1, accumulate=False,
                 d_grad=P, n_rows=10, dim=64, grad_stride=64, grad_dtype=B.F32, d_workspace=P, workspace_bytes=1 << 30)
 
     def refused(**kw):
@@ -66,7 +66,7 @@ def test_embed_grad_refuses():
     for bad in (dict(d_ids=0), dict(d_ids=P + 4), dict(id_type=7), dict(n_tokens=-1), dict(n_tokens=2 ** 26 + 1), dict(d_dy=0), dict(d_dy=P + 1),
                 dict(dy_stride=63), dict(dy_dtype=3), dict(d_grad=0), dict(d_grad=P + 2), dict(n_rows=-1), dict(n_rows=2 ** 31 - 1), dict(dim=-1),
                 dict(dim=2 ** 23 + 1), dict(grad_stride=63), dict(grad_dtype=-1), dict(d_workspace=0), dict(d_workspace=P + 128),
-                dict(workspace_bytes=B.embed_grad_workspace(100, 10, 64) - 1)):
+                dict(workspace_bytes=B.embed_grad_workspace(1000, 10, 64) - 1)):
         refused(**bad)
     B.embed_grad(*{**good, "n_rows": 0, "d_grad": 0}.values())
     B.embed_grad(*{**good, "n_tokens": 0, "accumulate": True, "d_ids": 0, "d_dy": 0, "d_workspace": 0, "workspace_bytes": 0}.values())
