@@ -93,7 +93,8 @@ int mgwfbp_act_backward(const int8_t* d_q, const float* d_scale, int64_t ld, int
 /* Weight and bias gradient of a linear layer, out[t,o] = sum over c of w[o,c] * x[t,c] + b[o], from the gradient dy of its
  * output [n_tokens][n_outputs] and the checkpoint of its input:
  *   dw[o,c] = sum over t of dy[t,o] * x^[t,c];  db[o] = sum over t of dy[t,o]        (d_db NULL: left out)
- * accumulate != 0 adds to what is in dw and db.  The products are exact; the sums binary32.
+ * accumulate != 0 adds to what is in dw and db.  The products are exact; the sums binary32.  A group's sum is one of
+ * dy * q, to which the scale is applied: dy stays below 2^114, so that 128 products of up to 127 stay finite.
  *   n_tokens 0..2^23, n_outputs 0..2^23; ceil(n_outputs/128) * ceil(n_channels/128) <= 2^22 */
 int mgwfbp_act_linear_grad_workspace(int64_t n_tokens, int64_t n_channels, int64_t n_outputs, uint64_t* bytes_out);
 int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, int64_t n_tokens, int64_t n_channels,

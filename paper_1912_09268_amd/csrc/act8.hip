@@ -68,7 +68,7 @@ template <typename T> struct Magnitudes {
 };
 
 // Four whole numbers of -127 .. 127 to bytes: added to 1.5 * 2^23 a number's last eight bits are those of the sum, which rounds to
-// nearest even on the way.  (NaN gives 0.)
+// nearest even on the way.
 __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d) {
     auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x + 12582912.f); };
     const uint32_t low = __builtin_amdgcn_perm(bits(b), bits(a), 0x0c0c0400), high = __builtin_amdgcn_perm(bits(d), bits(c), 0x04000c0c);
@@ -118,14 +118,15 @@ template <typename T, int KIND, bool Y> __global__ __launch_bounds__(THREADS) vo
         for (int w = 0; w < THREADS / 64; ++w) most.take(i, of_wave[w][lane * N + i]);
     if (col >= A.ld) return;
     float scale[VEC], inv[VEC];
+    u32x2 keep = {0, 0};                                     // a group that is not finite has codes of 0
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        // The bound keeps scale and its inverse normal numbers.  A group that is not finite has codes of 0: its elements times 0
-        // are 0 or NaN.
+        // The bound keeps scale and its inverse normal numbers.
         const float largest = most.get(i);
         const bool finite = __builtin_bit_cast(uint32_t, largest) < 0x7f800000u;
         scale[i] = max(largest, 0x1p-100f) * (1.f / 127.f);
-        inv[i] = finite ? 1.f / scale[i] : 0.f;
+        inv[i] = 1.f / scale[i];
+        keep[i / 4] |= finite ? 0xffu << (8 * (i % 4)) : 0u;
         scale[i] = i >= n ? 0.f : finite ? scale[i] : __builtin_nanf("");
     }
     if (row == 0) store8(A.scale + g * A.ld + col, scale);
@@ -136,7 +137,7 @@ template <typename T, int KIND, bool Y> __global__ __launch_bounds__(THREADS) vo
         float r[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) r[i] = get(x[s], i) * inv[i];
-        *reinterpret_cast<u32x2*>(q + s * (ROWS * A.ld)) = u32x2{four_codes(r[0], r[1], r[2], r[3]), four_codes(r[4], r[5], r[6], r[7])};
+        *reinterpret_cast<u32x2*>(q + s * (ROWS * A.ld)) = u32x2{four_codes(r[0], r[1], r[2], r[3]), four_codes(r[4], r[5], r[6], r[7])} & keep;
     }
 }
 

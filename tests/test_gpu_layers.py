@@ -589,6 +589,16 @@ def test_both_ways_of_taking_tensors_apart_agree(monkeypatch):
         layers.act_linear_grad(x, layers.act_store(x), torch.empty(48, 48, device="cuda"), workspace=torch.empty(16, device="cuda")[1:])
 
 
+def test_act_store_gives_codes_of_zero_for_every_nan():
+    """Whatever a NaN carries in its lower bits, and next to a finite channel."""
+    x = torch.randn(200, 24, device="cuda")
+    x.view(torch.int32)[3, 5], x.view(torch.int32)[150, 9], x[7, 6] = 0x7FC00001, -0x3FFF81, -math.inf
+    act = layers.act_store(x)
+    assert bool(act.scale[0, 5:7].isnan().all()) and bool(act.scale[1, 9].isnan()) and int(act.scale.isnan().sum()) == 3
+    assert not bool(act.q[:128, 5:7].any()) and not bool(act.q[128:, 9].any())
+    assert bool((act.q[128:, 5:7].abs().amax(0) == 127).all()) and int(act.q[:128, 9].abs().max()) == 127
+
+
 @pytest.mark.parametrize("spread", ["words", "one", "holes"])
 @pytest.mark.parametrize("tokens,rows,dim", [(131, 3, 200), (300, 4, 1025), (129, 4, 7), (40000, 4, 24), (5000, 1, 2056), (9001, 100, 17),
                                             (256, 9, 1100), (257, 9, 1100), (64, 5, 3000), (3, 70000, 24), (200, 100, 1),
