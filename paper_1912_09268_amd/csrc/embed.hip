@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "device_types.h"
 #include "mgwfbp_layers.h"
@@ -49,7 +50,8 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int32_t id_type, int64
 }
 
 // One lane for eight columns of a token.  Lanes run over the vectors of a token and on into the next token, so that
-// narrow tables fill wavefronts too.
+// narrow tables fill wavefronts too.  All of a token's ids, then all its rows are asked for at once: two waits for memory, which is
+// what bounds a short call (1 token of 1024 columns from three binary32 tables: 1.8 us).  4096 tokens: 6.3 us, 27 MB at 4.4 TB/s.
 template <typename TabT, typename OutT, int K>
 __global__ __launch_bounds__(THREADS) void embed_kernel(EmbedArgs A) {
     const uint32_t at = blockIdx.x * THREADS + threadIdx.x;
@@ -84,7 +86,7 @@ __global__ __launch_bounds__(THREADS) void embed_kernel(EmbedArgs A) {
 // gradient
 // ---------------------------------------------------------------------------------------------
 //
-// Up to FEW_TOKENS_MOST tokens need no order: every row looks for its own (direct_kernel; one launch).
+// Up to FEW_TOKENS_MOST tokens need no order: every row looks for its own (direct_kernel; one launch, see its rule).
 // A table of up to FEW_ROWS rows (token types) needs none either: every lane keeps a sum for each row (few_rows_kernel, and
 // few_join_kernel where there are several chunks of tokens).  4096 tokens of 1024 bfloat16 columns and 2 rows: 8 us, and 21
 // the other way.  For the rest:
@@ -338,7 +340,8 @@ __device__ __forceinline__ void write_partial(const GradArgs& A, uint32_t which,
 }
 
 // One lane for eight columns of a chunk.  A row that begins in a chunk and ends in the next one is summed by the lanes of the
-// first alone; only rows that reach further are joined.  What stands once for every token in the code is kept small (the
+// first alone; only rows that reach further are joined.  65543 tokens of 1024 binary32 columns into 30522 rows, 0.4 GB: 88 us, 4.5 TB/s,
+// the rate of a copy.  4096 bfloat16 tokens into as many rows: 13 us, of which writing 62 MB takes 9.  What stands once for every token in the code is kept small (the
 // stretch from before the chunk and the one that goes on behind it are written at the end): with everything in place, the
 // instructions of a short launch came from memory for longer than its data.
 template <typename DyT, typename GradT, bool ACCUMULATE> __global__ __launch_bounds__(THREADS) void sum_kernel(GradArgs A) {
@@ -488,7 +491,15 @@ constexpr int64_t FEW_TOKENS_MOST = 256;
 constexpr int DIRECT_WAVES = THREADS / 64;
 
 // Lanes hold the ids, LANE_IDS each; a row's tokens are the bits of as many comparisons.  A wavefront takes one row after the other,
-// and 512 columns: zeros where there are no tokens, else their sum in order, AHEAD of them on their way at a time.
+// and 512 columns: zeros where there are no tokens, else their sum in order, AHEAD of them on their way at a time.  Bound by
+// writing the table (30522 rows of 1024 bfloat16: 11 us, 5.5 TB/s), or by a launch (512 rows: 3 us).
+//
+// The rule.  256 tokens spread over 100 rows of 64 columns 3 us, over 30522 of 1024 columns 11, and 16 and 18 with an order; all in
+// one row, which one wavefront then adds alone, 21 and 12 (128 tokens: 11 and 12).  A row costs a wavefront its four comparisons however
+// short it is: 65536 rows of 64 columns 7 and 15 us, 200 thousand 15 and 16, of 512 columns 27 and 36.
+constexpr int64_t DIRECT_ROWS = 131072, DIRECT_DIM = 256;
+bool is_direct(int64_t tokens, int64_t n_rows, int64_t dim) { return tokens <= FEW_TOKENS_MOST && (n_rows <= DIRECT_ROWS || dim >= DIRECT_DIM); }
+
 template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) void direct_kernel(GradArgs A) {
     constexpr int LANE_IDS = FEW_TOKENS_MOST / 64;
     constexpr int AHEAD = sizeof(DyT) == 4 ? 8 : 16;
@@ -503,7 +514,10 @@ template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) vo
     }
     const int64_t col = (static_cast<int64_t>(blockIdx.y) * 64 + lane) * VEC;
     const int width = static_cast<int>(max(int64_t(0), min(A.dim - col, static_cast<int64_t>(VEC))));
-    const DyT* const dy = static_cast<const DyT*>(A.dy) + col;
+    // Lanes behind the last column read what the slice's first one reads: with nothing to read they would take another branch.
+    const int64_t in_col = width > 0 ? col : static_cast<int64_t>(blockIdx.y) * 64 * VEC;
+    const int in_width = static_cast<int>(min(A.dim - in_col, static_cast<int64_t>(VEC)));
+    const DyT* const dy = static_cast<const DyT*>(A.dy) + in_col;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * A.clear_rows, end = min(first + A.clear_rows, A.n_rows);
     for (int64_t r = first + wave; r < end; r += DIRECT_WAVES) {
         uint64_t mine[LANE_IDS];
@@ -512,32 +526,34 @@ template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) vo
         uint32_t count = 0;
 #pragma unroll
         for (int k = 0; k < LANE_IDS; ++k) count += __popcll(mine[k]);
-        if (count == 0 && A.accumulate) continue;
         float sum[VEC] = {};
-        for (uint32_t done = 0; done < count; done += AHEAD) {
-            Raw8<DyT> x[AHEAD];
+        if (count == 0) {
+            if (!A.accumulate && width > 0) store8(static_cast<GradT*>(A.grad) + r * A.grad_stride + col, sum, width);
+            continue;
+        }
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) {                    // the next token: the lowest bit that is left
-                uint32_t t = 0;
-                bool found = false;
+        for (int k = 0; k < LANE_IDS; ++k) {
+            uint64_t rest = mine[k];
+            auto take = [&](auto many) {                         // the next tokens: the lowest bits that are left
+                constexpr int N = decltype(many)::value;
+                Raw8<DyT> x[N];
 #pragma unroll
-                for (int k = 0; k < LANE_IDS; ++k)
-                    if (!found && mine[k] != 0) {
-                        t = k * 64 + __builtin_ctzll(mine[k]);
-                        mine[k] &= mine[k] - 1;
-                        found = true;
-                    }
-                x[j] = load8(dy + static_cast<int64_t>(t) * A.dy_stride, done + j < count ? width : 0);
-            }
+                for (int j = 0; j < N; ++j) {
+                    x[j] = load8(dy + static_cast<int64_t>(k * 64 + __builtin_ctzll(rest)) * A.dy_stride, in_width);
+                    rest &= rest - 1;
+                }
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j)
-                if (done + j < count)
+                for (int j = 0; j < N; ++j)
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) sum[i] += get(x[j], i);
+            };
+            uint32_t left = __popcll(rest);
+            for (; left >= AHEAD; left -= AHEAD) take(std::integral_constant<int, AHEAD>());
+            for (; left >= 4; left -= 4) take(std::integral_constant<int, 4>());
+            for (; left > 0; --left) take(std::integral_constant<int, 1>());
         }
         if (width > 0) {
-            if (count == 0) store8(static_cast<GradT*>(A.grad) + r * A.grad_stride + col, sum, width);
-            else if (A.accumulate) write_row<GradT, true>(A, static_cast<int32_t>(r), col, width, sum);
+            if (A.accumulate) write_row<GradT, true>(A, static_cast<int32_t>(r), col, width, sum);
             else write_row<GradT, false>(A, static_cast<int32_t>(r), col, width, sum);
         }
     }
@@ -549,7 +565,8 @@ constexpr int FEW_ROWS = 4;
 constexpr int FEW_LANES = 16, FEW_TOKENS = THREADS / FEW_LANES, FEW_AHEAD = 8;       // 128 columns of 16 tokens at a time
 
 // 128 columns of a chunk of tokens by a workgroup.  A token's vector is added to its row's sum and nothing to the others (a
-// selection, no product: what a token without a row holds does not matter).
+// selection, no product: what a token without a row holds does not matter).  Two launches of 4.4 and 3.5 us for 4096 tokens of 1024
+// bfloat16 columns, which are 8 MB: waits for memory and the launches themselves.
 template <typename DyT, typename GradT, int ROWS> __global__ __launch_bounds__(THREADS) void few_rows_kernel(GradArgs A) {
     __shared__ float sums[FEW_TOKENS][FEW_LANES * VEC + 4];
     const uint32_t lane = threadIdx.x % FEW_LANES, place = threadIdx.x / FEW_LANES;
@@ -644,7 +661,7 @@ struct GradPlan {
 // What is in the workspace, and where: every part begins on 256 bytes.
 GradPlan plan_of(int64_t tokens, int64_t n_rows, int64_t dim) {
     GradPlan p{};
-    p.direct = tokens <= FEW_TOKENS_MOST;
+    p.direct = tokens == 0 || is_direct(tokens, n_rows, dim);
     p.few = !p.direct && n_rows <= FEW_ROWS;
     p.ranked = tokens <= RANKED_TOKENS;
     if (p.direct) return p;                                  // no workspace

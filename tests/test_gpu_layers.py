@@ -601,7 +601,7 @@ def test_act_store_gives_codes_of_zero_for_every_nan():
 
 @pytest.mark.parametrize("spread", ["words", "one", "holes"])
 @pytest.mark.parametrize("tokens,rows,dim", [(131, 3, 200), (300, 4, 1025), (129, 4, 7), (40000, 4, 24), (5000, 1, 2056), (9001, 100, 17),
-                                            (256, 9, 1100), (257, 9, 1100), (64, 5, 3000), (3, 70000, 24), (200, 100, 1),
+                                            (256, 9, 1100), (257, 9, 1100), (64, 5, 3000), (3, 70000, 24), (200, 100, 1), (250, 140000, 24), (140, 140000, 260),
                                             (8200, 6, 520), (12000, 200000, 16), (6000, 300000, 8), (257, 30000, 48)])
 def test_embed_grad_in_every_form(tokens, rows, dim, spread):
     """Few rows in one and in several chunks of tokens; one, two and three passes of the sort; ranking with narrow and wide keys."""
