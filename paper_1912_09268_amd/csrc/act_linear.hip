@@ -207,6 +207,13 @@ __device__ __forceinline__ void write_tile(float* tile, const f32x16 (&value)[S:
 // the matrix cores go on right behind it.  RAGGED: the outputs are no multiple of eight, and the vector that holds the last ones is read element
 // by element (or there are no channels).  Other vectors behind the last output or channel are read from the last ones that exist: what they make
 // belongs to no element of dw.
+//
+// 1024 channels, 4096 outputs, 32775 binary16 tokens: 334 us with the join, 820 TFLOP/s; 4096 bfloat16 tokens 51 us, 43 of them
+// here and 7 for the join.  What bounds it is the matrix cores, and the power they draw: alone, without loads, LDS and scales, they
+// take 190 us at the 1.9 to 2.0 GHz they hold (273 us in all where every element is zero).  The rest is what does not fit behind
+// them: loads about 100 us, LDS reads 28 and writes 16, the scales 26.  Three buffers of 64 tokens, and writes between the products, come from
+// there; a higher priority of some wavefronts, loads between the products, and tiles in panels for each die are level or worse, and the
+// scales moved between the next group's products do not fit into the registers.
 template <typename DyT, typename GradT, typename S, bool RAGGED>
 __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     typedef typename Mma<DyT>::frag Frag;
@@ -389,7 +396,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
 
 // Few tokens, one group of them: what counts is dw, which is written once, so the tiles are small and many workgroups share a
 // compute unit: while some write their tiles, others read and multiply theirs.  A scale belongs to one sum; there is nothing to
-// join.
+// join.  32 tokens, 25088 channels, 4096 outputs, binary32: 71 us, 412 MB at 5.8 TB/s, nearly all of it the write of dw (a bare fill
+// writes 6.8).
 template <typename DyT> using Short = Shape<DyT, 1, 2, 2, 32, 1>;
 // A dw larger than the 256 MB memory-side cache is written past it.  32 tokens, 25088 channels, binary32, with a reader behind (a
 // maximum over dw): 392 MB 183 us streamed and 209 kept, 196 MB 99 and 91, 98 MB 57 and 47; the kernel alone is 1 to 7 %
@@ -473,7 +481,8 @@ __global__ __launch_bounds__(Short<DyT>::THREADS, SHORT_PER_CU) void linear_shor
 
 constexpr int JOIN_THREADS = 256;
 
-// The splits' sums, in order: a thread takes four channels of an output.  The first bias_blocks workgroups join the bias.
+// The splits' sums, in order: a thread takes four channels of an output.  The first bias_blocks workgroups join the bias.  Two splits of
+// 4096 outputs and 1024 channels, 42 MB: 7 us, half of it the launch and the first wait for memory.
 template <typename GradT> __global__ __launch_bounds__(JOIN_THREADS) void linear_join_kernel(LinearArgs A) {
     if (blockIdx.x < A.bias_blocks) {
         const int32_t o = blockIdx.x * JOIN_THREADS + threadIdx.x;
