@@ -340,9 +340,9 @@ __device__ __forceinline__ void write_partial(const GradArgs& A, uint32_t which,
 }
 
 // One lane for eight columns of a chunk.  A row that begins in a chunk and ends in the next one is summed by the lanes of the
-// first alone; only rows that reach further are joined.  65543 tokens of 1024 binary32 columns into 30522 rows, 0.4 GB: 88 us, 4.5 TB/s,
-// the rate of a copy.  4096 bfloat16 tokens into as many rows: 13 us, of which writing 62 MB takes 9.  What stands once for every token in the code is kept small (the
-// stretch from before the chunk and the one that goes on behind it are written at the end): with everything in place, the
+// first alone; only rows that reach further are joined.  65543 tokens of 1024 binary32 columns into 30522 rows, 0.4 GB: 88 us, 4.5
+// TB/s, the rate of a copy.  4096 bfloat16 tokens into as many rows: 13 us, of which writing 62 MB takes 9.  What stands once for every
+// token in the code is kept small (the stretch from before the chunk and the one that goes on behind it are written at the end): with everything in place, the
 // instructions of a short launch came from memory for longer than its data.
 template <typename DyT, typename GradT, bool ACCUMULATE> __global__ __launch_bounds__(THREADS) void sum_kernel(GradArgs A) {
     if (blockIdx.x >= A.sum_blocks) {
@@ -488,21 +488,31 @@ template <typename GradT> __global__ __launch_bounds__(THREADS) void join_kernel
 // ---- few tokens: no order, every row looks for its own ----
 
 constexpr int64_t FEW_TOKENS_MOST = 256;
+constexpr int FEW_ROWS = 4;              // for which there is a form of their own, below
 constexpr int DIRECT_WAVES = THREADS / 64;
 
 // Lanes hold the ids, LANE_IDS each; a row's tokens are the bits of as many comparisons.  A wavefront takes one row after the other,
-// and 512 columns: zeros where there are no tokens, else their sum in order, AHEAD of them on their way at a time.  Bound by
-// writing the table (30522 rows of 1024 bfloat16: 11 us, 5.5 TB/s), or by a launch (512 rows: 3 us).
+// and 512 columns: zeros where there are no tokens, else their sum in order, AHEAD of them on their way at a time.  Rows of more than LONG_ROW
+// tokens are left for the end, where all wavefronts take a part of each.  Bound by writing the table (30522 rows of 1024
+// bfloat16: 12 us, 5.2 TB/s), or by a launch (512 rows: 3 us).
 //
-// The rule.  256 tokens spread over 100 rows of 64 columns 3 us, over 30522 of 1024 columns 11, and 16 and 18 with an order; all in
-// one row, which one wavefront then adds alone, 21 and 12 (128 tokens: 11 and 12).  A row costs a wavefront its four comparisons however
-// short it is: 65536 rows of 64 columns 7 and 15 us, 200 thousand 15 and 16, of 512 columns 27 and 36.
+// The rule.  256 tokens spread over 100 rows of 64 columns 4 us, of frequencies like words' 7, all in one row 8, and 15, 17 and 12 with an
+// order; 30522 rows of 1024 columns 12, 18, 15 and 19, 19, 20.  With 512 tokens (and sixteen comparisons) 30522 rows take 17, 26,
+// 21 and 20, 20, 21.  A row costs a wavefront its comparisons however short it is: 65536 rows of 64 columns 7 and 14 us, 200
+// thousand 16 and 16, of 512 columns 28 and 36.  Up to FEW_ROWS rows a sum for each is better: 2 rows of 1024 columns 6, here 9.
 constexpr int64_t DIRECT_ROWS = 131072, DIRECT_DIM = 256;
-bool is_direct(int64_t tokens, int64_t n_rows, int64_t dim) { return tokens <= FEW_TOKENS_MOST && (n_rows <= DIRECT_ROWS || dim >= DIRECT_DIM); }
+bool is_direct(int64_t tokens, int64_t n_rows, int64_t dim) {
+    return tokens <= FEW_TOKENS_MOST && n_rows > FEW_ROWS && (n_rows <= DIRECT_ROWS || dim >= DIRECT_DIM);
+}
 
 template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) void direct_kernel(GradArgs A) {
     constexpr int LANE_IDS = FEW_TOKENS_MOST / 64;
     constexpr int AHEAD = sizeof(DyT) == 4 ? 8 : 16;
+    constexpr int LONG_ROW = 32, LONG_ROWS = LANE_IDS * 64 / LONG_ROW;
+    __shared__ int32_t long_row[DIRECT_WAVES][LONG_ROWS];
+    __shared__ uint32_t long_rows[DIRECT_WAVES];
+    __shared__ f32x4 part[DIRECT_WAVES][2][64];
+    static_assert(LANE_IDS == DIRECT_WAVES, "of a long row, a wavefront takes the mask of its number");
     const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t n = static_cast<uint32_t>(A.tokens);
     int32_t row[LANE_IDS];
@@ -518,50 +528,94 @@ template <typename DyT, typename GradT> __global__ __launch_bounds__(THREADS) vo
     const int64_t in_col = width > 0 ? col : static_cast<int64_t>(blockIdx.y) * 64 * VEC;
     const int in_width = static_cast<int>(min(A.dim - in_col, static_cast<int64_t>(VEC)));
     const DyT* const dy = static_cast<const DyT*>(A.dy) + in_col;
+    // Adds the tokens of the k-th 64 that are set in `rest`.
+    auto add = [&](float (&sum)[VEC], uint32_t k, uint64_t rest) {
+        auto take = [&](auto many) {                             // the next ones: the lowest bits that are left
+            constexpr int N = decltype(many)::value;
+            Raw8<DyT> x[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                x[j] = load8(dy + static_cast<int64_t>(k * 64 + __builtin_ctzll(rest)) * A.dy_stride, in_width);
+                rest &= rest - 1;
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum[i] += get(x[j], i);
+        };
+        uint32_t left = __popcll(rest);
+        for (; left >= AHEAD; left -= AHEAD) take(std::integral_constant<int, AHEAD>());
+        for (; left >= 4; left -= 4) take(std::integral_constant<int, 4>());
+        for (; left > 0; --left) take(std::integral_constant<int, 1>());
+    };
+    // Adds the tokens of those masks that are set in `which`.  (Lane k holds the k-th mask: in a loop there is one copy of
+    // the code above.)
+    auto add_all = [&](float (&sum)[VEC], const uint64_t (&mine)[LANE_IDS], uint64_t which) {
+        uint32_t low = 0, high = 0;
+#pragma unroll
+        for (int k = 0; k < LANE_IDS; ++k) {
+            low = lane == k ? static_cast<uint32_t>(mine[k]) : low;
+            high = lane == k ? static_cast<uint32_t>(mine[k] >> 32) : high;
+        }
+        for (uint64_t words = __ballot((low | high) != 0) & which; words != 0; words &= words - 1) {
+            const uint32_t k = __builtin_ctzll(words);
+            add(sum, k, static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(high, k))) << 32 |
+                            static_cast<uint32_t>(__builtin_amdgcn_readlane(low, k)));
+        }
+    };
+    auto write = [&](int64_t r, const float (&sum)[VEC]) {
+        if (width <= 0) return;
+        if (A.accumulate) write_row<GradT, true>(A, static_cast<int32_t>(r), col, width, sum);
+        else write_row<GradT, false>(A, static_cast<int32_t>(r), col, width, sum);
+    };
     const int64_t first = static_cast<int64_t>(blockIdx.x) * A.clear_rows, end = min(first + A.clear_rows, A.n_rows);
+    uint32_t found = 0;                                          // long rows
     for (int64_t r = first + wave; r < end; r += DIRECT_WAVES) {
-        uint64_t mine[LANE_IDS];
+        uint64_t mine[LANE_IDS], any = 0;
 #pragma unroll
-        for (int k = 0; k < LANE_IDS; ++k) mine[k] = __ballot(row[k] == static_cast<int32_t>(r));
-        uint32_t count = 0;
-#pragma unroll
-        for (int k = 0; k < LANE_IDS; ++k) count += __popcll(mine[k]);
+        for (int k = 0; k < LANE_IDS; ++k) any |= mine[k] = __ballot(row[k] == static_cast<int32_t>(r));
         float sum[VEC] = {};
-        if (count == 0) {
+        if (any == 0) {
             if (!A.accumulate && width > 0) store8(static_cast<GradT*>(A.grad) + r * A.grad_stride + col, sum, width);
             continue;
         }
+        uint32_t count = 0;
 #pragma unroll
-        for (int k = 0; k < LANE_IDS; ++k) {
-            uint64_t rest = mine[k];
-            auto take = [&](auto many) {                         // the next tokens: the lowest bits that are left
-                constexpr int N = decltype(many)::value;
-                Raw8<DyT> x[N];
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    x[j] = load8(dy + static_cast<int64_t>(k * 64 + __builtin_ctzll(rest)) * A.dy_stride, in_width);
-                    rest &= rest - 1;
-                }
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) sum[i] += get(x[j], i);
-            };
-            uint32_t left = __popcll(rest);
-            for (; left >= AHEAD; left -= AHEAD) take(std::integral_constant<int, AHEAD>());
-            for (; left >= 4; left -= 4) take(std::integral_constant<int, 4>());
-            for (; left > 0; --left) take(std::integral_constant<int, 1>());
+        for (int k = 0; k < LANE_IDS; ++k) count += __popcll(mine[k]);
+        if (count > LONG_ROW) {
+            if (lane == 0) long_row[wave][found] = static_cast<int32_t>(r);
+            ++found;
+            continue;
         }
-        if (width > 0) {
-            if (A.accumulate) write_row<GradT, true>(A, static_cast<int32_t>(r), col, width, sum);
-            else write_row<GradT, false>(A, static_cast<int32_t>(r), col, width, sum);
-        }
+        add_all(sum, mine, ~uint64_t(0));
+        write(r, sum);
     }
+    if (lane == 0) long_rows[wave] = found;
+    __syncthreads();
+    for (int w = 0; w < DIRECT_WAVES; ++w)
+        for (uint32_t i = 0; i < long_rows[w]; ++i) {            // by all wavefronts, 64 of the ids each
+            const int32_t r = long_row[w][i];
+            float sum[VEC] = {};
+            uint64_t mine[LANE_IDS];
+#pragma unroll
+            for (int k = 0; k < LANE_IDS; ++k) mine[k] = __ballot(row[k] == r);
+            add_all(sum, mine, uint64_t(1) << wave);
+            part[wave][0][lane] = f32x4{sum[0], sum[1], sum[2], sum[3]};
+            part[wave][1][lane] = f32x4{sum[4], sum[5], sum[6], sum[7]};
+            __syncthreads();
+            if (wave == 0) {
+#pragma unroll
+                for (int other = 1; other < DIRECT_WAVES; ++other)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[e] += part[other][e / 4][lane][e % 4];
+                write(r, sum);
+            }
+            __syncthreads();
+        }
 }
 
 // ---- few rows: no order, a sum for each row in every lane ----
 
-constexpr int FEW_ROWS = 4;
 constexpr int FEW_LANES = 16, FEW_TOKENS = THREADS / FEW_LANES, FEW_AHEAD = 8;       // 128 columns of 16 tokens at a time
 
 // 128 columns of a chunk of tokens by a workgroup.  A token's vector is added to its row's sum and nothing to the others (a
