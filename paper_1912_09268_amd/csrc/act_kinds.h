@@ -36,7 +36,8 @@ template <int KIND> __device__ __forceinline__ void activate(float x, float& val
         p = __builtin_fmaf(p, t, 0.09147620121370333f);
         p = __builtin_fmaf(p, t, 0.09317902474729383f);
         const float tail = p * t * e;
-        value = __builtin_fmaf(-__builtin_fabsf(x), tail, __builtin_fmaxf(x, 0.f));
+        // The tail is 0 far before 2^100, so the bound changes no finite x's product; +inf keeps its value, -inf is -inf * 0 = NaN.
+        value = __builtin_fmaf(-__builtin_fabsf(__builtin_fminf(x, 0x1p100f)), tail, __builtin_fmaxf(x, 0.f));
         const float below = x >= 0.f ? 1.f - tail : tail;      // Phi(x)
         slope = __builtin_fmaf(x * 0.3989422804014327f, e, below);
     } else if constexpr (KIND == MGWFBP_GELU_TANH) {
