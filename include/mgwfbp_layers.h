@@ -66,7 +66,8 @@ typedef enum mgwfbp_act_kind {  /* the function f between two layers            
     MGWFBP_GELU_TANH = 2,       /* x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2                    */
     MGWFBP_SILU = 3             /* x / (1 + exp(-x))                                                  */
 } mgwfbp_act_kind;
-/* Of an infinity they give what the formulas do: f(+inf) = +inf, f(-inf) = -inf * 0 = NaN (identity: -inf). */
+/* Of an infinity they give what the formulas do: f(+inf) = +inf, f(-inf) = -inf * 0 = NaN (identity: -inf);
+ * the slope is NaN there (identity: 1).  Of every finite number both are finite. */
 
 /* Activation checkpoints in 8 bits.  A checkpoint of x [n_tokens][n_channels] is
  *   q      int8 [n_tokens][ld]    whole numbers -127..127

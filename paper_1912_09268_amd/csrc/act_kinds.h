@@ -45,7 +45,9 @@ template <int KIND> __device__ __forceinline__ void activate(float x, float& val
         constexpr float A = 1.5957691216057308f, B = 0.044715f;            // 2 sqrt(2/pi)
         const float s = __builtin_amdgcn_rcpf(1.f + exp_of(-A * x * __builtin_fmaf(B * x, x, 1.f)));
         value = x * s;
-        slope = __builtin_fmaf(value * (1.f - s), A * __builtin_fmaf(3.f * B * x, x, 1.f), s);
+        // Beyond 64, s is 0 or 1 and the slope s to all digits; x^2 is bounded there, so that it is no infinity times 0.
+        const float near = __builtin_fminf(__builtin_fabsf(x), 64.f);
+        slope = __builtin_fmaf(value * (1.f - s), A * __builtin_fmaf(3.f * B * near, near, 1.f), s);
     } else {
         const float s = __builtin_amdgcn_rcpf(1.f + exp_of(-x));
         value = x * s;

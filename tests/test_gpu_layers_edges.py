@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_1912_09268_amd import layers
-from test_gpu_layers import DT, OWN, _close, _f64, _say
+from test_gpu_layers import DT, G, OWN, _close, _f64, _gen, _say
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,23 @@ def test_values_of_f_at_the_ends_of_the_range(kind, dtype):
     want = torch.where(finite, want, torch.where(x64 == math.inf, math.inf, torch.where(x64 == -math.inf, below, math.nan)))
     # beyond 64 the functions are x or 0 to all digits
     _close(y, want, OWN * x64.abs().nan_to_num(nan=0.0).clamp(max=64.0), "y")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind", KINDS)
+def test_slopes_of_enormous_activations(kind, dtype):
+    """The slope is 1 above and 0 below, however large a finite x^ is; y is x^ or 0."""
+    _say("slopes far out", kind, dtype)
+    size = torch.tensor([3e38, 1e30, 1e25, 5e19, 1e19, 1e13, 1e6, 1000.0, 100.0, 65.0, 64.0, 63.0, 20.0, 1.0, 0.0, 0.5], device="cuda")
+    act = layers.act_empty(130, 16)
+    act.q.copy_(torch.tensor([127, -127, 1, -1, 0, 63, -64], device="cuda").repeat(19)[:130, None].expand(130, 16))
+    act.scale.copy_((size / 127).expand(2, 16))
+    held = act.q.float() * act.scale.repeat_interleave(G, 0)[:130]
+    assert bool(held.isfinite().all())
+    dy = torch.randn(130, 16, generator=_gen(4), device="cuda").to(DT[dtype])
+    value, slope = _f64(kind, held.double())
+    y = torch.empty_like(dy) if dtype != "f16" else None                  # binary16 does not hold such a y
+    dx = layers.act_backward(act, dy, kind=kind, y=y)
+    _close(dx, dy.double() * slope, OWN * dy.double().abs(), "dx")
+    if y is not None:
+        _close(y, value, OWN * held.double().abs().clamp(max=64.0), "y")
