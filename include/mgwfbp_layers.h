@@ -81,7 +81,8 @@ int mgwfbp_act_dims(int64_t n_tokens, int64_t n_channels, int64_t* ld_out, int64
 /* Makes a checkpoint of x and, where d_y is not NULL, y = f(x) in the same pass (y of x's type; f sees x itself).
  *   scale = max(largest |x| of the group, 2^-100) * (1/127);  q = x * (1/scale), rounded to nearest even
  * A group with an infinity or NaN gets q = 0 and scale = NaN, so that what the backward pass makes of it is NaN and
- * the overflow is noticed.  Channels from n_channels to the next multiple of 16 become zeros. */
+ * the overflow is noticed.  Channels from n_channels to the next multiple of 16 become zeros; columns behind them, where ld
+ * is larger, are left as they are. */
 int mgwfbp_act_store(const void* d_x, int64_t x_stride, int32_t dtype, int64_t n_tokens, int64_t n_channels, int32_t kind,
                      int8_t* d_q, float* d_scale, int64_t ld, void* d_y, int64_t y_stride, void* hip_stream);
 

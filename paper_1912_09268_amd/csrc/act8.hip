@@ -13,6 +13,7 @@
 #include <cstdint>
 
 #include "act_kinds.h"
+#include "act_layout.h"
 #include "device_types.h"
 #include "mgwfbp_layers.h"
 
@@ -118,7 +119,7 @@ template <typename T, int KIND, bool Y> __global__ __launch_bounds__(THREADS) vo
     for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int w = 0; w < THREADS / 64; ++w) most.take(i, of_wave[w][lane * N + i]);
-    if (col >= A.ld) return;
+    if (col >= own_columns(A.channels)) return;
     float scale[VEC], inv[VEC];
     u32x2 keep = {0, 0};                                     // a group that is not finite has codes of 0
 #pragma unroll
@@ -218,7 +219,7 @@ extern "C" {
 
 int mgwfbp_act_dims(int64_t n_tokens, int64_t n_channels, int64_t* ld_out, int64_t* n_groups_out) {
     if (n_tokens < 0 || n_tokens > (int64_t(1) << 26) || n_channels < 0 || n_channels > (int64_t(1) << 23)) return MGWFBP_EINVAL;
-    if (ld_out != nullptr) *ld_out = ops::ceil_div(n_channels, 16) * 16;
+    if (ld_out != nullptr) *ld_out = own_columns(n_channels);
     if (n_groups_out != nullptr) *n_groups_out = ops::ceil_div(n_tokens, GROUP);
     return MGWFBP_OK;
 }

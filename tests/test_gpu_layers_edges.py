@@ -49,3 +49,18 @@ def test_slopes_of_enormous_activations(kind, dtype):
     _close(dx, dy.double() * slope, OWN * dy.double().abs(), "dx")
     if y is not None:
         _close(y, value, OWN * held.double().abs().clamp(max=64.0), "y")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,channels,ld", [(1, 1, 32), (130, 16, 64), (200, 17, 48), (129, 120, 256), (300, 130, 304), (5, 128, 1024)])
+def test_act_store_leaves_columns_behind_its_own(tokens, channels, ld, dtype):
+    """Zeros from the last channel to the next multiple of 16, nothing behind it."""
+    _say("act_store in a wider checkpoint", tokens, channels, ld, dtype)
+    x = torch.randn(tokens, channels, generator=_gen(tokens), device="cuda").to(DT[dtype])
+    own = -(-channels // 16) * 16
+    act = layers.Act8(torch.full((tokens, ld), 77, dtype=torch.int8, device="cuda"), torch.full((-(-tokens // G), ld), 5.0, device="cuda"), channels)
+    layers.act_store(x, act, kind="silu", y=torch.empty_like(x))
+    alone = layers.act_store(x)
+    assert torch.equal(act.q[:, :own], alone.q) and torch.equal(act.scale[:, :own], alone.scale)
+    assert not bool(act.q[:, channels:own].any()) and not bool(act.scale[:, channels:own].any())
+    assert bool((act.q[:, own:] == 77).all()) and bool((act.scale[:, own:] == 5.0).all())
