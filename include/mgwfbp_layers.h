@@ -73,7 +73,9 @@ typedef enum mgwfbp_act_kind {  /* the function f between two layers            
  *   q      int8 [n_tokens][ld]    whole numbers -127..127
  *   scale  float [n_groups][ld]   one for each channel and group of MGWFBP_ACT_GROUP consecutive tokens
  * and stands for x^[t,c] = q[t,c] * scale[t / MGWFBP_ACT_GROUP, c].  ld is a multiple of 16 and >= n_channels, q and
- * scale are aligned to 16 bytes.  mgwfbp_act_dims gives the smallest ld and the number of groups.
+ * scale are aligned to 16 bytes.  mgwfbp_act_dims gives the smallest ld and the number of groups.  A checkpoint's own columns are
+ * those up to the next multiple of 16 of n_channels; the ones behind them are neither read nor written, so that several checkpoints may lie
+ * side by side in one memory.
  *   n_tokens 0..2^26 (mgwfbp_act_linear_grad: 2^23), n_channels 0..2^23 */
 #define MGWFBP_ACT_GROUP 128
 int mgwfbp_act_dims(int64_t n_tokens, int64_t n_channels, int64_t* ld_out, int64_t* n_groups_out);

@@ -13,6 +13,7 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "act_layout.h"
 #include "device_types.h"
 #include "mgwfbp_layers.h"
 
@@ -36,6 +37,7 @@ struct LinearArgs {
     float* partial;                    // [splits][outputs][channels_padded], and the bias parts behind it
     float* bias_partial;               // [splits * bias_shares][outputs]
     int64_t dy_stride, ld, dw_stride, channels_padded;
+    int64_t q_columns;                 // of q: own_columns(channels)
     int32_t tokens, channels, outputs;
     uint32_t tiles_c, tiles, splits, groups, groups_per_split, bias_shares, bias_blocks;
     int32_t accumulate;
@@ -236,7 +238,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     const int32_t o_in = o0 + static_cast<int32_t>(dy_col);
     const int dy_n = RAGGED ? max(0, min(A.outputs - o_in, VEC)) : VEC;
     const DyT* const dy_at = static_cast<const DyT*>(A.dy) + (RAGGED ? o_in : min(o_in, A.outputs - VEC));
-    const int8_t* const q_at = A.q + min(static_cast<int64_t>(c0 + q_col), A.ld - S::XW);
+    const int8_t* const q_at = A.q + piece_at(c0 + q_col, A.q_columns, S::XW);
 
     const DyT* dy_next = dy_at + (t_first + static_cast<int64_t>(dy_row)) * A.dy_stride;      // the rows that are fetched next
     const int8_t* q_next = q_at + (t_first + static_cast<int64_t>(q_row)) * A.ld;
@@ -419,7 +421,7 @@ __global__ __launch_bounds__(Short<DyT>::THREADS, SHORT_PER_CU) void linear_shor
     const int32_t o_in = o0 + static_cast<int32_t>(dy_col);
     const int dy_n = RAGGED ? max(0, min(A.outputs - o_in, VEC)) : VEC;
     const DyT* const dy_at = static_cast<const DyT*>(A.dy) + (RAGGED ? o_in : min(o_in, A.outputs - VEC));
-    const int8_t* const q_at = A.q + min(static_cast<int64_t>(c0 + q_col), A.ld - S::XW);
+    const int8_t* const q_at = A.q + piece_at(c0 + q_col, A.q_columns, S::XW);
     const uint32_t r = lane / 32 * 8 + lane % 16 / 4, cc = lane / 16 % 2 * 16 + lane % 4 * 4;
     float scale[2];
 #pragma unroll
@@ -600,6 +602,7 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
     a.bias_partial = reinterpret_cast<float*>(static_cast<unsigned char*>(d_workspace) + p.bias_at);
     a.dy_stride = dy_stride;
     a.ld = ld;
+    a.q_columns = own_columns(n_channels);
     a.dw_stride = dw_stride;
     a.tokens = static_cast<int32_t>(n_tokens);
     a.channels = static_cast<int32_t>(n_channels);

@@ -5,6 +5,7 @@ import math
 import pytest
 import torch
 
+from paper_1912_09268_amd import layers_binding as M
 from paper_1912_09268_amd import layers
 from test_gpu_layers import DT, G, OWN, _close, _f64, _gen, _say
 
@@ -64,3 +65,35 @@ def test_act_store_leaves_columns_behind_its_own(tokens, channels, ld, dtype):
     assert torch.equal(act.q[:, :own], alone.q) and torch.equal(act.scale[:, :own], alone.scale)
     assert not bool(act.q[:, channels:own].any()) and not bool(act.scale[:, channels:own].any())
     assert bool((act.q[:, own:] == 77).all()) and bool((act.scale[:, own:] == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("tokens,outputs", [(1, 8), (100, 40), (129, 33), (2000, 64), (5000, 24)])
+def test_checkpoints_side_by_side(tokens, outputs, dtype):
+    """Several checkpoints in the columns of one memory, each made, gone back through and summed by itself: as those alone."""
+    _say("checkpoints side by side", tokens, outputs, dtype)
+    widths = [20, 16, 100, 1, 48]
+    ld = sum(-(-w // 16) * 16 for w in widths)
+    groups, g, code = -(-tokens // G), _gen(tokens), {"f32": M.F32, "bf16": M.BF16, "f16": M.F16}[dtype]
+    q, scale = torch.full((tokens, ld), 77, dtype=torch.int8, device="cuda"), torch.full((groups, ld), math.nan, device="cuda")
+    parts, at = [], 0
+    for w in widths:
+        x = torch.randn(tokens, w, generator=g, device="cuda").to(DT[dtype])
+        M.act_store(x.data_ptr(), w, code, tokens, w, M.GELU, q.data_ptr() + at, scale.data_ptr() + 4 * at, ld, 0, 0)
+        parts.append((at, w, x))
+        at += -(-w // 16) * 16
+    dy = torch.randn(tokens, outputs, generator=g, device="cuda").to(DT[dtype])
+    space = torch.empty(max(M.act_linear_grad_workspace(tokens, max(widths), outputs), M.act_linear_grad_workspace(tokens, 1, outputs)) + 256, dtype=torch.uint8, device="cuda")
+    for at, w, x in parts:
+        alone, own = layers.act_store(x), -(-w // 16) * 16
+        assert torch.equal(q[:, at:at + own], alone.q) and torch.equal(scale[:, at:at + own], alone.scale)
+        up, dx, y = torch.randn(tokens, w, generator=g, device="cuda").to(DT[dtype]), torch.empty_like(x), torch.empty_like(x)
+        M.act_backward(q.data_ptr() + at, scale.data_ptr() + 4 * at, ld, tokens, w, M.GELU, up.data_ptr(), w, dx.data_ptr(), w, y.data_ptr(), w, code)
+        y_alone = torch.empty_like(x)
+        assert torch.equal(dx, layers.act_backward(alone, up, kind="gelu", y=y_alone)) and torch.equal(y, y_alone)
+        dw, db = torch.empty(outputs, w, device="cuda"), torch.empty(outputs, device="cuda")
+        M.act_linear_grad(q.data_ptr() + at, scale.data_ptr() + 4 * at, ld, tokens, w, dy.data_ptr(), outputs, code, outputs, False, dw.data_ptr(), w, db.data_ptr(), M.F32,
+                          space.data_ptr(), space.numel())
+        dw_alone, db_alone = torch.empty_like(dw), torch.empty_like(db)
+        layers.act_linear_grad(dy, alone, dw_alone, db=db_alone)
+        assert torch.equal(dw, dw_alone) and torch.equal(db, db_alone)
