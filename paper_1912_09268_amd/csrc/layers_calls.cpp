@@ -2,9 +2,8 @@
 //
 // A call of an operator is a check of a handful of tensors and a launch or two.  In Python the checks and the marshalling take
 // 12 to 18 us, more than the kernels of small calls; here about 1.  A function returns NotImplemented for whatever it does
-// not take as it stands -- tensors that are to be refused, on another device than the current one, subclasses of tensors,
-// the library not loaded yet -- and layers.py goes the plain way, which refuses with the reason.  The module has no link to
-// the library: layers_binding.py loads that through ctypes and hands over the addresses of its entry points.
+// not take as it stands -- tensors that are to be refused, on another device than the current one, subclasses of tensors, the library not loaded yet -- and layers.py goes the plain way, which refuses with the reason.
+// The module has no link to the library: layers_binding.py loads that through ctypes and hands over the addresses of its entry points.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -16,6 +15,7 @@
 
 #include <cstdint>
 #include <cstring>
+#include <initializer_list>
 
 #include "mgwfbp_layers.h"
 
@@ -120,8 +120,13 @@ bool truth(PyObject* o, int32_t& v) {
 }
 
 PyObject* not_this_way() { Py_RETURN_NOTIMPLEMENTED; }
-PyObject* done(int which, int status) {
-    if (status == 0) Py_RETURN_NONE;
+// The end of a call: the tensors that it has written count as changed (those made in inference mode have no version).
+PyObject* done(int which, int status, std::initializer_list<const at::Tensor*> written) {
+    if (status == 0) {
+        for (const at::Tensor* t : written)
+            if (t != nullptr && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+        Py_RETURN_NONE;
+    }
     return PyObject_CallFunction(g_raise, "si", NAMES[which], status);     // raises
 }
 
@@ -183,7 +188,7 @@ PyObject* embed(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         Py_BEGIN_ALLOW_THREADS
         status = ENTRY(EMBED, mgwfbp_embed)(table, static_cast<int32_t>(n), table_type, tokens, dim, to, stride, out_type, stream);
         Py_END_ALLOW_THREADS
-        return done(EMBED, status);
+        return done(EMBED, status, {out});
     });
 }
 
@@ -212,7 +217,7 @@ PyObject* embed_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         status = ENTRY(EMBED_GRAD, mgwfbp_embed_grad)(i, id_type, tokens, d, dy_stride, dy_type, scale, padding, accumulate, g, rows, dim, grad_stride, grad_type,
                                                       space, size, stream);
         Py_END_ALLOW_THREADS
-        return done(EMBED_GRAD, status);
+        return done(EMBED_GRAD, status, {grad});
     });
 }
 
@@ -236,7 +241,7 @@ PyObject* act_store(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         Py_BEGIN_ALLOW_THREADS
         status = ENTRY(ACT_STORE, mgwfbp_act_store)(xp, x_stride, type, tokens, channels, static_cast<int32_t>(kind), qp, sp, ld, yp, y_stride, stream);
         Py_END_ALLOW_THREADS
-        return done(ACT_STORE, status);
+        return done(ACT_STORE, status, {q, scale, y});
     });
 }
 
@@ -265,7 +270,7 @@ PyObject* act_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         status = ENTRY(ACT_BACKWARD, mgwfbp_act_backward)(qp, sp, ld, tokens, channels, static_cast<int32_t>(kind), dyp, dy_stride, dxp, dx_stride, yp, y_stride, type,
                                                           stream);
         Py_END_ALLOW_THREADS
-        return done(ACT_BACKWARD, status);
+        return done(ACT_BACKWARD, status, {dx, y});
     });
 }
 
@@ -298,7 +303,7 @@ PyObject* act_linear_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         status = ENTRY(ACT_LINEAR_GRAD, mgwfbp_act_linear_grad)(qp, sp, ld, tokens, channels, d, dy_stride, dy_type, outputs, accumulate, w, dw_stride, b, grad_type,
                                                                 space, size, stream);
         Py_END_ALLOW_THREADS
-        return done(ACT_LINEAR_GRAD, status);
+        return done(ACT_LINEAR_GRAD, status, {dw, db});
     });
 }
 

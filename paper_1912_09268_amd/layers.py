@@ -5,6 +5,9 @@ Arguments are checked (ValueError) and handed to the library, in native code whe
 the tensors' device and on torch's current stream there, and does not wait for it.  A tensor made on another stream
 needs that stream's work to be waited for, and Tensor.record_stream where it is freed early, as with any other call.
 
+The operators are the backward pass, and autograd knows nothing of them: results have no graph.  Tensors that a call has written count as
+changed: autograd refuses to go on with one that it has saved before.
+
     h = layers.embed([word, position, token_type], [ids, places, types])          # bf16, from binary32 weights
     u = torch.empty_like(z)
     kept = layers.act_store(z, kind="gelu", y=u)                                  # z in 8 bits, u = gelu(z)
@@ -68,6 +71,13 @@ def _device(*tensors) -> torch.device:
         if t is not None and t.device != device:
             _fail(f"tensors are on {device} and on {t.device}")
     return device
+
+
+def _written(*tensors) -> None:
+    """Raises the versions of tensors that a call has written, so that autograd notices where it has saved one of them."""
+    for t in tensors:
+        if t is not None and not t.is_inference():
+            torch.autograd.graph.increment_version(t)
 
 
 class _on:
@@ -137,6 +147,7 @@ def embed(tables: Tensors, ids: Tensors, scales: Optional[Sequence[float]] = Non
     out_stride = _matrix(flat, "out", tokens, dim)
     with _on(device) as stream:
         B.embed(rows, _DTYPES[first.dtype], tokens, dim, flat.data_ptr(), out_stride, _DTYPES[out.dtype], stream)
+    _written(out)
     return out
 
 
@@ -159,6 +170,7 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, scale: f
         space = _workspace(workspace, B.embed_grad_workspace(tokens, rows, dim), device)
         B.embed_grad(ids.data_ptr(), _ID_TYPES[ids.dtype], tokens, dy.data_ptr(), dy_stride, _DTYPES[dy.dtype], scale, padding_row, accumulate,
                      grad.data_ptr(), rows, dim, grad_stride, _DTYPES[grad.dtype], space.data_ptr(), space.numel() * space.element_size(), stream)
+    _written(grad)
     return grad
 
 
@@ -202,6 +214,7 @@ def act_store(x: torch.Tensor, act: Optional[Act8] = None, kind: str = "identity
     with _on(device) as stream:
         B.act_store(x.data_ptr(), x_stride, _DTYPES[x.dtype], tokens, channels, _kind(kind), act.q.data_ptr(), act.scale.data_ptr(), ld,
                     _address(y), y_stride, stream)
+    _written(act.q, act.scale, y)
     return act
 
 
@@ -224,6 +237,7 @@ def act_backward(act: Act8, dy: Optional[torch.Tensor] = None, kind: str = "iden
     with _on(device) as stream:
         B.act_backward(act.q.data_ptr(), act.scale.data_ptr(), ld, tokens, act.channels, _kind(kind), _address(dy), strides[0],
                        _address(dx), strides[1], _address(y), strides[2], _DTYPES[one.dtype], stream)
+    _written(dx, y)
     return y if dy is None else dx
 
 
@@ -246,4 +260,5 @@ def act_linear_grad(dy: torch.Tensor, act: Act8, dw: torch.Tensor, db: Optional[
         B.act_linear_grad(act.q.data_ptr(), act.scale.data_ptr(), ld, tokens, act.channels, dy.data_ptr(), dy_stride, _DTYPES[dy.dtype], outputs,
                           accumulate, dw.data_ptr(), dw_stride, _address(db), _DTYPES[dw.dtype], space.data_ptr(),
                           space.numel() * space.element_size(), stream)
+    _written(dw, db)
     return dw

@@ -97,3 +97,44 @@ def test_checkpoints_side_by_side(tokens, outputs, dtype):
         dw_alone, db_alone = torch.empty_like(dw), torch.empty_like(db)
         layers.act_linear_grad(dy, alone, dw_alone, db=db_alone)
         assert torch.equal(dw, dw_alone) and torch.equal(db, db_alone)
+
+
+def _calls():
+    """Each operator on plain tensors: (name, tensors read, tensors written, call of all of them)."""
+    table, ids, x = torch.randn(30, 48, device="cuda"), torch.arange(64, device="cuda") % 30, torch.randn(64, 48, device="cuda")
+    act = layers.act_store(x)
+
+    def memory(*shape):
+        return torch.zeros(*shape, device="cuda")
+
+    return [("embed", [table], [memory(64, 48)], lambda r, w: layers.embed(r[0], ids, out=w[0])),
+            ("embed_grad", [x], [memory(30, 48)], lambda r, w: layers.embed_grad(r[0], ids, w[0])),
+            ("act_store", [x], [torch.empty_like(act.q), torch.empty_like(act.scale), memory(64, 48)],
+             lambda r, w: layers.act_store(r[0], layers.Act8(w[0], w[1], 48), kind="gelu", y=w[2])),
+            ("act_backward", [x], [memory(64, 48), memory(64, 48)], lambda r, w: layers.act_backward(act, r[0], kind="gelu", dx=w[0], y=w[1])),
+            ("act_linear_grad", [x], [memory(48, 48), memory(48)], lambda r, w: layers.act_linear_grad(r[0], act, w[0], db=w[1]))]
+
+
+@pytest.mark.parametrize("way", ["native", "plain"])
+def test_written_tensors_are_marked_as_changed(way, monkeypatch):
+    """A tensor that autograd has saved and a call has written since is noticed, as after any other change in place."""
+    if way == "plain":
+        for name in ("embed", "embed_grad", "act_store", "act_backward", "act_linear_grad"):
+            monkeypatch.setattr(layers._native, name, lambda *a: NotImplemented)
+    for name, read, written, call in _calls():
+        _say("versions", way, name)
+        before = [t._version for t in written]
+        call(read, written)
+        assert all(t._version > b for t, b in zip(written, before)), name
+        assert all(t._version == 0 for t in read), name
+        a = torch.ones_like(written[-1], requires_grad=True)
+        loss = (a * written[-1]).sum()                                    # saves what was written
+        call(read, written)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    with torch.inference_mode():
+        kept = [([t.clone() for t in read], [t.clone() for t in written], call) for _, read, written, call in _calls()]
+        for read, written, call in kept:
+            call(read, written)
+    for read, written, call in kept:                                      # tensors that have no version
+        call(read, written)
