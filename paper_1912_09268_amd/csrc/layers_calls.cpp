@@ -2,12 +2,14 @@
 //
 // A call of an operator is a check of a handful of tensors and a launch or two.  In Python the checks and the marshalling take
 // 12 to 18 us, more than the kernels of small calls; here about 1.  A function returns NotImplemented for whatever it does
-// not take as it stands -- tensors that are to be refused, on another device than the current one, subclasses of tensors, the library not loaded yet -- and layers.py goes the plain way, which refuses with the reason.
+// not take as it stands -- tensors that are to be refused (those that autograd follows among them), on another device than the
+// current one, subclasses of tensors, the library not loaded yet -- and layers.py goes the plain way, which refuses with the reason.
 // The module has no link to the library: layers_binding.py loads that through ctypes and hands over the addresses of its entry points.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -52,6 +54,7 @@ struct Call {
         if (!THPVariable_CheckExact(o)) return fail();
         const at::Tensor& t = THPVariable_Unpack(o);
         if (t.layout() != at::kStrided || !t.is_cuda()) return fail();
+        if (t.requires_grad() && c10::GradMode::is_enabled()) return fail();
         if (device < 0) {
             device = t.get_device();
             if (device != c10::hip::current_device()) return fail();

@@ -5,8 +5,9 @@ Arguments are checked (ValueError) and handed to the library, in native code whe
 the tensors' device and on torch's current stream there, and does not wait for it.  A tensor made on another stream
 needs that stream's work to be waited for, and Tensor.record_stream where it is freed early, as with any other call.
 
-The operators are the backward pass, and autograd knows nothing of them: results have no graph.  Tensors that a call has written count as
-changed: autograd refuses to go on with one that it has saved before.
+The operators are the backward pass, and autograd knows nothing of them: results have no graph.  So that no gradient is lost without
+a word, tensors that require grad are refused in grad mode; under torch.no_grad(), in an autograd.Function and detached they are
+taken.  Tensors that a call has written count as changed: autograd refuses to go on with one that it has saved before.
 
     h = layers.embed([word, position, token_type], [ids, places, types])          # bf16, from binary32 weights
     u = torch.empty_like(z)
@@ -64,6 +65,8 @@ def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: Optional[int]
 
 
 def _device(*tensors) -> torch.device:
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        _fail("autograd follows a tensor, and the operators have no graph: call them without grad mode, or detach it")
     device = tensors[0].device
     if device.type != "cuda":
         _fail(f"tensors must be on the GPU, not on {device}")

@@ -138,3 +138,31 @@ def test_written_tensors_are_marked_as_changed(way, monkeypatch):
             call(read, written)
     for read, written, call in kept:                                      # tensors that have no version
         call(read, written)
+
+
+@pytest.mark.parametrize("way", ["native", "plain"])
+def test_tensors_that_autograd_follows_are_refused(way, monkeypatch):
+    """The operators have no graph: a gradient would be lost without a word.  Without grad mode, and detached, they are taken."""
+    if way == "plain":
+        for name in ("embed", "embed_grad", "act_store", "act_backward", "act_linear_grad"):
+            monkeypatch.setattr(layers._native, name, lambda *a: NotImplemented)
+    for name, read, written, call in _calls():
+        _say("autograd", way, name)
+        call(read, written)
+        want = [t.clone() for t in written]
+        followed = [t.clone().requires_grad_(True) for t in read]
+        with pytest.raises(ValueError, match="autograd"):
+            call(followed, written)
+        if written[-1].is_floating_point():
+            with pytest.raises(ValueError, match="autograd"):
+                call(read, written[:-1] + [written[-1].clone().requires_grad_(True)])
+        for t in written:
+            t.zero_()
+        with torch.no_grad():
+            call(followed, written)
+        assert all(torch.equal(a, b) for a, b in zip(want, written)), name
+        call([t.detach() for t in followed], written)
+        with pytest.raises(ValueError, match="autograd"):
+            call([t * 1.0 for t in followed], written)
+    with pytest.raises(ValueError, match="autograd"):
+        layers.embed(torch.zeros(3, 4, device="cuda", requires_grad=True), torch.zeros(2, dtype=torch.int64, device="cuda"))
