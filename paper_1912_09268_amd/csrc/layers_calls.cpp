@@ -53,7 +53,7 @@ struct Call {
         if (optional && o == Py_None) return nullptr;
         if (!THPVariable_CheckExact(o)) return fail();
         const at::Tensor& t = THPVariable_Unpack(o);
-        if (t.layout() != at::kStrided || !t.is_cuda()) return fail();
+        if (t.layout() != at::kStrided || !t.is_cuda() || t.is_neg()) return fail();      // a negated view's memory is not its values
         if (t.requires_grad() && c10::GradMode::is_enabled()) return fail();
         if (device < 0) {
             device = t.get_device();

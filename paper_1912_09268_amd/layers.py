@@ -67,6 +67,8 @@ def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: Optional[int]
 def _device(*tensors) -> torch.device:
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         _fail("autograd follows a tensor, and the operators have no graph: call them without grad mode, or detach it")
+    if any(t is not None and t.is_neg() for t in tensors):
+        _fail("the memory of a tensor holds its values negated: take its resolve_neg()")
     device = tensors[0].device
     if device.type != "cuda":
         _fail(f"tensors must be on the GPU, not on {device}")

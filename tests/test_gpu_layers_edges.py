@@ -7,7 +7,7 @@ import torch
 
 from paper_1912_09268_amd import layers_binding as M
 from paper_1912_09268_amd import layers
-from test_gpu_layers import DT, G, OWN, _close, _f64, _gen, _say
+from test_gpu_layers import DT, F32, G, OWN, _close, _f64, _gen, _say
 
 pytestmark = pytest.mark.gpu
 
@@ -166,3 +166,21 @@ def test_tensors_that_autograd_follows_are_refused(way, monkeypatch):
             call([t * 1.0 for t in followed], written)
     with pytest.raises(ValueError, match="autograd"):
         layers.embed(torch.zeros(3, 4, device="cuda", requires_grad=True), torch.zeros(2, dtype=torch.int64, device="cuda"))
+
+
+def test_negated_views_are_refused():
+    """A tensor whose memory holds the negative of its values (the imaginary part of a conjugate)."""
+    x = torch.complex(torch.zeros(64, 1, device="cuda"), torch.ones(64, 1, device="cuda")).conj().imag
+    assert x.is_neg() and bool((x == -1.0).all())
+    with pytest.raises(ValueError, match="negat"):
+        layers.act_store(x)
+    with pytest.raises(ValueError, match="negat"):
+        layers.act_store(x, layers.act_empty(64, 1))
+    ids = torch.arange(64, device="cuda")
+    with pytest.raises(ValueError, match="negat"):
+        layers.embed(x, ids, out=torch.empty(64, 1, device="cuda"))
+    with pytest.raises(ValueError, match="negat"):
+        layers.embed(x.resolve_neg(), torch._neg_view(ids), out=torch.empty(64, 1, device="cuda"))
+    with pytest.raises(ValueError, match="negat"):
+        layers.embed_grad(torch.ones(64, 8, device="cuda"), ids, torch._neg_view(torch.empty(64, 8, device="cuda")))
+    assert bool((layers.embed(x.resolve_neg(), ids, dtype=F32) == -1.0).all())
