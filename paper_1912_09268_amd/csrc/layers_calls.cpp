@@ -13,6 +13,7 @@
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -133,14 +134,11 @@ PyObject* done(int which, int status, std::initializer_list<const at::Tensor*> w
     return PyObject_CallFunction(g_raise, "si", NAMES[which], status);     // raises
 }
 
-// Runs f, which throws nothing but what torch does (out of memory): that as a Python exception.
+// Runs f, which throws nothing but what torch does (out of memory): that as torch's own Python exception.
 template <typename F> PyObject* guarded(F&& f) {
-    try {
-        return f();
-    } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
-    }
+    HANDLE_TH_ERRORS
+    return f();
+    END_HANDLE_TH_ERRORS
 }
 
 // embed(tables, ids, scales, out): lists or tuples of one to four tensors, ids and numbers; out a tensor

@@ -184,3 +184,21 @@ def test_negated_views_are_refused():
     with pytest.raises(ValueError, match="negat"):
         layers.embed_grad(torch.ones(64, 8, device="cuda"), ids, torch._neg_view(torch.empty(64, 8, device="cuda")))
     assert bool((layers.embed(x.resolve_neg(), ids, dtype=F32) == -1.0).all())
+
+
+def test_memory_that_cannot_be_had_is_torchs_own_error():
+    """For a workspace, as for a tensor: callers that free and try again catch torch.OutOfMemoryError."""
+    tokens, rows, dim = 1 << 20, 5, 1                                     # a workspace of some 25 MB
+    dy, ids, grad = torch.ones(tokens, dim, device="cuda"), torch.zeros(tokens, dtype=torch.int64, device="cuda"), torch.empty(rows, dim, device="cuda")
+    layers.embed_grad(dy[:300], ids[:300], grad)                          # the library is loaded
+    assert M.embed_grad_workspace(tokens, rows, dim) > 4 << 20
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    torch.cuda.set_per_process_memory_fraction(1e-9)
+    try:
+        with pytest.raises(torch.OutOfMemoryError):
+            layers.embed_grad(dy, ids, grad)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    layers.embed_grad(dy, ids, grad)
+    assert float(grad[0, 0]) == tokens and not bool(grad[1:].any())
