@@ -64,6 +64,16 @@ def _matrix(t: torch.Tensor, name: str, rows: Optional[int], cols: Optional[int]
     return row if t.shape[0] > 1 else t.shape[1]
 
 
+def _flat(t: torch.Tensor, name: str, tokens: int, dim: int) -> torch.Tensor:
+    """A tensor of a row for each token, whatever its shape, as a matrix."""
+    if t.dim() == 2:
+        return t
+    try:
+        return t.view(tokens, dim)
+    except RuntimeError:
+        _fail(f"{name} has shape {tuple(t.shape)} and strides {t.stride()}: no {tokens} rows of {dim} at one distance")
+
+
 def _device(*tensors) -> torch.device:
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         _fail("autograd follows a tensor, and the operators have no graph: call them without grad mode, or detach it")
@@ -148,7 +158,7 @@ def embed(tables: Tensors, ids: Tensors, scales: Optional[Sequence[float]] = Non
         out = torch.empty(*shape, dim, dtype=dtype, device=device)
     if out.shape != (*shape, dim) and out.shape != (tokens, dim):
         _fail(f"out has shape {tuple(out.shape)}, wanted {(*shape, dim)}")
-    flat = out if out.dim() == 2 else out.view(tokens, dim)
+    flat = _flat(out, "out", tokens, dim)
     out_stride = _matrix(flat, "out", tokens, dim)
     with _on(device) as stream:
         B.embed(rows, _DTYPES[first.dtype], tokens, dim, flat.data_ptr(), out_stride, _DTYPES[out.dtype], stream)
@@ -169,7 +179,7 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, scale: f
     tokens = ids.numel()
     grad_stride = _matrix(grad, "grad", None, None)
     rows, dim = grad.shape
-    dy = dy if dy.dim() == 2 else dy.view(tokens, dim)
+    dy = _flat(dy, "dy", tokens, dim)
     dy_stride = _matrix(dy, "dy", tokens, dim)
     with _on(device) as stream:
         space = _workspace(workspace, B.embed_grad_workspace(tokens, rows, dim), device)

@@ -202,3 +202,20 @@ def test_memory_that_cannot_be_had_is_torchs_own_error():
         torch.cuda.set_per_process_memory_fraction(1.0)
     layers.embed_grad(dy, ids, grad)
     assert float(grad[0, 0]) == tokens and not bool(grad[1:].any())
+
+
+def test_tensors_that_are_no_matrix_are_refused_with_the_reason():
+    """What cannot be seen as [tokens, dim] without a copy, or has another number of elements: ValueError, as for any other shape."""
+    table, ids = torch.randn(10, 24, device="cuda"), torch.arange(12, device="cuda").view(3, 4) % 10
+    dy, grad = torch.ones(3, 5, 24, device="cuda"), torch.empty(10, 24, device="cuda")
+    with pytest.raises(ValueError, match="dy"):
+        layers.embed_grad(dy[:, :4], ids, grad)                           # rows of two strides
+    with pytest.raises(ValueError, match="dy"):
+        layers.embed_grad(dy, ids, grad)                                  # 15 tokens for 12 ids
+    with pytest.raises(ValueError, match="dy"):
+        layers.embed_grad(dy[0, 0], ids, grad)
+    with pytest.raises(ValueError, match="out"):
+        layers.embed(table, ids, out=torch.empty(3, 5, 24, device="cuda")[:, :4])
+    whole = torch.empty(3, 4, 30, device="cuda")                          # rows of one stride: taken
+    assert torch.equal(layers.embed(table, ids, out=whole[..., :24]), table[ids])
+    assert torch.equal(layers.embed_grad(torch.ones(3, 4, 30, device="cuda")[..., :24], ids, grad), torch.bincount(ids.view(-1), minlength=10).float()[:, None].expand(-1, 24))
