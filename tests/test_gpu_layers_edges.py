@@ -2,12 +2,13 @@
 that autograd follows, and the forms that only long calls take.  References and tolerances as in test_gpu_layers.py."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
 from paper_1912_09268_amd import layers_binding as M
 from paper_1912_09268_amd import layers
-from test_gpu_layers import DT, F32, G, OWN, _close, _f64, _gen, _say
+from test_gpu_layers import BF16, DT, F16, F32, G, OWN, _checkpoint, _close, _embed_grad_reference, _f64, _gen, _linear_slack, _say, _spread, _strided, _untouched
 
 pytestmark = pytest.mark.gpu
 
@@ -219,3 +220,64 @@ def test_tensors_that_are_no_matrix_are_refused_with_the_reason():
     whole = torch.empty(3, 4, 30, device="cuda")                          # rows of one stride: taken
     assert torch.equal(layers.embed(table, ids, out=whole[..., :24]), table[ids])
     assert torch.equal(layers.embed_grad(torch.ones(3, 4, 30, device="cuda")[..., :24], ids, grad), torch.bincount(ids.view(-1), minlength=10).float()[:, None].expand(-1, 24))
+
+
+@pytest.mark.parametrize("spread", ["words", "one", "holes"])
+@pytest.mark.parametrize("tokens,rows,dim,dy_t,grad_t,how", [(17003, 30522, 1024, F32, F32, "dense"), (33001, 700, 520, BF16, BF16, "strided"),
+                                                             (65543, 30522, 1024, F32, F32, "dense"), (70001, 40, 1021, F16, F32, "strided")])
+def test_embed_grad_of_long_chunks(tokens, rows, dim, dy_t, grad_t, how, spread):
+    """Chunks of 32 tokens (from 2.1 million vectors of eight on) and of 64 (from 8.4 million): several turns within a chunk, stretches that
+    go on behind it."""
+    _say("embed_grad, long chunks", tokens, rows, dim, dy_t, grad_t, how, spread)
+    vectors = tokens * -(-dim // 8)
+    assert vectors >= 64 * 131072 or vectors >= 32 * 65536
+    g = _gen(tokens)
+    ids = _spread(tokens, rows, spread, g).to(torch.int32 if tokens % 3 == 0 else torch.int64)
+    dy, _ = _strided((tokens, dim), dy_t, how)
+    dy.copy_(torch.randn(tokens, dim, generator=g, device="cuda"))
+    dy[(ids < 0) | (ids >= rows)] = float("nan")
+    grad, whole = _strided((rows, dim), grad_t, how)
+    scale = 0.37
+    layers.embed_grad(dy, ids, grad, scale=scale)
+    want, terms, count = _embed_grad_reference(dy, ids, rows, float(np.float32(scale)), -1)
+    _close(grad, want, (count + 2) * 2.0 ** -24 * terms, "embed_grad")
+    assert _untouched(grad, whole, float("nan"))
+    again = grad.clone()
+    layers.embed_grad(dy, ids, grad, scale=scale)
+    assert torch.equal(again, grad)
+    had = torch.randn(rows, dim, generator=g, device="cuda").to(grad_t)
+    grad.copy_(had)
+    pad = int(ids[0])
+    layers.embed_grad(dy, ids, grad, scale=scale, padding_row=pad, accumulate=True)
+    if 0 <= pad < rows:
+        want[pad], terms[pad], count[pad] = 0.0, 0.0, 0.0
+    _close(grad, want + had.double(), (count + 3) * 2.0 ** -24 * (terms + had.double().abs()), "accumulated")
+    rest = count.squeeze(1) == 0
+    assert torch.equal(grad[rest], had[rest])
+
+
+@pytest.mark.parametrize("dy_t,grad_t", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32")])
+@pytest.mark.parametrize("tokens,channels,outputs,how", [(32, 16392, 8200, "dense"), (77, 16385, 8203, "strided")])
+def test_act_linear_grad_of_gradients_past_the_caches(tokens, channels, outputs, how, dy_t, grad_t):
+    """dw of 256 MiB and more by few tokens: streamed tiles, whole and at the edges, and added to what is there."""
+    _say("act_linear_grad, streamed", tokens, channels, outputs, how, dy_t, grad_t)
+    assert outputs * channels * (4 if grad_t == "f32" else 2) >= 256 << 20
+    g = _gen(tokens)
+    act, x = _checkpoint(tokens, channels, g)
+    dy = torch.randn(tokens, outputs, generator=g, device="cuda").to(DT[dy_t])
+    dw, whole = _strided((outputs, channels), DT[grad_t], how)
+    db = torch.empty(outputs, dtype=DT[grad_t], device="cuda")
+    layers.act_linear_grad(dy, act, dw, db=db)
+    had = torch.randn(outputs, channels, generator=g, device="cuda").to(DT[grad_t])
+    first = dw.clone()
+    assert _untouched(dw, whole, float("nan"))
+    dw.copy_(had)
+    layers.act_linear_grad(dy, act, dw, accumulate=True)
+    d64 = dy.double().t().contiguous()
+    _close(db, d64.sum(1), (tokens + 8) * 2.0 ** -24 * d64.abs().sum(1), "db")
+    for o in range(0, outputs, 2048):                                     # in parts: the references are 64 bits
+        part = slice(o, min(o + 2048, outputs))
+        want, terms = d64[part] @ x, d64[part].abs() @ x.abs()
+        _close(first[part], want, _linear_slack(tokens, terms, 0.0), "dw")
+        h = had[part].double()
+        _close(dw[part], want + h, _linear_slack(tokens, terms, h.abs()), "accumulated dw")
