@@ -2,10 +2,15 @@
 //
 // The normal distribution's tail Q(z) = erfc(z / sqrt 2) / 2, z >= 0, is taken as exp(-z^2/2) times a polynomial in
 // t = 1 / (1 + p z) without constant term (the form of Hastings' approximations): erfc(u) exp(u^2) is smooth in t and tends
-// to 0 with it.  The coefficients are a least-maximum fit of the relative error over 0 <= u <= 10 (9.3e-8; 5.1e-7 with the
-// roundings of binary32), so that the tails keep their digits, too.  The exponential is the one that the slope needs anyway:
-// the function and its slope cost one v_exp_f32 and one v_rcp_f32 (1 ulp each).  The library's erff needs about three times
-// the instructions, with which these kernels would be bound by them and not by memory.
+// to 0 with it.  The coefficients are a least-maximum fit of the relative error over 0 <= u <= 10: 9.3e-8, and 5.1e-7 with the
+// roundings of the polynomial.  The exponential is the one that the slope needs anyway: the function and its slope cost one
+// v_exp_f32 and one v_rcp_f32 (1 ulp each).  The library's erff needs about three times the instructions, with which these
+// kernels would be bound by them and not by memory.
+//
+// Far below 0 the functions are as exact as their exponential.  Its argument is rounded to binary32, three times for GELU (x^2, the
+// constant, their product) and twice for SiLU, and an argument that is off by d moves the result by d of itself: up to
+// 5e-7 + 9e-8 x^2 of itself for GELU, 2e-7 + 1.2e-7 |x| for SiLU.  Carrying the remainders along would take four or five more
+// instructions for values that are all but 0 beside the others of their row.
 #ifndef MGWFBP_ACT_KINDS_H
 #define MGWFBP_ACT_KINDS_H
 

@@ -281,3 +281,20 @@ def test_act_linear_grad_of_gradients_past_the_caches(tokens, channels, outputs,
         _close(first[part], want, _linear_slack(tokens, terms, 0.0), "dw")
         h = had[part].double()
         _close(dw[part], want + h, _linear_slack(tokens, terms, h.abs()), "accumulated dw")
+
+
+@pytest.mark.parametrize("kind", KINDS[1:])
+def test_the_tails_keep_their_digits(kind):
+    """f(x) far below 0 relative to itself.  The exponential's argument has the roundings of binary32: three of 2^-24 of it each
+    for GELU (x^2, the constant, the product) and tanh GELU has the polynomial's two beside them, so f is off by that many parts of
+    |argument| beside the function's own error.  Where f is below 2^-100 nothing is asked."""
+    x = -torch.linspace(0.5, 14.0, 128 * 64, device="cuda").view(128, 64)
+    y = torch.empty_like(x)
+    layers.act_store(x, kind=kind, y=y)
+    x64 = x.double()
+    want, _ = _f64(kind, x64)
+    argument = {"gelu": x64 * x64 / 2, "silu": x64.abs(), "gelu_tanh": 2 * math.sqrt(2 / math.pi) * (x64.abs() + 0.044715 * x64.abs() ** 3)}[kind]
+    roundings = {"gelu": 3, "silu": 2, "gelu_tanh": 6}[kind]
+    slack = (OWN + roundings * 2.0 ** -24 * argument) * want.abs() + 2.0 ** -100
+    _close(y, want, slack, "y")
+    assert bool((want.abs() > 2.0 ** -90).sum() > 4000)
