@@ -78,8 +78,8 @@ __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float 
 
 // A workgroup takes 128 channels of a group: the whole of it stays in registers between the search for the largest magnitude
 // and the rounding, so x is read once.  y does not wait for that: it is made and written as rows arrive.  4096 tokens of 4096
-// bfloat16 channels with GELU: 20 us, 84 MB at 4.2 TB/s, and 15 without the function's arithmetic, which is what is left above the
-// rate of a copy.  (Fewer wavefronts side by side than the registers allow are level.)
+// bfloat16 channels with GELU: 21 us, 84 MB at 4.0 TB/s, and 15 without the function's arithmetic, which is what is left above the
+// rate of a copy (an instruction an element is 0.4 us).  (Fewer wavefronts side by side than the registers allow are level.)
 template <typename T, int KIND, bool Y> __global__ __launch_bounds__(THREADS) void store_kernel(StoreArgs A) {
     const uint32_t g = blockIdx.x / A.col_blocks, cb = blockIdx.x - g * A.col_blocks;
     const uint32_t lane = threadIdx.x % LANES, row = threadIdx.x / LANES;

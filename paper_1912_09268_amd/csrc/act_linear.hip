@@ -211,11 +211,12 @@ __device__ __forceinline__ void write_tile(float* tile, const f32x16 (&value)[S:
 // belongs to no element of dw.
 //
 // 1024 channels, 4096 outputs, 32775 binary16 tokens: 334 us with the join, 820 TFLOP/s; 4096 bfloat16 tokens 51 us, 43 of them
-// here and 7 for the join.  What bounds it is the matrix cores, and the power they draw: alone, without loads, LDS and scales, they
-// take 190 us at the 1.9 to 2.0 GHz they hold (273 us in all where every element is zero).  The rest is what does not fit behind
-// them: loads about 100 us, LDS reads 28 and writes 16, the scales 26.  Three buffers of 64 tokens, and writes between the products, come from
-// there; a higher priority of some wavefronts, loads between the products, and tiles in panels for each die are level or worse, and the
-// scales moved between the next group's products do not fit into the registers.
+// here and 7 for the join.  Nothing is busy all the time: by the counters of the long one the matrix cores are for 39 % of a compute unit's
+// cycles and LDS for as many; a wavefront spends 30 % of its life waiting for memory, LDS or a barrier and
+// 40 % for its turn to issue.  The clock is 2.0 GHz, held down by power: with zeros for every element the same call takes three
+// quarters of the time.  Three buffers of 64 tokens, and writes between the products, come from there; a higher priority of some wavefronts,
+// loads between the products, and tiles in panels for each die are level or worse, and the scales moved between the next
+// group's products do not fit into the registers.
 template <typename DyT, typename GradT, typename S, bool RAGGED>
 __global__ __launch_bounds__(S::THREADS, 2) void linear_kernel(LinearArgs A) {
     typedef typename Mma<DyT>::frag Frag;
@@ -531,7 +532,7 @@ struct LinearPlan {
 };
 
 // Which tiles.  Wide ones read least (binary16, 4096 channels and outputs, 8192 tokens: 333 us, square 423).  But where they are
-// fewer than the compute units they are split over the tokens and joined, and with few tokens that costs more than it
+// at most half as many as the compute units they are split over the tokens and joined, and with few tokens that costs more than it
 // gives: 1024 channels, 4096 outputs, 1024 tokens 31 us, square 17; 4096 tokens 55 and 54; 1024 outputs and 16384 tokens
 // 55 and 60; binary32 with 256 tokens, 1024 channels and outputs 18 and 13.
 constexpr int64_t SQUARE_GROUPS = 16;
@@ -544,7 +545,10 @@ LinearPlan plan_of(int64_t tokens, int64_t channels, int64_t outputs, bool parts
     p.tiles_c = static_cast<uint32_t>(std::max<int64_t>(ceil_div(channels, TILE_C[p.form]), 1));       // the bias is made with some tile
     p.tiles_o = static_cast<uint32_t>(ceil_div(outputs, TILE_O[p.form]));
     const int64_t tiles = static_cast<int64_t>(p.tiles_o) * p.tiles_c;
-    // enough workgroups for each of the 256 compute units, and two groups at the least for each of them
+    // As many workgroups as there are compute units, 256, at most, and two groups at the least for each of them.  In whole numbers: 129 to 255
+    // tiles are not split, and with more than 256 the last round of workgroups is as long as a full one.  bfloat16, 4096 tokens (32768):
+    // 1024 channels to 4096 outputs, 256 workgroups, 630 TFLOP/s (810); 1280 to 5120, 200 of them, 670 (700); 1536 to 6144, 288, 550 (550);
+    // 2048 to 8192, 512, 860 (840).
     int64_t splits = std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), std::max<uint32_t>(p.groups / 2, 1), MAX_SPLITS});
     splits = std::max<int64_t>(splits, 1);
     p.groups_per_split = static_cast<uint32_t>(ceil_div(std::max<uint32_t>(p.groups, 1), splits));

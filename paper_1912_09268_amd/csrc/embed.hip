@@ -144,7 +144,9 @@ __device__ __forceinline__ uint32_t first_place(const GradArgs& A, int32_t r) {
     return lo;
 }
 
-// Clears those rows from first on, at most A.clear_rows, that are not among the ordered tokens.
+// Clears those rows from first on, at most A.clear_rows, that are not among the ordered tokens.  It looks at every place of these rows, which
+// is nothing beside the sums but for very many tokens in very few rows: a million in 8 rows of 1024 bfloat16 columns 2.0 ms, of which
+// the sums are 0.42; in 100 rows 0.68.
 template <typename GradT> __device__ void clear_absent_rows(const GradArgs& A, int64_t first) {
     __shared__ uint8_t absent[THREADS];
     __shared__ uint32_t place[2];
