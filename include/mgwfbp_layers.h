@@ -1,7 +1,8 @@
 /*
  * mgwfbp_layers.h -- C ABI of the operators that make the per-layer gradients which mgwfbp.h merges, reduces and applies:
- *                    embedding lookup and its gradient, and activation checkpoints in 8 bits with what the backward
- *                    pass makes of them.  For MI355X (gfx950); a shared object of its own, libmgwfbp_layers.so.
+ *                    embedding lookup and its gradient, activation checkpoints in 8 bits with what the backward
+ *                    pass makes of them, root-mean-square norm, a gated linear recurrence and the last layer's loss, each with its
+ *                    way back.  For MI355X (gfx950); a shared object of its own, libmgwfbp_layers.so.
  *
  * The operators need no context: a call is described by its arguments, runs on the current device and on `hip_stream`
  * (a hipStream_t passed as void*; NULL is the default stream), returns without waiting, allocates nothing, keeps nothing
@@ -106,6 +107,84 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
                            const void* d_dy, int64_t dy_stride, int32_t dy_dtype, int64_t n_outputs, int32_t accumulate,
                            void* d_dw, int64_t dw_stride, void* d_db, int32_t grad_dtype, void* d_workspace,
                            uint64_t workspace_bytes, void* hip_stream);
+
+/* Root-mean-square norm between two layers, with the residual's addition:
+ *   h = x + residual, rounded to the stream's type (without a residual h is x itself)
+ *   rstd[t] = 1 / sqrt(mean over c of h[t,c]^2 + eps);  n = h * rstd;  y = n * weight          (d_weight NULL: 1)
+ * The mean is a binary64 sum, rstd is rounded to binary32 once, n and y are binary32 products, y rounded to x's type.
+ * x and y are of one type, residual and h of the same or of MGWFBP_F32.  d_h may be d_residual, with the same stride; otherwise outputs
+ * overlap nothing.  d_residual and d_h are NULL together (stream_dtype is dtype then).  eps 2^-100..2^100.
+ * Where d_q is not NULL, n is kept for mgwfbp_norm_backward as a checkpoint (above) of q and scale, with rstd [n_tokens]; and
+ * linear_scale, as large as scale, is scale * weight: q and linear_scale are a checkpoint of n * weight, of y before its rounding, for
+ * mgwfbp_act_linear_grad.  d_rstd, d_q, d_scale and d_linear_scale are NULL together.
+ *   n_tokens 0..2^26, n_channels 0..2^23 */
+int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_residual, int64_t residual_stride, int32_t stream_dtype,
+                int64_t n_tokens, int64_t n_channels, const void* d_weight, int32_t weight_dtype, double eps, void* d_h, int64_t h_stride,
+                void* d_y, int64_t y_stride, float* d_rstd, int8_t* d_q, float* d_scale, float* d_linear_scale, int64_t ld, void* hip_stream);
+
+/* Its way back: with n^ = q * scale and g = dy * weight,
+ *   dh = dresidual + rstd * (g - n^ * mean over c of g n^)     (d_dresidual, what flows into h by itself, NULL: 0)
+ *   dw[c] = sum over t of dy[t,c] * n^[t,c]                    (d_dw NULL: left out; accumulate != 0 adds to what is there)
+ * dh is the gradient of x and of residual alike; d_dx, where not NULL, gets it in dy's type, too.  dresidual and dh are of the stream's
+ * type; d_dh may be d_dresidual, with the same stride.  The workspace is needed for dw, and above 16384 channels. */
+int mgwfbp_norm_backward_workspace(int64_t n_tokens, int64_t n_channels, uint64_t* bytes_out);
+int mgwfbp_norm_backward(const int8_t* d_q, const float* d_scale, int64_t ld, const float* d_rstd, int64_t n_tokens, int64_t n_channels,
+                         const void* d_weight, int32_t weight_dtype, const void* d_dy, int64_t dy_stride, int32_t dtype, const void* d_dresidual,
+                         int64_t dresidual_stride, void* d_dh, int64_t dh_stride, int32_t stream_dtype, void* d_dx, int64_t dx_stride, int32_t accumulate,
+                         void* d_dw, int32_t grad_dtype, void* d_workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* Sequences in the rows of a matrix.  d_offsets NULL: n_sequences of n_tokens / n_sequences tokens each.  Otherwise sequence s has the
+ * rows offsets[s]..offsets[s+1]-1; offsets, [n_sequences + 1] on the device, begin with 0, do not decrease and end at n_tokens or
+ * before; rows behind the last sequence are neither read nor written.  (Offsets are kept within 0..n_tokens, whatever they are.) */
+typedef struct mgwfbp_sequences {
+    int64_t n_sequences;  /* 0..2^26 */
+    int64_t n_tokens;     /* of all, 0..2^26 */
+    const void* d_offsets;
+    int32_t offset_type;  /* mgwfbp_id_type */
+} mgwfbp_sequences;
+
+typedef enum mgwfbp_recur_kind { /* c(a), the factor of x */
+    MGWFBP_RECUR_FREE = 0,       /* 1                     */
+    MGWFBP_RECUR_CONVEX = 1,     /* 1 - a                 */
+    MGWFBP_RECUR_UNIT = 2        /* sqrt(1 - a^2)         */
+} mgwfbp_recur_kind;
+
+/* Gated linear recurrence, for every sequence and channel by itself:
+ *   a = 1 / (1 + exp(-gate));  h[t] = a[t] * h[t-1] + c(a[t]) * x[t];  y = h
+ * gate, x and y are of one type, h is binary32.  first [n_sequences][n_channels] is h before each sequence's first token (NULL: 0), last, as
+ * large, gets h behind its last one (NULL: left out; of a sequence without tokens: first).  d_last may be d_first where sequences are of
+ * one length: a step of an answer is a call with one token for each sequence.
+ * states (NULL: left out) gets what the way back needs, h before every MGWFBP_RECUR_BLOCK-th token, of each sequence where they are of one
+ * length, of all rows where there are offsets: mgwfbp_recur_states rows of n_channels. */
+#define MGWFBP_RECUR_BLOCK 128
+int mgwfbp_recur_states(const mgwfbp_sequences* sequences, int64_t* rows_out);
+int mgwfbp_recur_workspace(const mgwfbp_sequences* sequences, int64_t n_channels, int32_t dtype, uint64_t* bytes_out);
+int mgwfbp_recur(const mgwfbp_sequences* sequences, int64_t n_channels, int32_t kind, int32_t dtype, const void* d_gate, int64_t gate_stride,
+                 const void* d_x, int64_t x_stride, const float* d_first, void* d_y, int64_t y_stride, float* d_last, float* d_states,
+                 void* d_workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* Its way back: with D[t] = dy[t] + a[t+1] * D[t+1] within a sequence, dlast (NULL: 0) behind its last token,
+ *   dx = c(a) * D;  dgate = D * dh/dgate;  dfirst = a D at a sequence's first token (NULL: left out; of a sequence without tokens: dlast)
+ * from the same gate, x and first and the states that mgwfbp_recur has kept.  The workspace is as large as mgwfbp_recur's. */
+int mgwfbp_recur_backward(const mgwfbp_sequences* sequences, int64_t n_channels, int32_t kind, int32_t dtype, const void* d_gate, int64_t gate_stride,
+                          const void* d_x, int64_t x_stride, const float* d_first, const float* d_states, const void* d_dy, int64_t dy_stride,
+                          const float* d_dlast, void* d_dgate, int64_t dgate_stride, void* d_dx, int64_t dx_stride, float* d_dfirst,
+                          void* d_workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* Loss of a row of logits z against a label and against a teacher that is known by its top logits, and its gradient:
+ *   p_j = exp(s_j / tau) / sum over the row's entries
+ *   loss[t] = w * (label_weight * (-log softmax(z)[label]) + teacher_weight * tau^2 * sum over j of p_j * (log p_j - log softmax(z / tau)[id_j]))
+ *   dz[t,:] = its gradient, of z's type                        (d_dz NULL: left out; it may be d_z with the same stride)
+ * labels [n_tokens] (NULL: none; one outside 0..n_vocabulary-1: none), ids and teacher [n_tokens][n_top] with a stride each: an id outside
+ * 0..n_vocabulary-1 or a logit of -inf is no entry, the same id twice counts twice.  w = row_weight[t] (NULL: 1).  A row whose w is 0, or
+ * that has neither label nor entry (or a weight of 0 for what it has), is not looked at: its loss is 0 and its gradient zeros.  Otherwise an
+ * infinity of +inf or a NaN in the row makes both NaN; -inf is a place that is masked out.
+ *   n_vocabulary 1..2^23, n_top 0..MGWFBP_MAX_TOP, temperature 2^-20..2^20, weights finite */
+#define MGWFBP_MAX_TOP 1024
+int mgwfbp_distill(const void* d_z, int64_t z_stride, int32_t dtype, int64_t n_tokens, int64_t n_vocabulary, const void* d_labels, int32_t label_type,
+                   const void* d_ids, int64_t ids_stride, int32_t id_type, const void* d_teacher, int64_t teacher_stride, int32_t teacher_dtype, int32_t n_top,
+                   float temperature, float label_weight, float teacher_weight, const float* d_row_weight, float* d_loss, void* d_dz, int64_t dz_stride,
+                   void* hip_stream);
 
 int mgwfbp_layers_last_hip_error(void); /* hipError_t of the last failed HIP call of these operators on this thread, 0 if none */
 

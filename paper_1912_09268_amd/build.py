@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_NAME = "libmgwfbp.so"
 SOURCES = ("plan.cpp", "model.cpp", "layout.cpp", "kernels.hip")
 LAYERS_NAME = "libmgwfbp_layers.so"
-LAYERS_SOURCES = ("embed.hip", "act8.hip", "act_linear.hip")
+LAYERS_SOURCES = ("embed.hip", "act8.hip", "act_linear.hip", "norm.hip", "recur.hip", "distill.hip")
 AID_DIR = os.path.join(ROOT, "bench_aid")
 AID_LIB = os.path.join(AID_DIR, "libmgwfbp_bench_aid.so")
 

@@ -12,6 +12,7 @@
 #include <algorithm>
 #include <cstdint>
 
+#include "act_code.h"
 #include "act_kinds.h"
 #include "act_layout.h"
 #include "device_types.h"
@@ -24,7 +25,6 @@ using namespace ops;
 constexpr int THREADS = 256;
 constexpr int GROUP = MGWFBP_ACT_GROUP;
 
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // ---------------------------------------------------------------------------------------------
@@ -67,14 +67,6 @@ template <typename T> struct Magnitudes {
         else return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(m[i / 2] >> (16 * (i % 2)))));
     }
 };
-
-// Four whole numbers of -127 .. 127 to bytes: added to 1.5 * 2^23 a number's last eight bits are those of the sum, which rounds to
-// nearest even on the way.
-__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d) {
-    auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x + 12582912.f); };
-    const uint32_t low = __builtin_amdgcn_perm(bits(b), bits(a), 0x0c0c0400), high = __builtin_amdgcn_perm(bits(d), bits(c), 0x04000c0c);
-    return low | high;
-}
 
 // A workgroup takes 128 channels of a group: the whole of it stays in registers between the search for the largest magnitude
 // and the rounding, so x is read once.  y does not wait for that: it is made and written as rows arrive.  4096 tokens of 4096
@@ -189,9 +181,8 @@ template <typename T, int KIND, bool SLOPE, bool VALUE> __global__ __launch_boun
             float dx[VEC], y[VEC];
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const int32_t code = static_cast<int32_t>(q[r][i / 4]) << (24 - 8 * (i % 4)) >> 24;
                 float slope;
-                activate<KIND>(static_cast<float>(code) * get(scale, i), y[i], slope);
+                activate<KIND>(code_of(q[r], i) * get(scale, i), y[i], slope);
                 if constexpr (SLOPE) dx[i] = get(dy[r], i) * slope;
             }
             if constexpr (SLOPE) store8(static_cast<T*>(A.dx) + t * A.dx_stride + col, dx, n);

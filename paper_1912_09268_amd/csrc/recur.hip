@@ -1,0 +1,845 @@
+// Gated linear recurrence over the tokens of sequences, and its way back.
+//
+//   a = 1 / (1 + exp(-gate));  h[t] = a[t] * h[t-1] + c(a[t]) * x[t], for every channel by itself;  y = h
+//   c = 1 (free), 1 - a (convex) or sqrt(1 - a^2) (unit);  h before a sequence's first token is first[s], behind its last one last[s]
+//
+//   D[t] = dy[t] + a[t+1] * D[t+1], with dlast[s] behind a sequence's last token;  dfirst[s] = a D at its first token
+//   dx = c D;  dgate = D * a * (1 - a) * (h[t-1] + c'(a) x)
+//
+// A step is the map h -> a h + b, and such maps compose to maps of the same form: (A, B) then (a, b) is (a A, a B + b).  So a
+// block of 128 tokens is cut into eight wavefronts of sixteen tokens each, a lane for a channel or two: every wavefront composes its
+// own tokens in registers, the eight pairs meet in LDS, and with what comes in every wavefront goes through its tokens once
+// more.  The data is read once and written once, in tokens and channels as they lie; the next block is on its way meanwhile.  A
+// workgroup goes through the blocks of a sequence one after the other.  Where there are too few sequences and channels to fill the
+// chip, sequences are cut into segments, whose maps a launch before finds (fold_kernel): gate and x (or dy) are read twice then.
+//
+// The way back needs h[t-1].  It is made again from gate and x and a kept state before each block, 1/32 of a byte an element
+// for each byte of a channel's state, instead of kept for every token: y may be thrown away, and h is not rounded.
+//
+// Sequences lie side by side, all of one length, or one behind the other between offsets.  In the latter form a sequence's first token
+// drops what came before it wherever in a block it falls: its map has A = -0, which no product of gates is, and does not look at h, so
+// that an infinity or NaN stays in its sequence.
+//
+// The gate's exponential is exp2(-|gate| log2 e), whose argument is rounded to binary32 twice: the smaller of a and 1 - a is off by
+// 1.2e-7 |gate| + 3e-7 of itself, the larger one by 3e-7.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "device_types.h"
+#include "mgwfbp_layers.h"
+
+namespace {
+
+using namespace ops;
+
+constexpr int WAVES = 8, LANES = 64, TOKENS = 16;            // of a workgroup, of a wavefront, of a wavefront and block
+constexpr int BLOCK = WAVES * TOKENS;
+static_assert(BLOCK == MGWFBP_RECUR_BLOCK);
+constexpr int SHORT = 16;                                    // tokens up to which a lane goes through a sequence by itself
+
+struct RecurArgs {
+    const void* gate;
+    const void* x;
+    const void* dy;
+    const float* first;
+    const float* dlast;
+    const void* offsets;
+    void* y;
+    void* dgate;
+    void* dx;
+    float* last;
+    float* dfirst;
+    float* states;                       // [units][blocks][channels]
+    float* maps;                         // [units][segments][2][channels]: A and B of a segment
+    int64_t gate_stride, x_stride, dy_stride, y_stride, dgate_stride, dx_stride;
+    int64_t channels, sequences, tokens, blocks;             // tokens and blocks of a unit: of a sequence, or of all of them
+    uint32_t slabs, segments, per_segment;                   // pieces of the channels; pieces of a unit, and their blocks
+    int32_t offset_type;
+    int32_t copied;                      // first is in the maps' last segment: the caller's may be overwritten by last
+};
+
+// A map that begins a sequence: it gives b whatever comes in.
+constexpr float FRESH = -0.f;
+__device__ __forceinline__ bool is_fresh(float a) { return __builtin_bit_cast(uint32_t, a) == 0x80000000u; }
+__device__ __forceinline__ float through(float a, float b, float h) { return is_fresh(a) ? b : __builtin_fmaf(a, h, b); }
+// (a, b) and then (ma, mb), in (a, b)
+__device__ __forceinline__ void compose(float& a, float& b, float ma, float mb) {
+    b = through(ma, mb, b);
+    a = is_fresh(ma) ? FRESH : a * ma;                       // a product of FRESH and a gate is FRESH again
+}
+
+// CH neighbouring elements of a row, n of them there.
+template <typename T, int CH> struct Piece {
+    typedef T vec __attribute__((ext_vector_type(CH), aligned(alignof(T))));
+    vec v;
+    __device__ __forceinline__ void load(const T* p, int n) {
+        if (n >= CH) {
+            v = *reinterpret_cast<const vec*>(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) v[i] = i < n ? p[i] : static_cast<T>(0.f);
+        }
+    }
+    __device__ __forceinline__ float get(int i) const { return static_cast<float>(v[i]); }
+};
+
+// a and 1 - a of a gate, both to their own last digits.
+__device__ __forceinline__ void logistic(float g, float& a, float& rest) {
+    const float e = __builtin_amdgcn_exp2f(__builtin_fabsf(g) * -1.44269504088896341f);
+    const float near = __builtin_amdgcn_rcpf(1.f + e), far = e * near;
+    a = g >= 0.f ? near : far;
+    rest = g >= 0.f ? far : near;
+    if (g != g) a = rest = g;
+}
+template <int KIND> __device__ __forceinline__ float factor(float a, float rest) {
+    if constexpr (KIND == MGWFBP_RECUR_FREE) return 1.f;
+    else if constexpr (KIND == MGWFBP_RECUR_CONVEX) return rest;
+    else return __builtin_amdgcn_sqrtf(rest * (1.f + a));
+}
+// d h[t] / d gate[t]
+template <int KIND> __device__ __forceinline__ float slope(float a, float rest, float before, float x) {
+    if constexpr (KIND == MGWFBP_RECUR_FREE) return a * rest * before;
+    else if constexpr (KIND == MGWFBP_RECUR_CONVEX) return a * rest * (before - x);
+    else return a * (rest * before - a * factor<KIND>(a, rest) * __builtin_amdgcn_rcpf(1.f + a) * x);     // dc/da = -a / c
+}
+
+// Where sequences begin that lie one behind the other: offsets [count], not decreasing.  All lanes of a wavefront ask together.
+// Offsets are kept within 0 .. most, and every place that is read is one of the count, so wrong ones lead nowhere else.
+struct Bounds {
+    const void* p;
+    int type, count, most, held;
+    __device__ __forceinline__ int at(int i) const {
+        const int64_t v = type == MGWFBP_I64 ? static_cast<const int64_t*>(p)[i] : static_cast<const int32_t*>(p)[i];
+        return static_cast<int>(min(max(v, static_cast<int64_t>(0)), static_cast<int64_t>(most)));
+    }
+    __device__ __forceinline__ void open(const RecurArgs& A) {
+        p = A.offsets;
+        type = A.offset_type;
+        count = static_cast<int>(A.sequences) + 1;
+        most = static_cast<int>(A.tokens);
+        const int lane = threadIdx.x % LANES;
+        held = at(min(lane, count - 1));                     // up to 63 sequences: all there is
+    }
+    // How many offsets are <= t: of 64 places at a time, so two or three waits for memory where there are thousands.
+    __device__ __forceinline__ int up_to(int t) const {
+        const int lane = threadIdx.x % LANES;
+        if (count <= LANES) return __popcll(__ballot(lane < count && held <= t));
+        int lo = 0, hi = count;                              // those before lo are, those from hi on are not
+        while (hi - lo > LANES) {
+            const int step = (hi - lo + LANES - 1) / LANES, i = lo + (lane + 1) * step - 1;
+            const int k = __popcll(__ballot(i < hi && at(min(i, count - 1)) <= t));
+            hi = min(hi, lo + (k + 1) * step - 1);
+            lo += k * step;
+        }
+        return lo + __popcll(__ballot(lo + lane < hi && at(min(lo + lane, count - 1)) <= t));
+    }
+    __device__ __forceinline__ int sequence_of(int t) const { return min(max(up_to(t) - 1, 0), count - 2); }
+    // Bit i: an offset is t0 + i, 0 <= i <= TOKENS.
+    __device__ __forceinline__ uint32_t marks(int t0) const {
+        const int lane = threadIdx.x % LANES;
+        uint32_t bits = 0;
+        if (count <= LANES) {
+            const int i = held - t0;
+            const bool in = lane < count && i >= 0 && i <= TOKENS;
+            if (__ballot(in) == 0) return 0;
+            bits = in ? 1u << i : 0u;
+        } else {
+            const int from = up_to(t0 - 1), to = up_to(t0 + TOKENS);
+            if (from >= to) return 0;
+            for (int j = from + lane; j < to; j += LANES) {
+                const int i = at(j) - t0;
+                if (i >= 0 && i <= TOKENS) bits |= 1u << i;
+            }
+        }
+#pragma unroll
+        for (int d = LANES / 2; d > 0; d /= 2) bits |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(bits), d));
+        return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(bits)));
+    }
+};
+
+// What a wavefront knows of its place.
+template <bool PACKED, int CH> struct Place {
+    Bounds bounds;
+    int64_t unit, base;                  // base: the unit's first row
+    int64_t c;                           // the lane's first channel
+    int n;                               // and how many it has
+    int begin, end;                      // tokens of the unit that are sequences'
+    uint32_t segment, first_block, end_block;
+
+    __device__ __forceinline__ void open(const RecurArgs& A) {
+        const uint32_t slab = blockIdx.x % A.slabs, rest = blockIdx.x / A.slabs;
+        segment = rest % A.segments;
+        unit = rest / A.segments;
+        base = PACKED ? 0 : unit * A.tokens;
+        c = (static_cast<int64_t>(slab) * LANES + threadIdx.x % LANES) * CH;
+        n = static_cast<int>(max(static_cast<int64_t>(0), min(A.channels - c, static_cast<int64_t>(CH))));
+        begin = 0;
+        end = static_cast<int>(A.tokens);
+        if constexpr (PACKED) {
+            bounds.open(A);
+            begin = bounds.at(0);
+            end = bounds.at(bounds.count - 1);
+        }
+        first_block = segment * A.per_segment;
+        end_block = min(first_block + A.per_segment, static_cast<uint32_t>((end + BLOCK - 1) / BLOCK));
+    }
+    __device__ __forceinline__ int row(int t) const { return min(max(t, begin), max(end - 1, 0)); }      // one that may be read
+    // Bits of the TOKENS tokens from t0 on: a sequence's, the first of one, the last of one.
+    __device__ __forceinline__ void masks(int t0, uint32_t& valid, uint32_t& first, uint32_t& last) const {
+        constexpr uint32_t ALL = (1u << TOKENS) - 1;
+        const int lo = min(max(begin - t0, 0), TOKENS), hi = min(max(end - t0, 0), TOKENS);
+        valid = (ALL >> (TOKENS - hi)) & (ALL << lo) & ALL;
+        if (hi == 0) valid = 0;
+        uint32_t marks;
+        if constexpr (PACKED) marks = bounds.marks(t0);
+        else marks = (t0 == 0 ? 1u : 0u) | (end >= t0 && end - t0 <= TOKENS ? 1u << (end - t0) : 0u);
+        first = marks & valid;
+        last = marks >> 1 & valid;
+    }
+    __device__ __forceinline__ int64_t sequence_at(int t) const {
+        if constexpr (PACKED) return bounds.sequence_of(t);
+        else return unit;
+    }
+    __device__ __forceinline__ void state(const RecurArgs& A, const float* from, int64_t sequence, float (&out)[CH]) const {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) out[k] = from != nullptr && k < n ? from[sequence * A.channels + c + k] : 0.f;
+    }
+    __device__ __forceinline__ void put_state(const RecurArgs& A, float* to, int64_t sequence, const float (&in)[CH]) const {
+        if (to == nullptr) return;
+#pragma unroll
+        for (int k = 0; k < CH; ++k)
+            if (k < n) to[sequence * A.channels + c + k] = in[k];
+    }
+    // Sequences without tokens hand their state on.
+    __device__ __forceinline__ void empty_sequences(const RecurArgs& A, const float* from, float* to) const {
+        if constexpr (PACKED) {
+            if (to == nullptr) return;
+            for (int64_t s0 = threadIdx.x / LANES * LANES; s0 < A.sequences; s0 += WAVES * LANES) {
+                const int64_t s = s0 + threadIdx.x % LANES;
+                uint64_t empty = __ballot(s < A.sequences && bounds.at(static_cast<int>(min(s, A.sequences - 1))) >= bounds.at(static_cast<int>(min(s + 1, A.sequences))));
+                while (empty != 0) {
+                    const int64_t at = s0 + __ffsll(static_cast<unsigned long long>(empty)) - 1;
+                    empty &= empty - 1;
+                    float h[CH];
+                    state(A, from, at, h);
+                    put_state(A, to, at, h);
+                }
+            }
+        }
+    }
+};
+
+// A wavefront's tokens of a block, as they are in memory.
+template <typename T, int CH> struct Tokens {
+    Piece<T, CH> v[TOKENS];
+    template <bool PACKED> __device__ __forceinline__ void load(const Place<PACKED, CH>& at, const void* from, int64_t stride, int t0) {
+        const T* const p = static_cast<const T*>(from) + at.c;
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) v[i].load(p + (at.base + at.row(t0 + i)) * stride, at.n);
+    }
+};
+
+// Maps of wavefronts in LDS, two blocks in turn, so that one barrier a block is enough.
+template <int CH> struct Maps {
+    float m[2][WAVES][2][LANES * CH];
+    __device__ __forceinline__ void put(uint32_t turn, int wave, const float (&a)[CH], const float (&b)[CH]) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            m[turn][wave][0][k * LANES + threadIdx.x % LANES] = a[k];
+            m[turn][wave][1][k * LANES + threadIdx.x % LANES] = b[k];
+        }
+    }
+    // h through the map of a wavefront.
+    __device__ __forceinline__ void take(uint32_t turn, int wave, float (&h)[CH]) const {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) h[k] = through(m[turn][wave][0][k * LANES + threadIdx.x % LANES], m[turn][wave][1][k * LANES + threadIdx.x % LANES], h[k]);
+    }
+};
+
+// The state that comes into a segment through the maps of those before it (or, on the way back, behind it), which eight
+// wavefronts share.
+template <bool BACK, bool PACKED, int CH> __device__ __forceinline__ void through_segments(const RecurArgs& A, const Place<PACKED, CH>& at, Maps<CH>& room, float (&h)[CH]) {
+    const int wave = threadIdx.x / LANES;
+    const int count = static_cast<int>(BACK ? A.segments - 1 - at.segment : at.segment);
+    const int each = (count + WAVES - 1) / WAVES, from = min(wave * each, count), to = min(from + each, count);
+    float a[CH], b[CH];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        a[k] = 1.f;
+        b[k] = 0.f;
+    }
+#pragma unroll 4
+    for (int i = from; i < to; ++i) {
+        const int64_t s = at.unit * A.segments + (BACK ? A.segments - 1 - i : i);
+        const float* const map = A.maps + s * 2 * A.channels + at.c;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const float ma = k < at.n ? map[k] : 1.f, mb = k < at.n ? map[A.channels + k] : 0.f;
+            compose(a[k], b[k], ma, mb);
+        }
+    }
+    room.put(1, wave, a, b);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < CH; ++k) h[k] = 0.f;
+    for (int w = 0; w < WAVES; ++w) room.take(1, w, h);      // turn 1 is written again after another barrier
+}
+
+// The first state of a unit of one sequence.  `last` may be the same memory: it is read before the first barrier here, or from where
+// fold_kernel has put it.
+template <bool PACKED, int CH> __device__ __forceinline__ void unit_first(const RecurArgs& A, const Place<PACKED, CH>& at, float (&h)[CH]) {
+    if (A.copied) {
+        const float* const map = A.maps + (at.unit * A.segments + A.segments - 1) * 2 * A.channels + at.c;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) h[k] = k < at.n ? map[k] : 0.f;
+    } else {
+        at.state(A, A.first, at.unit, h);
+    }
+}
+
+// gate and x of a wavefront's tokens to the steps h -> a h + b; a token of no sequence changes nothing.
+template <typename T, int KIND, int CH> __device__ __forceinline__ void steps_of(const Tokens<T, CH>& gate, const Tokens<T, CH>& x, uint32_t valid, float (&a)[TOKENS][CH],
+                                                                                 float (&b)[TOKENS][CH]) {
+#pragma unroll
+    for (int i = 0; i < TOKENS; ++i)
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            float rest;
+            logistic(gate.v[i].get(k), a[i][k], rest);
+            b[i][k] = factor<KIND>(a[i][k], rest) * x.v[i].get(k);
+            if (!(valid >> i & 1)) {
+                a[i][k] = 1.f;
+                b[i][k] = 0.f;
+            }
+        }
+}
+
+// ---------------------------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------------------------
+
+template <typename T, int KIND, int CH, bool PACKED> __global__ __launch_bounds__(WAVES * LANES) void scan_kernel(RecurArgs A) {
+    __shared__ Maps<CH> maps;
+    Place<PACKED, CH> at;
+    at.open(A);
+    const int wave = threadIdx.x / LANES;
+    if (at.segment == 0) at.empty_sequences(A, A.first, A.last);
+    if (at.first_block >= at.end_block) return;
+    float carry[CH] = {}, first[CH];
+    if constexpr (!PACKED) unit_first(A, at, first);
+    if (at.segment > 0) through_segments<false>(A, at, maps, carry);
+    Tokens<T, CH> gate, x;
+    int t0 = static_cast<int>(at.first_block) * BLOCK + wave * TOKENS;
+    gate.load(at, A.gate, A.gate_stride, t0);
+    x.load(at, A.x, A.x_stride, t0);
+    for (uint32_t block = at.first_block; block < at.end_block; ++block, t0 += BLOCK) {
+        const uint32_t turn = (block - at.first_block) % 2;
+        uint32_t valid, begins, ends;
+        at.masks(t0, valid, begins, ends);
+        float a[TOKENS][CH], b[TOKENS][CH];
+        steps_of<T, KIND, CH>(gate, x, valid, a, b);
+        if (block + 1 < at.end_block) {
+            gate.load(at, A.gate, A.gate_stride, t0 + BLOCK);
+            x.load(at, A.x, A.x_stride, t0 + BLOCK);
+        }
+        auto reset = [&](int i, float (&h)[CH]) {
+            if constexpr (PACKED) at.state(A, A.first, at.sequence_at(t0 + i), h);
+            else
+#pragma unroll
+                for (int k = 0; k < CH; ++k) h[k] = first[k];
+        };
+        float ma[CH], mb[CH];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            ma[k] = 1.f;
+            mb[k] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            if (begins >> i & 1) {
+                reset(i, mb);
+#pragma unroll
+                for (int k = 0; k < CH; ++k) ma[k] = FRESH;
+            }
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                mb[k] = __builtin_fmaf(a[i][k], mb[k], b[i][k]);
+                ma[k] *= a[i][k];
+            }
+        }
+        maps.put(turn, wave, ma, mb);
+        __syncthreads();
+        float h[CH];
+        if (A.states != nullptr && wave == 0 && t0 >= at.begin) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) h[k] = carry[k];
+            if (begins & 1) reset(0, h);
+            at.put_state(A, A.states, at.unit * A.blocks + block, h);
+        }
+        for (int w = 0; w < WAVES; ++w) {
+            if (w == wave) {
+#pragma unroll
+                for (int k = 0; k < CH; ++k) h[k] = carry[k];
+            }
+            maps.take(turn, w, carry);
+        }
+        T* const to = static_cast<T*>(A.y) + at.c;
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            if (begins >> i & 1) reset(i, h);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) h[k] = __builtin_fmaf(a[i][k], h[k], b[i][k]);
+            if (valid >> i & 1) store_some(to + (at.base + t0 + i) * A.y_stride, h, at.n);
+            if (ends >> i & 1) at.put_state(A, A.last, at.sequence_at(t0 + i), h);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// backward
+// ---------------------------------------------------------------------------------------------
+
+template <typename T, int KIND, int CH, bool PACKED> __global__ __launch_bounds__(WAVES * LANES) void back_kernel(RecurArgs A) {
+    __shared__ Maps<CH> forth, back;
+    Place<PACKED, CH> at;
+    at.open(A);
+    const int wave = threadIdx.x / LANES;
+    if (at.segment == 0) at.empty_sequences(A, A.dlast, A.dfirst);
+    if (at.first_block >= at.end_block) return;
+    float carry[CH] = {}, state[CH];
+    if (at.segment + 1 < A.segments) through_segments<true>(A, at, back, carry);
+    Tokens<T, CH> gate, x, dy;
+    int t0 = static_cast<int>(at.end_block - 1) * BLOCK + wave * TOKENS;
+    gate.load(at, A.gate, A.gate_stride, t0);
+    x.load(at, A.x, A.x_stride, t0);
+    dy.load(at, A.dy, A.dy_stride, t0);
+    at.state(A, A.states, at.unit * A.blocks + at.end_block - 1, state);
+    for (uint32_t block = at.end_block; block-- > at.first_block; t0 -= BLOCK) {
+        const uint32_t turn = (at.end_block - 1 - block) % 2;
+        uint32_t valid, begins, ends;
+        at.masks(t0, valid, begins, ends);
+        float a[TOKENS][CH], b[TOKENS][CH];
+        steps_of<T, KIND, CH>(gate, x, valid, a, b);
+        auto flow_in = [&](int i, float (&g)[CH]) { at.state(A, A.dlast, at.sequence_at(t0 + i), g); };
+        auto state_in = [&](int i, float (&h)[CH]) { at.state(A, A.first, at.sequence_at(t0 + i), h); };
+        float ma[CH], mb[CH], ra[CH], rb[CH];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            ma[k] = ra[k] = 1.f;
+            mb[k] = rb[k] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            if (begins >> i & 1) {
+                state_in(i, mb);
+#pragma unroll
+                for (int k = 0; k < CH; ++k) ma[k] = FRESH;
+            }
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                mb[k] = __builtin_fmaf(a[i][k], mb[k], b[i][k]);
+                ma[k] *= a[i][k];
+            }
+        }
+#pragma unroll
+        for (int i = TOKENS - 1; i >= 0; --i) {
+            if (ends >> i & 1) {
+                flow_in(i, rb);
+#pragma unroll
+                for (int k = 0; k < CH; ++k) ra[k] = FRESH;
+            }
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                rb[k] = a[i][k] * (rb[k] + (valid >> i & 1 ? dy.v[i].get(k) : 0.f));
+                ra[k] *= a[i][k];
+            }
+        }
+        forth.put(turn, wave, ma, mb);
+        back.put(turn, wave, ra, rb);
+        __syncthreads();
+        float before[TOKENS][CH], flow[CH];
+        for (int w = 0; w < wave; ++w) forth.take(turn, w, state);
+        for (int w = WAVES - 1; w >= 0; --w) {
+            if (w == wave) {
+#pragma unroll
+                for (int k = 0; k < CH; ++k) flow[k] = carry[k];
+            }
+            back.take(turn, w, carry);
+        }
+#pragma unroll
+        for (int i = 0; i < TOKENS; ++i) {
+            if (begins >> i & 1) state_in(i, state);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                before[i][k] = state[k];
+                state[k] = __builtin_fmaf(a[i][k], state[k], b[i][k]);
+            }
+        }
+        T *const to_gate = static_cast<T*>(A.dgate) + at.c, *const to_x = static_cast<T*>(A.dx) + at.c;
+#pragma unroll
+        for (int i = TOKENS - 1; i >= 0; --i) {
+            if (ends >> i & 1) flow_in(i, flow);
+            if (!(valid >> i & 1)) continue;
+            float dg[CH], dx[CH];
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                const float d = flow[k] + dy.v[i].get(k);
+                float same, rest;
+                logistic(gate.v[i].get(k), same, rest);
+                dx[k] = factor<KIND>(same, rest) * d;
+                dg[k] = slope<KIND>(same, rest, before[i][k], x.v[i].get(k)) * d;
+                flow[k] = same * d;
+            }
+            store_some(to_gate + (at.base + t0 + i) * A.dgate_stride, dg, at.n);
+            store_some(to_x + (at.base + t0 + i) * A.dx_stride, dx, at.n);
+            if (begins >> i & 1) at.put_state(A, A.dfirst, at.sequence_at(t0 + i), flow);
+        }
+        if (block > at.first_block) {
+            gate.load(at, A.gate, A.gate_stride, t0 - BLOCK);
+            x.load(at, A.x, A.x_stride, t0 - BLOCK);
+            dy.load(at, A.dy, A.dy_stride, t0 - BLOCK);
+            at.state(A, A.states, at.unit * A.blocks + block - 1, state);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// segments
+// ---------------------------------------------------------------------------------------------
+
+// The map of a segment: every wavefront composes an eighth of its tokens.  On the way back (x is dy there) it is the map of what
+// flows from a token to the one before it, g -> a (dy + g).  The last segment's map (the first one's, on the way back) is
+// nobody's, so it is not made; its place keeps the first state where that may be overwritten.
+template <typename T, int KIND, int CH, bool PACKED, bool BACK> __global__ __launch_bounds__(WAVES * LANES) void fold_kernel(RecurArgs A) {
+    __shared__ Maps<CH> maps;
+    Place<PACKED, CH> at;
+    at.open(A);
+    const int wave = threadIdx.x / LANES;
+    if (!BACK && !PACKED && A.copied && at.segment == A.segments - 1 && wave == 0) {
+        float first[CH];
+        at.state(A, A.first, at.unit, first);
+        float* const map = A.maps + (at.unit * A.segments + at.segment) * 2 * A.channels + at.c;
+#pragma unroll
+        for (int k = 0; k < CH; ++k)
+            if (k < at.n) map[k] = first[k];
+    }
+    if (at.segment == (BACK ? 0 : A.segments - 1)) return;
+    float ma[CH], mb[CH];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        ma[k] = 1.f;
+        mb[k] = 0.f;
+    }
+    const int pieces = static_cast<int>(A.per_segment);      // of a wavefront
+    const int from = static_cast<int>(at.first_block) * BLOCK + wave * pieces * TOKENS;
+    if (at.first_block < at.end_block) {
+        Tokens<T, CH> gate, x;
+        auto start = [&](int p) { return from + (BACK ? pieces - 1 - p : p) * TOKENS; };
+        gate.load(at, A.gate, A.gate_stride, start(0));
+        x.load(at, BACK ? A.dy : A.x, BACK ? A.dy_stride : A.x_stride, start(0));
+        for (int p = 0; p < pieces; ++p) {
+            const int t0 = start(p);
+            uint32_t valid, begins, ends;
+            at.masks(t0, valid, begins, ends);
+            float a[TOKENS][CH], b[TOKENS][CH];
+            steps_of<T, BACK ? MGWFBP_RECUR_FREE : KIND, CH>(gate, x, valid, a, b);
+            if (p + 1 < pieces) {
+                gate.load(at, A.gate, A.gate_stride, start(p + 1));
+                x.load(at, BACK ? A.dy : A.x, BACK ? A.dy_stride : A.x_stride, start(p + 1));
+            }
+#pragma unroll
+            for (int j = 0; j < TOKENS; ++j) {
+                const int i = BACK ? TOKENS - 1 - j : j;
+                if ((BACK ? ends : begins) >> i & 1) {
+                    at.state(A, BACK ? A.dlast : A.first, at.sequence_at(t0 + i), mb);
+#pragma unroll
+                    for (int k = 0; k < CH; ++k) ma[k] = FRESH;
+                }
+#pragma unroll
+                for (int k = 0; k < CH; ++k) {
+                    mb[k] = BACK ? a[i][k] * (mb[k] + b[i][k]) : __builtin_fmaf(a[i][k], mb[k], b[i][k]);
+                    ma[k] *= a[i][k];
+                }
+            }
+        }
+    }
+    maps.put(0, wave, ma, mb);
+    __syncthreads();
+    if (wave != 0) return;
+    const int lane = threadIdx.x % LANES;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        float a = 1.f, b = 0.f;
+        for (int j = 0; j < WAVES; ++j) {
+            const int w = BACK ? WAVES - 1 - j : j;
+            compose(a, b, maps.m[0][w][0][k * LANES + lane], maps.m[0][w][1][k * LANES + lane]);
+        }
+        if (k < at.n) {
+            float* const map = A.maps + (at.unit * A.segments + at.segment) * 2 * A.channels + at.c + k;
+            map[0] = a;
+            map[A.channels] = b;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// short sequences of one length
+// ---------------------------------------------------------------------------------------------
+
+constexpr int SHORT_THREADS = 256;
+
+// A lane goes through eight channels of a sequence: a step of an answer is one token.
+template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void short_scan_kernel(RecurArgs A) {
+    const int64_t vecs = (A.channels + VEC - 1) / VEC, at = static_cast<int64_t>(blockIdx.x) * SHORT_THREADS + threadIdx.x;
+    const int64_t s = at / vecs, c = (at - s * vecs) * VEC;
+    if (s >= A.sequences) return;
+    const int n = static_cast<int>(min(A.channels - c, static_cast<int64_t>(VEC)));
+    const Raw8<float> first = load8(A.first != nullptr ? A.first + s * A.channels + c : nullptr, A.first != nullptr ? n : 0);
+    float h[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) h[k] = get(first, k);
+    if (A.states != nullptr && A.tokens > 0) store8(A.states + s * A.channels + c, h, n);
+    for (int64_t t = s * A.tokens; t < (s + 1) * A.tokens; ++t) {
+        const Raw8<T> gate = load8(static_cast<const T*>(A.gate) + t * A.gate_stride + c, n), x = load8(static_cast<const T*>(A.x) + t * A.x_stride + c, n);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            float a, rest;
+            logistic(get(gate, k), a, rest);
+            h[k] = __builtin_fmaf(a, h[k], factor<KIND>(a, rest) * get(x, k));
+        }
+        store8(static_cast<T*>(A.y) + t * A.y_stride + c, h, n);
+    }
+    if (A.last != nullptr) store8(A.last + s * A.channels + c, h, n);
+}
+
+// Its way back, a lane for two channels: the states of up to SHORT tokens stay in registers.
+template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void short_back_kernel(RecurArgs A) {
+    constexpr int CH = 2;
+    const int64_t pairs = (A.channels + CH - 1) / CH, at = static_cast<int64_t>(blockIdx.x) * SHORT_THREADS + threadIdx.x;
+    const int64_t s = at / pairs, c = (at - s * pairs) * CH;
+    if (s >= A.sequences) return;
+    const int n = static_cast<int>(min(A.channels - c, static_cast<int64_t>(CH))), tokens = static_cast<int>(A.tokens);
+    Piece<T, CH> gate[SHORT], x[SHORT], dy[SHORT];
+#pragma unroll
+    for (int i = 0; i < SHORT; ++i) {
+        const int64_t t = s * tokens + i;
+        const int m = i < tokens ? n : 0;
+        gate[i].load(static_cast<const T*>(A.gate) + t * A.gate_stride + c, m);
+        x[i].load(static_cast<const T*>(A.x) + t * A.x_stride + c, m);
+        dy[i].load(static_cast<const T*>(A.dy) + t * A.dy_stride + c, m);
+    }
+    float h[CH], flow[CH], before[SHORT][CH];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        h[k] = A.first != nullptr && k < n ? A.first[s * A.channels + c + k] : 0.f;
+        flow[k] = A.dlast != nullptr && k < n ? A.dlast[s * A.channels + c + k] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < SHORT; ++i) {
+        if (i >= tokens) break;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            float a, rest;
+            logistic(gate[i].get(k), a, rest);
+            before[i][k] = h[k];
+            h[k] = __builtin_fmaf(a, h[k], factor<KIND>(a, rest) * x[i].get(k));
+        }
+    }
+#pragma unroll
+    for (int i = SHORT - 1; i >= 0; --i) {
+        if (i >= tokens) continue;
+        float dg[CH], dx[CH];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            float a, rest;
+            logistic(gate[i].get(k), a, rest);
+            const float d = flow[k] + dy[i].get(k);
+            dx[k] = factor<KIND>(a, rest) * d;
+            dg[k] = slope<KIND>(a, rest, before[i][k], x[i].get(k)) * d;
+            flow[k] = a * d;
+        }
+        const int64_t t = s * tokens + i;
+        store_some(static_cast<T*>(A.dgate) + t * A.dgate_stride + c, dg, n);
+        store_some(static_cast<T*>(A.dx) + t * A.dx_stride + c, dx, n);
+    }
+    if (A.dfirst != nullptr) store_some(A.dfirst + s * A.channels + c, flow, n);
+}
+
+// ---- host side -------------------------------------------------------------------------------
+
+constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_CHANNELS = int64_t(1) << 23;
+
+// How the work is cut.
+struct Cut {
+    int64_t units, tokens, blocks, slabs, segments, per_segment;
+    int ch;
+};
+
+constexpr int64_t FILL = 512;            // workgroups that are wanted
+
+Cut cut_of(int64_t sequences, int64_t tokens, int64_t channels, bool packed, int32_t dtype) {
+    Cut c{};
+    c.units = packed ? 1 : sequences;
+    c.tokens = tokens;
+    c.blocks = ceil_div(tokens, BLOCK);
+    c.ch = dtype == MGWFBP_F32 ? 1 : 2;
+    c.slabs = ceil_div(channels, static_cast<int64_t>(LANES) * c.ch);
+    const int64_t whole = c.units * c.slabs;
+    c.segments = std::max<int64_t>(1, std::min(c.blocks, FILL / std::max<int64_t>(whole, 1)));
+    c.per_segment = std::max<int64_t>(1, ceil_div(c.blocks, c.segments));
+    c.segments = std::max<int64_t>(1, ceil_div(c.blocks, c.per_segment));
+    return c;
+}
+
+bool sizes_ok(const mgwfbp_sequences* s, int64_t channels) {
+    if (s == nullptr || s->n_sequences < 0 || s->n_sequences > MOST_TOKENS || s->n_tokens < 0 || s->n_tokens > MOST_TOKENS || channels < 0 || channels > MOST_CHANNELS)
+        return false;
+    if (s->d_offsets == nullptr) return s->n_sequences == 0 ? s->n_tokens == 0 : s->n_tokens % s->n_sequences == 0;
+    return (s->offset_type == MGWFBP_I32 || s->offset_type == MGWFBP_I64) && is_aligned(s->d_offsets, s->offset_type == MGWFBP_I64 ? 8 : 4);
+}
+int64_t unit_tokens(const mgwfbp_sequences& s) { return s.d_offsets != nullptr ? s.n_tokens : s.n_sequences == 0 ? 0 : s.n_tokens / s.n_sequences; }
+bool is_short(const mgwfbp_sequences& s) { return s.d_offsets == nullptr && unit_tokens(s) <= SHORT; }
+bool is_kind(int32_t k) { return k == MGWFBP_RECUR_FREE || k == MGWFBP_RECUR_CONVEX || k == MGWFBP_RECUR_UNIT; }
+bool side_ok(const void* p, int64_t tokens, int64_t channels, int64_t stride, int32_t dtype) {
+    return tokens == 0 || (p != nullptr && is_aligned(p, dtype_bytes(dtype)) && is_matrix(tokens, channels, stride, dtype_bytes(dtype)));
+}
+bool states_ok(const float* p) { return is_aligned(p, 4); }
+
+uint64_t workspace_of(const mgwfbp_sequences& s, int64_t channels, int32_t dtype) {
+    if (s.n_sequences == 0 || channels == 0 || is_short(s)) return 0;
+    const Cut c = cut_of(s.n_sequences, unit_tokens(s), channels, s.d_offsets != nullptr, dtype);
+    return c.segments == 1 ? 0 : static_cast<uint64_t>(c.units * c.segments * 2 * channels) * 4;
+}
+
+template <int K> struct Kind { static constexpr int value = K; };
+template <typename F> int with_kind(int32_t kind, F&& f) {
+    switch (kind) {
+        case MGWFBP_RECUR_FREE: return f(Kind<MGWFBP_RECUR_FREE>());
+        case MGWFBP_RECUR_CONVEX: return f(Kind<MGWFBP_RECUR_CONVEX>());
+        case MGWFBP_RECUR_UNIT: return f(Kind<MGWFBP_RECUR_UNIT>());
+        default: return MGWFBP_EINVAL;
+    }
+}
+
+template <bool BACK> int run(const mgwfbp_sequences& s, int32_t kind, int32_t dtype, RecurArgs& a, void* workspace, uint64_t workspace_bytes, void* stream) {
+    const bool packed = s.d_offsets != nullptr;
+    const int64_t channels = a.channels;
+    a.sequences = s.n_sequences;
+    a.tokens = unit_tokens(s);
+    a.offsets = s.d_offsets;
+    a.offset_type = s.offset_type;
+    if (is_short(s)) {
+        const int64_t lanes = a.sequences * ceil_div(channels, BACK ? 2 : VEC);
+        const int64_t groups = ceil_div(lanes, SHORT_THREADS);
+        if (groups >= (int64_t(1) << 31)) return MGWFBP_EINVAL;
+        return with_dtype(dtype, [&](auto* type) {
+            return with_kind(kind, [&](auto k) {
+                typedef std::remove_pointer_t<decltype(type)> T;
+                void (*kernel)(RecurArgs) = BACK ? short_back_kernel<T, decltype(k)::value> : short_scan_kernel<T, decltype(k)::value>;
+                return launch(kernel, a, dim3(static_cast<uint32_t>(groups)), dim3(SHORT_THREADS), stream);
+            });
+        });
+    }
+    const Cut cut = cut_of(a.sequences, a.tokens, channels, packed, dtype);
+    const int64_t groups = cut.units * cut.segments * cut.slabs;
+    if (groups >= (int64_t(1) << 31)) return MGWFBP_EINVAL;
+    a.blocks = cut.blocks;
+    a.slabs = static_cast<uint32_t>(cut.slabs);
+    a.segments = static_cast<uint32_t>(cut.segments);
+    a.per_segment = static_cast<uint32_t>(cut.per_segment);
+    if (cut.segments > 1) {
+        if (workspace == nullptr || !is_aligned(workspace, 256) || workspace_bytes < workspace_of(s, channels, dtype)) return MGWFBP_EINVAL;
+        a.maps = static_cast<float*>(workspace);
+        a.copied = !BACK && !packed && a.first != nullptr && a.first == a.last;
+    }
+    const dim3 grid(static_cast<uint32_t>(groups)), block(WAVES * LANES);
+    return with_dtype(dtype, [&](auto* type) {
+        return with_kind(kind, [&](auto k) {
+            typedef std::remove_pointer_t<decltype(type)> T;
+            constexpr int K = decltype(k)::value, CH = sizeof(T) == 4 ? 1 : 2;
+            if (cut.segments > 1) {
+                const int status = launch(packed ? fold_kernel<T, K, CH, true, BACK> : fold_kernel<T, K, CH, false, BACK>, a, grid, block, stream);
+                if (status != MGWFBP_OK) return status;
+            }
+            if constexpr (BACK) return launch(packed ? back_kernel<T, K, CH, true> : back_kernel<T, K, CH, false>, a, grid, block, stream);
+            else return launch(packed ? scan_kernel<T, K, CH, true> : scan_kernel<T, K, CH, false>, a, grid, block, stream);
+        });
+    });
+}
+
+}  // namespace
+
+extern "C" {
+
+int mgwfbp_recur_states(const mgwfbp_sequences* sequences, int64_t* rows_out) {
+    if (!sizes_ok(sequences, 0) || rows_out == nullptr) return MGWFBP_EINVAL;
+    *rows_out = (sequences->d_offsets != nullptr ? 1 : sequences->n_sequences) * ceil_div(unit_tokens(*sequences), BLOCK);
+    return MGWFBP_OK;
+}
+
+int mgwfbp_recur_workspace(const mgwfbp_sequences* sequences, int64_t n_channels, int32_t dtype, uint64_t* bytes_out) {
+    if (!sizes_ok(sequences, n_channels) || !is_dtype(dtype) || bytes_out == nullptr) return MGWFBP_EINVAL;
+    *bytes_out = workspace_of(*sequences, n_channels, dtype);
+    return MGWFBP_OK;
+}
+
+int mgwfbp_recur(const mgwfbp_sequences* sequences, int64_t n_channels, int32_t kind, int32_t dtype, const void* d_gate, int64_t gate_stride,
+                 const void* d_x, int64_t x_stride, const float* d_first, void* d_y, int64_t y_stride, float* d_last, float* d_states,
+                 void* d_workspace, uint64_t workspace_bytes, void* hip_stream) {
+    if (!sizes_ok(sequences, n_channels) || !is_dtype(dtype) || !is_kind(kind)) return MGWFBP_EINVAL;
+    const int64_t tokens = sequences->n_tokens;
+    if (sequences->n_sequences == 0 || n_channels == 0) return MGWFBP_OK;
+    if (!side_ok(d_gate, tokens, n_channels, gate_stride, dtype) || !side_ok(d_x, tokens, n_channels, x_stride, dtype) ||
+        !side_ok(d_y, tokens, n_channels, y_stride, dtype) || !states_ok(d_first) || !states_ok(d_last) || !states_ok(d_states) ||
+        !is_matrix(sequences->n_sequences, n_channels, n_channels, 4))
+        return MGWFBP_EINVAL;
+    if (sequences->d_offsets != nullptr && d_first != nullptr && d_first == d_last) return MGWFBP_EINVAL;
+    RecurArgs a{};
+    a.gate = d_gate;
+    a.x = d_x;
+    a.first = d_first;
+    a.y = d_y;
+    a.last = d_last;
+    a.states = d_states;
+    a.gate_stride = gate_stride;
+    a.x_stride = x_stride;
+    a.y_stride = y_stride;
+    a.channels = n_channels;
+    return run<false>(*sequences, kind, dtype, a, d_workspace, workspace_bytes, hip_stream);
+}
+
+int mgwfbp_recur_backward(const mgwfbp_sequences* sequences, int64_t n_channels, int32_t kind, int32_t dtype, const void* d_gate, int64_t gate_stride,
+                          const void* d_x, int64_t x_stride, const float* d_first, const float* d_states, const void* d_dy, int64_t dy_stride,
+                          const float* d_dlast, void* d_dgate, int64_t dgate_stride, void* d_dx, int64_t dx_stride, float* d_dfirst,
+                          void* d_workspace, uint64_t workspace_bytes, void* hip_stream) {
+    if (!sizes_ok(sequences, n_channels) || !is_dtype(dtype) || !is_kind(kind)) return MGWFBP_EINVAL;
+    const int64_t tokens = sequences->n_tokens;
+    if (sequences->n_sequences == 0 || n_channels == 0) return MGWFBP_OK;
+    if (!side_ok(d_gate, tokens, n_channels, gate_stride, dtype) || !side_ok(d_x, tokens, n_channels, x_stride, dtype) ||
+        !side_ok(d_dy, tokens, n_channels, dy_stride, dtype) || !side_ok(d_dgate, tokens, n_channels, dgate_stride, dtype) ||
+        !side_ok(d_dx, tokens, n_channels, dx_stride, dtype) || !states_ok(d_first) || !states_ok(d_states) || !states_ok(d_dlast) || !states_ok(d_dfirst) ||
+        (tokens > 0 && !is_short(*sequences) && d_states == nullptr) || !is_matrix(sequences->n_sequences, n_channels, n_channels, 4))
+        return MGWFBP_EINVAL;
+    RecurArgs a{};
+    a.gate = d_gate;
+    a.x = d_x;
+    a.dy = d_dy;
+    a.first = d_first;
+    a.dlast = d_dlast;
+    a.dgate = d_dgate;
+    a.dx = d_dx;
+    a.dfirst = d_dfirst;
+    a.states = const_cast<float*>(d_states);
+    a.gate_stride = gate_stride;
+    a.x_stride = x_stride;
+    a.dy_stride = dy_stride;
+    a.dgate_stride = dgate_stride;
+    a.dx_stride = dx_stride;
+    a.channels = n_channels;
+    return run<true>(*sequences, kind, dtype, a, d_workspace, workspace_bytes, hip_stream);
+}
+
+}  // extern "C"

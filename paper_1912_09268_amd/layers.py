@@ -1,5 +1,6 @@
-"""The operators that make per-layer gradients, on torch tensors: embedding lookup and its gradient, and activation
-checkpoints in 8 bits with what the backward pass makes of them.
+"""The operators that make per-layer gradients, on torch tensors: embedding lookup and its gradient, activation
+checkpoints in 8 bits with what the backward pass makes of them, and what lies between and behind the linear layers of a language
+model: root-mean-square norm, a gated linear recurrence over the tokens, and the loss against labels and a teacher's top logits.
 
 Arguments are checked (ValueError) and handed to the library, in native code where the extension module is there; memory and streams are torch's.  Every call runs on
 the tensors' device and on torch's current stream there, and does not wait for it.  A tensor made on another stream
@@ -16,6 +17,13 @@ taken.  Tensors that a call has written count as changed: autograd refuses to go
     layers.act_backward(kept, du, kind="gelu", dx=dz)                             # dz = du * gelu'(z)
     layers.act_linear_grad(dz, kept_input, grad_of_w, db=grad_of_b)
     layers.embed_grad(dh, ids, grad_of_word)
+
+    y, h = layers.norm(branch, weight, residual=stream, kept=kept)                # h = stream + branch, y = h / rms(h) * weight
+    layers.act_linear_grad(dz, kept.linear, grad_of_w)                            # of the linear layer that y goes into
+    layers.norm_backward(kept, dy, weight, dres=dstream, dh=dstream, dw=grad_of_weight)
+    y = layers.recur(gate, x, states=states)                                      # [sequences, length, channels]
+    dgate, dx = layers.recur_backward(gate, x, states, dy)
+    loss = layers.distill(logits, top_ids, top_logits, labels=labels, temperature=2.0, dlogits=logits)
 
 The gradients may be the very tensors that the merged-gradient calls read: `DeviceModel.grads` holds 16-bit gradients as
 raw bits, so view them, e.g. `dm.grads[w][i].view(torch.bfloat16).view(rows, dim)`."""
@@ -34,10 +42,12 @@ try:
 except ImportError:             # not built for this Python and torch: every call goes the plain way
     class _native:
         embed = embed_grad = act_store = act_backward = act_linear_grad = staticmethod(lambda *args: NotImplemented)
+        norm = norm_backward = recur = recur_backward = distill = staticmethod(lambda *args: NotImplemented)
 
 _DTYPES = {torch.float32: B.F32, torch.bfloat16: B.BF16, torch.float16: B.F16}
 _ID_TYPES = {torch.int32: B.I32, torch.int64: B.I64}
 KINDS = {"identity": B.IDENTITY, "gelu": B.GELU, "gelu_tanh": B.GELU_TANH, "silu": B.SILU}
+RECUR_KINDS = {"free": B.FREE, "convex": B.CONVEX, "unit": B.UNIT}
 
 
 class Act8(NamedTuple):
@@ -277,3 +287,263 @@ def act_linear_grad(dy: torch.Tensor, act: Act8, dw: torch.Tensor, db: Optional[
                           space.numel() * space.element_size(), stream)
     _written(dw, db)
     return dw
+
+
+class Norm8(NamedTuple):
+    """What norm keeps: `act`, the normed values before the weight in 8 bits; `rstd` float32 [tokens]; and `linear`, what the next linear layer
+    sees, values times weight: the same q with scales of its own."""
+    act: Act8
+    rstd: torch.Tensor
+    linear: Act8
+
+
+def norm_empty(tokens: int, channels: int, device="cuda") -> Norm8:
+    """Memory for what norm keeps of [tokens, channels]."""
+    act = act_empty(tokens, channels, device)
+    return Norm8(act, torch.empty(tokens, device=device), Act8(act.q, torch.empty_like(act.scale), channels))
+
+
+def _kept(kept: Norm8):
+    """Checks what norm keeps -> (tokens, ld)."""
+    act, rstd, linear = kept
+    tokens, ld = _act(act)
+    if linear.q.data_ptr() != act.q.data_ptr() or linear.channels != act.channels or _act(linear) != (tokens, ld):
+        _fail("the two checkpoints of a norm have one q")
+    _vector(rstd, "rstd", tokens, (torch.float32,))
+    return tokens, ld
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int, dtypes=_DTYPES) -> int:
+    """Checks a contiguous vector, which may be left out, and returns its address."""
+    if t is None:
+        return 0
+    if t.dtype not in dtypes or t.shape != (n,) or not t.is_contiguous():
+        _fail(f"{name} must be a contiguous tensor of {n} elements of {' or '.join(str(d) for d in dtypes)}, not {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def _code(t: Optional[torch.Tensor], of=_DTYPES) -> int:
+    return 0 if t is None else of[t.dtype]
+
+
+def _same_place(a: torch.Tensor, b: Optional[torch.Tensor]) -> bool:
+    return b is not None and a.data_ptr() == b.data_ptr()
+
+
+def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+         h: Optional[torch.Tensor] = None, kept: Optional[Norm8] = None, eps: float = 1e-6):
+    """h = x + residual and y = h / sqrt(mean(h^2) + eps) * weight over the channels of x [tokens, channels]; returns (y, h).
+
+    weight [channels] (None: 1).  residual, and h with it, are of x's type or float32; h may be residual, None makes a new tensor; without a residual
+    h is x.  y is of x's type.  `kept` (norm_empty) takes what norm_backward and the next layer's act_linear_grad need."""
+    if y is not None and (residual is None) == (h is None) and isinstance(eps, float):
+        act, rstd, linear = (None, None, None) if kept is None else kept
+        if kept is None or (linear.q is act.q and linear.channels == act.channels):
+            if _native.norm(x, weight, residual, y, h, act and act.q, act and act.scale, act and act.channels, rstd, linear and linear.scale, eps) is None:
+                return y, x if residual is None else h
+    x_stride = _matrix(x, "x", None, None)
+    tokens, channels = x.shape
+    if y is None:
+        y = torch.empty(tokens, channels, dtype=x.dtype, device=x.device)
+    if residual is None and h is not None:
+        _fail("without a residual h is x itself")
+    if residual is not None and h is None:
+        h = torch.empty(tokens, channels, dtype=residual.dtype, device=x.device)
+    memory = () if kept is None else (kept.act.q, kept.act.scale, kept.rstd, kept.linear.scale)
+    device = _device(x, weight, residual, y, h, *memory)
+    w = _vector(weight, "weight", channels)
+    y_stride = _matrix(y, "y", tokens, channels, (x.dtype,))
+    stream_type, res_stride, h_stride = x.dtype, 0, 0
+    if residual is not None:
+        stream_type = residual.dtype
+        res_stride = _matrix(residual, "residual", tokens, channels, (x.dtype, torch.float32))
+        h_stride = _matrix(h, "h", tokens, channels, (stream_type,))
+        if _same_place(h, residual) and h_stride != res_stride:
+            _fail("h over residual must have its strides")
+    ld = 0
+    if kept is not None:
+        rows, ld = _kept(kept)
+        if rows != tokens or kept.act.channels != channels:
+            _fail(f"x has shape {tuple(x.shape)}, what is kept is of {(rows, kept.act.channels)}")
+    with _on(device) as stream:
+        B.norm(x.data_ptr(), x_stride, _DTYPES[x.dtype], _address(residual), res_stride, _DTYPES[stream_type], tokens, channels, w, _code(weight), float(eps),
+               _address(h), h_stride, y.data_ptr(), y_stride, *((m.data_ptr() for m in (kept.rstd, kept.act.q, kept.act.scale, kept.linear.scale)) if kept else (0, 0, 0, 0)),
+               ld, stream)
+    _written(y, h, *memory)
+    return y, x if residual is None else h
+
+
+def norm_backward(kept: Norm8, dy: torch.Tensor, weight: Optional[torch.Tensor] = None, dres: Optional[torch.Tensor] = None,
+                  dh: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, accumulate: bool = False,
+                  workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient of norm's h, from the gradient dy [tokens, channels] of its y and what it has kept, plus `dres`, what flows into h by itself;
+    that is the gradient of x and of residual.  Where given, `dx` gets it in dy's type, too, and `dw` [channels] the weight's gradient (added to
+    what is there where `accumulate`).  dres and dh are of dy's type or float32, dh may be dres, None makes a new tensor.
+    `workspace`: device memory of layers_binding.norm_backward_workspace(tokens, channels) bytes; None takes torch's.  Returns dh."""
+    if dh is not None and kept.linear.q is kept.act.q:
+        if _native.norm_backward(kept.act.q, kept.act.scale, kept.act.channels, kept.rstd, dy, weight, dres, dh, dx, dw, accumulate, workspace) is None:
+            return dh
+    tokens, ld = _kept(kept)
+    channels = kept.act.channels
+    if dh is None:
+        dh = torch.empty(tokens, channels, dtype=dy.dtype if dres is None else dres.dtype, device=dy.device)
+    device = _device(dy, kept.act.q, kept.act.scale, kept.rstd, weight, dres, dh, dx, dw, workspace)
+    dy_stride = _matrix(dy, "dy", tokens, channels)
+    dh_stride = _matrix(dh, "dh", tokens, channels, (dy.dtype, torch.float32))
+    dres_stride = 0 if dres is None else _matrix(dres, "dres", tokens, channels, (dh.dtype,))
+    dx_stride = 0 if dx is None else _matrix(dx, "dx", tokens, channels, (dy.dtype,))
+    if _same_place(dh, dres) and dh_stride != dres_stride:
+        _fail("dh over dres must have its strides")
+    w, to = _vector(weight, "weight", channels), _vector(dw, "dw", channels)
+    with _on(device) as stream:
+        space = _workspace(workspace, B.norm_backward_workspace(tokens, channels), device)
+        B.norm_backward(kept.act.q.data_ptr(), kept.act.scale.data_ptr(), ld, kept.rstd.data_ptr(), tokens, channels, w, _code(weight), dy.data_ptr(), dy_stride,
+                        _DTYPES[dy.dtype], _address(dres), dres_stride, dh.data_ptr(), dh_stride, _DTYPES[dh.dtype], _address(dx), dx_stride, accumulate, to,
+                        _code(dw), space.data_ptr(), space.numel() * space.element_size(), stream)
+    _written(dh, dx, dw)
+    return dh
+
+
+def _sequences(t: torch.Tensor, offsets: Optional[torch.Tensor]):
+    """Checks the shape of a tensor of tokens -> (sequences, tokens, channels)."""
+    if offsets is None:
+        if t.dim() not in (2, 3):
+            _fail(f"tokens are [length, channels], or [sequences, length, channels]: not {tuple(t.shape)}")
+        count = 1 if t.dim() == 2 else t.shape[0]
+        tokens = t.shape[0] if t.dim() == 2 else t.shape[0] * t.shape[1]
+        return B.Sequences(count, tokens, 0, 0), tokens, t.shape[-1]
+    if t.dim() != 2:
+        _fail(f"tokens with offsets are [tokens, channels]: not {tuple(t.shape)}")
+    if offsets.dtype not in _ID_TYPES or offsets.dim() != 1 or offsets.numel() == 0 or not offsets.is_contiguous():
+        _fail("offsets must be a contiguous int32 or int64 tensor of one element more than there are sequences")
+    return B.Sequences(offsets.numel() - 1, t.shape[0], offsets.data_ptr(), _ID_TYPES[offsets.dtype]), t.shape[0], t.shape[1]
+
+
+def _tokens(t: torch.Tensor, name: str, like: torch.Tensor, tokens: int, channels: int):
+    """Checks a tensor of tokens of `like`'s shape and type -> (address, distance of its rows)."""
+    if t.shape != like.shape:
+        _fail(f"{name} has shape {tuple(t.shape)}, wanted {tuple(like.shape)}")
+    if t.numel() == 0:
+        if t.dtype != like.dtype:
+            _fail(f"{name} has type {t.dtype}")
+        return t.data_ptr(), channels
+    flat = _flat(t, name, tokens, channels)
+    return flat.data_ptr(), _matrix(flat, name, tokens, channels, (like.dtype,))
+
+
+def _states(t: Optional[torch.Tensor], name: str, rows: int, channels: int) -> int:
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or t.shape != (rows, channels) or not t.is_contiguous():
+        _fail(f"{name} must be a contiguous float32 tensor of shape {(rows, channels)}, not {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def _recur_kind(kind: str) -> int:
+    if kind not in RECUR_KINDS:
+        _fail(f"unknown kind {kind!r}; choose from {tuple(RECUR_KINDS)}")
+    return RECUR_KINDS[kind]
+
+
+def recur_empty(gate: torch.Tensor, offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Memory for the states that recur keeps for recur_backward: one for every 128 tokens of a sequence, or of all where there are offsets."""
+    sequences, _, channels = _sequences(gate, offsets)
+    return torch.empty(B.recur_states(sequences), channels, device=gate.device)
+
+
+def recur(gate: torch.Tensor, x: torch.Tensor, kind: str = "convex", first: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+          y: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None, states: Optional[torch.Tensor] = None,
+          workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y[t] = h[t] = a[t] * h[t-1] + c * x[t] with a = sigmoid(gate), for every channel by itself; c is 1 ("free"), 1 - a ("convex") or
+    sqrt(1 - a^2) ("unit").
+
+    gate, x and y are of one type: [length, channels], [sequences, length, channels], or with `offsets` [sequences + 1] sequences one behind the other
+    in [tokens, channels], offsets[s] .. offsets[s+1]-1 being sequence s (rows behind the last one are left as they are; a new y has zeros there).
+    h is float32: `first` [sequences, channels] goes in (None: 0) and `last`, which may be first where there are no offsets, comes out.  `states`
+    (recur_empty) takes what recur_backward needs.  `workspace`: device memory of layers_binding.recur_workspace bytes; None takes torch's."""
+    if y is not None and _native.recur(gate, x, RECUR_KINDS.get(kind), first, offsets, y, last, states, workspace) is None:
+        return y
+    sequences, tokens, channels = _sequences(gate, offsets)
+    if y is None:
+        y = (torch.empty if offsets is None else torch.zeros)(gate.shape, dtype=gate.dtype, device=gate.device)
+    device = _device(gate, x, first, offsets, y, last, states, workspace)
+    if gate.dtype not in _DTYPES:
+        _fail(f"gate has type {gate.dtype}")
+    sides = [_tokens(t, name, gate, tokens, channels) for t, name in ((gate, "gate"), (x, "x"), (y, "y"))]
+    first_at, last_at = (_states(t, name, sequences.n_sequences, channels) for t, name in ((first, "first"), (last, "last")))
+    if offsets is not None and first_at and first_at == last_at:
+        _fail("last over first takes sequences of one length")
+    states_at = _states(states, "states", B.recur_states(sequences), channels)
+    with _on(device) as stream:
+        space = _workspace(workspace, B.recur_workspace(sequences, channels, _DTYPES[gate.dtype]), device)
+        B.recur(sequences, channels, _recur_kind(kind), _DTYPES[gate.dtype], *sides[0], *sides[1], first_at, *sides[2], last_at, states_at, space.data_ptr(),
+                space.numel() * space.element_size(), stream)
+    _written(y, last, states)
+    return y
+
+
+def recur_backward(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, dy: torch.Tensor, kind: str = "convex", first: Optional[torch.Tensor] = None,
+                   offsets: Optional[torch.Tensor] = None, dlast: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                   dx: Optional[torch.Tensor] = None, dfirst: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients of recur's gate and x, and of `first` where `dfirst` is given, from those of its y and, where given, of `last`; gate, x, kind, first and offsets as
+    they were, `states` as recur has written them.  Returns (dgate, dx); rows behind the last sequence are left as they are (new tensors have zeros there)."""
+    if dgate is not None and dx is not None and _native.recur_backward(gate, x, states, dy, RECUR_KINDS.get(kind), first, offsets, dlast, dgate, dx, dfirst, workspace) is None:
+        return dgate, dx
+    sequences, tokens, channels = _sequences(gate, offsets)
+    fresh = torch.empty if offsets is None else torch.zeros
+    dgate = fresh(gate.shape, dtype=gate.dtype, device=gate.device) if dgate is None else dgate
+    dx = fresh(gate.shape, dtype=gate.dtype, device=gate.device) if dx is None else dx
+    device = _device(gate, x, states, dy, first, offsets, dlast, dgate, dx, dfirst, workspace)
+    if gate.dtype not in _DTYPES:
+        _fail(f"gate has type {gate.dtype}")
+    sides = [_tokens(t, name, gate, tokens, channels) for t, name in ((gate, "gate"), (x, "x"), (dy, "dy"), (dgate, "dgate"), (dx, "dx"))]
+    first_at, dlast_at, dfirst_at = (_states(t, name, sequences.n_sequences, channels) for t, name in ((first, "first"), (dlast, "dlast"), (dfirst, "dfirst")))
+    states_at = _states(states, "states", B.recur_states(sequences), channels)
+    with _on(device) as stream:
+        space = _workspace(workspace, B.recur_workspace(sequences, channels, _DTYPES[gate.dtype]), device)
+        B.recur_backward(sequences, channels, _recur_kind(kind), _DTYPES[gate.dtype], *sides[0], *sides[1], first_at, states_at, *sides[2], dlast_at, *sides[3],
+                         *sides[4], dfirst_at, space.data_ptr(), space.numel() * space.element_size(), stream)
+    _written(dgate, dx, dfirst)
+    return dgate, dx
+
+
+def distill(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, teacher: Optional[torch.Tensor] = None, labels: Optional[torch.Tensor] = None,
+            temperature: float = 1.0, label_weight: float = 1.0, teacher_weight: float = 1.0, row_weight: Optional[torch.Tensor] = None,
+            loss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The loss of every row of logits [tokens, vocabulary], and its gradient where `dlogits` is given (of logits' type; it may be logits):
+
+      row_weight * (label_weight * cross_entropy(logits, labels)
+                    + teacher_weight * temperature^2 * KL(p, softmax(logits / temperature))),  p = softmax(teacher / temperature)
+
+    labels [tokens] (integers, contiguous; one outside the vocabulary: none) and the teacher's top logits `teacher` [tokens, top] with their `ids`; either may be
+    left out (labels alone: cross entropy).  An id outside the vocabulary or a logit of -inf is no entry.  row_weight float32 [tokens] (None: 1).
+    Rows with weight 0, and those with neither label nor entry, have loss 0 and gradient 0 whatever is in them.  Returns `loss`, float32 [tokens]."""
+    if loss is not None and _native.distill(logits, ids, teacher, labels, temperature, label_weight, teacher_weight, row_weight, loss, dlogits) is None:
+        return loss
+    stride = _matrix(logits, "logits", None, None)
+    tokens, vocabulary = logits.shape
+    if loss is None:
+        loss = torch.empty(tokens, device=logits.device)
+    device = _device(logits, ids, teacher, labels, row_weight, loss, dlogits)
+    if vocabulary < 1 or (ids is None) != (teacher is None):
+        _fail("a vocabulary of one logit or more, and ids and teacher together")
+    top, ids_stride, teacher_stride = 0, 0, 0
+    if ids is not None:
+        ids_stride = _matrix(ids, "ids", tokens, None, _ID_TYPES)
+        top = ids.shape[1]
+        teacher_stride = _matrix(teacher, "teacher", tokens, top)
+        if top > B.MAX_TOP:
+            _fail(f"{top} entries of the teacher, at most {B.MAX_TOP}")
+    labels_at, weight_at, loss_at = (_vector(labels, "labels", tokens, _ID_TYPES), _vector(row_weight, "row_weight", tokens, (torch.float32,)),
+                                     _vector(loss, "loss", tokens, (torch.float32,)))
+    dz_stride = 0
+    if dlogits is not None:
+        dz_stride = _matrix(dlogits, "dlogits", tokens, vocabulary, (logits.dtype,))
+        if _same_place(dlogits, logits) and dz_stride != stride:
+            _fail("dlogits over logits must have its strides")
+    with _on(device) as stream:
+        B.distill(logits.data_ptr(), stride, _DTYPES[logits.dtype], tokens, vocabulary, labels_at, _code(labels, _ID_TYPES), _address(ids), ids_stride,
+                  _code(ids, _ID_TYPES), _address(teacher), teacher_stride, _code(teacher), top, temperature, label_weight, teacher_weight, weight_at, loss_at,
+                  _address(dlogits), dz_stride, stream)
+    _written(loss, dlogits)
+    return loss

@@ -14,11 +14,14 @@ I32, I64 = 0, 1                                             # mgwfbp_id_type
 IDENTITY, GELU, GELU_TANH, SILU = range(4)                  # mgwfbp_act_kind
 ACT_GROUP = 128                                             # MGWFBP_ACT_GROUP
 MAX_TABLES = 4                                              # MGWFBP_MAX_TABLES
+FREE, CONVEX, UNIT = range(3)                               # mgwfbp_recur_kind
+RECUR_BLOCK = 128                                           # MGWFBP_RECUR_BLOCK
+MAX_TOP = 1024                                              # MGWFBP_MAX_TOP
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB: Optional[C.CDLL] = None
 
-_i32, _i64, _u64, _f32, _vp = C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_void_p
+_i32, _i64, _u64, _f32, _f64, _vp = C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_double, C.c_void_p
 _i64p, _u64p = C.POINTER(C.c_int64), C.POINTER(C.c_uint64)
 
 _SIGNATURES = {
@@ -30,6 +33,15 @@ _SIGNATURES = {
     "mgwfbp_act_backward": (C.c_int, [_vp, _vp, _i64, _i64, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp]),
     "mgwfbp_act_linear_grad_workspace": (C.c_int, [_i64, _i64, _i64, _u64p]),
     "mgwfbp_act_linear_grad": (C.c_int, [_vp, _vp, _i64, _i64, _i64, _vp, _i64, _i32, _i64, _i32, _vp, _i64, _vp, _i32, _vp, _u64, _vp]),
+    "mgwfbp_norm": (C.c_int, [_vp, _i64, _i32, _vp, _i64, _i32, _i64, _i64, _vp, _i32, _f64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "mgwfbp_norm_backward_workspace": (C.c_int, [_i64, _i64, _u64p]),
+    "mgwfbp_norm_backward": (C.c_int, [_vp, _vp, _i64, _vp, _i64, _i64, _vp, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _i32, _vp, _i64, _i32, _vp, _i32, _vp, _u64,
+                                       _vp]),
+    "mgwfbp_recur_states": (C.c_int, [_vp, _i64p]),
+    "mgwfbp_recur_workspace": (C.c_int, [_vp, _i64, _i32, _u64p]),
+    "mgwfbp_recur": (C.c_int, [_vp, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _u64, _vp]),
+    "mgwfbp_recur_backward": (C.c_int, [_vp, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _u64, _vp]),
+    "mgwfbp_distill": (C.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _i32, _vp, _i64, _i32, _vp, _i64, _i32, _i32, _f32, _f32, _f32, _vp, _vp, _vp, _i64, _vp]),
     "mgwfbp_layers_last_hip_error": (C.c_int, []),
 }
 
@@ -37,6 +49,11 @@ _SIGNATURES = {
 class Table(C.Structure):
     """mgwfbp_table: one table of an embedding lookup and the rows that are taken from it."""
     _fields_ = [("d_rows", _vp), ("d_ids", _vp), ("n_rows", _i64), ("row_stride", _i64), ("scale", _f32), ("id_type", _i32)]
+
+
+class Sequences(C.Structure):
+    """mgwfbp_sequences: sequences in the rows of a matrix, of one length (d_offsets 0) or between offsets."""
+    _fields_ = [("n_sequences", _i64), ("n_tokens", _i64), ("d_offsets", _vp), ("offset_type", _i32)]
 
 
 def library_path() -> str:
@@ -135,3 +152,67 @@ def act_linear_grad(d_q: int, d_scale: int, ld: int, n_tokens: int, n_channels: 
     _check("mgwfbp_act_linear_grad", lib().mgwfbp_act_linear_grad(d_q, d_scale, ld, n_tokens, n_channels, d_dy, dy_stride, dy_dtype, n_outputs,
                                                                   bool(accumulate), d_dw, dw_stride, d_db, grad_dtype, d_workspace,
                                                                   workspace_bytes, stream))
+
+
+def norm(d_x: int, x_stride: int, dtype: int, d_residual: int, residual_stride: int, stream_dtype: int, n_tokens: int, n_channels: int, d_weight: int,
+         weight_dtype: int, eps: float, d_h: int, h_stride: int, d_y: int, y_stride: int, d_rstd: int = 0, d_q: int = 0, d_scale: int = 0,
+         d_linear_scale: int = 0, ld: int = 0, stream: int = 0) -> None:
+    """mgwfbp_norm."""
+    _check("mgwfbp_norm", lib().mgwfbp_norm(d_x, x_stride, dtype, d_residual, residual_stride, stream_dtype, n_tokens, n_channels, d_weight, weight_dtype,
+                                            eps, d_h, h_stride, d_y, y_stride, d_rstd, d_q, d_scale, d_linear_scale, ld, stream))
+
+
+@functools.lru_cache(maxsize=1024)
+def norm_backward_workspace(n_tokens: int, n_channels: int) -> int:
+    """mgwfbp_norm_backward_workspace: bytes."""
+    out = C.c_uint64()
+    _check("mgwfbp_norm_backward_workspace", lib().mgwfbp_norm_backward_workspace(n_tokens, n_channels, C.byref(out)))
+    return out.value
+
+
+def norm_backward(d_q: int, d_scale: int, ld: int, d_rstd: int, n_tokens: int, n_channels: int, d_weight: int, weight_dtype: int, d_dy: int, dy_stride: int,
+                  dtype: int, d_dresidual: int, dresidual_stride: int, d_dh: int, dh_stride: int, stream_dtype: int, d_dx: int, dx_stride: int,
+                  accumulate: bool, d_dw: int, grad_dtype: int, d_workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """mgwfbp_norm_backward."""
+    _check("mgwfbp_norm_backward", lib().mgwfbp_norm_backward(d_q, d_scale, ld, d_rstd, n_tokens, n_channels, d_weight, weight_dtype, d_dy, dy_stride, dtype,
+                                                              d_dresidual, dresidual_stride, d_dh, dh_stride, stream_dtype, d_dx, dx_stride, bool(accumulate),
+                                                              d_dw, grad_dtype, d_workspace, workspace_bytes, stream))
+
+
+def recur_states(sequences: Sequences) -> int:
+    """mgwfbp_recur_states: rows."""
+    out = C.c_int64()
+    _check("mgwfbp_recur_states", lib().mgwfbp_recur_states(C.byref(sequences), C.byref(out)))
+    return out.value
+
+
+def recur_workspace(sequences: Sequences, n_channels: int, dtype: int) -> int:
+    """mgwfbp_recur_workspace: bytes."""
+    out = C.c_uint64()
+    _check("mgwfbp_recur_workspace", lib().mgwfbp_recur_workspace(C.byref(sequences), n_channels, dtype, C.byref(out)))
+    return out.value
+
+
+def recur(sequences: Sequences, n_channels: int, kind: int, dtype: int, d_gate: int, gate_stride: int, d_x: int, x_stride: int, d_first: int, d_y: int,
+          y_stride: int, d_last: int, d_states: int, d_workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """mgwfbp_recur."""
+    _check("mgwfbp_recur", lib().mgwfbp_recur(C.byref(sequences), n_channels, kind, dtype, d_gate, gate_stride, d_x, x_stride, d_first, d_y, y_stride, d_last,
+                                              d_states, d_workspace, workspace_bytes, stream))
+
+
+def recur_backward(sequences: Sequences, n_channels: int, kind: int, dtype: int, d_gate: int, gate_stride: int, d_x: int, x_stride: int, d_first: int,
+                   d_states: int, d_dy: int, dy_stride: int, d_dlast: int, d_dgate: int, dgate_stride: int, d_dx: int, dx_stride: int, d_dfirst: int,
+                   d_workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    """mgwfbp_recur_backward."""
+    _check("mgwfbp_recur_backward", lib().mgwfbp_recur_backward(C.byref(sequences), n_channels, kind, dtype, d_gate, gate_stride, d_x, x_stride, d_first, d_states,
+                                                                d_dy, dy_stride, d_dlast, d_dgate, dgate_stride, d_dx, dx_stride, d_dfirst, d_workspace,
+                                                                workspace_bytes, stream))
+
+
+def distill(d_z: int, z_stride: int, dtype: int, n_tokens: int, n_vocabulary: int, d_labels: int, label_type: int, d_ids: int, ids_stride: int, id_type: int,
+            d_teacher: int, teacher_stride: int, teacher_dtype: int, n_top: int, temperature: float, label_weight: float, teacher_weight: float,
+            d_row_weight: int, d_loss: int, d_dz: int, dz_stride: int, stream: int = 0) -> None:
+    """mgwfbp_distill."""
+    _check("mgwfbp_distill", lib().mgwfbp_distill(d_z, z_stride, dtype, n_tokens, n_vocabulary, d_labels, label_type, d_ids, ids_stride, id_type, d_teacher,
+                                                  teacher_stride, teacher_dtype, n_top, temperature, label_weight, teacher_weight, d_row_weight, d_loss, d_dz,
+                                                  dz_stride, stream))
