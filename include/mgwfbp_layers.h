@@ -181,10 +181,11 @@ int mgwfbp_recur_backward(const mgwfbp_sequences* sequences, int64_t n_channels,
  * infinity of +inf or a NaN in the row makes both NaN; -inf is a place that is masked out.
  *   n_vocabulary 1..2^23, n_top 0..MGWFBP_MAX_TOP, temperature 2^-20..2^20, weights finite */
 #define MGWFBP_MAX_TOP 1024
+int mgwfbp_distill_workspace(int64_t n_tokens, int64_t n_vocabulary, int32_t n_top, uint64_t* bytes_out);
 int mgwfbp_distill(const void* d_z, int64_t z_stride, int32_t dtype, int64_t n_tokens, int64_t n_vocabulary, const void* d_labels, int32_t label_type,
                    const void* d_ids, int64_t ids_stride, int32_t id_type, const void* d_teacher, int64_t teacher_stride, int32_t teacher_dtype, int32_t n_top,
                    float temperature, float label_weight, float teacher_weight, const float* d_row_weight, float* d_loss, void* d_dz, int64_t dz_stride,
-                   void* hip_stream);
+                   void* d_workspace, uint64_t workspace_bytes, void* hip_stream);
 
 int mgwfbp_layers_last_hip_error(void); /* hipError_t of the last failed HIP call of these operators on this thread, 0 if none */
 

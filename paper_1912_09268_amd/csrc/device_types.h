@@ -136,10 +136,10 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Records a failed HIP call for mgwfbp_layers_last_hip_error() on this thread.
 int note(hipError_t e);
 
-// Launch of `kernel` with its one argument structure.
-template <typename A> int launch(void (*kernel)(A), const A& args, dim3 grid, dim3 block, void* stream) {
+// Launch of `kernel` with its one argument structure, and `lds` bytes of LDS beside what the kernel declares.
+template <typename A> int launch(void (*kernel)(A), const A& args, dim3 grid, dim3 block, void* stream, int lds = 0) {
     void* list[] = {const_cast<A*>(&args)};
-    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, list, 0, static_cast<hipStream_t>(stream));
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, list, static_cast<size_t>(lds), static_cast<hipStream_t>(stream));
     if (e != hipSuccess) (void)hipGetLastError();        // reported here, not to whoever asks next
     return note(e);
 }

@@ -23,6 +23,8 @@ namespace {
 
 using namespace ops;
 
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr float LOG2_E = 1.44269504088896341f;
 constexpr int MOST_TOP = MGWFBP_MAX_TOP;
 
@@ -34,7 +36,9 @@ struct DistillArgs {
     const void* teacher;
     const float* row_weight;
     float* loss;
-    int64_t z_stride, dz_stride, ids_stride, teacher_stride;
+    float* stats;                        // [tokens][parts][3]: of a row's part, its largest value and its sums of exp z and exp z / tau
+    float* kept_z;                       // [tokens][kept_stride]: z of the teacher's entries and of the label
+    int64_t z_stride, dz_stride, ids_stride, teacher_stride, kept_stride, parts;
     int64_t tokens, vocabulary;
     float label_weight, teacher_weight, tau, over_tau;
     int32_t top, label_type, id_type, teacher_type;
@@ -51,213 +55,598 @@ __device__ __forceinline__ int32_t id_at(const void* p, int32_t type, int64_t i,
     return id >= 0 && id < vocabulary ? static_cast<int32_t>(id) : -1;
 }
 
-template <int THREADS> __device__ __forceinline__ float workgroup_max(float x, float* room) {
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) x = __builtin_fmaxf(x, __shfl_xor(x, d));
-    if constexpr (THREADS == 64) return x;
-    if (threadIdx.x % 64 == 0) room[threadIdx.x / 64] = x;
-    __syncthreads();
-    x = room[0];
-#pragma unroll
-    for (int w = 1; w < THREADS / 64; ++w) x = __builtin_fmaxf(x, room[w]);
-    return x;
-}
-template <int THREADS, int N> __device__ __forceinline__ void workgroup_sums(float (&x)[N], float (*room)[N]) {
+// Over the lanes of a workgroup, in every lane: the largest of each of N numbers, or the sum.  `room` is used once.
+template <int THREADS, int N, typename F> __device__ __forceinline__ void workgroup_all(float (&x)[N], float (*room)[N], F&& join) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int d = 32; d > 0; d /= 2) x[i] += __shfl_xor(x[i], d);
-    if constexpr (THREADS == 64) return;
-    if (threadIdx.x % 64 == 0)
+        for (int d = 32; d > 0; d /= 2) x[i] = join(x[i], __shfl_xor(x[i], d));
+    if constexpr (THREADS > 64) {
+        if (threadIdx.x % 64 == 0)
 #pragma unroll
-        for (int i = 0; i < N; ++i) room[threadIdx.x / 64][i] = x[i];
-    __syncthreads();
+            for (int i = 0; i < N; ++i) room[threadIdx.x / 64][i] = x[i];
+        __syncthreads();
+        // sixteen lanes take a wavefront's each
+        constexpr int WAVES = THREADS / 64;
+        const int w = threadIdx.x % WAVES;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        x[i] = room[0][i];
+        for (int i = 0; i < N; ++i) {
+            x[i] = room[w][i];
 #pragma unroll
-        for (int w = 1; w < THREADS / 64; ++w) x[i] += room[w][i];
+            for (int d = WAVES / 2; d > 0; d /= 2) x[i] = join(x[i], __shfl_xor(x[i], d));
+        }
     }
 }
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log_of(float x) { return __builtin_logf(x); }
 
-// V vectors of eight elements a lane hold a row; V = 0: they do not.
-template <typename T, int THREADS, int V> __global__ __launch_bounds__(THREADS) void distill_kernel(DistillArgs A) {
-    __shared__ int32_t at_id[MOST_TOP + 1];                  // the teacher's entries and, behind them, the label
-    __shared__ float at_z[MOST_TOP + 1], at_p[MOST_TOP + 1];
-    __shared__ float room_max[2][THREADS / 64], room_sum[THREADS / 64][4];
+// The label's place behind the teacher's entries: the next multiple of four.
+__host__ __device__ constexpr int label_place(int top) { return (top + 3) / 4 * 4; }
+
+// The teacher's entries of a row and its label in LDS, as much as there are.  Entry j belongs to lane j % THREADS from beginning to end.
+template <int THREADS> struct Entries {
+    int32_t* id;                                             // -1: none
+    float* p;                                                // the teacher's logit, and exp of it later
+    float* z;
+    uint8_t* again;                                          // another entry has the same index
+    static __host__ __device__ constexpr int bytes(int top) { return (label_place(top) + 4) * (3 * 4 + 1); }
+    __device__ __forceinline__ explicit Entries(int top) {
+        extern __shared__ __attribute__((aligned(16))) int32_t memory[];
+        const int room = label_place(top) + 4;               // so that all begin on 16 bytes
+        id = memory;
+        p = reinterpret_cast<float*>(memory + room);
+        z = p + room;
+        again = reinterpret_cast<uint8_t*>(z + room);
+    }
+    // One lane: the places between the entries and the label, and the label.
+    __device__ __forceinline__ void close(int top, int32_t label) {
+        const int end = label_place(top);
+        for (int j = top; j < end; ++j) id[j] = -1;
+        id[end] = label;
+        p[end] = 0.f;
+    }
+    // After a barrier: whether an entry's index is another one's, too.  Nearly none is.
+    __device__ __forceinline__ void find_again(int top) {
+        const int end = label_place(top);
+        for (int j = threadIdx.x; j <= end; j += THREADS) {
+            const int32_t mine = id[j];
+            int same = j == end;
+            if (mine >= 0) {
+#pragma unroll 4
+                for (int i = 0; i < end; i += 4) {
+                    const i32x4 four = *reinterpret_cast<const i32x4*>(id + i);
+                    same += (four[0] == mine) + (four[1] == mine) + (four[2] == mine) + (four[3] == mine);
+                }
+            }
+            again[j] = same > 1;
+        }
+    }
+    // What all entries of one's index have together, in their order.
+    __device__ __forceinline__ float together(int j, int top) const {
+        if (!again[j]) return p[j];
+        const int32_t mine = id[j];
+        float sum = 0.f;
+        for (int i = 0; i < top; i += 4) {
+            const i32x4 four = *reinterpret_cast<const i32x4*>(id + i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (four[k] == mine) sum += p[i + k];
+        }
+        return sum;
+    }
+};
+
+// What is asked of a row, and its softmaxes: one or two of them; where tau is 1 or only one part is asked for, one, with both weights.
+struct Asked {
+    float weight, c, ct;
+    int32_t label;
+    bool taught, both;
+    __device__ __forceinline__ void settle(const DistillArgs& A, bool taught_) {
+        taught = taught_;
+        both = label >= 0 && taught && A.tau != 1.f;
+        c = label >= 0 || A.tau == 1.f ? LOG2_E : LOG2_E * A.over_tau;
+        ct = LOG2_E * A.over_tau;
+    }
+};
+
+// sums: of exp z, exp z / tau, the teacher's exp and its terms -> the loss
+__device__ __forceinline__ float loss_of(const DistillArgs& A, const Asked& row, const float (&sums)[4], float below) {
+    float loss = 0.f;
+    if (row.label >= 0) loss = A.label_weight * (log_of(sums[0]) + below);
+    if (row.taught) loss += A.teacher_weight * A.tau * A.tau * (sums[3] / sums[2] - log_of(sums[2]) + log_of(sums[1]));
+    return row.weight * loss;
+}
+
+// The gradient of a logit, but for the label and the teacher's entries.
+struct Slope {
+    float high, c, ct, f, ft, by_label, per_entry;
+    bool both;
+    __device__ __forceinline__ Slope(const DistillArgs& A, const Asked& row, const float (&sums)[4], float high_) : high(high_), c(row.c), ct(row.ct), both(row.both) {
+        by_label = row.label >= 0 ? row.weight * A.label_weight : 0.f;
+        const float by_teacher = row.taught ? row.weight * A.teacher_weight * A.tau : 0.f;
+        f = (both ? by_label : by_label + by_teacher) / sums[0];
+        ft = both ? by_teacher / sums[1] : 0.f;
+        per_entry = row.taught ? by_teacher / sums[2] : 0.f;
+    }
+    __device__ __forceinline__ float operator()(float value) const {
+        const float d = value - high;
+        const float g = exp2_of(d * c) * f;
+        return both ? __builtin_fmaf(exp2_of(d * ct), ft, g) : g;
+    }
+    template <typename T> __device__ __forceinline__ void of(const Raw8<T>& r, float (&g)[VEC]) const {
+        if (both) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float d = get(r, i) - high;
+                g[i] = __builtin_fmaf(exp2_of(d * ct), ft, exp2_of(d * c) * f);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) g[i] = exp2_of((get(r, i) - high) * c) * f;
+        }
+    }
+};
+
+// exp of the teacher's entries and their terms, a lane's own ones.
+template <int THREADS> __device__ __forceinline__ void teach(const DistillArgs& A, Entries<THREADS>& at, int top, float best, float high, float& sum, float& terms) {
+    for (int j = threadIdx.x; j < top; j += THREADS) {
+        if (at.id[j] < 0) {
+            at.p[j] = 0.f;
+            continue;
+        }
+        const float d = (at.p[j] - best) * A.over_tau, e = exp2_of(d * LOG2_E);
+        at.p[j] = e;
+        sum += e;
+        if (!(e == 0.f)) terms += e * (d - (at.z[j] - high) * A.over_tau);
+    }
+}
+
+// The elements i, from <= i < VEC, of eight.
+template <typename T> __device__ __forceinline__ void add(const Raw8<T>& r, int from, float high, const Asked& row, float (&sums)[4]) {
+    if (row.both) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (i >= from) {
+                const float d = get(r, i) - high;
+                sums[0] += exp2_of(d * row.c);
+                sums[1] += exp2_of(d * row.ct);
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (i >= from) sums[0] += exp2_of((get(r, i) - high) * row.c);
+    }
+}
+
+constexpr int AHEAD = 4;                 // vectors of a lane on their way where a row does not stay in registers
+
+// V vectors of eight elements a lane hold a row of eight elements or more; V = 0: they do not.
+//
+// The last vector of a row that is no multiple of eight begins before its place, so that it ends with the row; lanes behind it take it, too.
+// What they have in common with the lane before is neither summed twice nor, being the same, wrong where it is written twice.
+template <typename T, int THREADS, int V, int PER_SIMD> __global__ __launch_bounds__(THREADS, PER_SIMD) void distill_kernel(DistillArgs A) {
+    __shared__ float room[THREADS / 64][3], room_sums[THREADS / 64][4];
+    Entries<THREADS> at(A.top);
     const int64_t t = blockIdx.x;
     const T* const z = static_cast<const T*>(A.z) + t * A.z_stride;
     T* const dz = static_cast<T*>(A.dz) + t * A.dz_stride;
-    const int64_t first = static_cast<int64_t>(threadIdx.x) * VEC;
-    constexpr int64_t STEP = THREADS * VEC;
-    auto left = [&](int64_t col) { return static_cast<int>(max(static_cast<int64_t>(0), min(A.vocabulary - col, static_cast<int64_t>(VEC)))); };
+    const uint32_t vocabulary = static_cast<uint32_t>(A.vocabulary), first = threadIdx.x * VEC, last = vocabulary - VEC;
+    constexpr uint32_t STEP = THREADS * VEC;
+    constexpr int HELD = V > 0 ? V : AHEAD;
 
-    const float weight = A.row_weight == nullptr ? 1.f : A.row_weight[t];
-    const int32_t label = A.labels == nullptr || A.label_weight == 0.f ? -1 : id_at(A.labels, A.label_type, t, A.vocabulary);
-    const int top = A.teacher_weight == 0.f || weight == 0.f ? 0 : A.top;
-    Raw8<T> x[V > 0 ? V : 1];
-    if constexpr (V > 0) {
+    Asked row;
+    row.weight = A.row_weight == nullptr ? 1.f : A.row_weight[t];
+    row.label = A.labels == nullptr || A.label_weight == 0.f ? -1 : id_at(A.labels, A.label_type, t, A.vocabulary);
+    const int top = A.teacher_weight == 0.f || row.weight == 0.f ? 0 : A.top;
+    // a lane's first entry is asked for before the row and its z behind it, so that neither waits
+    const float LEAST = -__builtin_inff();
+    const bool entry = static_cast<int>(threadIdx.x) < top;
+    int32_t id = -1;
+    float s = LEAST;
+    if (entry) {
+        id = id_at(A.ids, A.id_type, t * A.ids_stride + threadIdx.x, A.vocabulary);
+        s = number_at(A.teacher, A.teacher_type, t * A.teacher_stride + threadIdx.x);
+    }
+    Raw8<T> x[HELD];
+    if (row.weight != 0.f) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = load8(z + first + v * STEP, weight != 0.f ? left(first + v * STEP) : 0);
+        for (int v = 0; v < HELD; ++v) x[v] = load8(z + min(first + v * STEP, last));
     }
-    // the teacher's entries: an index outside and a logit of -inf are no entry
-    float best = -__builtin_inff();
-    for (int j = threadIdx.x; j < top; j += THREADS) {
-        int32_t id = id_at(A.ids, A.id_type, t * A.ids_stride + j, A.vocabulary);
-        const float s = number_at(A.teacher, A.teacher_type, t * A.teacher_stride + j);
-        if (s == -__builtin_inff()) id = -1;
-        at_id[j] = id;
-        at_p[j] = s;
-        at_z[j] = id >= 0 ? static_cast<float>(z[id]) : 0.f;
-        if (id >= 0) best = __builtin_fmaxf(best, s);       // a NaN is no maximum, but the sums have it
+    float most[3] = {LEAST, LEAST, 0.f};                     // of the row, of the teacher's entries, and whether there are any
+    auto enter = [&](int j, int32_t id, float s) {           // an index outside and a logit of -inf are no entry
+        at.id[j] = id;
+        at.p[j] = s;
+        if (id >= 0) {
+            most[1] = __builtin_fmaxf(most[1], s);           // a NaN is no maximum, but the sums have it
+            most[2] = 1.f;
+        }
+    };
+    if (s == LEAST) id = -1;
+    float z_entry = 0.f;
+    if (entry) {
+        enter(threadIdx.x, id, s);
+        if (id >= 0) z_entry = static_cast<float>(z[id]);
     }
-    if (threadIdx.x == 0) {
-        at_id[top] = label;
-        at_z[top] = label >= 0 ? static_cast<float>(z[label]) : 0.f;
-        at_p[top] = 0.f;
+    for (int j = threadIdx.x + THREADS; j < top; j += THREADS) {
+        int32_t more = id_at(A.ids, A.id_type, t * A.ids_stride + j, A.vocabulary);
+        const float logit = number_at(A.teacher, A.teacher_type, t * A.teacher_stride + j);
+        if (logit == LEAST) more = -1;
+        enter(j, more, logit);
+        at.z[j] = more >= 0 ? static_cast<float>(z[more]) : 0.f;
     }
-    bool some = false;
-    for (int j = threadIdx.x; j < top; j += THREADS) some |= at_id[j] >= 0;
-    const bool taught = __syncthreads_or(some);
-    if (weight == 0.f || (label < 0 && !taught)) {           // nothing is asked of this row
+    float z_label = 0.f;
+    const int place_of_label = label_place(top);
+    const bool labelled = static_cast<int>(threadIdx.x) == place_of_label % THREADS;         // the lane of the label's place
+    if (labelled) at.close(top, row.label);
+    if (labelled && row.label >= 0) z_label = static_cast<float>(z[row.label]);
+    if constexpr (V > 0) {
+        if (row.weight != 0.f) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) most[0] = __builtin_fmaxf(most[0], get(x[v], i));
+        }
+    }
+    workgroup_all<THREADS>(most, room, [](float a, float b) { return __builtin_fmaxf(a, b); });
+    row.settle(A, most[2] != 0.f);
+    if (row.weight == 0.f || (row.label < 0 && !row.taught)) {                  // nothing is asked of this row
         if (threadIdx.x == 0) A.loss[t] = 0.f;
         if (A.dz != nullptr) {
             const float zero[VEC] = {};
-            for (int64_t col = first; col < A.vocabulary; col += STEP) store8(dz + col, zero, left(col));
+            for (uint32_t col = first; col < vocabulary; col += STEP) store8(dz + min(col, last), zero);
         }
         return;
     }
-    best = workgroup_max<THREADS>(best, room_max[0]);
-
-    // One softmax or two: where tau is 1 or only one part is asked for, one of them, with both weights.
-    const bool both = label >= 0 && taught && A.tau != 1.f;
-    const float c = label >= 0 || A.tau == 1.f ? LOG2_E : LOG2_E * A.over_tau, ct = LOG2_E * A.over_tau;
-    float most = -__builtin_inff();
-    float sums[4] = {};                                      // of exp z, exp z / tau, the teacher's exp, and its terms
-    auto add = [&](const Raw8<T>& r, int n, float from) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i)
-            if (i < n) {
-                const float d = get(r, i) - from;
-                sums[0] += exp2_of(d * c);
-                if (both) sums[1] += exp2_of(d * ct);
-            }
-    };
+    if (entry) at.z[threadIdx.x] = z_entry;
+    if (labelled) at.z[place_of_label] = z_label;
+    at.find_again(top);
+    float high = most[0], sums[4] = {};
     if constexpr (V > 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                if (i < left(first + v * STEP)) most = __builtin_fmaxf(most, get(x[v], i));
-        most = workgroup_max<THREADS>(most, room_max[1]);
-#pragma unroll
-        for (int v = 0; v < V; ++v) add(x[v], left(first + v * STEP), most);
+        for (int v = 0; v < V; ++v) {
+            const uint32_t col = first + v * STEP;
+            if (col <= last) add(x[v], 0, high, row, sums);
+            else if (col < vocabulary) add(x[v], static_cast<int>(col - last), high, row, sums);
+        }
     } else {
-        for (int64_t col = first; col < A.vocabulary; col += STEP) {
-            const int n = left(col);
-            const Raw8<T> r = load8(z + col, n);
-            float higher = most;
+        float mine = LEAST;
+        for (uint32_t base = first; base < vocabulary; base += AHEAD * STEP) {
+            Raw8<T> now[AHEAD];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                if (i < n) higher = __builtin_fmaxf(higher, get(r, i));
-            const float from = higher == -__builtin_inff() ? 0.f : higher;       // nothing but -inf so far: they add 0
-            if (higher != most) {
-                sums[0] *= exp2_of((most - from) * c);
-                sums[1] *= exp2_of((most - from) * ct);
-                most = higher;
+            for (int v = 0; v < AHEAD; ++v) now[v] = x[v];
+#pragma unroll
+            for (int v = 0; v < AHEAD; ++v) x[v] = load8(z + min(base + (AHEAD + v) * STEP, last));
+            float higher = mine;                             // a vector taken twice does no harm here
+#pragma unroll
+            for (int v = 0; v < AHEAD; ++v)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) higher = __builtin_fmaxf(higher, get(now[v], i));
+            const float origin = higher == LEAST ? 0.f : higher;                 // nothing but -inf so far: they add 0
+            if (higher != mine) {
+                sums[0] *= exp2_of((mine - origin) * row.c);
+                sums[1] *= exp2_of((mine - origin) * row.ct);
+                mine = higher;
             }
-            add(r, n, from);
+#pragma unroll
+            for (int v = 0; v < AHEAD; ++v) {
+                const uint32_t col = base + v * STEP;
+                if (col <= last) add(now[v], 0, origin, row, sums);
+                else if (col < vocabulary) add(now[v], static_cast<int>(col - last), origin, row, sums);
+            }
         }
-        const float mine = most;
-        most = workgroup_max<THREADS>(most, room_max[1]);
-        if (mine != most) {
-            const float d = mine - most;
-            sums[0] *= exp2_of(d * c);
-            sums[1] *= exp2_of(d * ct);
+        float all[1] = {mine};
+        __shared__ float room_high[THREADS / 64][1];
+        workgroup_all<THREADS>(all, room_high, [](float a, float b) { return __builtin_fmaxf(a, b); });
+        high = all[0];
+        if (mine != high) {
+            sums[0] *= exp2_of((mine - high) * row.c);
+            sums[1] *= exp2_of((mine - high) * row.ct);
         }
     }
-    for (int j = threadIdx.x; j < top; j += THREADS) {       // a lane's own entries
-        if (at_id[j] < 0) {
-            at_p[j] = 0.f;
-            continue;
-        }
-        const float d = (at_p[j] - best) * A.over_tau, e = exp2_of(d * LOG2_E);
-        at_p[j] = e;
-        sums[2] += e;
-        if (!(e == 0.f)) sums[3] += e * (d - (at_z[j] - most) * A.over_tau);
-    }
-    workgroup_sums<THREADS>(sums, room_sum);
-    if (!both) sums[1] = sums[0];
-    if (threadIdx.x == 0) {
-        float loss = 0.f;
-        if (label >= 0) loss = A.label_weight * (log_of(sums[0]) - (at_z[top] - most));
-        if (taught) loss += A.teacher_weight * A.tau * A.tau * (sums[3] / sums[2] - log_of(sums[2]) + log_of(sums[1]));
-        A.loss[t] = weight * loss;
-    }
+    teach(A, at, top, most[1], high, sums[2], sums[3]);
+    workgroup_all<THREADS>(sums, room_sums, [](float a, float b) { return a + b; });
+    if (!row.both) sums[1] = sums[0];
+    if (labelled) A.loss[t] = loss_of(A, row, sums, high - at.z[place_of_label]);
     if (A.dz == nullptr) return;
-    const float by_label = label >= 0 ? weight * A.label_weight : 0.f, by_teacher = taught ? weight * A.teacher_weight * A.tau : 0.f;
-    const float f = (both ? by_label : by_label + by_teacher) / sums[0], ft = both ? by_teacher / sums[1] : 0.f;
-    auto slope = [&](float value) {
-        const float d = value - most;
-        float g = exp2_of(d * c) * f;
-        if (both) g = __builtin_fmaf(exp2_of(d * ct), ft, g);
-        return g;
-    };
-    auto put = [&](const Raw8<T>& r, int64_t col) {
-        float g[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) g[i] = slope(get(r, i));
-        store8(dz + col, g, left(col));
-    };
+    const Slope slope(A, row, sums, high);
+    float g[VEC];
     if constexpr (V > 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (first + v * STEP < A.vocabulary) put(x[v], first + v * STEP);
+            if (first + v * STEP < vocabulary) {
+                slope.of(x[v], g);
+                store8(dz + min(first + v * STEP, last), g);
+            }
     } else {
-        for (int64_t col = first; col < A.vocabulary; col += STEP) put(load8(z + col, left(col)), col);
+        // From behind: what was read last is nearest.  dz may be z: a lane's vectors are on their way before it writes those ahead of them, and
+        // what two lanes have in common is written by the first of them alone.
+        const uint32_t turns = (vocabulary + AHEAD * STEP - 1) / (AHEAD * STEP);
+#pragma unroll
+        for (int v = 0; v < AHEAD; ++v) x[v] = load8(z + min(first + ((turns - 1) * AHEAD + v) * STEP, last));
+        for (uint32_t turn = turns; turn-- > 0;) {
+            Raw8<T> now[AHEAD];
+#pragma unroll
+            for (int v = 0; v < AHEAD; ++v) now[v] = x[v];
+            if (turn > 0) {
+#pragma unroll
+                for (int v = 0; v < AHEAD; ++v) x[v] = load8(z + min(first + ((turn - 1) * AHEAD + v) * STEP, last));
+            }
+#pragma unroll
+            for (int v = 0; v < AHEAD; ++v) {
+                const uint32_t col = first + (turn * AHEAD + v) * STEP;
+                if (col >= vocabulary) continue;
+                slope.of(now[v], g);
+                if (col <= last) {
+                    store8(dz + col, g);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i)
+                        if (i >= static_cast<int>(col - last)) dz[last + i] = rounded<T>(g[i]);
+                }
+            }
+        }
     }
     __syncthreads();                                         // the places of entries are written again
-    const float per_entry = by_teacher / sums[2];
-    for (int j = threadIdx.x; j <= top; j += THREADS) {
-        const int32_t id = at_id[j];
-        if (id < 0) continue;
-        float p = 0.f;
-        for (int i = 0; i < top; ++i) p += at_id[i] == id ? at_p[i] : 0.f;
-        float g = slope(at_z[j]);
-        if (taught) g -= per_entry * p;
-        if (id == label) g -= by_label;
-        dz[id] = rounded<T>(g);
+    for (int j = threadIdx.x; j <= place_of_label; j += THREADS) {
+        const int32_t place = at.id[j];
+        if (place >= 0) dz[place] = rounded<T>(slope(at.z[j]) - slope.per_entry * at.together(j, top) - (place == row.label ? slope.by_label : 0.f));
     }
+}
+
+constexpr int64_t FEW_ROWS = 192, FEW_ROWS_LOGITS = 16384;
+
+// Few rows: each in parts of 256 lanes times V vectors.  First every part's largest value and sums, and the z of the row's entries, since dz may
+// be z ...
+constexpr int PART = 256;
+template <typename T, int V> __global__ __launch_bounds__(PART) void part_kernel(DistillArgs A) {
+    __shared__ float room[PART / 64][1], room_sums[PART / 64][2];
+    const int64_t t = blockIdx.y;
+    const T* const z = static_cast<const T*>(A.z) + t * A.z_stride;
+    const uint32_t vocabulary = static_cast<uint32_t>(A.vocabulary), last = vocabulary - VEC, first = blockIdx.x * (PART * VEC * V) + threadIdx.x * VEC;
+    Raw8<T> x[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[v] = load8(z + min(first + v * (PART * VEC), last));
+    if (blockIdx.x == 0) {
+        float* const kept = A.kept_z + t * A.kept_stride;
+        for (int j = threadIdx.x; j < A.top; j += PART) {
+            const int32_t id = id_at(A.ids, A.id_type, t * A.ids_stride + j, A.vocabulary);
+            kept[j] = id >= 0 ? static_cast<float>(z[id]) : 0.f;
+        }
+        if (threadIdx.x == 0 && A.labels != nullptr) {
+            const int32_t label = id_at(A.labels, A.label_type, t, A.vocabulary);
+            kept[label_place(A.top)] = label >= 0 ? static_cast<float>(z[label]) : 0.f;
+        }
+    }
+    float high[1] = {-__builtin_inff()}, sums[2] = {};
+    // lanes behind the row take its last vector, which may be another part's, too: an origin that is larger than need be does no harm
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) high[0] = __builtin_fmaxf(high[0], get(x[v], i));
+    workgroup_all<PART>(high, room, [](float a, float b) { return __builtin_fmaxf(a, b); });
+    const float origin = high[0] == -__builtin_inff() ? 0.f : high[0], c = LOG2_E, ct = LOG2_E * A.over_tau;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const uint32_t col = first + v * (PART * VEC);
+        const int from = col <= last ? 0 : col < vocabulary ? static_cast<int>(col - last) : VEC;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (i >= from) {
+                const float d = get(x[v], i) - origin;
+                sums[0] += exp2_of(d * c);
+                if (A.tau != 1.f) sums[1] += exp2_of(d * ct);
+            }
+    }
+    workgroup_all<PART>(sums, room_sums, [](float a, float b) { return a + b; });
+    if (threadIdx.x == 0) {
+        float* const to = A.stats + (t * gridDim.x + blockIdx.x) * 3;
+        to[0] = high[0];
+        to[1] = sums[0];
+        to[2] = A.tau != 1.f ? sums[1] : sums[0];
+    }
+}
+
+// ... then the row's, from all parts', and the gradient.
+template <typename T, int V> __global__ __launch_bounds__(PART) void part_slope_kernel(DistillArgs A) {
+    __shared__ float room[PART / 64][3], room_sums[PART / 64][4];
+    Entries<PART> at(A.top);
+    const int64_t t = blockIdx.y;
+    const T* const z = static_cast<const T*>(A.z) + t * A.z_stride;
+    T* const dz = static_cast<T*>(A.dz) + t * A.dz_stride;
+    const uint32_t vocabulary = static_cast<uint32_t>(A.vocabulary), last = vocabulary - VEC, begin = blockIdx.x * (PART * VEC * V), first = begin + threadIdx.x * VEC;
+    Asked row;
+    row.weight = A.row_weight == nullptr ? 1.f : A.row_weight[t];
+    row.label = A.labels == nullptr || A.label_weight == 0.f ? -1 : id_at(A.labels, A.label_type, t, A.vocabulary);
+    const int top = A.teacher_weight == 0.f || row.weight == 0.f ? 0 : A.top, place_of_label = label_place(top);
+    const float LEAST = -__builtin_inff();
+    const float *const kept = A.kept_z + t * A.kept_stride, *const stats = A.stats + t * A.parts * 3;
+    Raw8<T> x[V];
+    if (A.dz != nullptr && row.weight != 0.f) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = load8(z + min(first + v * (PART * VEC), last));
+    }
+    float most[3] = {LEAST, LEAST, 0.f};
+    for (int j = threadIdx.x; j < top; j += PART) {
+        int32_t id = id_at(A.ids, A.id_type, t * A.ids_stride + j, A.vocabulary);
+        const float s = number_at(A.teacher, A.teacher_type, t * A.teacher_stride + j);
+        if (s == LEAST) id = -1;
+        at.id[j] = id;
+        at.p[j] = s;
+        at.z[j] = kept[j];
+        if (id >= 0) {
+            most[1] = __builtin_fmaxf(most[1], s);
+            most[2] = 1.f;
+        }
+    }
+    if (static_cast<int>(threadIdx.x) == place_of_label % PART) {
+        at.close(top, row.label);
+        at.z[place_of_label] = row.label >= 0 ? kept[label_place(A.top)] : 0.f;
+    }
+    for (int p = threadIdx.x; p < A.parts; p += PART) most[0] = __builtin_fmaxf(most[0], stats[p * 3]);
+    workgroup_all<PART>(most, room, [](float a, float b) { return __builtin_fmaxf(a, b); });
+    row.settle(A, most[2] != 0.f);
+    float g[VEC] = {};
+    if (row.weight == 0.f || (row.label < 0 && !row.taught)) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) A.loss[t] = 0.f;
+        if (A.dz != nullptr) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (first + v * (PART * VEC) < vocabulary) store8(dz + min(first + v * (PART * VEC), last), g);
+        }
+        return;
+    }
+    at.find_again(top);
+    const float high = most[0];
+    float sums[4] = {};
+    for (int p = threadIdx.x; p < A.parts; p += PART) {
+        const float d = stats[p * 3] - high;
+        if (row.label >= 0 || A.tau == 1.f) sums[0] += stats[p * 3 + 1] * exp2_of(d * LOG2_E);
+        else sums[0] += stats[p * 3 + 2] * exp2_of(d * row.ct);
+        sums[1] += stats[p * 3 + 2] * exp2_of(d * row.ct);
+    }
+    teach(A, at, top, most[1], high, sums[2], sums[3]);
+    workgroup_all<PART>(sums, room_sums, [](float a, float b) { return a + b; });
+    if (!row.both) sums[1] = sums[0];
+    if (blockIdx.x == 0 && static_cast<int>(threadIdx.x) == place_of_label % PART) A.loss[t] = loss_of(A, row, sums, high - at.z[place_of_label]);
+    if (A.dz == nullptr) return;
+    const Slope slope(A, row, sums, high);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const uint32_t col = first + v * (PART * VEC);
+        if (col >= vocabulary) continue;
+        slope.of(x[v], g);
+        if (col <= last) {
+            store8(dz + col, g);
+        } else {                                             // dz may be z, and what lies before is another part's
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (i >= static_cast<int>(col - last)) dz[last + i] = rounded<T>(g[i]);
+        }
+    }
+    __syncthreads();
+    const uint32_t end = begin + PART * VEC * V;
+    for (int j = threadIdx.x; j <= place_of_label; j += PART) {
+        const int32_t place = at.id[j];
+        if (place >= 0 && static_cast<uint32_t>(place) >= begin && static_cast<uint32_t>(place) < end)
+            dz[place] = rounded<T>(slope(at.z[j]) - slope.per_entry * at.together(j, top) - (place == row.label ? slope.by_label : 0.f));
+    }
+}
+
+// Vocabularies of fewer than eight logits: a lane for a row.
+template <typename T> __global__ __launch_bounds__(64) void tiny_kernel(DistillArgs A) {
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x;
+    if (t >= A.tokens) return;
+    const T* const z = static_cast<const T*>(A.z) + t * A.z_stride;
+    T* const dz = static_cast<T*>(A.dz) + t * A.dz_stride;
+    const int vocabulary = static_cast<int>(A.vocabulary);
+    Asked row;
+    row.weight = A.row_weight == nullptr ? 1.f : A.row_weight[t];
+    row.label = A.labels == nullptr || A.label_weight == 0.f ? -1 : id_at(A.labels, A.label_type, t, A.vocabulary);
+    const int top = A.teacher_weight == 0.f || row.weight == 0.f ? 0 : A.top;
+    const float LEAST = -__builtin_inff();
+    auto entry = [&](int j, float& s) {
+        const int32_t id = id_at(A.ids, A.id_type, t * A.ids_stride + j, A.vocabulary);
+        s = number_at(A.teacher, A.teacher_type, t * A.teacher_stride + j);
+        return s == LEAST ? -1 : id;
+    };
+    float best = LEAST, high = LEAST, s, value[VEC] = {}, share[VEC] = {}, sums[4] = {}, g[VEC] = {};
+    bool taught = false;
+    for (int j = 0; j < top; ++j)
+        if (entry(j, s) >= 0) {
+            taught = true;
+            best = __builtin_fmaxf(best, s);
+        }
+    row.settle(A, taught);
+    const bool asked = row.weight != 0.f && (row.label >= 0 || taught);
+    A.loss[t] = 0.f;
+    if (asked) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (i < vocabulary) {
+                value[i] = static_cast<float>(z[i]);
+                high = __builtin_fmaxf(high, value[i]);
+            }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (i < vocabulary) {
+                sums[0] += exp2_of((value[i] - high) * row.c);
+                sums[1] += exp2_of((value[i] - high) * row.ct);
+            }
+        for (int j = 0; j < top; ++j) {
+            const int32_t id = entry(j, s);
+            if (id < 0) continue;
+            const float d = (s - best) * A.over_tau, e = exp2_of(d * LOG2_E);
+            sums[2] += e;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (i == id) {
+                    share[i] += e;
+                    if (!(e == 0.f)) sums[3] += e * (d - (value[i] - high) * A.over_tau);
+                }
+        }
+        if (!row.both) sums[1] = sums[0];
+        float below = 0.f;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (i == row.label) below = high - value[i];
+        A.loss[t] = loss_of(A, row, sums, below);
+        const Slope slope(A, row, sums, high);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) g[i] = slope(value[i]) - (taught ? slope.per_entry * share[i] : 0.f) - (i == row.label ? slope.by_label : 0.f);
+    }
+    if (A.dz != nullptr) store8(dz, g, vocabulary);
 }
 
 bool side_ok(const void* p, int64_t rows, int64_t width, int64_t stride, int64_t bytes) { return p != nullptr && is_aligned(p, bytes) && is_matrix(rows, width, stride, bytes); }
 bool ids_ok(int32_t type) { return type == MGWFBP_I32 || type == MGWFBP_I64; }
 
-template <int T_, int V_> struct Shape { static constexpr int threads = T_, vecs = V_; };
+template <int T_, int V_, int P_> struct Shape { static constexpr int threads = T_, vecs = V_, per_simd = P_; };
 template <typename T, typename F> int with_shape(int64_t vocabulary, F&& f) {
     constexpr bool WIDE = sizeof(T) == 4;
-    if (vocabulary <= 512) return f(Shape<64, 1>());
-    if (vocabulary <= 2048) return f(Shape<256, 1>());
-    if (vocabulary <= 8192) return f(Shape<256, 4>());
-    if (vocabulary <= 16384) return f(Shape<512, 4>());
-    if (vocabulary <= 32768) return f(Shape<1024, 4>());
-    if (vocabulary <= 65536) return f(Shape<1024, 8>());
+    if (vocabulary <= 512) return f(Shape<64, 1, 8>());
+    if (vocabulary <= 2048) return f(Shape<256, 1, 8>());
+    if (vocabulary <= 8192) return f(Shape<256, 4, WIDE ? 6 : 8>());
+    if (vocabulary <= 16384) return f(Shape<512, 4, WIDE ? 6 : 8>());
+    if (vocabulary <= 32768) return f(Shape<1024, 4, WIDE ? 4 : 8>());
+    if (vocabulary <= 65536) return f(Shape<1024, 8, WIDE ? 4 : 8>());
     if constexpr (!WIDE)
-        if (vocabulary <= 131072) return f(Shape<1024, 16>());
-    return f(Shape<1024, 0>());
+        if (vocabulary <= 131072) return f(Shape<1024, 16, 4>());
+    return f(Shape<1024, 0, 4>());
+}
+
+// How few rows are cut into parts: how many, and of how many vectors a lane; 0 where rows are not cut.
+struct Cut {
+    int64_t parts, vecs;
+};
+Cut cut_of(int64_t tokens, int64_t vocabulary) {
+    if (tokens > FEW_ROWS || vocabulary < FEW_ROWS_LOGITS) return {0, 0};
+    Cut c{0, 1};
+    while (c.vecs < 8 && tokens * ceil_div(vocabulary, PART * VEC * c.vecs) > 1024) c.vecs *= 2;
+    c.parts = ceil_div(vocabulary, PART * VEC * c.vecs);
+    return c;
+}
+uint64_t workspace_of(int64_t tokens, int64_t vocabulary, int32_t top) {
+    const Cut c = cut_of(tokens, vocabulary);
+    return c.parts == 0 ? 0 : static_cast<uint64_t>(tokens * (c.parts * 3 + label_place(top) + 1)) * 4;
 }
 
 }  // namespace
 
 extern "C" {
 
+int mgwfbp_distill_workspace(int64_t n_tokens, int64_t n_vocabulary, int32_t n_top, uint64_t* bytes_out) {
+    if (n_tokens < 0 || n_tokens > (int64_t(1) << 26) || n_vocabulary < 1 || n_vocabulary > (int64_t(1) << 23) || n_top < 0 || n_top > MOST_TOP ||
+        bytes_out == nullptr)
+        return MGWFBP_EINVAL;
+    *bytes_out = n_tokens == 0 ? 0 : workspace_of(n_tokens, n_vocabulary, n_top);
+    return MGWFBP_OK;
+}
+
 int mgwfbp_distill(const void* d_z, int64_t z_stride, int32_t dtype, int64_t n_tokens, int64_t n_vocabulary, const void* d_labels, int32_t label_type,
                    const void* d_ids, int64_t ids_stride, int32_t id_type, const void* d_teacher, int64_t teacher_stride, int32_t teacher_dtype, int32_t n_top,
                    float temperature, float label_weight, float teacher_weight, const float* d_row_weight, float* d_loss, void* d_dz, int64_t dz_stride,
-                   void* hip_stream) {
+                   void* d_workspace, uint64_t workspace_bytes, void* hip_stream) {
     if (!is_dtype(dtype) || n_tokens < 0 || n_tokens > (int64_t(1) << 26) || n_vocabulary < 1 || n_vocabulary > (int64_t(1) << 23)) return MGWFBP_EINVAL;
     if (n_top < 0 || n_top > MOST_TOP || !(temperature >= 0x1p-20f && temperature <= 0x1p20f) || !std::isfinite(label_weight) || !std::isfinite(teacher_weight))
         return MGWFBP_EINVAL;
@@ -293,12 +682,32 @@ int mgwfbp_distill(const void* d_z, int64_t z_stride, int32_t dtype, int64_t n_t
     a.label_type = label_type;
     a.id_type = id_type;
     a.teacher_type = teacher_dtype;
+    const Cut cut = cut_of(n_tokens, n_vocabulary);
+    if (cut.parts > 0) {
+        if (d_workspace == nullptr || !is_aligned(d_workspace, 256) || workspace_bytes < workspace_of(n_tokens, n_vocabulary, n_top)) return MGWFBP_EINVAL;
+        a.stats = static_cast<float*>(d_workspace);
+        a.parts = cut.parts;
+        a.kept_z = a.stats + n_tokens * cut.parts * 3;
+        a.kept_stride = label_place(n_top) + 1;
+    }
     return with_dtype(dtype, [&](auto* type) {
         typedef std::remove_pointer_t<decltype(type)> T;
+        if (n_vocabulary < VEC) return launch(tiny_kernel<T>, a, dim3(static_cast<uint32_t>(ceil_div(n_tokens, 64))), dim3(64), hip_stream);
+        if (cut.parts > 0) {
+            auto of = [&](void (*parts)(DistillArgs), void (*slopes)(DistillArgs)) {
+                const uint32_t n = static_cast<uint32_t>(cut.parts), rows = static_cast<uint32_t>(n_tokens);
+                const int status = launch(parts, a, dim3(n, rows), dim3(PART), hip_stream);
+                return status != MGWFBP_OK ? status : launch(slopes, a, dim3(d_dz == nullptr ? 1 : n, rows), dim3(PART), hip_stream, Entries<PART>::bytes(n_top));
+            };
+            if (cut.vecs == 1) return of(part_kernel<T, 1>, part_slope_kernel<T, 1>);
+            if (cut.vecs == 2) return of(part_kernel<T, 2>, part_slope_kernel<T, 2>);
+            if (cut.vecs == 4) return of(part_kernel<T, 4>, part_slope_kernel<T, 4>);
+            return of(part_kernel<T, 8>, part_slope_kernel<T, 8>);
+        }
         return with_shape<T>(n_vocabulary, [&](auto s) {
             constexpr int THREADS = decltype(s)::threads;
-            void (*kernel)(DistillArgs) = distill_kernel<T, THREADS, decltype(s)::vecs>;
-            return launch(kernel, a, dim3(static_cast<uint32_t>(n_tokens)), dim3(THREADS), hip_stream);
+            void (*kernel)(DistillArgs) = distill_kernel<T, THREADS, decltype(s)::vecs, decltype(s)::per_simd>;
+            return launch(kernel, a, dim3(static_cast<uint32_t>(n_tokens)), dim3(THREADS), hip_stream, Entries<THREADS>::bytes(n_top));
         });
     });
 }

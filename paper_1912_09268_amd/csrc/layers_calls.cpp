@@ -26,11 +26,11 @@ namespace {
 
 // The entry points, in the order of NAMES; written by set_functions, under the interpreter lock.
 enum { EMBED, EMBED_GRAD, EMBED_GRAD_WORKSPACE, ACT_STORE, ACT_BACKWARD, ACT_LINEAR_GRAD, ACT_LINEAR_GRAD_WORKSPACE, NORM, NORM_BACKWARD,
-       NORM_BACKWARD_WORKSPACE, RECUR, RECUR_BACKWARD, RECUR_STATES, RECUR_WORKSPACE, DISTILL, N_ENTRIES };
+       NORM_BACKWARD_WORKSPACE, RECUR, RECUR_BACKWARD, RECUR_STATES, RECUR_WORKSPACE, DISTILL, DISTILL_WORKSPACE, N_ENTRIES };
 const char* const NAMES[N_ENTRIES] = {"mgwfbp_embed", "mgwfbp_embed_grad", "mgwfbp_embed_grad_workspace", "mgwfbp_act_store",
                                       "mgwfbp_act_backward", "mgwfbp_act_linear_grad", "mgwfbp_act_linear_grad_workspace", "mgwfbp_norm", "mgwfbp_norm_backward",
                                       "mgwfbp_norm_backward_workspace", "mgwfbp_recur", "mgwfbp_recur_backward", "mgwfbp_recur_states", "mgwfbp_recur_workspace",
-                                      "mgwfbp_distill"};
+                                      "mgwfbp_distill", "mgwfbp_distill_workspace"};
 void* g_entry[N_ENTRIES];
 PyObject* g_raise = nullptr;     // layers_binding._check
 
@@ -490,14 +490,14 @@ PyObject* recur_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     });
 }
 
-// distill(logits, ids, teacher, labels, temperature, label_weight, teacher_weight, row_weight, loss, dlogits)
+// distill(logits, ids, teacher, labels, temperature, label_weight, teacher_weight, row_weight, loss, dlogits, workspace)
 PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return guarded([&]() -> PyObject* {
         float tau, label_weight, teacher_weight;
-        if (nargs != 10 || g_entry[DISTILL] == nullptr || !number(args[4], tau) || !number(args[5], label_weight) || !number(args[6], teacher_weight)) return not_this_way();
+        if (nargs != 11 || g_entry[DISTILL] == nullptr || !number(args[4], tau) || !number(args[5], label_weight) || !number(args[6], teacher_weight)) return not_this_way();
         Call call;
         const at::Tensor *z = call.tensor(args[0]), *ids = call.tensor(args[1], true), *teacher = call.tensor(args[2], true), *labels = call.tensor(args[3], true),
-                         *row_weight = call.tensor(args[7], true), *loss = call.tensor(args[8]), *dz = call.tensor(args[9], true);
+                         *row_weight = call.tensor(args[7], true), *loss = call.tensor(args[8]), *dz = call.tensor(args[9], true), *given = call.tensor(args[10], true);
         if (!call.ok || z->dim() != 2 || (ids == nullptr) != (teacher == nullptr)) return not_this_way();
         const int64_t tokens = z->size(0), vocabulary = z->size(1), z_stride = call.matrix(z, tokens, vocabulary), dz_stride = call.matrix(dz, tokens, vocabulary);
         int64_t top = 0, ids_stride = 0, teacher_stride = 0;
@@ -513,6 +513,11 @@ PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         float* const l = static_cast<float*>(call.vector(loss, tokens, at::kFloat));
         if (!call.ok || vocabulary < 1 || (dz != nullptr && (dz->scalar_type() != z->scalar_type() || (dz->data_ptr() == z->data_ptr() && dz_stride != z_stride))))
             return not_this_way();
+        uint64_t bytes = 0, size = 0;
+        if (ENTRY(DISTILL_WORKSPACE, mgwfbp_distill_workspace)(tokens, vocabulary, static_cast<int32_t>(top), &bytes) != 0) return not_this_way();
+        at::Tensor keep;
+        void* const space = bytes == 0 && given == nullptr ? nullptr : call.workspace(given, bytes, keep, size);
+        if (!call.ok) return not_this_way();
         const int type = dtype_of(*z), label_type = labels == nullptr ? 0 : id_type_of(*labels), id_type = ids == nullptr ? 0 : id_type_of(*ids),
                   teacher_type = teacher == nullptr ? 0 : dtype_of(*teacher);
         void *const zp = z->data_ptr(), *const lp = at_or_null(labels), *const ip = at_or_null(ids), *const tp = at_or_null(teacher), *const dp = at_or_null(dz),
@@ -520,7 +525,7 @@ PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         int status;
         Py_BEGIN_ALLOW_THREADS
         status = ENTRY(DISTILL, mgwfbp_distill)(zp, z_stride, type, tokens, vocabulary, lp, label_type, ip, ids_stride, id_type, tp, teacher_stride, teacher_type,
-                                                static_cast<int32_t>(top), tau, label_weight, teacher_weight, w, l, dp, dz_stride, stream);
+                                                static_cast<int32_t>(top), tau, label_weight, teacher_weight, w, l, dp, dz_stride, space, size, stream);
         Py_END_ALLOW_THREADS
         return done(DISTILL, status, {loss, dz});
     });
@@ -559,7 +564,7 @@ PyMethodDef functions[] = {{"embed", fast(embed), METH_FASTCALL, "embed(tables, 
                            {"recur_backward", fast(recur_backward), METH_FASTCALL,
                             "recur_backward(gate, x, states, dy, kind, first, offsets, dlast, dgate, dx, dfirst, workspace)"},
                            {"distill", fast(distill), METH_FASTCALL,
-                            "distill(logits, ids, teacher, labels, temperature, label_weight, teacher_weight, row_weight, loss, dlogits)"},
+                            "distill(logits, ids, teacher, labels, temperature, label_weight, teacher_weight, row_weight, loss, dlogits, workspace)"},
                            {"set_functions", set_functions, METH_VARARGS, "set_functions(check, {name: address} or None)"},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layers_calls", "calls of layers", -1, functions, nullptr, nullptr, nullptr, nullptr};

@@ -509,7 +509,7 @@ def recur_backward(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, dy
 
 def distill(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, teacher: Optional[torch.Tensor] = None, labels: Optional[torch.Tensor] = None,
             temperature: float = 1.0, label_weight: float = 1.0, teacher_weight: float = 1.0, row_weight: Optional[torch.Tensor] = None,
-            loss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None) -> torch.Tensor:
+            loss: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The loss of every row of logits [tokens, vocabulary], and its gradient where `dlogits` is given (of logits' type; it may be logits):
 
       row_weight * (label_weight * cross_entropy(logits, labels)
@@ -517,14 +517,15 @@ def distill(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, teacher: O
 
     labels [tokens] (integers, contiguous; one outside the vocabulary: none) and the teacher's top logits `teacher` [tokens, top] with their `ids`; either may be
     left out (labels alone: cross entropy).  An id outside the vocabulary or a logit of -inf is no entry.  row_weight float32 [tokens] (None: 1).
-    Rows with weight 0, and those with neither label nor entry, have loss 0 and gradient 0 whatever is in them.  Returns `loss`, float32 [tokens]."""
-    if loss is not None and _native.distill(logits, ids, teacher, labels, temperature, label_weight, teacher_weight, row_weight, loss, dlogits) is None:
+    Rows with weight 0, and those with neither label nor entry, have loss 0 and gradient 0 whatever is in them.
+    `workspace`: device memory of layers_binding.distill_workspace(tokens, vocabulary, top) bytes; None takes torch's.  Returns `loss`, float32 [tokens]."""
+    if loss is not None and _native.distill(logits, ids, teacher, labels, temperature, label_weight, teacher_weight, row_weight, loss, dlogits, workspace) is None:
         return loss
     stride = _matrix(logits, "logits", None, None)
     tokens, vocabulary = logits.shape
     if loss is None:
         loss = torch.empty(tokens, device=logits.device)
-    device = _device(logits, ids, teacher, labels, row_weight, loss, dlogits)
+    device = _device(logits, ids, teacher, labels, row_weight, loss, dlogits, workspace)
     if vocabulary < 1 or (ids is None) != (teacher is None):
         _fail("a vocabulary of one logit or more, and ids and teacher together")
     top, ids_stride, teacher_stride = 0, 0, 0
@@ -542,8 +543,9 @@ def distill(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, teacher: O
         if _same_place(dlogits, logits) and dz_stride != stride:
             _fail("dlogits over logits must have its strides")
     with _on(device) as stream:
+        space = _workspace(workspace, B.distill_workspace(tokens, vocabulary, top), device)
         B.distill(logits.data_ptr(), stride, _DTYPES[logits.dtype], tokens, vocabulary, labels_at, _code(labels, _ID_TYPES), _address(ids), ids_stride,
                   _code(ids, _ID_TYPES), _address(teacher), teacher_stride, _code(teacher), top, temperature, label_weight, teacher_weight, weight_at, loss_at,
-                  _address(dlogits), dz_stride, stream)
+                  _address(dlogits), dz_stride, space.data_ptr(), space.numel() * space.element_size(), stream)
     _written(loss, dlogits)
     return loss

@@ -41,7 +41,8 @@ _SIGNATURES = {
     "mgwfbp_recur_workspace": (C.c_int, [_vp, _i64, _i32, _u64p]),
     "mgwfbp_recur": (C.c_int, [_vp, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _u64, _vp]),
     "mgwfbp_recur_backward": (C.c_int, [_vp, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _u64, _vp]),
-    "mgwfbp_distill": (C.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _i32, _vp, _i64, _i32, _vp, _i64, _i32, _i32, _f32, _f32, _f32, _vp, _vp, _vp, _i64, _vp]),
+    "mgwfbp_distill_workspace": (C.c_int, [_i64, _i64, _i32, _u64p]),
+    "mgwfbp_distill": (C.c_int, [_vp, _i64, _i32, _i64, _i64, _vp, _i32, _vp, _i64, _i32, _vp, _i64, _i32, _i32, _f32, _f32, _f32, _vp, _vp, _vp, _i64, _vp, _u64, _vp]),
     "mgwfbp_layers_last_hip_error": (C.c_int, []),
 }
 
@@ -209,10 +210,18 @@ def recur_backward(sequences: Sequences, n_channels: int, kind: int, dtype: int,
                                                                 workspace_bytes, stream))
 
 
+@functools.lru_cache(maxsize=1024)
+def distill_workspace(n_tokens: int, n_vocabulary: int, n_top: int) -> int:
+    """mgwfbp_distill_workspace: bytes."""
+    out = C.c_uint64()
+    _check("mgwfbp_distill_workspace", lib().mgwfbp_distill_workspace(n_tokens, n_vocabulary, n_top, C.byref(out)))
+    return out.value
+
+
 def distill(d_z: int, z_stride: int, dtype: int, n_tokens: int, n_vocabulary: int, d_labels: int, label_type: int, d_ids: int, ids_stride: int, id_type: int,
             d_teacher: int, teacher_stride: int, teacher_dtype: int, n_top: int, temperature: float, label_weight: float, teacher_weight: float,
-            d_row_weight: int, d_loss: int, d_dz: int, dz_stride: int, stream: int = 0) -> None:
+            d_row_weight: int, d_loss: int, d_dz: int, dz_stride: int, d_workspace: int, workspace_bytes: int, stream: int = 0) -> None:
     """mgwfbp_distill."""
     _check("mgwfbp_distill", lib().mgwfbp_distill(d_z, z_stride, dtype, n_tokens, n_vocabulary, d_labels, label_type, d_ids, ids_stride, id_type, d_teacher,
                                                   teacher_stride, teacher_dtype, n_top, temperature, label_weight, teacher_weight, d_row_weight, d_loss, d_dz,
-                                                  dz_stride, stream))
+                                                  dz_stride, d_workspace, workspace_bytes, stream))

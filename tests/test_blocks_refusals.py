@@ -71,13 +71,21 @@ def test_recur_refuses():
 
 def test_distill_refuses():
     good = dict(d_z=P, z_stride=50, dtype=B.F16, n_tokens=9, n_vocabulary=50, d_labels=P, label_type=B.I64, d_ids=P, ids_stride=4, id_type=B.I32, d_teacher=P, teacher_stride=4,
-                teacher_dtype=B.BF16, n_top=4, temperature=2.0, label_weight=1.0, teacher_weight=1.0, d_row_weight=P, d_loss=P, d_dz=P, dz_stride=50)
+                teacher_dtype=B.BF16, n_top=4, temperature=2.0, label_weight=1.0, teacher_weight=1.0, d_row_weight=P, d_loss=P, d_dz=P, dz_stride=50,
+                d_workspace=0, workspace_bytes=0)
     for bad in (dict(d_z=0), dict(d_z=P + 1), dict(z_stride=49), dict(dtype=3), dict(n_tokens=-1), dict(n_tokens=2 ** 26 + 1), dict(n_vocabulary=0), dict(n_vocabulary=2 ** 23 + 1),
                 dict(d_labels=P + 4), dict(label_type=2), dict(d_ids=0), dict(d_ids=P + 2), dict(ids_stride=3), dict(id_type=-1), dict(d_teacher=0), dict(d_teacher=P + 1),
                 dict(teacher_stride=3), dict(teacher_dtype=4), dict(n_top=-1), dict(n_top=B.MAX_TOP + 1, ids_stride=9999, teacher_stride=9999), dict(temperature=0.0),
                 dict(temperature=-1.0), dict(temperature=math.nan), dict(temperature=math.inf), dict(label_weight=math.nan), dict(teacher_weight=math.inf), dict(d_row_weight=P + 2),
                 dict(d_loss=0), dict(d_loss=P + 2), dict(d_dz=P + 1), dict(dz_stride=49)):
         _refused(B.distill, *{**good, **bad}.values())
+    size = B.distill_workspace(2, 100000, 4)                  # few rows, cut into parts
+    long = dict(n_tokens=2, n_vocabulary=100000, z_stride=100000, dz_stride=100000, d_workspace=P, workspace_bytes=size)
+    assert size > 0 and B.distill_workspace(9, 50, 4) == 0 and B.lib().mgwfbp_distill_workspace(1, 1, 1, None) == -1
+    for bad in (dict(d_workspace=0), dict(d_workspace=P + 128), dict(workspace_bytes=size - 1)):
+        _refused(B.distill, *{**good, **long, **bad}.values())
+    for bad in ((-1, 5, 0), (1, 0, 0), (1, 5, -1), (1, 5, B.MAX_TOP + 1)):
+        _refused(B.distill_workspace, *bad)
     B.distill(*{**good, "n_tokens": 0, "d_z": 0, "d_loss": 0, "d_ids": 0}.values())
 
 
