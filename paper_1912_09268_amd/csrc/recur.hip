@@ -35,9 +35,7 @@ namespace {
 
 using namespace ops;
 
-constexpr int WAVES = 8, LANES = 64, TOKENS = 16;            // of a workgroup, of a wavefront, of a wavefront and block
-constexpr int BLOCK = WAVES * TOKENS;
-static_assert(BLOCK == MGWFBP_RECUR_BLOCK);
+constexpr int LANES = 64, BLOCK = MGWFBP_RECUR_BLOCK;
 constexpr int SHORT = 16;                                    // tokens up to which a lane goes through a sequence by itself
 
 struct RecurArgs {
@@ -61,29 +59,30 @@ struct RecurArgs {
     int32_t copied;                      // first is in the maps' last segment: the caller's may be overwritten by last
 };
 
-// A map that begins a sequence: it gives b whatever comes in.
-constexpr float FRESH = -0.f;
-__device__ __forceinline__ bool is_fresh(float a) { return __builtin_bit_cast(uint32_t, a) == 0x80000000u; }
-__device__ __forceinline__ float through(float a, float b, float h) { return is_fresh(a) ? b : __builtin_fmaf(a, h, b); }
-// (a, b) and then (ma, mb), in (a, b)
-__device__ __forceinline__ void compose(float& a, float& b, float ma, float mb) {
-    b = through(ma, mb, b);
-    a = is_fresh(ma) ? FRESH : a * ma;                       // a product of FRESH and a gate is FRESH again
-}
+// The wavefront's number, as what it is: the same in all its lanes, so that what follows from it is computed once for them.
+__device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / LANES)); }
 
-// CH neighbouring elements of a row, n of them there.
+// CH neighbouring elements of a row, as bits: two of 16 bits share a register.
+template <int BYTES> struct Bits;
+template <> struct Bits<2> { typedef uint16_t type; };
+template <> struct Bits<4> { typedef uint32_t type; };
 template <typename T, int CH> struct Piece {
     typedef T vec __attribute__((ext_vector_type(CH), aligned(alignof(T))));
-    vec v;
-    __device__ __forceinline__ void load(const T* p, int n) {
-        if (n >= CH) {
-            v = *reinterpret_cast<const vec*>(p);
-        } else {
+    typedef typename Bits<CH * sizeof(T)>::type bits;
+    bits v;
+    __device__ __forceinline__ void load(const T* p) { v = __builtin_bit_cast(bits, *reinterpret_cast<const vec*>(p)); }
+    __device__ __forceinline__ void load(const T* p, int n) {            // the first n of them
+        typedef typename Bits<sizeof(T)>::type one;
+        v = 0;
 #pragma unroll
-            for (int i = 0; i < CH; ++i) v[i] = i < n ? p[i] : static_cast<T>(0.f);
-        }
+        for (int i = 0; i < CH; ++i)
+            if (i < n) v |= static_cast<bits>(static_cast<bits>(reinterpret_cast<const one*>(p)[i]) << (8 * sizeof(T) * i % 32));
     }
-    __device__ __forceinline__ float get(int i) const { return static_cast<float>(v[i]); }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, v);
+        else if constexpr (__is_same(T, __bf16)) return __builtin_bit_cast(float, i == 0 ? static_cast<uint32_t>(v) << 16 : static_cast<uint32_t>(v) & 0xffff0000u);
+        else return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(v >> (16 * i % 32))));
+    }
 };
 
 // a and 1 - a of a gate, both to their own last digits.
@@ -92,12 +91,11 @@ __device__ __forceinline__ void logistic(float g, float& a, float& rest) {
     const float near = __builtin_amdgcn_rcpf(1.f + e), far = e * near;
     a = g >= 0.f ? near : far;
     rest = g >= 0.f ? far : near;
-    if (g != g) a = rest = g;
 }
 template <int KIND> __device__ __forceinline__ float factor(float a, float rest) {
     if constexpr (KIND == MGWFBP_RECUR_FREE) return 1.f;
     else if constexpr (KIND == MGWFBP_RECUR_CONVEX) return rest;
-    else return __builtin_amdgcn_sqrtf(rest * (1.f + a));
+    else return __builtin_amdgcn_sqrtf(__builtin_fmaf(rest, a, rest));
 }
 // d h[t] / d gate[t]
 template <int KIND> __device__ __forceinline__ float slope(float a, float rest, float before, float x) {
@@ -137,21 +135,21 @@ struct Bounds {
         return lo + __popcll(__ballot(lo + lane < hi && at(min(lo + lane, count - 1)) <= t));
     }
     __device__ __forceinline__ int sequence_of(int t) const { return min(max(up_to(t) - 1, 0), count - 2); }
-    // Bit i: an offset is t0 + i, 0 <= i <= TOKENS.
-    __device__ __forceinline__ uint32_t marks(int t0) const {
+    // Bit i: an offset is t0 + i, 0 <= i <= N.
+    template <int N> __device__ __forceinline__ uint32_t marks(int t0) const {
         const int lane = threadIdx.x % LANES;
         uint32_t bits = 0;
         if (count <= LANES) {
             const int i = held - t0;
-            const bool in = lane < count && i >= 0 && i <= TOKENS;
+            const bool in = lane < count && i >= 0 && i <= N;
             if (__ballot(in) == 0) return 0;
             bits = in ? 1u << i : 0u;
         } else {
-            const int from = up_to(t0 - 1), to = up_to(t0 + TOKENS);
+            const int from = up_to(t0 - 1), to = up_to(t0 + N);
             if (from >= to) return 0;
             for (int j = from + lane; j < to; j += LANES) {
                 const int i = at(j) - t0;
-                if (i >= 0 && i <= TOKENS) bits |= 1u << i;
+                if (i >= 0 && i <= N) bits |= 1u << i;
             }
         }
 #pragma unroll
@@ -160,12 +158,16 @@ struct Bounds {
     }
 };
 
-// What a wavefront knows of its place.
-template <bool PACKED, int CH> struct Place {
+// What a wavefront knows of its place: W of them share a block, N tokens each.
+template <bool PACKED_, int CH_, int W> struct Place {
+    static constexpr bool PACKED = PACKED_;
+    static constexpr int CH = CH_, N = BLOCK / W;
+    static constexpr uint32_t ALL = static_cast<uint32_t>((uint64_t(1) << N) - 1);
     Bounds bounds;
     int64_t unit, base;                  // base: the unit's first row
-    int64_t c;                           // the lane's first channel
+    uint32_t c;                          // the lane's first channel
     int n;                               // and how many it has
+    bool full;                           // all lanes have CH
     int begin, end;                      // tokens of the unit that are sequences'
     uint32_t segment, first_block, end_block;
 
@@ -174,35 +176,33 @@ template <bool PACKED, int CH> struct Place {
         segment = rest % A.segments;
         unit = rest / A.segments;
         base = PACKED ? 0 : unit * A.tokens;
-        c = (static_cast<int64_t>(slab) * LANES + threadIdx.x % LANES) * CH;
+        c = (slab * LANES + threadIdx.x % LANES) * CH;
         n = static_cast<int>(max(static_cast<int64_t>(0), min(A.channels - c, static_cast<int64_t>(CH))));
+        full = static_cast<int64_t>(slab + 1) * LANES * CH <= A.channels;
         begin = 0;
         end = static_cast<int>(A.tokens);
         if constexpr (PACKED) {
             bounds.open(A);
-            begin = bounds.at(0);
-            end = bounds.at(bounds.count - 1);
+            begin = __builtin_amdgcn_readfirstlane(bounds.at(0));
+            end = __builtin_amdgcn_readfirstlane(bounds.at(bounds.count - 1));
         }
         first_block = segment * A.per_segment;
         end_block = min(first_block + A.per_segment, static_cast<uint32_t>((end + BLOCK - 1) / BLOCK));
     }
     __device__ __forceinline__ int row(int t) const { return min(max(t, begin), max(end - 1, 0)); }      // one that may be read
-    // Bits of the TOKENS tokens from t0 on: a sequence's, the first of one, the last of one.
+    __device__ __forceinline__ bool whole(int t0) const { return full && t0 >= begin && t0 + N <= end; }
+    // Bits of the N tokens from t0 on: a sequence's; and where they lie one behind the other, the first of one, the last of one.
     __device__ __forceinline__ void masks(int t0, uint32_t& valid, uint32_t& first, uint32_t& last) const {
-        constexpr uint32_t ALL = (1u << TOKENS) - 1;
-        const int lo = min(max(begin - t0, 0), TOKENS), hi = min(max(end - t0, 0), TOKENS);
-        valid = (ALL >> (TOKENS - hi)) & (ALL << lo) & ALL;
-        if (hi == 0) valid = 0;
-        uint32_t marks;
-        if constexpr (PACKED) marks = bounds.marks(t0);
-        else marks = (t0 == 0 ? 1u : 0u) | (end >= t0 && end - t0 <= TOKENS ? 1u << (end - t0) : 0u);
-        first = marks & valid;
-        last = marks >> 1 & valid;
+        const int lo = min(max(begin - t0, 0), N), hi = min(max(end - t0, 0), N);
+        valid = ALL >> (N - hi) & (ALL << lo) & ALL;
+        first = last = 0;
+        if constexpr (PACKED) {
+            const uint32_t marks = bounds.template marks<N>(t0);
+            first = marks & valid;
+            last = marks >> 1 & valid;
+        }
     }
-    __device__ __forceinline__ int64_t sequence_at(int t) const {
-        if constexpr (PACKED) return bounds.sequence_of(t);
-        else return unit;
-    }
+    __device__ __forceinline__ int64_t sequence_at(int t) const { return bounds.sequence_of(t); }
     __device__ __forceinline__ void state(const RecurArgs& A, const float* from, int64_t sequence, float (&out)[CH]) const {
 #pragma unroll
         for (int k = 0; k < CH; ++k) out[k] = from != nullptr && k < n ? from[sequence * A.channels + c + k] : 0.f;
@@ -217,7 +217,7 @@ template <bool PACKED, int CH> struct Place {
     __device__ __forceinline__ void empty_sequences(const RecurArgs& A, const float* from, float* to) const {
         if constexpr (PACKED) {
             if (to == nullptr) return;
-            for (int64_t s0 = threadIdx.x / LANES * LANES; s0 < A.sequences; s0 += WAVES * LANES) {
+            for (int64_t s0 = wave_of() * LANES; s0 < A.sequences; s0 += W * LANES) {
                 const int64_t s = s0 + threadIdx.x % LANES;
                 uint64_t empty = __ballot(s < A.sequences && bounds.at(static_cast<int>(min(s, A.sequences - 1))) >= bounds.at(static_cast<int>(min(s + 1, A.sequences))));
                 while (empty != 0) {
@@ -233,18 +233,33 @@ template <bool PACKED, int CH> struct Place {
 };
 
 // A wavefront's tokens of a block, as they are in memory.
-template <typename T, int CH> struct Tokens {
-    Piece<T, CH> v[TOKENS];
-    template <bool PACKED> __device__ __forceinline__ void load(const Place<PACKED, CH>& at, const void* from, int64_t stride, int t0) {
-        const T* const p = static_cast<const T*>(from) + at.c;
+template <typename T, typename P> struct Tokens {
+    Piece<T, P::CH> v[P::N];
+    __device__ __forceinline__ void load(const P& at, const void* from, int64_t stride, int t0) {
+        if (at.whole(t0)) {
+            const T* row = static_cast<const T*>(from) + (at.base + t0) * stride;
 #pragma unroll
-        for (int i = 0; i < TOKENS; ++i) v[i].load(p + (at.base + at.row(t0 + i)) * stride, at.n);
+            for (int i = 0; i < P::N; ++i, row += stride) v[i].load(row + at.c);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P::N; ++i) v[i].load(static_cast<const T*>(from) + (at.base + at.row(t0 + i)) * stride + at.c, at.n);
+        }
     }
 };
 
+// A map that begins a sequence: it gives b whatever comes in.  Sequences of one length need none: they begin with a workgroup's work.
+constexpr float FRESH = -0.f;
+template <bool PACKED> __device__ __forceinline__ bool is_fresh(float a) { return PACKED && __builtin_bit_cast(uint32_t, a) == 0x80000000u; }
+template <bool PACKED> __device__ __forceinline__ float through(float a, float b, float h) { return is_fresh<PACKED>(a) ? b : __builtin_fmaf(a, h, b); }
+// (a, b) and then (ma, mb), in (a, b)
+template <bool PACKED> __device__ __forceinline__ void compose(float& a, float& b, float ma, float mb) {
+    b = through<PACKED>(ma, mb, b);
+    a = is_fresh<PACKED>(ma) ? FRESH : a * ma;               // a product of FRESH and a gate is FRESH again
+}
+
 // Maps of wavefronts in LDS, two blocks in turn, so that one barrier a block is enough.
-template <int CH> struct Maps {
-    float m[2][WAVES][2][LANES * CH];
+template <bool PACKED, int CH, int W> struct Maps {
+    float m[2][W][2][LANES * CH];
     __device__ __forceinline__ void put(uint32_t turn, int wave, const float (&a)[CH], const float (&b)[CH]) {
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
@@ -255,22 +270,26 @@ template <int CH> struct Maps {
     // h through the map of a wavefront.
     __device__ __forceinline__ void take(uint32_t turn, int wave, float (&h)[CH]) const {
 #pragma unroll
-        for (int k = 0; k < CH; ++k) h[k] = through(m[turn][wave][0][k * LANES + threadIdx.x % LANES], m[turn][wave][1][k * LANES + threadIdx.x % LANES], h[k]);
+        for (int k = 0; k < CH; ++k) h[k] = through<PACKED>(m[turn][wave][0][k * LANES + threadIdx.x % LANES], m[turn][wave][1][k * LANES + threadIdx.x % LANES], h[k]);
     }
 };
 
-// The state that comes into a segment through the maps of those before it (or, on the way back, behind it), which eight
-// wavefronts share.
-template <bool BACK, bool PACKED, int CH> __device__ __forceinline__ void through_segments(const RecurArgs& A, const Place<PACKED, CH>& at, Maps<CH>& room, float (&h)[CH]) {
-    const int wave = threadIdx.x / LANES;
-    const int count = static_cast<int>(BACK ? A.segments - 1 - at.segment : at.segment);
-    const int each = (count + WAVES - 1) / WAVES, from = min(wave * each, count), to = min(from + each, count);
-    float a[CH], b[CH];
+template <int CH> __device__ __forceinline__ void nothing_yet(float (&ma)[CH], float (&mb)[CH]) {
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-        a[k] = 1.f;
-        b[k] = 0.f;
+        ma[k] = 1.f;
+        mb[k] = 0.f;
     }
+}
+
+// h, which comes into a unit, through the maps of the segments before a workgroup's (or, on the way back, behind it); the wavefronts
+// share them.
+template <bool BACK, bool PACKED, int CH, int W> __device__ __forceinline__ void through_segments(const RecurArgs& A, const Place<PACKED, CH, W>& at, Maps<PACKED, CH, W>& room, float (&h)[CH]) {
+    const int wave = wave_of();
+    const int count = static_cast<int>(BACK ? A.segments - 1 - at.segment : at.segment);
+    const int each = (count + W - 1) / W, from = min(wave * each, count), to = min(from + each, count);
+    float a[CH], b[CH];
+    nothing_yet(a, b);
 #pragma unroll 4
     for (int i = from; i < to; ++i) {
         const int64_t s = at.unit * A.segments + (BACK ? A.segments - 1 - i : i);
@@ -278,19 +297,17 @@ template <bool BACK, bool PACKED, int CH> __device__ __forceinline__ void throug
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const float ma = k < at.n ? map[k] : 1.f, mb = k < at.n ? map[A.channels + k] : 0.f;
-            compose(a[k], b[k], ma, mb);
+            compose<PACKED>(a[k], b[k], ma, mb);
         }
     }
     room.put(1, wave, a, b);
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < CH; ++k) h[k] = 0.f;
-    for (int w = 0; w < WAVES; ++w) room.take(1, w, h);      // turn 1 is written again after another barrier
+    for (int w = 0; w < W; ++w) room.take(1, w, h);          // turn 1 is written again after another barrier
 }
 
-// The first state of a unit of one sequence.  `last` may be the same memory: it is read before the first barrier here, or from where
-// fold_kernel has put it.
-template <bool PACKED, int CH> __device__ __forceinline__ void unit_first(const RecurArgs& A, const Place<PACKED, CH>& at, float (&h)[CH]) {
+// The first state of a unit of one sequence.  `last` may be the same memory: a workgroup that has a whole unit reads it long before it
+// writes the last state; where there are more, fold_kernel has put it elsewhere.
+template <int CH, int W> __device__ __forceinline__ void unit_first(const RecurArgs& A, const Place<false, CH, W>& at, float (&h)[CH]) {
     if (A.copied) {
         const float* const map = A.maps + (at.unit * A.segments + A.segments - 1) * 2 * A.channels + at.c;
 #pragma unroll
@@ -301,100 +318,147 @@ template <bool PACKED, int CH> __device__ __forceinline__ void unit_first(const 
 }
 
 // gate and x of a wavefront's tokens to the steps h -> a h + b; a token of no sequence changes nothing.
-template <typename T, int KIND, int CH> __device__ __forceinline__ void steps_of(const Tokens<T, CH>& gate, const Tokens<T, CH>& x, uint32_t valid, float (&a)[TOKENS][CH],
-                                                                                 float (&b)[TOKENS][CH]) {
+template <int KIND, typename T, typename P> __device__ __forceinline__ void steps_of(const Tokens<T, P>& gate, const Tokens<T, P>& x, uint32_t valid, float (&a)[P::N][P::CH],
+                                                                                     float (&rest)[P::N][P::CH], float (&b)[P::N][P::CH]) {
 #pragma unroll
-    for (int i = 0; i < TOKENS; ++i)
+    for (int i = 0; i < P::N; ++i)
+#pragma unroll
+        for (int k = 0; k < P::CH; ++k) {
+            logistic(gate.v[i].get(k), a[i][k], rest[i][k]);
+            b[i][k] = factor<KIND>(a[i][k], rest[i][k]) * x.v[i].get(k);
+        }
+    if (valid != P::ALL) {
+#pragma unroll
+        for (int i = 0; i < P::N; ++i)
+#pragma unroll
+            for (int k = 0; k < P::CH; ++k) {
+                a[i][k] = valid >> i & 1 ? a[i][k] : 1.f;
+                b[i][k] = valid >> i & 1 ? b[i][k] : 0.f;
+            }
+    }
+}
+
+// The map of a wavefront's tokens; reset(i, h) puts the state before token i, which begins a sequence, into h.
+template <int N, int CH, typename F> __device__ __forceinline__ void compose_steps(const float (&a)[N][CH], const float (&b)[N][CH], uint32_t begins, F&& reset, float (&ma)[CH],
+                                                                                   float (&mb)[CH]) {
+    auto step = [&](int i) {
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            float rest;
-            logistic(gate.v[i].get(k), a[i][k], rest);
-            b[i][k] = factor<KIND>(a[i][k], rest) * x.v[i].get(k);
-            if (!(valid >> i & 1)) {
-                a[i][k] = 1.f;
-                b[i][k] = 0.f;
-            }
+            mb[k] = __builtin_fmaf(a[i][k], mb[k], b[i][k]);
+            ma[k] *= a[i][k];
         }
+    };
+    if (begins == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) step(i);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (begins >> i & 1) {
+            reset(i, mb);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) ma[k] = FRESH;
+        }
+        step(i);
+    }
+}
+// The same from the end, for what flows from a token to the one before it, g -> a (dy + g), a being 1 for tokens of no sequence.
+template <int N, int CH, typename T, typename P, typename F> __device__ __forceinline__ void compose_flows(const float (&a)[N][CH], const Tokens<T, P>& dy, uint32_t valid, uint32_t ends,
+                                                                                                          F&& reset, float (&ma)[CH], float (&mb)[CH]) {
+    auto step = [&](int i, bool valid) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            mb[k] = a[i][k] * (mb[k] + (valid ? dy.v[i].get(k) : 0.f));
+            ma[k] *= a[i][k];
+        }
+    };
+    if (ends == 0 && valid == P::ALL) {
+#pragma unroll
+        for (int i = N - 1; i >= 0; --i) step(i, true);
+        return;
+    }
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) {
+        if (ends >> i & 1) {
+            reset(i, mb);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) ma[k] = FRESH;
+        }
+        step(i, valid >> i & 1);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------
 
-template <typename T, int KIND, int CH, bool PACKED> __global__ __launch_bounds__(WAVES * LANES) void scan_kernel(RecurArgs A) {
-    __shared__ Maps<CH> maps;
-    Place<PACKED, CH> at;
+template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_bounds__(W * LANES) void scan_kernel(RecurArgs A) {
+    typedef Place<PACKED, CH, W> P;
+    constexpr int N = P::N;
+    __shared__ Maps<PACKED, CH, W> maps;
+    P at;
     at.open(A);
-    const int wave = threadIdx.x / LANES;
+    const int wave = wave_of();
     if (at.segment == 0) at.empty_sequences(A, A.first, A.last);
     if (at.first_block >= at.end_block) return;
-    float carry[CH] = {}, first[CH];
-    if constexpr (!PACKED) unit_first(A, at, first);
-    if (at.segment > 0) through_segments<false>(A, at, maps, carry);
-    Tokens<T, CH> gate, x;
-    int t0 = static_cast<int>(at.first_block) * BLOCK + wave * TOKENS;
+    Tokens<T, P> gate, x;
+    int t0 = static_cast<int>(at.first_block) * BLOCK + wave * N;
     gate.load(at, A.gate, A.gate_stride, t0);
     x.load(at, A.x, A.x_stride, t0);
+    float carry[CH] = {};
+    if constexpr (!PACKED) unit_first(A, at, carry);
+    if (at.segment > 0) through_segments<false>(A, at, maps, carry);
     for (uint32_t block = at.first_block; block < at.end_block; ++block, t0 += BLOCK) {
         const uint32_t turn = (block - at.first_block) % 2;
         uint32_t valid, begins, ends;
         at.masks(t0, valid, begins, ends);
-        float a[TOKENS][CH], b[TOKENS][CH];
-        steps_of<T, KIND, CH>(gate, x, valid, a, b);
+        float a[N][CH], rest[N][CH], b[N][CH];
+        steps_of<KIND>(gate, x, valid, a, rest, b);
         if (block + 1 < at.end_block) {
             gate.load(at, A.gate, A.gate_stride, t0 + BLOCK);
             x.load(at, A.x, A.x_stride, t0 + BLOCK);
         }
-        auto reset = [&](int i, float (&h)[CH]) {
-            if constexpr (PACKED) at.state(A, A.first, at.sequence_at(t0 + i), h);
-            else
-#pragma unroll
-                for (int k = 0; k < CH; ++k) h[k] = first[k];
-        };
-        float ma[CH], mb[CH];
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            ma[k] = 1.f;
-            mb[k] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < TOKENS; ++i) {
-            if (begins >> i & 1) {
-                reset(i, mb);
-#pragma unroll
-                for (int k = 0; k < CH; ++k) ma[k] = FRESH;
-            }
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                mb[k] = __builtin_fmaf(a[i][k], mb[k], b[i][k]);
-                ma[k] *= a[i][k];
-            }
-        }
+        auto reset = [&](int i, float (&h)[CH]) { at.state(A, A.first, at.sequence_at(t0 + i), h); };
+        float ma[CH], mb[CH], h[CH];
+        nothing_yet(ma, mb);
+        compose_steps(a, b, begins, reset, ma, mb);
         maps.put(turn, wave, ma, mb);
         __syncthreads();
-        float h[CH];
         if (A.states != nullptr && wave == 0 && t0 >= at.begin) {
 #pragma unroll
             for (int k = 0; k < CH; ++k) h[k] = carry[k];
             if (begins & 1) reset(0, h);
             at.put_state(A, A.states, at.unit * A.blocks + block, h);
         }
-        for (int w = 0; w < WAVES; ++w) {
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
             if (w == wave) {
 #pragma unroll
                 for (int k = 0; k < CH; ++k) h[k] = carry[k];
             }
             maps.take(turn, w, carry);
         }
-        T* const to = static_cast<T*>(A.y) + at.c;
+        T* row = static_cast<T*>(A.y) + (at.base + t0) * A.y_stride;
+        if (at.full && valid == P::ALL && (begins | ends) == 0) {
 #pragma unroll
-        for (int i = 0; i < TOKENS; ++i) {
-            if (begins >> i & 1) reset(i, h);
+            for (int i = 0; i < N; ++i, row += A.y_stride) {
 #pragma unroll
-            for (int k = 0; k < CH; ++k) h[k] = __builtin_fmaf(a[i][k], h[k], b[i][k]);
-            if (valid >> i & 1) store_some(to + (at.base + t0 + i) * A.y_stride, h, at.n);
-            if (ends >> i & 1) at.put_state(A, A.last, at.sequence_at(t0 + i), h);
+                for (int k = 0; k < CH; ++k) h[k] = __builtin_fmaf(a[i][k], h[k], b[i][k]);
+                store_some(row + at.c, h, CH);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i, row += A.y_stride) {
+                if (begins >> i & 1) reset(i, h);
+#pragma unroll
+                for (int k = 0; k < CH; ++k) h[k] = __builtin_fmaf(a[i][k], h[k], b[i][k]);
+                if (valid >> i & 1) store_some(row + at.c, h, at.n);
+                if (ends >> i & 1) at.put_state(A, A.last, at.sequence_at(t0 + i), h);
+            }
         }
+        // tokens behind a sequence's last one have changed nothing
+        if (!PACKED && wave == W - 1 && block + 1 == A.blocks) at.put_state(A, A.last, at.unit, h);
     }
 }
 
@@ -402,105 +466,101 @@ template <typename T, int KIND, int CH, bool PACKED> __global__ __launch_bounds_
 // backward
 // ---------------------------------------------------------------------------------------------
 
-template <typename T, int KIND, int CH, bool PACKED> __global__ __launch_bounds__(WAVES * LANES) void back_kernel(RecurArgs A) {
-    __shared__ Maps<CH> forth, back;
-    Place<PACKED, CH> at;
+template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_bounds__(W * LANES) void back_kernel(RecurArgs A) {
+    typedef Place<PACKED, CH, W> P;
+    constexpr int N = P::N;
+    __shared__ Maps<PACKED, CH, W> forth, back;
+    P at;
     at.open(A);
-    const int wave = threadIdx.x / LANES;
+    const int wave = wave_of();
     if (at.segment == 0) at.empty_sequences(A, A.dlast, A.dfirst);
     if (at.first_block >= at.end_block) return;
+    Tokens<T, P> gate, x, dy;
     float carry[CH] = {}, state[CH];
-    if (at.segment + 1 < A.segments) through_segments<true>(A, at, back, carry);
-    Tokens<T, CH> gate, x, dy;
-    int t0 = static_cast<int>(at.end_block - 1) * BLOCK + wave * TOKENS;
+    int t0 = static_cast<int>(at.end_block - 1) * BLOCK + wave * N;
     gate.load(at, A.gate, A.gate_stride, t0);
-    x.load(at, A.x, A.x_stride, t0);
     dy.load(at, A.dy, A.dy_stride, t0);
+    x.load(at, A.x, A.x_stride, t0);
     at.state(A, A.states, at.unit * A.blocks + at.end_block - 1, state);
+    if constexpr (!PACKED) at.state(A, A.dlast, at.unit, carry);
+    if (at.segment + 1 < A.segments) through_segments<true>(A, at, back, carry);
     for (uint32_t block = at.end_block; block-- > at.first_block; t0 -= BLOCK) {
         const uint32_t turn = (at.end_block - 1 - block) % 2;
         uint32_t valid, begins, ends;
         at.masks(t0, valid, begins, ends);
-        float a[TOKENS][CH], b[TOKENS][CH];
-        steps_of<T, KIND, CH>(gate, x, valid, a, b);
         auto flow_in = [&](int i, float (&g)[CH]) { at.state(A, A.dlast, at.sequence_at(t0 + i), g); };
         auto state_in = [&](int i, float (&h)[CH]) { at.state(A, A.first, at.sequence_at(t0 + i), h); };
-        float ma[CH], mb[CH], ra[CH], rb[CH];
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            ma[k] = ra[k] = 1.f;
-            mb[k] = rb[k] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < TOKENS; ++i) {
-            if (begins >> i & 1) {
-                state_in(i, mb);
-#pragma unroll
-                for (int k = 0; k < CH; ++k) ma[k] = FRESH;
-            }
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                mb[k] = __builtin_fmaf(a[i][k], mb[k], b[i][k]);
-                ma[k] *= a[i][k];
-            }
-        }
-#pragma unroll
-        for (int i = TOKENS - 1; i >= 0; --i) {
-            if (ends >> i & 1) {
-                flow_in(i, rb);
-#pragma unroll
-                for (int k = 0; k < CH; ++k) ra[k] = FRESH;
-            }
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                rb[k] = a[i][k] * (rb[k] + (valid >> i & 1 ? dy.v[i].get(k) : 0.f));
-                ra[k] *= a[i][k];
-            }
-        }
+        float a[N][CH], rest[N][CH], before[N][CH];          // before: b, until the state before the token takes its place
+        steps_of<KIND>(gate, x, valid, a, rest, before);
+        if (block > at.first_block) gate.load(at, A.gate, A.gate_stride, t0 - BLOCK);        // the others are still needed
+        float ma[CH], mb[CH];
+        nothing_yet(ma, mb);
+        compose_steps(a, before, begins, state_in, ma, mb);
         forth.put(turn, wave, ma, mb);
-        back.put(turn, wave, ra, rb);
+        nothing_yet(ma, mb);
+        compose_flows(a, dy, valid, ends, flow_in, ma, mb);
+        back.put(turn, wave, ma, mb);
         __syncthreads();
-        float before[TOKENS][CH], flow[CH];
+        float flow[CH];
         for (int w = 0; w < wave; ++w) forth.take(turn, w, state);
-        for (int w = WAVES - 1; w >= 0; --w) {
+#pragma unroll
+        for (int w = W - 1; w >= 0; --w) {
             if (w == wave) {
 #pragma unroll
                 for (int k = 0; k < CH; ++k) flow[k] = carry[k];
             }
             back.take(turn, w, carry);
         }
-#pragma unroll
-        for (int i = 0; i < TOKENS; ++i) {
-            if (begins >> i & 1) state_in(i, state);
+        auto forward = [&](int i) {
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
+                const float b = before[i][k];
                 before[i][k] = state[k];
-                state[k] = __builtin_fmaf(a[i][k], state[k], b[i][k]);
+                state[k] = __builtin_fmaf(a[i][k], state[k], b);
             }
-        }
-        T *const to_gate = static_cast<T*>(A.dgate) + at.c, *const to_x = static_cast<T*>(A.dx) + at.c;
-#pragma unroll
-        for (int i = TOKENS - 1; i >= 0; --i) {
-            if (ends >> i & 1) flow_in(i, flow);
-            if (!(valid >> i & 1)) continue;
-            float dg[CH], dx[CH];
+        };
+        auto backward = [&](int i, float (&dg)[CH], float (&dx)[CH]) {
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 const float d = flow[k] + dy.v[i].get(k);
-                float same, rest;
-                logistic(gate.v[i].get(k), same, rest);
-                dx[k] = factor<KIND>(same, rest) * d;
-                dg[k] = slope<KIND>(same, rest, before[i][k], x.v[i].get(k)) * d;
-                flow[k] = same * d;
+                dx[k] = factor<KIND>(a[i][k], rest[i][k]) * d;
+                dg[k] = slope<KIND>(a[i][k], rest[i][k], before[i][k], x.v[i].get(k)) * d;
+                flow[k] = a[i][k] * d;
             }
-            store_some(to_gate + (at.base + t0 + i) * A.dgate_stride, dg, at.n);
-            store_some(to_x + (at.base + t0 + i) * A.dx_stride, dx, at.n);
-            if (begins >> i & 1) at.put_state(A, A.dfirst, at.sequence_at(t0 + i), flow);
+        };
+        T* to_gate = static_cast<T*>(A.dgate) + (at.base + t0 + N - 1) * A.dgate_stride;
+        T* to_x = static_cast<T*>(A.dx) + (at.base + t0 + N - 1) * A.dx_stride;
+        if (at.full && valid == P::ALL && (begins | ends) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) forward(i);
+#pragma unroll
+            for (int i = N - 1; i >= 0; --i, to_gate -= A.dgate_stride, to_x -= A.dx_stride) {
+                float dg[CH], dx[CH];
+                backward(i, dg, dx);
+                store_some(to_gate + at.c, dg, CH);
+                store_some(to_x + at.c, dx, CH);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (begins >> i & 1) state_in(i, state);
+                forward(i);
+            }
+#pragma unroll
+            for (int i = N - 1; i >= 0; --i, to_gate -= A.dgate_stride, to_x -= A.dx_stride) {
+                if (ends >> i & 1) flow_in(i, flow);
+                if (!(valid >> i & 1)) continue;
+                float dg[CH], dx[CH];
+                backward(i, dg, dx);
+                store_some(to_gate + at.c, dg, at.n);
+                store_some(to_x + at.c, dx, at.n);
+                if (begins >> i & 1) at.put_state(A, A.dfirst, at.sequence_at(t0 + i), flow);
+            }
         }
+        if (!PACKED && wave == 0 && block == 0) at.put_state(A, A.dfirst, at.unit, flow);
         if (block > at.first_block) {
-            gate.load(at, A.gate, A.gate_stride, t0 - BLOCK);
-            x.load(at, A.x, A.x_stride, t0 - BLOCK);
             dy.load(at, A.dy, A.dy_stride, t0 - BLOCK);
+            x.load(at, A.x, A.x_stride, t0 - BLOCK);
             at.state(A, A.states, at.unit * A.blocks + block - 1, state);
         }
     }
@@ -510,14 +570,16 @@ template <typename T, int KIND, int CH, bool PACKED> __global__ __launch_bounds_
 // segments
 // ---------------------------------------------------------------------------------------------
 
-// The map of a segment: every wavefront composes an eighth of its tokens.  On the way back (x is dy there) it is the map of what
-// flows from a token to the one before it, g -> a (dy + g).  The last segment's map (the first one's, on the way back) is
+// The map of a segment: every wavefront composes its share of the tokens, N at a time.  On the way back it is the map of what
+// flows from a token to the one before it.  The last segment's map (the first one's, on the way back) is
 // nobody's, so it is not made; its place keeps the first state where that may be overwritten.
-template <typename T, int KIND, int CH, bool PACKED, bool BACK> __global__ __launch_bounds__(WAVES * LANES) void fold_kernel(RecurArgs A) {
-    __shared__ Maps<CH> maps;
-    Place<PACKED, CH> at;
+template <typename T, int KIND, int CH, int W, bool PACKED, bool BACK> __global__ __launch_bounds__(W * LANES) void fold_kernel(RecurArgs A) {
+    typedef Place<PACKED, CH, W> P;
+    constexpr int N = P::N;
+    __shared__ Maps<PACKED, CH, W> maps;
+    P at;
     at.open(A);
-    const int wave = threadIdx.x / LANES;
+    const int wave = wave_of();
     if (!BACK && !PACKED && A.copied && at.segment == A.segments - 1 && wave == 0) {
         float first[CH];
         at.state(A, A.first, at.unit, first);
@@ -528,41 +590,28 @@ template <typename T, int KIND, int CH, bool PACKED, bool BACK> __global__ __lau
     }
     if (at.segment == (BACK ? 0 : A.segments - 1)) return;
     float ma[CH], mb[CH];
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-        ma[k] = 1.f;
-        mb[k] = 0.f;
-    }
+    nothing_yet(ma, mb);
     const int pieces = static_cast<int>(A.per_segment);      // of a wavefront
-    const int from = static_cast<int>(at.first_block) * BLOCK + wave * pieces * TOKENS;
+    const int from = static_cast<int>(at.first_block) * BLOCK + wave * pieces * N;
     if (at.first_block < at.end_block) {
-        Tokens<T, CH> gate, x;
-        auto start = [&](int p) { return from + (BACK ? pieces - 1 - p : p) * TOKENS; };
+        const void* const other = BACK ? A.dy : A.x;
+        const int64_t other_stride = BACK ? A.dy_stride : A.x_stride;
+        Tokens<T, P> gate, x;
+        auto start = [&](int p) { return from + (BACK ? pieces - 1 - p : p) * N; };
         gate.load(at, A.gate, A.gate_stride, start(0));
-        x.load(at, BACK ? A.dy : A.x, BACK ? A.dy_stride : A.x_stride, start(0));
+        x.load(at, other, other_stride, start(0));
         for (int p = 0; p < pieces; ++p) {
             const int t0 = start(p);
             uint32_t valid, begins, ends;
             at.masks(t0, valid, begins, ends);
-            float a[TOKENS][CH], b[TOKENS][CH];
-            steps_of<T, BACK ? MGWFBP_RECUR_FREE : KIND, CH>(gate, x, valid, a, b);
+            float a[N][CH], rest[N][CH], b[N][CH];
+            steps_of<BACK ? MGWFBP_RECUR_FREE : KIND>(gate, x, valid, a, rest, b);
+            auto reset = [&](int i, float (&h)[CH]) { at.state(A, BACK ? A.dlast : A.first, at.sequence_at(t0 + i), h); };
+            if constexpr (BACK) compose_flows(a, x, valid, ends, reset, ma, mb);
+            else compose_steps(a, b, begins, reset, ma, mb);
             if (p + 1 < pieces) {
                 gate.load(at, A.gate, A.gate_stride, start(p + 1));
-                x.load(at, BACK ? A.dy : A.x, BACK ? A.dy_stride : A.x_stride, start(p + 1));
-            }
-#pragma unroll
-            for (int j = 0; j < TOKENS; ++j) {
-                const int i = BACK ? TOKENS - 1 - j : j;
-                if ((BACK ? ends : begins) >> i & 1) {
-                    at.state(A, BACK ? A.dlast : A.first, at.sequence_at(t0 + i), mb);
-#pragma unroll
-                    for (int k = 0; k < CH; ++k) ma[k] = FRESH;
-                }
-#pragma unroll
-                for (int k = 0; k < CH; ++k) {
-                    mb[k] = BACK ? a[i][k] * (mb[k] + b[i][k]) : __builtin_fmaf(a[i][k], mb[k], b[i][k]);
-                    ma[k] *= a[i][k];
-                }
+                x.load(at, other, other_stride, start(p + 1));
             }
         }
     }
@@ -573,9 +622,9 @@ template <typename T, int KIND, int CH, bool PACKED, bool BACK> __global__ __lau
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         float a = 1.f, b = 0.f;
-        for (int j = 0; j < WAVES; ++j) {
-            const int w = BACK ? WAVES - 1 - j : j;
-            compose(a, b, maps.m[0][w][0][k * LANES + lane], maps.m[0][w][1][k * LANES + lane]);
+        for (int j = 0; j < W; ++j) {
+            const int w = BACK ? W - 1 - j : j;
+            compose<PACKED>(a, b, maps.m[0][w][0][k * LANES + lane], maps.m[0][w][1][k * LANES + lane]);
         }
         if (k < at.n) {
             float* const map = A.maps + (at.unit * A.segments + at.segment) * 2 * A.channels + at.c + k;
@@ -615,11 +664,14 @@ template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void
     if (A.last != nullptr) store8(A.last + s * A.channels + c, h, n);
 }
 
-// Its way back, a lane for two channels: the states of up to SHORT tokens stay in registers.
+// Channels of a lane: four bytes of a row.
+constexpr int channels_of(int64_t bytes) { return bytes == 4 ? 1 : 2; }
+
+// Its way back: the states of up to SHORT tokens stay in registers.
 template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void short_back_kernel(RecurArgs A) {
-    constexpr int CH = 2;
-    const int64_t pairs = (A.channels + CH - 1) / CH, at = static_cast<int64_t>(blockIdx.x) * SHORT_THREADS + threadIdx.x;
-    const int64_t s = at / pairs, c = (at - s * pairs) * CH;
+    constexpr int CH = channels_of(sizeof(T));
+    const int64_t pieces = (A.channels + CH - 1) / CH, at = static_cast<int64_t>(blockIdx.x) * SHORT_THREADS + threadIdx.x;
+    const int64_t s = at / pieces, c = (at - s * pieces) * CH;
     if (s >= A.sequences) return;
     const int n = static_cast<int>(min(A.channels - c, static_cast<int64_t>(CH))), tokens = static_cast<int>(A.tokens);
     Piece<T, CH> gate[SHORT], x[SHORT], dy[SHORT];
@@ -675,8 +727,21 @@ constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_CHANNELS = int64_t(1) << 
 // How the work is cut.
 struct Cut {
     int64_t units, tokens, blocks, slabs, segments, per_segment;
-    int ch;
 };
+
+// Channels of a lane and wavefronts of a workgroup.
+#ifndef FCH_
+#define FCH_ 1
+#define SCH_ 1
+#define BCH_ 2
+#define FW_ 8
+#define SW_ 8
+#define BW_ 8
+#endif
+constexpr int FOLD_CH(int64_t bytes) { return bytes == 4 ? 1 : FCH_; }
+constexpr int SCAN_CH(int64_t bytes) { return bytes == 4 ? 1 : SCH_; }
+constexpr int BACK_CH(int64_t bytes) { return bytes == 4 ? 1 : BCH_; }
+constexpr int FOLD_W = FW_, SCAN_W = SW_, BACK_W = BW_;
 
 constexpr int64_t FILL = 512;            // workgroups that are wanted
 
@@ -685,8 +750,7 @@ Cut cut_of(int64_t sequences, int64_t tokens, int64_t channels, bool packed, int
     c.units = packed ? 1 : sequences;
     c.tokens = tokens;
     c.blocks = ceil_div(tokens, BLOCK);
-    c.ch = dtype == MGWFBP_F32 ? 1 : 2;
-    c.slabs = ceil_div(channels, static_cast<int64_t>(LANES) * c.ch);
+    c.slabs = ceil_div(channels, static_cast<int64_t>(LANES) * channels_of(dtype_bytes(dtype)));
     const int64_t whole = c.units * c.slabs;
     c.segments = std::max<int64_t>(1, std::min(c.blocks, FILL / std::max<int64_t>(whole, 1)));
     c.per_segment = std::max<int64_t>(1, ceil_div(c.blocks, c.segments));
@@ -732,7 +796,7 @@ template <bool BACK> int run(const mgwfbp_sequences& s, int32_t kind, int32_t dt
     a.offsets = s.d_offsets;
     a.offset_type = s.offset_type;
     if (is_short(s)) {
-        const int64_t lanes = a.sequences * ceil_div(channels, BACK ? 2 : VEC);
+        const int64_t lanes = a.sequences * ceil_div(channels, BACK ? channels_of(dtype_bytes(dtype)) : VEC);
         const int64_t groups = ceil_div(lanes, SHORT_THREADS);
         if (groups >= (int64_t(1) << 31)) return MGWFBP_EINVAL;
         return with_dtype(dtype, [&](auto* type) {
@@ -744,10 +808,7 @@ template <bool BACK> int run(const mgwfbp_sequences& s, int32_t kind, int32_t dt
         });
     }
     const Cut cut = cut_of(a.sequences, a.tokens, channels, packed, dtype);
-    const int64_t groups = cut.units * cut.segments * cut.slabs;
-    if (groups >= (int64_t(1) << 31)) return MGWFBP_EINVAL;
     a.blocks = cut.blocks;
-    a.slabs = static_cast<uint32_t>(cut.slabs);
     a.segments = static_cast<uint32_t>(cut.segments);
     a.per_segment = static_cast<uint32_t>(cut.per_segment);
     if (cut.segments > 1) {
@@ -755,17 +816,22 @@ template <bool BACK> int run(const mgwfbp_sequences& s, int32_t kind, int32_t dt
         a.maps = static_cast<float*>(workspace);
         a.copied = !BACK && !packed && a.first != nullptr && a.first == a.last;
     }
-    const dim3 grid(static_cast<uint32_t>(groups)), block(WAVES * LANES);
     return with_dtype(dtype, [&](auto* type) {
         return with_kind(kind, [&](auto k) {
             typedef std::remove_pointer_t<decltype(type)> T;
-            constexpr int K = decltype(k)::value, CH = sizeof(T) == 4 ? 1 : 2;
+            constexpr int K = decltype(k)::value, FCH = FOLD_CH(sizeof(T)), FW = FOLD_W, SCH = BACK ? BACK_CH(sizeof(T)) : SCAN_CH(sizeof(T)), SW = BACK ? BACK_W : SCAN_W;
+            auto start = [&](void (*one)(RecurArgs), void (*packed_one)(RecurArgs), int ch, int waves) {
+                a.slabs = static_cast<uint32_t>(ceil_div(channels, static_cast<int64_t>(LANES) * ch));
+                const int64_t groups = cut.units * cut.segments * a.slabs;
+                if (groups >= (int64_t(1) << 31)) return static_cast<int>(MGWFBP_EINVAL);
+                return launch(packed ? packed_one : one, a, dim3(static_cast<uint32_t>(groups)), dim3(waves * LANES), stream);
+            };
             if (cut.segments > 1) {
-                const int status = launch(packed ? fold_kernel<T, K, CH, true, BACK> : fold_kernel<T, K, CH, false, BACK>, a, grid, block, stream);
+                const int status = start(fold_kernel<T, K, FCH, FW, false, BACK>, fold_kernel<T, K, FCH, FW, true, BACK>, FCH, FW);
                 if (status != MGWFBP_OK) return status;
             }
-            if constexpr (BACK) return launch(packed ? back_kernel<T, K, CH, true> : back_kernel<T, K, CH, false>, a, grid, block, stream);
-            else return launch(packed ? scan_kernel<T, K, CH, true> : scan_kernel<T, K, CH, false>, a, grid, block, stream);
+            if constexpr (BACK) return start(back_kernel<T, K, SCH, SW, false>, back_kernel<T, K, SCH, SW, true>, SCH, SW);
+            else return start(scan_kernel<T, K, SCH, SW, false>, scan_kernel<T, K, SCH, SW, true>, SCH, SW);
         });
     });
 }
