@@ -36,7 +36,10 @@ namespace {
 using namespace ops;
 
 constexpr int LANES = 64, BLOCK = MGWFBP_RECUR_BLOCK;
-constexpr int SHORT = 16;                                    // tokens up to which a lane goes through a sequence by itself
+
+// How sequences lie in a unit of work: a sequence is one; several of one length share a block; or between offsets.
+enum { ONE, EVEN, PACKED };
+constexpr int SHORT = 4;                                     // tokens up to which a lane goes through a sequence by itself
 
 struct RecurArgs {
     const void* gate;
@@ -53,7 +56,8 @@ struct RecurArgs {
     float* states;                       // [units][blocks][channels]
     float* maps;                         // [units][segments][2][channels]: A and B of a segment
     int64_t gate_stride, x_stride, dy_stride, y_stride, dgate_stride, dx_stride;
-    int64_t channels, sequences, tokens, blocks;             // tokens and blocks of a unit: of a sequence, or of all of them
+    int64_t channels, sequences, tokens, blocks;             // tokens and blocks of a unit: of a sequence, of those that share a block, or of all
+    int64_t length, rows;                // EVEN: tokens of a sequence, and of all of them
     uint32_t slabs, segments, per_segment;                   // pieces of the channels; pieces of a unit, and their blocks
     int32_t offset_type;
     int32_t copied;                      // first is in the maps' last segment: the caller's may be overwritten by last
@@ -159,8 +163,8 @@ struct Bounds {
 };
 
 // What a wavefront knows of its place: W of them share a block, N tokens each.
-template <bool PACKED_, int CH_, int W> struct Place {
-    static constexpr bool PACKED = PACKED_;
+template <int MODE_, int CH_, int W> struct Place {
+    static constexpr int MODE = MODE_;
     static constexpr int CH = CH_, N = BLOCK / W;
     static constexpr uint32_t ALL = static_cast<uint32_t>((uint64_t(1) << N) - 1);
     Bounds bounds;
@@ -169,19 +173,24 @@ template <bool PACKED_, int CH_, int W> struct Place {
     int n;                               // and how many it has
     bool full;                           // all lanes have CH
     int begin, end;                      // tokens of the unit that are sequences'
+    int length;                          // EVEN: of a sequence
     uint32_t segment, first_block, end_block;
 
     __device__ __forceinline__ void open(const RecurArgs& A) {
         const uint32_t slab = blockIdx.x % A.slabs, rest = blockIdx.x / A.slabs;
         segment = rest % A.segments;
         unit = rest / A.segments;
-        base = PACKED ? 0 : unit * A.tokens;
+        base = MODE == PACKED ? 0 : unit * A.tokens;
         c = (slab * LANES + threadIdx.x % LANES) * CH;
         n = static_cast<int>(max(static_cast<int64_t>(0), min(A.channels - c, static_cast<int64_t>(CH))));
         full = static_cast<int64_t>(slab + 1) * LANES * CH <= A.channels;
         begin = 0;
         end = static_cast<int>(A.tokens);
-        if constexpr (PACKED) {
+        if constexpr (MODE == EVEN) {
+            end = static_cast<int>(min(A.tokens, A.rows - base));
+            length = static_cast<int>(A.length);
+        }
+        if constexpr (MODE == PACKED) {
             bounds.open(A);
             begin = __builtin_amdgcn_readfirstlane(bounds.at(0));
             end = __builtin_amdgcn_readfirstlane(bounds.at(bounds.count - 1));
@@ -196,13 +205,22 @@ template <bool PACKED_, int CH_, int W> struct Place {
         const int lo = min(max(begin - t0, 0), N), hi = min(max(end - t0, 0), N);
         valid = ALL >> (N - hi) & (ALL << lo) & ALL;
         first = last = 0;
-        if constexpr (PACKED) {
-            const uint32_t marks = bounds.template marks<N>(t0);
+        if constexpr (MODE != ONE) {
+            uint32_t marks = 0;
+            if constexpr (MODE == PACKED) {
+                marks = bounds.template marks<N>(t0);
+            } else {
+                for (int t = (t0 + length - 1) / length * length; t <= t0 + N; t += length) marks |= 1u << (t - t0);
+            }
             first = marks & valid;
             last = marks >> 1 & valid;
         }
     }
-    __device__ __forceinline__ int64_t sequence_at(int t) const { return bounds.sequence_of(t); }
+    __device__ __forceinline__ int64_t sequence_at(int t) const {
+        if constexpr (MODE == PACKED) return bounds.sequence_of(t);
+        else if constexpr (MODE == EVEN) return (base + t) / length;
+        else return unit;
+    }
     __device__ __forceinline__ void state(const RecurArgs& A, const float* from, int64_t sequence, float (&out)[CH]) const {
 #pragma unroll
         for (int k = 0; k < CH; ++k) out[k] = from != nullptr && k < n ? from[sequence * A.channels + c + k] : 0.f;
@@ -215,7 +233,7 @@ template <bool PACKED_, int CH_, int W> struct Place {
     }
     // Sequences without tokens hand their state on.
     __device__ __forceinline__ void empty_sequences(const RecurArgs& A, const float* from, float* to) const {
-        if constexpr (PACKED) {
+        if constexpr (MODE == PACKED) {
             if (to == nullptr) return;
             for (int64_t s0 = wave_of() * LANES; s0 < A.sequences; s0 += W * LANES) {
                 const int64_t s = s0 + threadIdx.x % LANES;
@@ -247,18 +265,18 @@ template <typename T, typename P> struct Tokens {
     }
 };
 
-// A map that begins a sequence: it gives b whatever comes in.  Sequences of one length need none: they begin with a workgroup's work.
+// A map that begins a sequence: it gives b whatever comes in.  A unit of one sequence needs none: it begins with what comes in.
 constexpr float FRESH = -0.f;
-template <bool PACKED> __device__ __forceinline__ bool is_fresh(float a) { return PACKED && __builtin_bit_cast(uint32_t, a) == 0x80000000u; }
-template <bool PACKED> __device__ __forceinline__ float through(float a, float b, float h) { return is_fresh<PACKED>(a) ? b : __builtin_fmaf(a, h, b); }
+template <int MODE> __device__ __forceinline__ bool is_fresh(float a) { return MODE != ONE && __builtin_bit_cast(uint32_t, a) == 0x80000000u; }
+template <int MODE> __device__ __forceinline__ float through(float a, float b, float h) { return is_fresh<MODE>(a) ? b : __builtin_fmaf(a, h, b); }
 // (a, b) and then (ma, mb), in (a, b)
-template <bool PACKED> __device__ __forceinline__ void compose(float& a, float& b, float ma, float mb) {
-    b = through<PACKED>(ma, mb, b);
-    a = is_fresh<PACKED>(ma) ? FRESH : a * ma;               // a product of FRESH and a gate is FRESH again
+template <int MODE> __device__ __forceinline__ void compose(float& a, float& b, float ma, float mb) {
+    b = through<MODE>(ma, mb, b);
+    a = is_fresh<MODE>(ma) ? FRESH : a * ma;               // a product of FRESH and a gate is FRESH again
 }
 
 // Maps of wavefronts in LDS, two blocks in turn, so that one barrier a block is enough.
-template <bool PACKED, int CH, int W> struct Maps {
+template <int MODE, int CH, int W> struct Maps {
     float m[2][W][2][LANES * CH];
     __device__ __forceinline__ void put(uint32_t turn, int wave, const float (&a)[CH], const float (&b)[CH]) {
 #pragma unroll
@@ -270,7 +288,7 @@ template <bool PACKED, int CH, int W> struct Maps {
     // h through the map of a wavefront.
     __device__ __forceinline__ void take(uint32_t turn, int wave, float (&h)[CH]) const {
 #pragma unroll
-        for (int k = 0; k < CH; ++k) h[k] = through<PACKED>(m[turn][wave][0][k * LANES + threadIdx.x % LANES], m[turn][wave][1][k * LANES + threadIdx.x % LANES], h[k]);
+        for (int k = 0; k < CH; ++k) h[k] = through<MODE>(m[turn][wave][0][k * LANES + threadIdx.x % LANES], m[turn][wave][1][k * LANES + threadIdx.x % LANES], h[k]);
     }
 };
 
@@ -284,7 +302,7 @@ template <int CH> __device__ __forceinline__ void nothing_yet(float (&ma)[CH], f
 
 // h, which comes into a unit, through the maps of the segments before a workgroup's (or, on the way back, behind it); the wavefronts
 // share them.
-template <bool BACK, bool PACKED, int CH, int W> __device__ __forceinline__ void through_segments(const RecurArgs& A, const Place<PACKED, CH, W>& at, Maps<PACKED, CH, W>& room, float (&h)[CH]) {
+template <bool BACK, int MODE, int CH, int W> __device__ __forceinline__ void through_segments(const RecurArgs& A, const Place<MODE, CH, W>& at, Maps<MODE, CH, W>& room, float (&h)[CH]) {
     const int wave = wave_of();
     const int count = static_cast<int>(BACK ? A.segments - 1 - at.segment : at.segment);
     const int each = (count + W - 1) / W, from = min(wave * each, count), to = min(from + each, count);
@@ -297,7 +315,7 @@ template <bool BACK, bool PACKED, int CH, int W> __device__ __forceinline__ void
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const float ma = k < at.n ? map[k] : 1.f, mb = k < at.n ? map[A.channels + k] : 0.f;
-            compose<PACKED>(a[k], b[k], ma, mb);
+            compose<MODE>(a[k], b[k], ma, mb);
         }
     }
     room.put(1, wave, a, b);
@@ -307,7 +325,7 @@ template <bool BACK, bool PACKED, int CH, int W> __device__ __forceinline__ void
 
 // The first state of a unit of one sequence.  `last` may be the same memory: a workgroup that has a whole unit reads it long before it
 // writes the last state; where there are more, fold_kernel has put it elsewhere.
-template <int CH, int W> __device__ __forceinline__ void unit_first(const RecurArgs& A, const Place<false, CH, W>& at, float (&h)[CH]) {
+template <int CH, int W> __device__ __forceinline__ void unit_first(const RecurArgs& A, const Place<ONE, CH, W>& at, float (&h)[CH]) {
     if (A.copied) {
         const float* const map = A.maps + (at.unit * A.segments + A.segments - 1) * 2 * A.channels + at.c;
 #pragma unroll
@@ -393,10 +411,10 @@ template <int N, int CH, typename T, typename P, typename F> __device__ __forcei
 // forward
 // ---------------------------------------------------------------------------------------------
 
-template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_bounds__(W * LANES) void scan_kernel(RecurArgs A) {
-    typedef Place<PACKED, CH, W> P;
+template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bounds__(W * LANES) void scan_kernel(RecurArgs A) {
+    typedef Place<MODE, CH, W> P;
     constexpr int N = P::N;
-    __shared__ Maps<PACKED, CH, W> maps;
+    __shared__ Maps<MODE, CH, W> maps;
     P at;
     at.open(A);
     const int wave = wave_of();
@@ -407,7 +425,7 @@ template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_
     gate.load(at, A.gate, A.gate_stride, t0);
     x.load(at, A.x, A.x_stride, t0);
     float carry[CH] = {};
-    if constexpr (!PACKED) unit_first(A, at, carry);
+    if constexpr (MODE == ONE) unit_first(A, at, carry);
     if (at.segment > 0) through_segments<false>(A, at, maps, carry);
     for (uint32_t block = at.first_block; block < at.end_block; ++block, t0 += BLOCK) {
         const uint32_t turn = (block - at.first_block) % 2;
@@ -419,16 +437,38 @@ template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_
             gate.load(at, A.gate, A.gate_stride, t0 + BLOCK);
             x.load(at, A.x, A.x_stride, t0 + BLOCK);
         }
-        auto reset = [&](int i, float (&h)[CH]) { at.state(A, A.first, at.sequence_at(t0 + i), h); };
+        // The step of a token that begins a sequence gives its state whatever comes in: its first state is read here and not again, since `last`
+        // may be the same memory.
+        if (begins != 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (!(begins >> i & 1)) continue;
+                float first[CH];
+                at.state(A, A.first, at.sequence_at(t0 + i), first);
+                if (MODE == EVEN) at.put_state(A, A.states, at.sequence_at(t0 + i), first);
+#pragma unroll
+                for (int k = 0; k < CH; ++k) {
+                    b[i][k] = __builtin_fmaf(a[i][k], first[k], b[i][k]);
+                    a[i][k] = FRESH;
+                }
+            }
+        }
         float ma[CH], mb[CH], h[CH];
         nothing_yet(ma, mb);
-        compose_steps(a, b, begins, reset, ma, mb);
+        if (begins == 0) {
+            compose_steps(a, b, 0, [](int, float (&)[CH]) {}, ma, mb);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int k = 0; k < CH; ++k) compose<MODE>(ma[k], mb[k], a[i][k], b[i][k]);
+        }
         maps.put(turn, wave, ma, mb);
         __syncthreads();
-        if (A.states != nullptr && wave == 0 && t0 >= at.begin) {
+        if (MODE != EVEN && A.states != nullptr && wave == 0 && t0 >= at.begin) {
 #pragma unroll
             for (int k = 0; k < CH; ++k) h[k] = carry[k];
-            if (begins & 1) reset(0, h);
+            if (begins & 1) at.state(A, A.first, at.sequence_at(t0), h);         // offsets: first is not last
             at.put_state(A, A.states, at.unit * A.blocks + block, h);
         }
 #pragma unroll
@@ -450,15 +490,14 @@ template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i, row += A.y_stride) {
-                if (begins >> i & 1) reset(i, h);
 #pragma unroll
-                for (int k = 0; k < CH; ++k) h[k] = __builtin_fmaf(a[i][k], h[k], b[i][k]);
+                for (int k = 0; k < CH; ++k) h[k] = through<MODE>(a[i][k], b[i][k], h[k]);
                 if (valid >> i & 1) store_some(row + at.c, h, at.n);
                 if (ends >> i & 1) at.put_state(A, A.last, at.sequence_at(t0 + i), h);
             }
         }
         // tokens behind a sequence's last one have changed nothing
-        if (!PACKED && wave == W - 1 && block + 1 == A.blocks) at.put_state(A, A.last, at.unit, h);
+        if (MODE == ONE && wave == W - 1 && block + 1 == A.blocks) at.put_state(A, A.last, at.unit, h);
     }
 }
 
@@ -466,10 +505,10 @@ template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_
 // backward
 // ---------------------------------------------------------------------------------------------
 
-template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_bounds__(W * LANES) void back_kernel(RecurArgs A) {
-    typedef Place<PACKED, CH, W> P;
+template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bounds__(W * LANES) void back_kernel(RecurArgs A) {
+    typedef Place<MODE, CH, W> P;
     constexpr int N = P::N;
-    __shared__ Maps<PACKED, CH, W> forth, back;
+    __shared__ Maps<MODE, CH, W> forth, back;
     P at;
     at.open(A);
     const int wave = wave_of();
@@ -481,8 +520,11 @@ template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_
     gate.load(at, A.gate, A.gate_stride, t0);
     dy.load(at, A.dy, A.dy_stride, t0);
     x.load(at, A.x, A.x_stride, t0);
-    at.state(A, A.states, at.unit * A.blocks + at.end_block - 1, state);
-    if constexpr (!PACKED) at.state(A, A.dlast, at.unit, carry);
+    if constexpr (MODE != EVEN) at.state(A, A.states, at.unit * A.blocks + at.end_block - 1, state);       // EVEN: every block begins a sequence
+    else
+#pragma unroll
+        for (int k = 0; k < CH; ++k) state[k] = 0.f;
+    if constexpr (MODE == ONE) at.state(A, A.dlast, at.unit, carry);
     if (at.segment + 1 < A.segments) through_segments<true>(A, at, back, carry);
     for (uint32_t block = at.end_block; block-- > at.first_block; t0 -= BLOCK) {
         const uint32_t turn = (at.end_block - 1 - block) % 2;
@@ -557,11 +599,11 @@ template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_
                 if (begins >> i & 1) at.put_state(A, A.dfirst, at.sequence_at(t0 + i), flow);
             }
         }
-        if (!PACKED && wave == 0 && block == 0) at.put_state(A, A.dfirst, at.unit, flow);
+        if (MODE == ONE && wave == 0 && block == 0) at.put_state(A, A.dfirst, at.unit, flow);
         if (block > at.first_block) {
             dy.load(at, A.dy, A.dy_stride, t0 - BLOCK);
             x.load(at, A.x, A.x_stride, t0 - BLOCK);
-            at.state(A, A.states, at.unit * A.blocks + block - 1, state);
+            if constexpr (MODE != EVEN) at.state(A, A.states, at.unit * A.blocks + block - 1, state);
         }
     }
 }
@@ -573,14 +615,14 @@ template <typename T, int KIND, int CH, int W, bool PACKED> __global__ __launch_
 // The map of a segment: every wavefront composes its share of the tokens, N at a time.  On the way back it is the map of what
 // flows from a token to the one before it.  The last segment's map (the first one's, on the way back) is
 // nobody's, so it is not made; its place keeps the first state where that may be overwritten.
-template <typename T, int KIND, int CH, int W, bool PACKED, bool BACK> __global__ __launch_bounds__(W * LANES) void fold_kernel(RecurArgs A) {
-    typedef Place<PACKED, CH, W> P;
+template <typename T, int KIND, int CH, int W, int MODE, bool BACK> __global__ __launch_bounds__(W * LANES) void fold_kernel(RecurArgs A) {
+    typedef Place<MODE, CH, W> P;
     constexpr int N = P::N;
-    __shared__ Maps<PACKED, CH, W> maps;
+    __shared__ Maps<MODE, CH, W> maps;
     P at;
     at.open(A);
     const int wave = wave_of();
-    if (!BACK && !PACKED && A.copied && at.segment == A.segments - 1 && wave == 0) {
+    if (!BACK && MODE == ONE && A.copied && at.segment == A.segments - 1 && wave == 0) {
         float first[CH];
         at.state(A, A.first, at.unit, first);
         float* const map = A.maps + (at.unit * A.segments + at.segment) * 2 * A.channels + at.c;
@@ -624,7 +666,7 @@ template <typename T, int KIND, int CH, int W, bool PACKED, bool BACK> __global_
         float a = 1.f, b = 0.f;
         for (int j = 0; j < W; ++j) {
             const int w = BACK ? W - 1 - j : j;
-            compose<PACKED>(a, b, maps.m[0][w][0][k * LANES + lane], maps.m[0][w][1][k * LANES + lane]);
+            compose<MODE>(a, b, maps.m[0][w][0][k * LANES + lane], maps.m[0][w][1][k * LANES + lane]);
         }
         if (k < at.n) {
             float* const map = A.maps + (at.unit * A.segments + at.segment) * 2 * A.channels + at.c + k;
@@ -691,7 +733,7 @@ template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void
     }
 #pragma unroll
     for (int i = 0; i < SHORT; ++i) {
-        if (i >= tokens) break;
+        if (i >= tokens) continue;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             float a, rest;
@@ -724,35 +766,37 @@ template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void
 
 constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_CHANNELS = int64_t(1) << 23;
 
+// Channels of a lane and wavefronts of a workgroup.
+constexpr int FOLD_CH(int64_t) { return 1; }
+constexpr int SCAN_CH(int64_t) { return 1; }
+constexpr int BACK_CH(int64_t bytes) { return channels_of(bytes); }
+constexpr int FOLD_W = 8, SCAN_W = 8, BACK_W = 8;
+
 // How the work is cut.
 struct Cut {
-    int64_t units, tokens, blocks, slabs, segments, per_segment;
+    int mode;
+    int64_t units, tokens, blocks, segments, per_segment;
 };
 
-// Channels of a lane and wavefronts of a workgroup.
-#ifndef FCH_
-#define FCH_ 1
-#define SCH_ 1
-#define BCH_ 2
-#define FW_ 8
-#define SW_ 8
-#define BW_ 8
-#endif
-constexpr int FOLD_CH(int64_t bytes) { return bytes == 4 ? 1 : FCH_; }
-constexpr int SCAN_CH(int64_t bytes) { return bytes == 4 ? 1 : SCH_; }
-constexpr int BACK_CH(int64_t bytes) { return bytes == 4 ? 1 : BCH_; }
-constexpr int FOLD_W = FW_, SCAN_W = SW_, BACK_W = BW_;
+// Sequences of up to EVEN_MOST tokens share a block: 256 of 20 tokens and 512 bfloat16 channels 28 us each by itself and 9
+// together, back 46 and 21.
+constexpr int64_t EVEN_MOST = BLOCK / 2;
+// Workgroups that are wanted.  Segments cost a launch and a second reading; 8 x 4096 tokens of 1024 bfloat16 channels whole, with 256, 512 and
+// 1024 workgroups: forward 88, 76, 76, 74 us, back 198, 99, 103, 107; 65543 binary16 tokens 1315, 152, 158, 159 and 3272, 213, 235, 244.  Forward, few blocks
+// are faster whole on half the compute units: 8 x 512 tokens bfloat16 12.4 and 13.1 us, binary32 13.7 and 15.9 (back 23 and 18, 19.4 and 20.6).
+constexpr int64_t FILL = 256, WHOLE_FILL = 128, WHOLE_BLOCKS = 8;
 
-constexpr int64_t FILL = 512;            // workgroups that are wanted
-
-Cut cut_of(int64_t sequences, int64_t tokens, int64_t channels, bool packed, int32_t dtype) {
+Cut cut_of(const mgwfbp_sequences& s, int64_t channels, int32_t dtype, bool back) {
     Cut c{};
-    c.units = packed ? 1 : sequences;
-    c.tokens = tokens;
-    c.blocks = ceil_div(tokens, BLOCK);
-    c.slabs = ceil_div(channels, static_cast<int64_t>(LANES) * channels_of(dtype_bytes(dtype)));
-    const int64_t whole = c.units * c.slabs;
+    const int64_t length = s.d_offsets != nullptr ? s.n_tokens : s.n_tokens / s.n_sequences;
+    c.mode = s.d_offsets != nullptr ? PACKED : length <= EVEN_MOST ? EVEN : ONE;
+    const int64_t together = c.mode == EVEN ? std::max<int64_t>(1, BLOCK / std::max<int64_t>(length, 1)) : 1;
+    c.units = c.mode == PACKED ? 1 : ceil_div(s.n_sequences, together);
+    c.tokens = length * together;
+    c.blocks = ceil_div(c.tokens, BLOCK);
+    const int64_t slabs = ceil_div(channels, static_cast<int64_t>(LANES) * channels_of(dtype_bytes(dtype))), whole = c.units * slabs;
     c.segments = std::max<int64_t>(1, std::min(c.blocks, FILL / std::max<int64_t>(whole, 1)));
+    if (!back && c.blocks <= WHOLE_BLOCKS && c.units * ceil_div(channels, LANES) >= WHOLE_FILL) c.segments = 1;
     c.per_segment = std::max<int64_t>(1, ceil_div(c.blocks, c.segments));
     c.segments = std::max<int64_t>(1, ceil_div(c.blocks, c.per_segment));
     return c;
@@ -774,8 +818,12 @@ bool states_ok(const float* p) { return is_aligned(p, 4); }
 
 uint64_t workspace_of(const mgwfbp_sequences& s, int64_t channels, int32_t dtype) {
     if (s.n_sequences == 0 || channels == 0 || is_short(s)) return 0;
-    const Cut c = cut_of(s.n_sequences, unit_tokens(s), channels, s.d_offsets != nullptr, dtype);
-    return c.segments == 1 ? 0 : static_cast<uint64_t>(c.units * c.segments * 2 * channels) * 4;
+    uint64_t bytes = 0;
+    for (const bool back : {false, true}) {
+        const Cut c = cut_of(s, channels, dtype, back);
+        if (c.segments > 1) bytes = std::max(bytes, static_cast<uint64_t>(c.units * c.segments * 2 * channels) * 4);
+    }
+    return bytes;
 }
 
 template <int K> struct Kind { static constexpr int value = K; };
@@ -789,10 +837,10 @@ template <typename F> int with_kind(int32_t kind, F&& f) {
 }
 
 template <bool BACK> int run(const mgwfbp_sequences& s, int32_t kind, int32_t dtype, RecurArgs& a, void* workspace, uint64_t workspace_bytes, void* stream) {
-    const bool packed = s.d_offsets != nullptr;
     const int64_t channels = a.channels;
     a.sequences = s.n_sequences;
-    a.tokens = unit_tokens(s);
+    a.tokens = a.length = unit_tokens(s);
+    a.rows = s.n_tokens;
     a.offsets = s.d_offsets;
     a.offset_type = s.offset_type;
     if (is_short(s)) {
@@ -807,31 +855,32 @@ template <bool BACK> int run(const mgwfbp_sequences& s, int32_t kind, int32_t dt
             });
         });
     }
-    const Cut cut = cut_of(a.sequences, a.tokens, channels, packed, dtype);
+    const Cut cut = cut_of(s, channels, dtype, BACK);
+    a.tokens = cut.tokens;
     a.blocks = cut.blocks;
     a.segments = static_cast<uint32_t>(cut.segments);
     a.per_segment = static_cast<uint32_t>(cut.per_segment);
     if (cut.segments > 1) {
         if (workspace == nullptr || !is_aligned(workspace, 256) || workspace_bytes < workspace_of(s, channels, dtype)) return MGWFBP_EINVAL;
         a.maps = static_cast<float*>(workspace);
-        a.copied = !BACK && !packed && a.first != nullptr && a.first == a.last;
+        a.copied = !BACK && cut.mode == ONE && a.first != nullptr && a.first == a.last;
     }
     return with_dtype(dtype, [&](auto* type) {
         return with_kind(kind, [&](auto k) {
             typedef std::remove_pointer_t<decltype(type)> T;
             constexpr int K = decltype(k)::value, FCH = FOLD_CH(sizeof(T)), FW = FOLD_W, SCH = BACK ? BACK_CH(sizeof(T)) : SCAN_CH(sizeof(T)), SW = BACK ? BACK_W : SCAN_W;
-            auto start = [&](void (*one)(RecurArgs), void (*packed_one)(RecurArgs), int ch, int waves) {
+            auto start = [&](void (*one)(RecurArgs), void (*even)(RecurArgs), void (*packed)(RecurArgs), int ch, int waves) {
                 a.slabs = static_cast<uint32_t>(ceil_div(channels, static_cast<int64_t>(LANES) * ch));
                 const int64_t groups = cut.units * cut.segments * a.slabs;
                 if (groups >= (int64_t(1) << 31)) return static_cast<int>(MGWFBP_EINVAL);
-                return launch(packed ? packed_one : one, a, dim3(static_cast<uint32_t>(groups)), dim3(waves * LANES), stream);
+                return launch(cut.mode == PACKED ? packed : cut.mode == EVEN ? even : one, a, dim3(static_cast<uint32_t>(groups)), dim3(waves * LANES), stream);
             };
             if (cut.segments > 1) {
-                const int status = start(fold_kernel<T, K, FCH, FW, false, BACK>, fold_kernel<T, K, FCH, FW, true, BACK>, FCH, FW);
+                const int status = start(fold_kernel<T, K, FCH, FW, ONE, BACK>, nullptr, fold_kernel<T, K, FCH, FW, PACKED, BACK>, FCH, FW);       // a unit of EVEN is a block
                 if (status != MGWFBP_OK) return status;
             }
-            if constexpr (BACK) return start(back_kernel<T, K, SCH, SW, false>, back_kernel<T, K, SCH, SW, true>, SCH, SW);
-            else return start(scan_kernel<T, K, SCH, SW, false>, scan_kernel<T, K, SCH, SW, true>, SCH, SW);
+            if constexpr (BACK) return start(back_kernel<T, K, SCH, SW, ONE>, back_kernel<T, K, SCH, SW, EVEN>, back_kernel<T, K, SCH, SW, PACKED>, SCH, SW);
+            else return start(scan_kernel<T, K, SCH, SW, ONE>, scan_kernel<T, K, SCH, SW, EVEN>, scan_kernel<T, K, SCH, SW, PACKED>, SCH, SW);
         });
     });
 }
