@@ -126,7 +126,7 @@ int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_
  *   dh = dresidual + rstd * (g - n^ * mean over c of g n^)     (d_dresidual, what flows into h by itself, NULL: 0)
  *   dw[c] = sum over t of dy[t,c] * n^[t,c]                    (d_dw NULL: left out; accumulate != 0 adds to what is there)
  * dh is the gradient of x and of residual alike; d_dx, where not NULL, gets it in dy's type, too.  dresidual and dh are of the stream's
- * type; d_dh may be d_dresidual, with the same stride.  The workspace is needed for dw, and above 16384 channels. */
+ * type; d_dh may be d_dresidual, with the same stride.  The workspace is needed for dw, and above 8192 channels. */
 int mgwfbp_norm_backward_workspace(int64_t n_tokens, int64_t n_channels, uint64_t* bytes_out);
 int mgwfbp_norm_backward(const int8_t* d_q, const float* d_scale, int64_t ld, const float* d_rstd, int64_t n_tokens, int64_t n_channels,
                          const void* d_weight, int32_t weight_dtype, const void* d_dy, int64_t dy_stride, int32_t dtype, const void* d_dresidual,

@@ -72,6 +72,9 @@ struct NormArgs {
 };
 
 // A team of TEAM lanes has a row, V vectors of eight columns a lane: the row stays in registers between the sum and the product.
+// Bound by memory and, in short calls, by the launch and two waits: 4096 tokens of 1024 bfloat16 channels with residual 8.0 us, 34 MB at
+// 4.2 TB/s; 32775 tokens of 4096 binary16 channels on a binary32 stream, with the codes, 410 us, 2.3 GB at 5.5 TB/s.  (Two rows a team at a time, which
+// halves the readings of the weight, are level to 5 % slower.)
 template <typename T, typename S, int TEAM, int V> __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_kernel(NormArgs A) {
     constexpr int THREADS = TEAM < 256 ? 256 : TEAM;
     const uint32_t lane = threadIdx.x % TEAM;
@@ -176,15 +179,12 @@ struct CodeArgs {
 };
 
 constexpr int CODE_THREADS = 256;
-constexpr int LANES = 16;                                    // lanes side by side: 128 channels, whole lines of q and of a 16-bit h
-constexpr int BLOCK_COLS = LANES * VEC;
-constexpr int ROWS = CODE_THREADS / LANES;
-constexpr int STEPS = GROUP / ROWS;
 
-// n = h * rstd in 8 bits: a workgroup has 128 channels of a group of tokens in registers while it looks for the largest magnitude.
-// h has just been written or read and mostly comes from the caches.
-template <typename S> __global__ __launch_bounds__(CODE_THREADS) void code_kernel(CodeArgs A) {
-    const uint32_t g = blockIdx.x / A.col_blocks, cb = blockIdx.x - g * A.col_blocks;
+// n = h * rstd in 8 bits: a workgroup has 8 LANES channels of a group of tokens in registers while it looks for the largest magnitude.
+// h has just been written or read and mostly comes from the caches, the last groups first.
+template <typename S, int LANES> __global__ __launch_bounds__(CODE_THREADS) void code_kernel(CodeArgs A) {
+    constexpr int BLOCK_COLS = LANES * VEC, ROWS = CODE_THREADS / LANES, STEPS = GROUP / ROWS;
+    const uint32_t from_end = blockIdx.x / A.col_blocks, cb = blockIdx.x - from_end * A.col_blocks, g = gridDim.x / A.col_blocks - 1 - from_end;
     const uint32_t lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
     const int64_t col = static_cast<int64_t>(cb) * BLOCK_COLS + lane * VEC;
     const int n = columns_at(A.channels, col);
@@ -208,8 +208,8 @@ template <typename S> __global__ __launch_bounds__(CODE_THREADS) void code_kerne
     __shared__ uint32_t of_wave[CODE_THREADS / 64][BLOCK_COLS];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        most[i] = max(most[i], static_cast<uint32_t>(__shfl_xor(static_cast<int>(most[i]), 16)));
-        most[i] = max(most[i], static_cast<uint32_t>(__shfl_xor(static_cast<int>(most[i]), 32)));
+#pragma unroll
+        for (int d = LANES; d < 64; d *= 2) most[i] = max(most[i], static_cast<uint32_t>(__shfl_xor(static_cast<int>(most[i]), d)));
         if (threadIdx.x % 64 < LANES) of_wave[threadIdx.x / 64][lane * VEC + i] = most[i];
     }
     __syncthreads();
@@ -275,9 +275,13 @@ template <typename T, typename S> __device__ __forceinline__ void finish(const B
 }
 
 // A team of TEAM lanes goes through `rows` consecutive rows, V vectors of eight columns a lane, the next row on its way while one is
-// worked on; the lanes' columns stay the same, so their share of dw stays in registers.
-template <typename T, typename S, int TEAM, int V> __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void back_kernel(BackArgs A) {
-    constexpr int THREADS = TEAM < 256 ? 256 : TEAM, TEAMS = THREADS / TEAM;
+// worked on; the lanes' columns stay the same, so their share of dw stays in registers.  Bound by memory: 32775 tokens of 4096 binary16 channels on
+// a binary32 stream 297 us, 1.5 GB at 5.0 TB/s; 4096 tokens of 1024 bfloat16 channels 12 us, of which joining dw is a launch of 4.
+// Small teams share a workgroup, so that there are few sums of dw to join.
+constexpr int back_threads(int team, int vecs) { return team >= 256 ? team : vecs == 1 ? 1024 : 512; }
+
+template <typename T, typename S, int TEAM, int V> __global__ __launch_bounds__(back_threads(TEAM, V)) void back_kernel(BackArgs A) {
+    constexpr int THREADS = back_threads(TEAM, V), TEAMS = THREADS / TEAM;
     const uint32_t lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
     const int64_t begin = (static_cast<int64_t>(blockIdx.x) * TEAMS + team) * A.rows;
     const int64_t end = min(begin + A.rows, A.tokens);
@@ -322,16 +326,14 @@ template <typename T, typename S, int TEAM, int V> __global__ __launch_bounds__(
 #pragma unroll
             for (int v = 0; v < V; ++v) scale[v] = load8(A.scale + group * A.ld + col[v], n[v]);
         }
-        float dot = 0.f, normed[V][VEC], g[V][VEC];
+        float dot = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                normed[v][i] = code_of(now.q[v], i) * get(scale[v], i);
-                const float dy = get(now.dy[v], i);
-                sum[v][i] = __builtin_fmaf(dy, normed[v][i], sum[v][i]);
-                g[v][i] = dy * w[v][i];
-                dot = __builtin_fmaf(g[v][i], normed[v][i], dot);
+                const float normed = code_of(now.q[v], i) * get(scale[v], i), dy = get(now.dy[v], i);
+                sum[v][i] = __builtin_fmaf(dy, normed, sum[v][i]);
+                dot = __builtin_fmaf(dy * w[v][i], normed, dot);
             }
         if constexpr (TEAM <= 64) dot = lanes_sum<TEAM>(dot);
         else dot = workgroup_sum<TEAM>(dot, room + (t % 2) * (TEAM / 64));
@@ -341,7 +343,7 @@ template <typename T, typename S, int TEAM, int V> __global__ __launch_bounds__(
             if (n[v] <= 0) continue;
             float grad[VEC];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) grad[i] = now.rstd * (g[v][i] - normed[v][i] * mean);
+            for (int i = 0; i < VEC; ++i) grad[i] = now.rstd * (get(now.dy[v], i) * w[v][i] - code_of(now.q[v], i) * get(scale[v], i) * mean);
             finish<T, S>(A, t, col[v], n[v], grad, now.dres[v]);
         }
     }
@@ -452,9 +454,13 @@ __global__ __launch_bounds__(JOIN_COLS * JOIN_ROWS) void join_kernel(JoinArgs A)
 
 // ---- host side -------------------------------------------------------------------------------
 
-constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_CHANNELS = int64_t(1) << 23, TEAM_CHANNELS = 16384;
+constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_CHANNELS = int64_t(1) << 23, TEAM_CHANNELS = 16384, BACK_TEAM_CHANNELS = 8192;
 
-// Calls f with the team and the vectors of a lane for rows of `channels` columns, up to TEAM_CHANNELS.
+// Pieces of 128 channels and 128 tokens below which a workgroup takes half of one: 1003 tokens of 1001 binary32 channels 5.9 and 4.8 us; beyond, whole lines of
+// q are better: 32775 tokens of 4096 channels 412 and 435 us for norm and codes.
+constexpr int64_t NARROW_BELOW = 256;
+
+// Calls f with the team and the vectors of a lane for rows of `channels` columns, up to BACK_TEAM_CHANNELS.
 template <int T_, int V_> struct Shape { static constexpr int team = T_, vecs = V_; };
 template <typename F> auto with_shape(int64_t channels, F&& f) {
     if (channels <= 128) return f(Shape<16, 1>());
@@ -462,8 +468,7 @@ template <typename F> auto with_shape(int64_t channels, F&& f) {
     if (channels <= 1024) return f(Shape<64, 2>());
     if (channels <= 2048) return f(Shape<256, 1>());
     if (channels <= 4096) return f(Shape<256, 2>());
-    if (channels <= 8192) return f(Shape<512, 2>());
-    return f(Shape<1024, 2>());
+    return f(Shape<512, 2>());
 }
 
 // How the way back is cut: workgroups, rows of a team (or of a tile).
@@ -474,15 +479,15 @@ struct Cut {
 Cut cut_of(int64_t tokens, int64_t channels) {
     Cut c{};
     c.padded = ceil_div(channels, VEC) * VEC;
-    c.wide = channels > TEAM_CHANNELS;
+    c.wide = channels > BACK_TEAM_CHANNELS;
     if (c.wide) {
         c.rows = std::max<int64_t>(16, ceil_div(tokens, std::max<int64_t>(1, 1024 / ceil_div(channels, TILE * VEC))));
         c.rows = std::max(c.rows, ceil_div(tokens, 65535));
         c.workgroups = ceil_div(tokens, c.rows);
         return c;
     }
-    const int64_t teams = with_shape(channels, [](auto s) { return static_cast<int64_t>(decltype(s)::team < 256 ? 256 / decltype(s)::team : 1); });
-    c.rows = ceil_div(ceil_div(tokens, 512), teams);
+    const int64_t teams = with_shape(channels, [](auto s) { return static_cast<int64_t>(back_threads(decltype(s)::team, decltype(s)::vecs) / decltype(s)::team); });
+    c.rows = ceil_div(tokens, (teams > 1 ? 256 : 512) * teams);
     c.workgroups = ceil_div(tokens, c.rows * teams);
     return c;
 }
@@ -526,7 +531,8 @@ int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_
         return MGWFBP_EINVAL;
     if (keep && (!kept_ok(d_q, d_scale, d_rstd, n_tokens, n_channels, ld) || !is_aligned(d_linear_scale, 16))) return MGWFBP_EINVAL;
     CodeArgs c{};
-    c.col_blocks = static_cast<uint32_t>(ceil_div(n_channels, BLOCK_COLS));
+    const bool narrow = ceil_div(n_channels, 128) * ceil_div(n_tokens, GROUP) < NARROW_BELOW;
+    c.col_blocks = static_cast<uint32_t>(ceil_div(n_channels, narrow ? 64 : 128));
     const int64_t code_blocks = c.col_blocks * ceil_div(n_tokens, GROUP);
     if (keep && code_blocks >= (int64_t(1) << 24)) return MGWFBP_EINVAL;
     NormArgs a{};
@@ -548,6 +554,7 @@ int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_
         typedef std::remove_pointer_t<decltype(type)> T;
         typedef std::remove_pointer_t<decltype(stream_type)> S;
         if (n_channels > TEAM_CHANNELS) return launch(norm_long_kernel<T, S>, a, dim3(static_cast<uint32_t>(n_tokens)), dim3(1024), hip_stream);
+        if (n_channels > BACK_TEAM_CHANNELS) return launch(norm_kernel<T, S, 1024, 2>, a, dim3(static_cast<uint32_t>(n_tokens)), dim3(1024), hip_stream);
         return with_shape(n_channels, [&](auto s) {
             constexpr int TEAM = decltype(s)::team, THREADS = TEAM < 256 ? 256 : TEAM;
             void (*kernel)(NormArgs) = norm_kernel<T, S, TEAM, decltype(s)::vecs>;
@@ -567,7 +574,8 @@ int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_
     c.channels = n_channels;
     c.weight_type = weight_dtype;
     return with_dtype(stream_dtype, [&](auto* type) {
-        return launch(code_kernel<std::remove_pointer_t<decltype(type)>>, c, dim3(static_cast<uint32_t>(code_blocks)), dim3(CODE_THREADS), hip_stream);
+        typedef std::remove_pointer_t<decltype(type)> S;
+        return launch(narrow ? code_kernel<S, 8> : code_kernel<S, 16>, c, dim3(static_cast<uint32_t>(code_blocks)), dim3(CODE_THREADS), hip_stream);
     });
 }
 
@@ -637,8 +645,8 @@ int mgwfbp_norm_backward(const int8_t* d_q, const float* d_scale, int64_t ld, co
                           hip_stream);
         }
         return with_shape(n_channels, [&](auto s) {
-            constexpr int TEAM = decltype(s)::team, THREADS = TEAM < 256 ? 256 : TEAM;
-            void (*kernel)(BackArgs) = back_kernel<T, S, TEAM, decltype(s)::vecs>;
+            constexpr int TEAM = decltype(s)::team, V = decltype(s)::vecs, THREADS = back_threads(TEAM, V);
+            void (*kernel)(BackArgs) = back_kernel<T, S, TEAM, V>;
             return launch(kernel, a, dim3(static_cast<uint32_t>(cut.workgroups)), dim3(THREADS), hip_stream);
         });
     });
