@@ -177,7 +177,11 @@ template <int MODE_, int CH_, int W> struct Place {
     uint32_t segment, first_block, end_block;
 
     __device__ __forceinline__ void open(const RecurArgs& A) {
-        const uint32_t slab = blockIdx.x % A.slabs, rest = blockIdx.x / A.slabs;
+        // Workgroups go round the eight dies; each die takes a stretch of the work, so that it has whole rows, all their lines.
+        constexpr uint32_t DIES = 8;
+        const uint32_t die = blockIdx.x % DIES, share = gridDim.x / DIES, more = gridDim.x % DIES;
+        const uint32_t work = die * share + min(die, more) + blockIdx.x / DIES;
+        const uint32_t slab = work % A.slabs, rest = work / A.slabs;
         segment = rest % A.segments;
         unit = rest / A.segments;
         base = MODE == PACKED ? 0 : unit * A.tokens;
@@ -197,6 +201,17 @@ template <int MODE_, int CH_, int W> struct Place {
         }
         first_block = segment * A.per_segment;
         end_block = min(first_block + A.per_segment, static_cast<uint32_t>((end + BLOCK - 1) / BLOCK));
+    }
+    // The lane's distance from a row's first element, in bytes and 32 bits, made anew where it is used: memory instructions add it to an address
+    // that all lanes share, if the compiler sees both; carried along in 64 bits it would cost an addition for every access.
+    template <typename T> __device__ __forceinline__ uint32_t lane_bytes() const {
+        uint32_t bytes = static_cast<uint32_t>(c * sizeof(T));
+        asm volatile("" : "+v"(bytes));
+        return bytes;
+    }
+    template <typename T> static __device__ __forceinline__ T* in(T* row, uint32_t bytes) {
+        typedef std::conditional_t<std::is_const_v<T>, const char, char> byte;
+        return reinterpret_cast<T*>(reinterpret_cast<byte*>(row) + bytes);
     }
     __device__ __forceinline__ int row(int t) const { return min(max(t, begin), max(end - 1, 0)); }      // one that may be read
     __device__ __forceinline__ bool whole(int t0) const { return full && t0 >= begin && t0 + N <= end; }
@@ -256,8 +271,9 @@ template <typename T, typename P> struct Tokens {
     __device__ __forceinline__ void load(const P& at, const void* from, int64_t stride, int t0) {
         if (at.whole(t0)) {
             const T* row = static_cast<const T*>(from) + (at.base + t0) * stride;
+            const uint32_t bytes = at.template lane_bytes<T>();
 #pragma unroll
-            for (int i = 0; i < P::N; ++i, row += stride) v[i].load(row + at.c);
+            for (int i = 0; i < P::N; ++i, row += stride) v[i].load(at.in(row, bytes));
         } else {
 #pragma unroll
             for (int i = 0; i < P::N; ++i) v[i].load(static_cast<const T*>(from) + (at.base + at.row(t0 + i)) * stride + at.c, at.n);
@@ -346,12 +362,14 @@ template <int KIND, typename T, typename P> __device__ __forceinline__ void step
             b[i][k] = factor<KIND>(a[i][k], rest[i][k]) * x.v[i].get(k);
         }
     if (valid != P::ALL) {
+        // taken here, so that the selections stay in the branch
+        const uint32_t some = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(valid)));
 #pragma unroll
         for (int i = 0; i < P::N; ++i)
 #pragma unroll
             for (int k = 0; k < P::CH; ++k) {
-                a[i][k] = valid >> i & 1 ? a[i][k] : 1.f;
-                b[i][k] = valid >> i & 1 ? b[i][k] : 0.f;
+                a[i][k] = some >> i & 1 ? a[i][k] : 1.f;
+                b[i][k] = some >> i & 1 ? b[i][k] : 0.f;
             }
     }
 }
@@ -481,11 +499,12 @@ template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bou
         }
         T* row = static_cast<T*>(A.y) + (at.base + t0) * A.y_stride;
         if (at.full && valid == P::ALL && (begins | ends) == 0) {
+            const uint32_t bytes = at.template lane_bytes<T>();
 #pragma unroll
             for (int i = 0; i < N; ++i, row += A.y_stride) {
 #pragma unroll
                 for (int k = 0; k < CH; ++k) h[k] = __builtin_fmaf(a[i][k], h[k], b[i][k]);
-                store_some(row + at.c, h, CH);
+                store_some(at.in(row, bytes), h, CH);
             }
         } else {
 #pragma unroll
@@ -573,14 +592,15 @@ template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bou
         T* to_gate = static_cast<T*>(A.dgate) + (at.base + t0 + N - 1) * A.dgate_stride;
         T* to_x = static_cast<T*>(A.dx) + (at.base + t0 + N - 1) * A.dx_stride;
         if (at.full && valid == P::ALL && (begins | ends) == 0) {
+            const uint32_t bytes = at.template lane_bytes<T>();
 #pragma unroll
             for (int i = 0; i < N; ++i) forward(i);
 #pragma unroll
             for (int i = N - 1; i >= 0; --i, to_gate -= A.dgate_stride, to_x -= A.dx_stride) {
                 float dg[CH], dx[CH];
                 backward(i, dg, dx);
-                store_some(to_gate + at.c, dg, CH);
-                store_some(to_x + at.c, dx, CH);
+                store_some(at.in(to_gate, bytes), dg, CH);
+                store_some(at.in(to_x, bytes), dx, CH);
             }
         } else {
 #pragma unroll
