@@ -655,7 +655,7 @@ int mgwfbp_distill(const void* d_z, int64_t z_stride, int32_t dtype, int64_t n_t
     if (n_tokens == 0) return MGWFBP_OK;
     const int64_t bytes = dtype_bytes(dtype);
     if (!side_ok(d_z, n_tokens, n_vocabulary, z_stride, bytes) || (d_dz != nullptr && !side_ok(d_dz, n_tokens, n_vocabulary, dz_stride, bytes)) ||
-        d_loss == nullptr || !is_aligned(d_loss, 4) || !is_aligned(d_row_weight, 4))
+        (d_dz == d_z && n_tokens > 1 && dz_stride != z_stride) || d_loss == nullptr || !is_aligned(d_loss, 4) || !is_aligned(d_row_weight, 4))
         return MGWFBP_EINVAL;
     if (n_top > 0 && (!side_ok(d_ids, n_tokens, n_top, ids_stride, id_type == MGWFBP_I64 ? 8 : 4) ||
                       !side_ok(d_teacher, n_tokens, n_top, teacher_stride, dtype_bytes(teacher_dtype))))

@@ -475,7 +475,7 @@ PyObject* recur_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         const float *const kept = call.states(states, rows, channels), *const f = call.states(first, s.n_sequences, channels),
                     *const l = call.states(dlast, s.n_sequences, channels);
         float* const df = call.states(dfirst, s.n_sequences, channels);
-        if (!call.ok) return not_this_way();
+        if (!call.ok || (l != nullptr && l == df)) return not_this_way();
         at::Tensor keep;
         void* const space = bytes == 0 && given == nullptr ? nullptr : call.workspace(given, bytes, keep, size);
         if (!call.ok) return not_this_way();

@@ -527,7 +527,8 @@ int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_
     if (keep != (d_rstd != nullptr) || keep != (d_scale != nullptr) || keep != (d_linear_scale != nullptr)) return MGWFBP_EINVAL;
     if (!side_ok(d_x, n_tokens, n_channels, x_stride, dtype) || !side_ok(d_y, n_tokens, n_channels, y_stride, dtype)) return MGWFBP_EINVAL;
     if (d_residual != nullptr && (!side_ok(d_residual, n_tokens, n_channels, residual_stride, stream_dtype) ||
-                                  !side_ok(d_h, n_tokens, n_channels, h_stride, stream_dtype)))
+                                  !side_ok(d_h, n_tokens, n_channels, h_stride, stream_dtype) ||
+                                  (d_h == d_residual && n_tokens > 1 && h_stride != residual_stride)))
         return MGWFBP_EINVAL;
     if (keep && (!kept_ok(d_q, d_scale, d_rstd, n_tokens, n_channels, ld) || !is_aligned(d_linear_scale, 16))) return MGWFBP_EINVAL;
     CodeArgs c{};
@@ -604,7 +605,8 @@ int mgwfbp_norm_backward(const int8_t* d_q, const float* d_scale, int64_t ld, co
     if (n_tokens == 0) return d_dw == nullptr || accumulate ? static_cast<int>(MGWFBP_OK) : launch(join_kernel, j, join_grid, dim3(JOIN_COLS * JOIN_ROWS), hip_stream);
     if (!kept_ok(d_q, d_scale, d_rstd, n_tokens, n_channels, ld) || !side_ok(d_dy, n_tokens, n_channels, dy_stride, dtype) ||
         !side_ok(d_dh, n_tokens, n_channels, dh_stride, stream_dtype) ||
-        (d_dresidual != nullptr && !side_ok(d_dresidual, n_tokens, n_channels, dresidual_stride, stream_dtype)) ||
+        (d_dresidual != nullptr && (!side_ok(d_dresidual, n_tokens, n_channels, dresidual_stride, stream_dtype) ||
+                                    (d_dh == d_dresidual && n_tokens > 1 && dh_stride != dresidual_stride))) ||
         (d_dx != nullptr && !side_ok(d_dx, n_tokens, n_channels, dx_stride, dtype)))
         return MGWFBP_EINVAL;
     const Cut cut = cut_of(n_tokens, n_channels);

@@ -339,8 +339,8 @@ template <bool BACK, int MODE, int CH, int W> __device__ __forceinline__ void th
     for (int w = 0; w < W; ++w) room.take(1, w, h);          // turn 1 is written again after another barrier
 }
 
-// The first state of a unit of one sequence.  `last` may be the same memory: a workgroup that has a whole unit reads it long before it
-// writes the last state; where there are more, fold_kernel has put it elsewhere.
+// The first state of a unit of one sequence.  `last` may be the same memory: a workgroup that has a whole unit has read it before its first
+// barrier and writes the last state behind it; where there are more, fold_kernel has put it elsewhere.
 template <int CH, int W> __device__ __forceinline__ void unit_first(const RecurArgs& A, const Place<ONE, CH, W>& at, float (&h)[CH]) {
     if (A.copied) {
         const float* const map = A.maps + (at.unit * A.segments + A.segments - 1) * 2 * A.channels + at.c;
@@ -482,6 +482,10 @@ template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bou
                 for (int k = 0; k < CH; ++k) compose<MODE>(ma[k], mb[k], a[i][k], b[i][k]);
         }
         maps.put(turn, wave, ma, mb);
+        if constexpr (MODE == ONE) {                         // what came in is here, and not on its way, when another wavefront may write over it
+#pragma unroll
+            for (int k = 0; k < CH; ++k) asm volatile("" ::"v"(carry[k]));
+        }
         __syncthreads();
         if (MODE != EVEN && A.states != nullptr && wave == 0 && t0 >= at.begin) {
 #pragma unroll
@@ -956,7 +960,7 @@ int mgwfbp_recur_backward(const mgwfbp_sequences* sequences, int64_t n_channels,
     if (!side_ok(d_gate, tokens, n_channels, gate_stride, dtype) || !side_ok(d_x, tokens, n_channels, x_stride, dtype) ||
         !side_ok(d_dy, tokens, n_channels, dy_stride, dtype) || !side_ok(d_dgate, tokens, n_channels, dgate_stride, dtype) ||
         !side_ok(d_dx, tokens, n_channels, dx_stride, dtype) || !states_ok(d_first) || !states_ok(d_states) || !states_ok(d_dlast) || !states_ok(d_dfirst) ||
-        (tokens > 0 && !is_short(*sequences) && d_states == nullptr) || !is_matrix(sequences->n_sequences, n_channels, n_channels, 4))
+        (tokens > 0 && !is_short(*sequences) && d_states == nullptr) || (d_dlast != nullptr && d_dlast == d_dfirst) || !is_matrix(sequences->n_sequences, n_channels, n_channels, 4))
         return MGWFBP_EINVAL;
     RecurArgs a{};
     a.gate = d_gate;

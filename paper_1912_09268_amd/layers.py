@@ -498,6 +498,8 @@ def recur_backward(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, dy
         _fail(f"gate has type {gate.dtype}")
     sides = [_tokens(t, name, gate, tokens, channels) for t, name in ((gate, "gate"), (x, "x"), (dy, "dy"), (dgate, "dgate"), (dx, "dx"))]
     first_at, dlast_at, dfirst_at = (_states(t, name, sequences.n_sequences, channels) for t, name in ((first, "first"), (dlast, "dlast"), (dfirst, "dfirst")))
+    if dlast_at and dlast_at == dfirst_at:
+        _fail("dfirst must be other memory than dlast")
     states_at = _states(states, "states", B.recur_states(sequences), channels)
     with _on(device) as stream:
         space = _workspace(workspace, B.recur_workspace(sequences, channels, _DTYPES[gate.dtype]), device)

@@ -25,7 +25,7 @@ def test_norm_refuses():
                 dict(d_residual=0, d_h=0), dict(n_tokens=-1), dict(n_tokens=2 ** 26 + 1), dict(n_channels=-1), dict(n_channels=2 ** 23 + 1), dict(d_weight=P + 2),
                 dict(weight_dtype=7), dict(eps=0.0), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(d_y=0), dict(d_y=P + 1), dict(y_stride=19), dict(d_rstd=0),
                 dict(d_q=0), dict(d_scale=0), dict(d_linear_scale=0), dict(d_rstd=P + 2), dict(d_q=P + 8), dict(d_scale=P + 4), dict(d_linear_scale=P + 4), dict(ld=16),
-                dict(ld=40)):
+                dict(ld=40), dict(d_h=P, residual_stride=21), dict(d_residual=2 * P, d_h=2 * P, h_stride=24)):
         _refused(B.norm, *{**good, **bad}.values())
     B.norm(*{**good, "n_tokens": 0, "d_x": 0, "d_residual": 0, "d_y": 0, "d_q": 0}.values())
     back = dict(d_q=P, d_scale=P, ld=32, d_rstd=P, n_tokens=9, n_channels=20, d_weight=P, weight_dtype=B.BF16, d_dy=P, dy_stride=20, dtype=B.BF16, d_dresidual=P,
@@ -34,7 +34,7 @@ def test_norm_refuses():
     for bad in (dict(d_q=0), dict(d_q=P + 8), dict(d_scale=0), dict(d_scale=P + 8), dict(ld=20), dict(ld=16), dict(d_rstd=0), dict(n_tokens=-1), dict(n_tokens=2 ** 26 + 1),
                 dict(n_channels=2 ** 23 + 1), dict(d_weight=P + 1), dict(weight_dtype=-1), dict(d_dy=0), dict(dy_stride=19), dict(dtype=9), dict(d_dresidual=P + 2),
                 dict(dresidual_stride=19), dict(d_dh=0), dict(dh_stride=19), dict(stream_dtype=B.F16), dict(d_dx=P + 1), dict(dx_stride=19), dict(d_dw=P + 2), dict(grad_dtype=3),
-                dict(d_workspace=0), dict(d_workspace=P + 64), dict(workspace_bytes=B.norm_backward_workspace(9, 20) - 1),
+                dict(d_dh=P, dh_stride=21), dict(d_workspace=0), dict(d_workspace=P + 64), dict(workspace_bytes=B.norm_backward_workspace(9, 20) - 1),
                 dict(n_channels=20000, ld=20000, dy_stride=20000, dh_stride=20000, dx_stride=20000, dresidual_stride=20000, d_dw=0, d_workspace=0)):
         _refused(B.norm_backward, *{**back, **bad}.values())
     B.norm_backward(*{**back, "n_tokens": 0, "d_q": 0, "d_dw": 0, "d_workspace": 0}.values())
@@ -47,7 +47,7 @@ def test_recur_refuses():
     good = dict(sequences=one, n_channels=20, kind=B.UNIT, dtype=B.BF16, d_gate=P, gate_stride=20, d_x=P, x_stride=20, d_first=P, d_y=P, y_stride=20, d_last=2 * P,
                 d_states=P, d_workspace=P, workspace_bytes=1 << 20)
     back = dict(sequences=one, n_channels=20, kind=B.UNIT, dtype=B.BF16, d_gate=P, gate_stride=20, d_x=P, x_stride=20, d_first=P, d_states=P, d_dy=P, dy_stride=20,
-                d_dlast=P, d_dgate=P, dgate_stride=20, d_dx=P, dx_stride=20, d_dfirst=P, d_workspace=P, workspace_bytes=1 << 20)
+                d_dlast=P, d_dgate=P, dgate_stride=20, d_dx=P, dx_stride=20, d_dfirst=2 * P, d_workspace=P, workspace_bytes=1 << 20)
     wrong = [B.Sequences(-1, 300, 0, 0), B.Sequences(7, 300, 0, 0), B.Sequences(3, -3, 0, 0), B.Sequences(3, 3 * 2 ** 25, 0, 0), B.Sequences(0, 5, 0, 0), B.Sequences(3, 300, P + 4, B.I64),
              B.Sequences(3, 300, P, 2), B.Sequences(2 ** 26 + 1, 0, 0, 0)]
     assert B.recur_workspace(one, 20, B.BF16) > 0
@@ -57,7 +57,7 @@ def test_recur_refuses():
     for bad in common + [dict(d_y=0), dict(y_stride=19), dict(d_last=P + 2), dict(sequences=packed, d_last=P)]:
         _refused(B.recur, *{**good, **bad}.values())
     for bad in common + [dict(d_states=0), dict(d_dy=0), dict(dy_stride=19), dict(d_dlast=P + 2), dict(d_dgate=0), dict(dgate_stride=19), dict(d_dx=0), dict(dx_stride=19),
-                         dict(d_dfirst=P + 1)]:
+                         dict(d_dfirst=P + 1), dict(d_dfirst=P)]:
         _refused(B.recur_backward, *{**back, **bad}.values())
     none = B.Sequences(0, 0, 0, 0)
     B.recur(*{**good, "sequences": none, "d_gate": 0}.values())
@@ -77,7 +77,8 @@ def test_distill_refuses():
                 dict(d_labels=P + 4), dict(label_type=2), dict(d_ids=0), dict(d_ids=P + 2), dict(ids_stride=3), dict(id_type=-1), dict(d_teacher=0), dict(d_teacher=P + 1),
                 dict(teacher_stride=3), dict(teacher_dtype=4), dict(n_top=-1), dict(n_top=B.MAX_TOP + 1, ids_stride=9999, teacher_stride=9999), dict(temperature=0.0),
                 dict(temperature=-1.0), dict(temperature=math.nan), dict(temperature=math.inf), dict(label_weight=math.nan), dict(teacher_weight=math.inf), dict(d_row_weight=P + 2),
-                dict(d_loss=0), dict(d_loss=P + 2), dict(d_dz=P + 1), dict(dz_stride=49)):
+                dict(d_loss=0), dict(d_loss=P + 2), dict(d_dz=P + 1), dict(dz_stride=49),
+                dict(dz_stride=51)):
         _refused(B.distill, *{**good, **bad}.values())
     size = B.distill_workspace(2, 100000, 4)                  # few rows, cut into parts
     long = dict(n_tokens=2, n_vocabulary=100000, z_stride=100000, dz_stride=100000, d_workspace=P, workspace_bytes=size)
@@ -187,5 +188,7 @@ def test_both_ways_take_and_refuse_the_same(way, monkeypatch):
         layers.norm(x[:65], w, residual=over.view(65, 96)[:, :48], y=y[:65], h=over[:65])
     with pytest.raises(ValueError):
         layers.recur(x, r, offsets=torch.tensor([0, 130], device=d), first=first, last=first, y=y)
+    with pytest.raises(ValueError):
+        layers.recur_backward(x, r, states, x, dlast=first, dfirst=first, dgate=y, dx=h)
     with pytest.raises(ValueError):
         layers.norm(x, w, y=y, kept=kept._replace(linear=layers.Act8(kept.act.q, kept.act.scale[:1], 48)))

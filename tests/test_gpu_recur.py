@@ -254,6 +254,27 @@ def test_offsets_that_are_wrong_lead_nowhere_else(offsets):
     assert bool((whole[0] == 7).all()) and bool((whole[2] == 7).all()) and bool((last[0] == 7).all()) and bool((last[3] == 7).all()) and not bool(states[-1].any())
 
 
+def test_sequences_without_tokens_or_channels():
+    first = torch.randn(3, 8, device="cuda")
+    last, dfirst = torch.empty(3, 8, device="cuda"), torch.empty(3, 8, device="cuda")
+    none = torch.empty(3, 0, 8, device="cuda")
+    states = layers.recur_empty(none)
+    assert states.shape == (0, 8) and layers.recur(none, none, first=first, last=last, states=states).shape == none.shape
+    assert torch.equal(last, first)
+    layers.recur(none, none, last=last)
+    assert not bool(last.any())
+    layers.recur_backward(none, none, states, none, dlast=first, dfirst=dfirst)
+    assert torch.equal(dfirst, first)
+    for shape in ((0, 5, 8), (3, 5, 0), (0, 8), (5, 0)):
+        t = torch.empty(shape, device="cuda")
+        states = layers.recur_empty(t)
+        assert layers.recur(t, t, states=states).shape == shape
+        assert layers.recur_backward(t, t, states, t)[0].shape == shape
+    offsets = torch.zeros(1, dtype=torch.int64, device="cuda")           # no sequence at all
+    t = torch.randn(7, 8, device="cuda")
+    assert not bool(layers.recur(t, t, offsets=offsets).any())
+
+
 def test_step_by_step_is_the_whole():
     """An answer's tokens one by one, the state going in and out in place, against all at once."""
     g = _gen(3)
