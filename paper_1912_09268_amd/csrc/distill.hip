@@ -18,6 +18,7 @@
 
 #include "device_types.h"
 #include "mgwfbp_layers.h"
+#include "teams.h"
 
 namespace {
 
@@ -58,9 +59,7 @@ __device__ __forceinline__ int32_t id_at(const void* p, int32_t type, int64_t i,
 // Over the lanes of a workgroup, in every lane: the largest of each of N numbers, or the sum.  `room` is used once.
 template <int THREADS, int N, typename F> __device__ __forceinline__ void workgroup_all(float (&x)[N], float (*room)[N], F&& join) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int d = 32; d > 0; d /= 2) x[i] = join(x[i], __shfl_xor(x[i], d));
+    for (int i = 0; i < N; ++i) x[i] = lanes_all<64>(x[i], join);
     if constexpr (THREADS > 64) {
         if (threadIdx.x % 64 == 0)
 #pragma unroll
@@ -71,9 +70,7 @@ template <int THREADS, int N, typename F> __device__ __forceinline__ void workgr
         const int w = threadIdx.x % WAVES;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            x[i] = room[w][i];
-#pragma unroll
-            for (int d = WAVES / 2; d > 0; d /= 2) x[i] = join(x[i], __shfl_xor(x[i], d));
+            x[i] = lanes_all<WAVES>(room[w][i], join);
         }
     }
 }

@@ -25,16 +25,19 @@ __device__ __forceinline__ double from_lane(double x, int lane) {
     return __builtin_bit_cast(double, static_cast<uint64_t>(high) << 32 | low);
 }
 
-// The sum of x over the wavefront's aligned pieces of 16 or 64 lanes, in every lane, in one order: neighbours, pairs, mirrored halves of eight, of
+// join of x over the wavefront's aligned pieces of LANES lanes, in every lane, in one order: neighbours, pairs, mirrored halves of eight, of
 // sixteen, and the four sixteens.
-template <int LANES, typename F> __device__ __forceinline__ F lanes_sum(F x) {
-    static_assert(LANES == 16 || LANES == 64);
-    x += lane_of<0xb1>(x);                                   // 1 0 3 2
-    x += lane_of<0x4e>(x);                                   // 2 3 0 1
-    x += lane_of<0x141>(x);                                  // eight lanes mirrored
-    x += lane_of<0x140>(x);                                  // sixteen lanes mirrored
-    if constexpr (LANES == 64) x = (from_lane(x, 0) + from_lane(x, 16)) + (from_lane(x, 32) + from_lane(x, 48));
+template <int LANES, typename F, typename J> __device__ __forceinline__ F lanes_all(F x, J&& join) {
+    static_assert(LANES == 1 || LANES == 2 || LANES == 4 || LANES == 8 || LANES == 16 || LANES == 64);
+    if constexpr (LANES > 1) x = join(x, lane_of<0xb1>(x));  // 1 0 3 2
+    if constexpr (LANES > 2) x = join(x, lane_of<0x4e>(x));  // 2 3 0 1
+    if constexpr (LANES > 4) x = join(x, lane_of<0x141>(x)); // eight lanes mirrored
+    if constexpr (LANES > 8) x = join(x, lane_of<0x140>(x)); // sixteen lanes mirrored
+    if constexpr (LANES == 64) x = join(join(from_lane(x, 0), from_lane(x, 16)), join(from_lane(x, 32), from_lane(x, 48)));
     return x;
+}
+template <int LANES, typename F> __device__ __forceinline__ F lanes_sum(F x) {
+    return lanes_all<LANES>(x, [](F a, F b) { return a + b; });
 }
 
 // The sum of x over the THREADS lanes of a workgroup, in every lane; `room` holds a number for each wavefront and may be used
