@@ -41,7 +41,9 @@ constexpr int LANES = 64, BLOCK = MGWFBP_RECUR_BLOCK;
 
 // How sequences lie in a unit of work: a sequence is one; several of one length share a block; or between offsets.
 enum { ONE, EVEN, PACKED };
-constexpr int SHORT = 4;                                     // tokens up to which a lane goes through a sequence by itself
+// Tokens up to which a lane goes through a sequence by itself.  Us forward and back, 1024 bfloat16 channels, that and blocks: 8 sequences of 8 tokens 6.8 and 7.3,
+// 6.2 and 14.9; 256 of 6 6.7 and 10.4, 8.2 and 24.6; 4096 of 8 51 and 129, 76 and 131.  Twice as many: 256 of 16 13.9 and 22.9, 9.8 and 16.1.
+constexpr int SHORT = 8;
 
 struct RecurArgs {
     const void* gate;
@@ -431,6 +433,8 @@ template <int N, int CH, typename T, typename P, typename F> __device__ __forcei
 // forward
 // ---------------------------------------------------------------------------------------------
 
+// Bound by memory: with the chip full the data passes once at 5.1 TB/s, what a large copy reaches (65543 tokens of 1024 binary16 channels, 403 MB, 83 us; with the
+// segments' maps before it 154).  32 x 128 tokens of 512 channels, in one block each, 5.7 us.
 template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bounds__(W * LANES) void scan_kernel(RecurArgs A) {
     typedef Place<MODE, CH, W> P;
     constexpr int N = P::N;
@@ -530,6 +534,8 @@ template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bou
 // backward
 // ---------------------------------------------------------------------------------------------
 
+// Bound by memory: gate, x and dy in, dgate and dx out, a state for every 128 tokens: 32775 tokens of 1001 binary32 channels, 37 sequences one behind the other, 656 MB, 143 us,
+// 4.6 TB/s; with the segments' maps 212.  8 x 512 tokens of 1024 bfloat16 channels 11 us and 4 for the maps.
 template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bounds__(W * LANES) void back_kernel(RecurArgs A) {
     typedef Place<MODE, CH, W> P;
     constexpr int N = P::N;
@@ -640,7 +646,10 @@ template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bou
 
 // The map of a segment: every wavefront composes its share of the tokens, N at a time.  On the way back it is the map of what
 // flows from a token to the one before it.  The last segment's map (the first one's, on the way back) is
-// nobody's, so it is not made; its place keeps the first state where that may be overwritten.
+// nobody's, so it is not made; its place keeps the first state where that may be overwritten.  Bound by memory: 65543 tokens of 1024 binary16 channels 75 us, 268 MB at
+// 3.6 TB/s, and as much again is read by the launch behind it.  Workgroups of a block each that wait within one launch for the maps of the blocks before theirs read
+// everything once; they were 154 -> 516 us forward and 214 -> 251 back here, since the some 500 workgroups that fit the chip are one stretch of the chain after the other,
+// each with its loads, its wait and its stores by themselves; only wide binary32 rows gained on the way back (2 x 16384 tokens 184 -> 145).
 template <typename T, int KIND, int CH, int W, int MODE, bool BACK> __global__ __launch_bounds__(W * LANES) void fold_kernel(RecurArgs A) {
     typedef Place<MODE, CH, W> P;
     constexpr int N = P::N;
@@ -708,7 +717,8 @@ template <typename T, int KIND, int CH, int W, int MODE, bool BACK> __global__ _
 
 constexpr int SHORT_THREADS = 256;
 
-// A lane goes through eight channels of a sequence: a step of an answer is one token.
+// A lane goes through eight channels of a sequence: a step of an answer is one token.  Bound by the launch (8 sequences of one token: 3.0 us, 3.9 the call); 4096 of
+// 8 tokens and 1024 bfloat16 channels 51 us, 3.9 TB/s.
 template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void short_scan_kernel(RecurArgs A) {
     const int64_t vecs = (A.channels + VEC - 1) / VEC, at = static_cast<int64_t>(blockIdx.x) * SHORT_THREADS + threadIdx.x;
     const int64_t s = at / vecs, c = (at - s * vecs) * VEC;
@@ -719,15 +729,25 @@ template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void
 #pragma unroll
     for (int k = 0; k < VEC; ++k) h[k] = get(first, k);
     if (A.states != nullptr && A.tokens > 0) store8(A.states + s * A.channels + c, h, n);
-    for (int64_t t = s * A.tokens; t < (s + 1) * A.tokens; ++t) {
-        const Raw8<T> gate = load8(static_cast<const T*>(A.gate) + t * A.gate_stride + c, n), x = load8(static_cast<const T*>(A.x) + t * A.x_stride + c, n);
+    const int64_t t0 = s * A.tokens;
+    const int tokens = static_cast<int>(A.tokens);
+    Raw8<T> gate, x, next_gate, next_x;
+    const auto ask = [&](int i, Raw8<T>& gate_of, Raw8<T>& x_of) {
+        gate_of = load8(static_cast<const T*>(A.gate) + (t0 + i) * A.gate_stride + c, i < tokens ? n : 0);
+        x_of = load8(static_cast<const T*>(A.x) + (t0 + i) * A.x_stride + c, i < tokens ? n : 0);
+    };
+    ask(0, next_gate, next_x);
+    for (int i = 0; i < tokens; ++i) {
+        gate = next_gate;
+        x = next_x;
+        ask(i + 1, next_gate, next_x);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
             float a, rest;
             logistic(get(gate, k), a, rest);
             h[k] = __builtin_fmaf(a, h[k], factor<KIND>(a, rest) * get(x, k));
         }
-        store8(static_cast<T*>(A.y) + t * A.y_stride + c, h, n);
+        store8(static_cast<T*>(A.y) + (t0 + i) * A.y_stride + c, h, n);
     }
     if (A.last != nullptr) store8(A.last + s * A.channels + c, h, n);
 }
@@ -735,30 +755,31 @@ template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void
 // Channels of a lane: four bytes of a row.
 constexpr int channels_of(int64_t bytes) { return bytes == 4 ? 1 : 2; }
 
-// Its way back: the states of up to SHORT tokens stay in registers.
-template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void short_back_kernel(RecurArgs A) {
+// Its way back: the states of up to MOST tokens stay in registers, for four tokens fewer of them: 4096 sequences of 1 token and 1024 bfloat16 channels 18 us, 24 with
+// room for eight.
+template <typename T, int KIND, int MOST> __global__ __launch_bounds__(SHORT_THREADS) void short_back_kernel(RecurArgs A) {
     constexpr int CH = channels_of(sizeof(T));
     const int64_t pieces = (A.channels + CH - 1) / CH, at = static_cast<int64_t>(blockIdx.x) * SHORT_THREADS + threadIdx.x;
     const int64_t s = at / pieces, c = (at - s * pieces) * CH;
     if (s >= A.sequences) return;
     const int n = static_cast<int>(min(A.channels - c, static_cast<int64_t>(CH))), tokens = static_cast<int>(A.tokens);
-    Piece<T, CH> gate[SHORT], x[SHORT], dy[SHORT];
+    Piece<T, CH> gate[MOST], x[MOST], dy[MOST];
 #pragma unroll
-    for (int i = 0; i < SHORT; ++i) {
+    for (int i = 0; i < MOST; ++i) {
         const int64_t t = s * tokens + i;
         const int m = i < tokens ? n : 0;
         gate[i].load(static_cast<const T*>(A.gate) + t * A.gate_stride + c, m);
         x[i].load(static_cast<const T*>(A.x) + t * A.x_stride + c, m);
         dy[i].load(static_cast<const T*>(A.dy) + t * A.dy_stride + c, m);
     }
-    float h[CH], flow[CH], before[SHORT][CH];
+    float h[CH], flow[CH], before[MOST][CH];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         h[k] = A.first != nullptr && k < n ? A.first[s * A.channels + c + k] : 0.f;
         flow[k] = A.dlast != nullptr && k < n ? A.dlast[s * A.channels + c + k] : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < SHORT; ++i) {
+    for (int i = 0; i < MOST; ++i) {
         if (i >= tokens) continue;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
@@ -769,7 +790,7 @@ template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void
         }
     }
 #pragma unroll
-    for (int i = SHORT - 1; i >= 0; --i) {
+    for (int i = MOST - 1; i >= 0; --i) {
         if (i >= tokens) continue;
         float dg[CH], dx[CH];
 #pragma unroll
@@ -792,7 +813,8 @@ template <typename T, int KIND> __global__ __launch_bounds__(SHORT_THREADS) void
 
 constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_CHANNELS = int64_t(1) << 23;
 
-// Channels of a lane and wavefronts of a workgroup.
+// Channels of a lane and wavefronts of a workgroup.  65543 binary16 tokens of 1024 channels, one channel a lane and two: forward 86 and 99 us, back 192 and 158, the maps of the way
+// back 68 and 90.  Sixteen wavefronts of eight tokens are level.
 constexpr int FOLD_CH(int64_t) { return 1; }
 constexpr int SCAN_CH(int64_t) { return 1; }
 constexpr int BACK_CH(int64_t bytes) { return channels_of(bytes); }
@@ -876,7 +898,8 @@ template <bool BACK> int run(const mgwfbp_sequences& s, int32_t kind, int32_t dt
         return with_dtype(dtype, [&](auto* type) {
             return with_kind(kind, [&](auto k) {
                 typedef std::remove_pointer_t<decltype(type)> T;
-                void (*kernel)(RecurArgs) = BACK ? short_back_kernel<T, decltype(k)::value> : short_scan_kernel<T, decltype(k)::value>;
+                constexpr int K = decltype(k)::value;
+                void (*kernel)(RecurArgs) = !BACK ? short_scan_kernel<T, K> : a.tokens <= SHORT / 2 ? short_back_kernel<T, K, SHORT / 2> : short_back_kernel<T, K, SHORT>;
                 return launch(kernel, a, dim3(static_cast<uint32_t>(groups)), dim3(SHORT_THREADS), stream);
             });
         });

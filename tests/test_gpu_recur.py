@@ -160,7 +160,7 @@ def _strided_like(t, how):
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("sequences,length,channels", [(1, 1, 1), (8, 1, 1024), (3, 2, 7), (5, 16, 130), (4, 17, 65), (2, 127, 64), (2, 128, 129), (3, 129, 33), (1, 500, 200), (2, 1000, 24), (3, 4, 70), (300, 5, 40), (77, 13, 64), (50, 63, 20), (41, 64, 130),
-                                                       (700, 20, 9), (1, 4099, 16), (600, 130, 5), (2, 300, 1)])
+                                                       (700, 20, 9), (1, 4099, 16), (600, 130, 5), (2, 300, 1), (5, 6, 130), (9, 7, 33), (40, 8, 65), (40, 9, 65)])
 def test_sequences_of_one_length(sequences, length, channels, kind, dtype):
     how = "strided" if (length + channels) % 2 else "dense"
     _say("one length", sequences, length, channels, kind, dtype, how)
