@@ -73,7 +73,7 @@ struct NormArgs {
 
 // A team of TEAM lanes has a row, V vectors of eight columns a lane: the row stays in registers between the sum and the product.
 // Bound by memory and, in short calls, by the launch and two waits: 4096 tokens of 1024 bfloat16 channels with residual 8.0 us, 34 MB at
-// 4.2 TB/s; 32775 tokens of 4096 binary16 channels on a binary32 stream, with the codes, 410 us, 2.3 GB at 5.5 TB/s.  (Two rows a team at a time, which
+// 4.2 TB/s; 32775 tokens of 4096 binary16 channels on a binary32 stream, with the codes, 400 us, 2.3 GB at 5.6 TB/s.  (Two rows a team at a time, which
 // halves the readings of the weight, are level to 5 % slower.)
 template <typename T, typename S, int TEAM, int V> __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void norm_kernel(NormArgs A) {
     constexpr int THREADS = TEAM < 256 ? 256 : TEAM;
@@ -181,7 +181,8 @@ struct CodeArgs {
 constexpr int CODE_THREADS = 256;
 
 // n = h * rstd in 8 bits: a workgroup has 8 LANES channels of a group of tokens in registers while it looks for the largest magnitude.
-// h has just been written or read and mostly comes from the caches, the last groups first.
+// h has just been written or read and mostly comes from the caches, the last groups first.  Its magnitudes are known behind the whole group alone, so the norm,
+// which has whole rows, cannot make them: 4096 tokens of 1024 bfloat16 channels 5.0 us, 13 MB, a launch and two waits.
 template <typename S, int LANES> __global__ __launch_bounds__(CODE_THREADS) void code_kernel(CodeArgs A) {
     constexpr int BLOCK_COLS = LANES * VEC, ROWS = CODE_THREADS / LANES, STEPS = GROUP / ROWS;
     const uint32_t from_end = blockIdx.x / A.col_blocks, cb = blockIdx.x - from_end * A.col_blocks, g = gridDim.x / A.col_blocks - 1 - from_end;
@@ -276,7 +277,7 @@ template <typename T, typename S> __device__ __forceinline__ void finish(const B
 
 // A team of TEAM lanes goes through `rows` consecutive rows, V vectors of eight columns a lane, the next row on its way while one is
 // worked on; the lanes' columns stay the same, so their share of dw stays in registers.  Bound by memory: 32775 tokens of 4096 binary16 channels on
-// a binary32 stream 297 us, 1.5 GB at 5.0 TB/s; 4096 tokens of 1024 bfloat16 channels 12 us, of which joining dw is a launch of 4.
+// a binary32 stream 291 us, 1.5 GB at 5.1 TB/s; 4096 tokens of 1024 bfloat16 channels 12 us, of which joining dw is a launch of 4.
 // Small teams share a workgroup, so that there are few sums of dw to join.
 constexpr int back_threads(int team, int vecs) { return team >= 256 ? team : vecs == 1 ? 1024 : 512; }
 
@@ -460,14 +461,17 @@ constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_CHANNELS = int64_t(1) << 
 // q are better: 32775 tokens of 4096 channels 412 and 435 us for norm and codes.
 constexpr int64_t NARROW_BELOW = 256;
 
-// Calls f with the team and the vectors of a lane for rows of `channels` columns, up to BACK_TEAM_CHANNELS.
+// Calls f with the team and the vectors of a lane for rows of `channels` columns, up to BACK_TEAM_CHANNELS.  Us forward and back, bfloat16, the other shape
+// behind the one taken: 65536 tokens of 128 channels 16 x 1 12 and 14, 64 x 1 27 and 30; 32768 of 512 64 x 1 25 and 30, 16 x 4 25 and 53; 32768 of 1024
+// 64 x 2 46 and 53, 256 x 1 58 and 86; 8192 of 2048 256 x 1 25 and 31, 64 x 4 26 and 53; 32775 of 4096, binary16 on a binary32 stream, 512 x 1 280 and 291,
+// 256 x 2 293 and 296; 4096 of 6000 512 x 2 41 and 59, 1024 x 1 45 and 57.
 template <int T_, int V_> struct Shape { static constexpr int team = T_, vecs = V_; };
 template <typename F> auto with_shape(int64_t channels, F&& f) {
     if (channels <= 128) return f(Shape<16, 1>());
     if (channels <= 512) return f(Shape<64, 1>());
     if (channels <= 1024) return f(Shape<64, 2>());
     if (channels <= 2048) return f(Shape<256, 1>());
-    if (channels <= 4096) return f(Shape<256, 2>());
+    if (channels <= 4096) return f(Shape<512, 1>());
     return f(Shape<512, 2>());
 }
 
