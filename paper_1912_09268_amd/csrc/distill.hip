@@ -218,7 +218,9 @@ template <typename T> __device__ __forceinline__ void add(const Raw8<T>& r, int 
 
 constexpr int AHEAD = 4;                 // vectors of a lane on their way where a row does not stay in registers
 
-// V vectors of eight elements a lane hold a row of eight elements or more; V = 0: they do not.
+// V vectors of eight elements a lane hold a row of eight elements or more; V = 0: they do not.  Bound by memory, and by the exponentials where there are two
+// softmaxes: 4096 rows of 30522 bfloat16 logits, 500 MB, with labels alone 94 us, 5.3 TB/s, with labels and 64 entries at another temperature 106; 129 rows of 100003
+// binary32 logits, too long for registers, 31 us, 3.3 TB/s (4.9 counting both readings), as long as the last of them.
 //
 // The last vector of a row that is no multiple of eight begins before its place, so that it ends with the row; lanes behind it take it, too.
 // What they have in common with the lane before is neither summed twice nor, being the same, wrong where it is written twice.
@@ -596,13 +598,25 @@ template <typename T> __global__ __launch_bounds__(64) void tiny_kernel(DistillA
 bool side_ok(const void* p, int64_t rows, int64_t width, int64_t stride, int64_t bytes) { return p != nullptr && is_aligned(p, bytes) && is_matrix(rows, width, stride, bytes); }
 bool ids_ok(int32_t type) { return type == MGWFBP_I32 || type == MGWFBP_I64; }
 
+// Lanes and vectors of a lane for a row, and wavefronts a SIMD.  Few lanes with many vectors have fewer barriers and joins, many lanes with few have
+// registers for more rows at once.  Us, bfloat16, labels and 32 entries unless said otherwise, the other shape behind the one taken:
+//   16384 rows of 512 logits            64 x 1    20    256 x 1     45
+//   16384 rows of 2048 logits           64 x 4    38    256 x 1     56      labels alone 28, 38; 128 entries, 2000 rows: 26, 16
+//   8192 rows of 8192 logits           256 x 4    59    1024 x 1    97
+//   4096 rows of 16384 logits          512 x 4    60    1024 x 2    75
+//   4096 rows of 30522 logits          512 x 8   106    1024 x 4   113      labels alone 106, 94, so theirs is the other; binary32 199, 194
+//   2048 rows of 50001 logits         1024 x 8   105    re-read    157
+//   1024 rows of 100003 logits        1024 x 16  132    re-read    137      (of 131072: 151, 145)
 template <int T_, int V_, int P_> struct Shape { static constexpr int threads = T_, vecs = V_, per_simd = P_; };
-template <typename T, typename F> int with_shape(int64_t vocabulary, F&& f) {
+template <typename T, typename F> int with_shape(int64_t vocabulary, int32_t top, bool both, F&& f) {
     constexpr bool WIDE = sizeof(T) == 4;
     if (vocabulary <= 512) return f(Shape<64, 1, 8>());
+    if (vocabulary <= 2048 && top <= 64) return f(Shape<64, 4, WIDE ? 6 : 8>());
     if (vocabulary <= 2048) return f(Shape<256, 1, 8>());
     if (vocabulary <= 8192) return f(Shape<256, 4, WIDE ? 6 : 8>());
     if (vocabulary <= 16384) return f(Shape<512, 4, WIDE ? 6 : 8>());
+    if constexpr (!WIDE)
+        if (both && vocabulary <= 32768) return f(Shape<512, 8, 4>());
     if (vocabulary <= 32768) return f(Shape<1024, 4, WIDE ? 4 : 8>());
     if (vocabulary <= 65536) return f(Shape<1024, 8, WIDE ? 4 : 8>());
     if constexpr (!WIDE)
@@ -704,7 +718,7 @@ int mgwfbp_distill(const void* d_z, int64_t z_stride, int32_t dtype, int64_t n_t
             if (cut.vecs == 4) return of(part_kernel<T, 4>, part_slope_kernel<T, 4>);
             return of(part_kernel<T, 8>, part_slope_kernel<T, 8>);
         }
-        return with_shape<T>(n_vocabulary, [&](auto s) {
+        return with_shape<T>(n_vocabulary, n_top, d_labels != nullptr && n_top > 0 && temperature != 1.f, [&](auto s) {
             constexpr int THREADS = decltype(s)::threads;
             void (*kernel)(DistillArgs) = distill_kernel<T, THREADS, decltype(s)::vecs, decltype(s)::per_simd>;
             return launch(kernel, a, dim3(static_cast<uint32_t>(n_tokens)), dim3(THREADS), hip_stream, Entries<THREADS>::bytes(n_top));

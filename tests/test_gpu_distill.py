@@ -86,7 +86,7 @@ def _case(tokens, vocabulary, top, dtype, seed, how="dense", teacher_t="f32", id
 
 
 SIZES = [(1, 1, 1), (1, 131072, 64), (5, 3, 2), (7, 512, 8), (9, 513, 33), (33, 2048, 64), (8, 2049, 1), (6, 8191, 100), (5, 16385, 17), (9, 30522, 64), (4, 32769, 16),
-         (3, 65536, 8), (4, 100003, 40), (3, 131073, 5), (2, 200001, 1000), (65, 1000, 0), (101, 40001, 9), (70, 66001, 3), (110, 131100, 4)]
+         (3, 65536, 8), (4, 100003, 40), (3, 131073, 5), (2, 200001, 1000), (65, 1000, 0), (101, 40001, 9), (70, 66001, 3), (110, 131100, 4), (6, 1500, 65), (5, 16384, 5), (200, 20003, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
