@@ -113,11 +113,11 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
  *   rstd[t] = 1 / sqrt(mean over c of h[t,c]^2 + eps);  n = h * rstd;  y = n * weight          (d_weight NULL: 1)
  * The mean is a binary64 sum, rstd is rounded to binary32 once, n and y are binary32 products, y rounded to x's type.
  * x and y are of one type, residual and h of the same or of MGWFBP_F32.  d_h may be d_residual, with the same stride; otherwise outputs
- * overlap nothing.  d_residual and d_h are NULL together (stream_dtype is dtype then).  eps 2^-100..2^100.
+ * overlap nothing (y over h, or over an x of which n is kept, is refused).  d_residual and d_h are NULL together (stream_dtype is dtype then).  eps 2^-100..2^100.
  * Where d_q is not NULL, n is kept for mgwfbp_norm_backward as a checkpoint (above) of q and scale, with rstd [n_tokens]; and
  * linear_scale, as large as scale, is scale * weight: q and linear_scale are a checkpoint of n * weight, of y before its rounding, for
  * mgwfbp_act_linear_grad.  d_rstd, d_q, d_scale and d_linear_scale are NULL together.
- *   n_tokens 0..2^26, n_channels 0..2^23 */
+ *   n_tokens 0..2^26, n_channels 0..2^23; of 2^32 lanes or more (a row takes up to 1024) a call is refused, here and below */
 int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_residual, int64_t residual_stride, int32_t stream_dtype,
                 int64_t n_tokens, int64_t n_channels, const void* d_weight, int32_t weight_dtype, double eps, void* d_h, int64_t h_stride,
                 void* d_y, int64_t y_stride, float* d_rstd, int8_t* d_q, float* d_scale, float* d_linear_scale, int64_t ld, void* hip_stream);

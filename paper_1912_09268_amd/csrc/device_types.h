@@ -138,6 +138,7 @@ int note(hipError_t e);
 
 // Launch of `kernel` with its one argument structure, and `lds` bytes of LDS beside what the kernel declares.
 template <typename A> int launch(void (*kernel)(A), const A& args, dim3 grid, dim3 block, void* stream, int lds = 0) {
+    if (static_cast<uint64_t>(grid.x) * block.x >> 32 != 0) return MGWFBP_EINVAL;        // more lanes than a launch can number
     void* list[] = {const_cast<A*>(&args)};
     const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, list, static_cast<size_t>(lds), static_cast<hipStream_t>(stream));
     if (e != hipSuccess) (void)hipGetLastError();        // reported here, not to whoever asks next

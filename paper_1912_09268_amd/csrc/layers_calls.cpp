@@ -355,7 +355,8 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             ld = q->size(1);
         }
         float* const r = static_cast<float*>(call.vector(rstd, tokens, at::kFloat));
-        if (!call.ok || (h != nullptr && (h->scalar_type() != residual->scalar_type() || (h->data_ptr() == residual->data_ptr() && h_stride != r_stride))))
+        if (!call.ok || (h != nullptr && (h->scalar_type() != residual->scalar_type() || (h->data_ptr() == residual->data_ptr() && h_stride != r_stride))) ||
+            (h != nullptr ? y->data_ptr() == h->data_ptr() : q != nullptr && y->data_ptr() == x->data_ptr()))
             return not_this_way();
         const int type = dtype_of(*x), stream_type = residual == nullptr ? type : dtype_of(*residual), w_type = weight == nullptr ? 0 : dtype_of(*weight);
         if (stream_type != type && stream_type != MGWFBP_F32) return not_this_way();

@@ -534,6 +534,7 @@ int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_
                                   !side_ok(d_h, n_tokens, n_channels, h_stride, stream_dtype) ||
                                   (d_h == d_residual && n_tokens > 1 && h_stride != residual_stride)))
         return MGWFBP_EINVAL;
+    if (d_h != nullptr ? d_y == d_h : keep && d_y == d_x) return MGWFBP_EINVAL;         // the codes are made of h, behind y
     if (keep && (!kept_ok(d_q, d_scale, d_rstd, n_tokens, n_channels, ld) || !is_aligned(d_linear_scale, 16))) return MGWFBP_EINVAL;
     CodeArgs c{};
     const bool narrow = ceil_div(n_channels, 128) * ceil_div(n_tokens, GROUP) < NARROW_BELOW;

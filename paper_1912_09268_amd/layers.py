@@ -335,7 +335,7 @@ def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optio
     """h = x + residual and y = h / sqrt(mean(h^2) + eps) * weight over the channels of x [tokens, channels]; returns (y, h).
 
     weight [channels] (None: 1).  residual, and h with it, are of x's type or float32; h may be residual, None makes a new tensor; without a residual
-    h is x.  y is of x's type.  `kept` (norm_empty) takes what norm_backward and the next layer's act_linear_grad need."""
+    h is x.  y is of x's type; it is other memory than h.  `kept` (norm_empty) takes what norm_backward and the next layer's act_linear_grad need."""
     if y is not None and (residual is None) == (h is None) and isinstance(eps, float):
         act, rstd, linear = (None, None, None) if kept is None else kept
         if kept is None or (linear.q is act.q and linear.channels == act.channels):
@@ -360,6 +360,8 @@ def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optio
         h_stride = _matrix(h, "h", tokens, channels, (stream_type,))
         if _same_place(h, residual) and h_stride != res_stride:
             _fail("h over residual must have its strides")
+    if tokens and channels and (_same_place(y, h) if h is not None else kept is not None and _same_place(y, x)):
+        _fail("y must be other memory than h, and than an x that is kept in 8 bits")
     ld = 0
     if kept is not None:
         rows, ld = _kept(kept)

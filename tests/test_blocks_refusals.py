@@ -25,8 +25,11 @@ def test_norm_refuses():
                 dict(d_residual=0, d_h=0), dict(n_tokens=-1), dict(n_tokens=2 ** 26 + 1), dict(n_channels=-1), dict(n_channels=2 ** 23 + 1), dict(d_weight=P + 2),
                 dict(weight_dtype=7), dict(eps=0.0), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(d_y=0), dict(d_y=P + 1), dict(y_stride=19), dict(d_rstd=0),
                 dict(d_q=0), dict(d_scale=0), dict(d_linear_scale=0), dict(d_rstd=P + 2), dict(d_q=P + 8), dict(d_scale=P + 4), dict(d_linear_scale=P + 4), dict(ld=16),
-                dict(ld=40), dict(d_h=P, residual_stride=21), dict(d_residual=2 * P, d_h=2 * P, h_stride=24)):
+                dict(ld=40), dict(d_y=4 * P, d_h=4 * P), dict(d_residual=0, d_h=0, stream_dtype=B.BF16, d_y=P), dict(d_h=P, residual_stride=21), dict(d_residual=2 * P, d_h=2 * P, h_stride=24)):
         _refused(B.norm, *{**good, **bad}.values())
+    wide = dict(n_tokens=2 ** 24, n_channels=9000, d_h=2 * P, d_y=4 * P, **{k: 9000 for k in ("x_stride", "residual_stride", "h_stride", "y_stride")}, d_rstd=0, d_q=0,
+                d_scale=0, d_linear_scale=0)                          # 2^34 lanes
+    _refused(B.norm, *{**good, **wide}.values())
     B.norm(*{**good, "n_tokens": 0, "d_x": 0, "d_residual": 0, "d_y": 0, "d_q": 0}.values())
     back = dict(d_q=P, d_scale=P, ld=32, d_rstd=P, n_tokens=9, n_channels=20, d_weight=P, weight_dtype=B.BF16, d_dy=P, dy_stride=20, dtype=B.BF16, d_dresidual=P,
                 dresidual_stride=20, d_dh=P, dh_stride=20, stream_dtype=B.F32, d_dx=P, dx_stride=20, accumulate=False, d_dw=P, grad_dtype=B.F32, d_workspace=P,
@@ -188,6 +191,9 @@ def test_both_ways_take_and_refuse_the_same(way, monkeypatch):
         layers.norm(x[:65], w, residual=over.view(65, 96)[:, :48], y=y[:65], h=over[:65])
     with pytest.raises(ValueError):
         layers.recur(x, r, offsets=torch.tensor([0, 130], device=d), first=first, last=first, y=y)
+    for more in (dict(y=x, kept=kept), dict(residual=r, y=over, h=over), dict(residual=over, y=over, h=over)):        # y over what the codes are made of
+        with pytest.raises(ValueError):
+            layers.norm(x, w, **more)
     with pytest.raises(ValueError):
         layers.recur_backward(x, r, states, x, dlast=first, dfirst=first, dgate=y, dx=h)
     with pytest.raises(ValueError):
