@@ -12,7 +12,10 @@
  * Matrices are row-major; `stride` is the distance of two rows in elements (>= the row's length; any value for a
  * single row), pointers need the alignment of an element only, unless said otherwise.  Element types are
  * mgwfbp_dtype; all sums are binary32 and are rounded once, to nearest even.  Their order follows from the sizes
- * and ids alone, so that the same call gives the same bits.  Buffers that a call writes must not overlap any other.
+ * and ids alone, so that the same call gives the same bits.  Buffers that a call writes must not overlap any other, unless said
+ * otherwise.  (Matrices whose rows are equally far apart may lie beside each other in the same rows.  norm, recur, their ways back and distill
+ * refuse calls whose outputs overlap something, their workspace included; the ranges of matrices with rows at different distances have to be apart there.)
+ * Where an output may be an input, it is so as a whole: the same address, size of an element and stride.
  * Sizes of zero are accepted.  Errors: MGWFBP_EINVAL (null or misaligned pointer, unknown type, a size out of range or
  * a workspace too small: nothing has been enqueued), MGWFBP_EHIP (a launch failed; earlier launches of the same call
  * may have been enqueued).
@@ -112,8 +115,8 @@ int mgwfbp_act_linear_grad(const int8_t* d_q, const float* d_scale, int64_t ld, 
  *   h = x + residual, rounded to the stream's type (without a residual h is x itself)
  *   rstd[t] = 1 / sqrt(mean over c of h[t,c]^2 + eps);  n = h * rstd;  y = n * weight          (d_weight NULL: 1)
  * The mean is a binary64 sum, rstd is rounded to binary32 once, n and y are binary32 products, y rounded to x's type.
- * x and y are of one type, residual and h of the same or of MGWFBP_F32.  d_h may be d_residual, with the same stride; otherwise outputs
- * overlap nothing (y over h, or over an x of which n is kept, is refused).  d_residual and d_h are NULL together (stream_dtype is dtype then).  eps 2^-100..2^100.
+ * x and y are of one type, residual and h of the same or of MGWFBP_F32.  d_h and d_y may each be d_residual or d_x (but not an x of which n is
+ * kept).  d_residual and d_h are NULL together (stream_dtype is dtype then).  eps 2^-100..2^100.
  * Where d_q is not NULL, n is kept for mgwfbp_norm_backward as a checkpoint (above) of q and scale, with rstd [n_tokens]; and
  * linear_scale, as large as scale, is scale * weight: q and linear_scale are a checkpoint of n * weight, of y before its rounding, for
  * mgwfbp_act_linear_grad.  d_rstd, d_q, d_scale and d_linear_scale are NULL together.
@@ -126,7 +129,7 @@ int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_
  *   dh = dresidual + rstd * (g - n^ * mean over c of g n^)     (d_dresidual, what flows into h by itself, NULL: 0)
  *   dw[c] = sum over t of dy[t,c] * n^[t,c]                    (d_dw NULL: left out; accumulate != 0 adds to what is there)
  * dh is the gradient of x and of residual alike; d_dx, where not NULL, gets it in dy's type, too.  dresidual and dh are of the stream's
- * type; d_dh may be d_dresidual, with the same stride.  The workspace is needed for dw, and above 8192 channels. */
+ * type; d_dh and d_dx may each be d_dresidual or d_dy.  The workspace is needed for dw, and above 8192 channels. */
 int mgwfbp_norm_backward_workspace(int64_t n_tokens, int64_t n_channels, uint64_t* bytes_out);
 int mgwfbp_norm_backward(const int8_t* d_q, const float* d_scale, int64_t ld, const float* d_rstd, int64_t n_tokens, int64_t n_channels,
                          const void* d_weight, int32_t weight_dtype, const void* d_dy, int64_t dy_stride, int32_t dtype, const void* d_dresidual,
@@ -153,7 +156,7 @@ typedef enum mgwfbp_recur_kind { /* c(a), the factor of x */
  *   a = 1 / (1 + exp(-gate));  h[t] = a[t] * h[t-1] + c(a[t]) * x[t];  y = h
  * gate, x and y are of one type, h is binary32.  first [n_sequences][n_channels] is h before each sequence's first token (NULL: 0), last, as
  * large, gets h behind its last one (NULL: left out; of a sequence without tokens: first).  d_last may be d_first where sequences are of
- * one length: a step of an answer is a call with one token for each sequence.
+ * one length: a step of an answer is a call with one token for each sequence.  d_y may be d_gate or d_x.
  * states (NULL: left out) gets what the way back needs, h before every MGWFBP_RECUR_BLOCK-th token, of each sequence where they are of one
  * length, of all rows where there are offsets: mgwfbp_recur_states rows of n_channels. */
 #define MGWFBP_RECUR_BLOCK 128
@@ -165,7 +168,7 @@ int mgwfbp_recur(const mgwfbp_sequences* sequences, int64_t n_channels, int32_t 
 
 /* Its way back: with D[t] = dy[t] + a[t+1] * D[t+1] within a sequence, dlast (NULL: 0) behind its last token,
  *   dx = c(a) * D;  dgate = D * dh/dgate;  dfirst = a D at a sequence's first token (NULL: left out; of a sequence without tokens: dlast)
- * from the same gate, x and first and the states that mgwfbp_recur has kept.  The workspace is as large as mgwfbp_recur's. */
+ * from the same gate, x and first and the states that mgwfbp_recur has kept.  d_dgate and d_dx may each be d_gate, d_x or d_dy.  The workspace is as large as mgwfbp_recur's. */
 int mgwfbp_recur_backward(const mgwfbp_sequences* sequences, int64_t n_channels, int32_t kind, int32_t dtype, const void* d_gate, int64_t gate_stride,
                           const void* d_x, int64_t x_stride, const float* d_first, const float* d_states, const void* d_dy, int64_t dy_stride,
                           const float* d_dlast, void* d_dgate, int64_t dgate_stride, void* d_dx, int64_t dx_stride, float* d_dfirst,
@@ -174,7 +177,7 @@ int mgwfbp_recur_backward(const mgwfbp_sequences* sequences, int64_t n_channels,
 /* Loss of a row of logits z against a label and against a teacher that is known by its top logits, and its gradient:
  *   p_j = exp(s_j / tau) / sum over the row's entries
  *   loss[t] = w * (label_weight * (-log softmax(z)[label]) + teacher_weight * tau^2 * sum over j of p_j * (log p_j - log softmax(z / tau)[id_j]))
- *   dz[t,:] = its gradient, of z's type                        (d_dz NULL: left out; it may be d_z with the same stride)
+ *   dz[t,:] = its gradient, of z's type                        (d_dz NULL: left out; it may be d_z)
  * labels [n_tokens] (NULL: none; one outside 0..n_vocabulary-1: none), ids and teacher [n_tokens][n_top] with a stride each: an id outside
  * 0..n_vocabulary-1 or a logit of -inf is no entry, the same id twice counts twice.  w = row_weight[t] (NULL: 1).  A row whose w is 0, or
  * that has neither label nor entry (or a weight of 0 for what it has), is not looked at: its loss is 0 and its gradient zeros.  Otherwise an

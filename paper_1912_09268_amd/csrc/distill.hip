@@ -18,6 +18,7 @@
 
 #include "device_types.h"
 #include "mgwfbp_layers.h"
+#include "spans.h"
 #include "teams.h"
 
 namespace {
@@ -669,10 +670,20 @@ int mgwfbp_distill(const void* d_z, int64_t z_stride, int32_t dtype, int64_t n_t
     if (n_tokens == 0) return MGWFBP_OK;
     const int64_t bytes = dtype_bytes(dtype);
     if (!side_ok(d_z, n_tokens, n_vocabulary, z_stride, bytes) || (d_dz != nullptr && !side_ok(d_dz, n_tokens, n_vocabulary, dz_stride, bytes)) ||
-        (d_dz == d_z && n_tokens > 1 && dz_stride != z_stride) || d_loss == nullptr || !is_aligned(d_loss, 4) || !is_aligned(d_row_weight, 4))
+        d_loss == nullptr || !is_aligned(d_loss, 4) || !is_aligned(d_row_weight, 4))
         return MGWFBP_EINVAL;
     if (n_top > 0 && (!side_ok(d_ids, n_tokens, n_top, ids_stride, id_type == MGWFBP_I64 ? 8 : 4) ||
                       !side_ok(d_teacher, n_tokens, n_top, teacher_stride, dtype_bytes(teacher_dtype))))
+        return MGWFBP_EINVAL;
+    const uint64_t needed = workspace_of(n_tokens, n_vocabulary, n_top);
+    const auto ids_bytes = [](int32_t type) { return type == MGWFBP_I64 ? 8 : 4; };
+    const uint32_t DZ = 2;
+    if (tangled({vector_span(d_loss, n_tokens, 4), matrix_span(d_dz, n_tokens, n_vocabulary, dz_stride, bytes), vector_span(d_workspace, static_cast<int64_t>(needed), 1)},
+                {{matrix_span(d_z, n_tokens, n_vocabulary, z_stride, bytes), DZ},
+                 {vector_span(d_labels, n_tokens, ids_bytes(label_type)), 0},
+                 {matrix_span(d_ids, n_tokens, n_top, ids_stride, ids_bytes(id_type)), 0},
+                 {matrix_span(d_teacher, n_tokens, n_top, teacher_stride, dtype_bytes(teacher_dtype)), 0},
+                 {vector_span(d_row_weight, n_tokens, 4), 0}}))
         return MGWFBP_EINVAL;
     DistillArgs a{};
     a.z = d_z;
@@ -698,7 +709,7 @@ int mgwfbp_distill(const void* d_z, int64_t z_stride, int32_t dtype, int64_t n_t
     a.teacher_type = teacher_dtype;
     const Cut cut = cut_of(n_tokens, n_vocabulary);
     if (cut.parts > 0) {
-        if (d_workspace == nullptr || !is_aligned(d_workspace, 256) || workspace_bytes < workspace_of(n_tokens, n_vocabulary, n_top)) return MGWFBP_EINVAL;
+        if (d_workspace == nullptr || !is_aligned(d_workspace, 256) || workspace_bytes < needed) return MGWFBP_EINVAL;
         a.stats = static_cast<float*>(d_workspace);
         a.parts = cut.parts;
         a.kept_z = a.stats + n_tokens * cut.parts * 3;

@@ -148,13 +148,15 @@ bool truth(PyObject* o, int32_t& v) {
 }
 
 PyObject* not_this_way() { Py_RETURN_NOTIMPLEMENTED; }
-// The end of a call: the tensors that it has written count as changed (those made in inference mode have no version).
+// The end of a call: the tensors that it has written count as changed (those made in inference mode have no version).  What the library refuses,
+// without having done anything, goes the plain way, too, which says why.
 PyObject* done(int which, int status, std::initializer_list<const at::Tensor*> written) {
     if (status == 0) {
         for (const at::Tensor* t : written)
             if (t != nullptr && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
         Py_RETURN_NONE;
     }
+    if (status == MGWFBP_EINVAL) return not_this_way();
     return PyObject_CallFunction(g_raise, "si", NAMES[which], status);     // raises
 }
 

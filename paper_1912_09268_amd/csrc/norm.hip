@@ -22,6 +22,7 @@
 #include "act_layout.h"
 #include "device_types.h"
 #include "mgwfbp_layers.h"
+#include "spans.h"
 #include "teams.h"
 
 namespace {
@@ -514,6 +515,7 @@ bool kept_ok(const int8_t* q, const float* scale, const float* rstd, int64_t tok
 bool side_ok(const void* p, int64_t tokens, int64_t channels, int64_t stride, int32_t dtype) {
     return p != nullptr && is_aligned(p, dtype_bytes(dtype)) && is_matrix(tokens, channels, stride, dtype_bytes(dtype));
 }
+int64_t weight_bytes(const void* w, int32_t type) { return w == nullptr ? 0 : dtype_bytes(type); }
 bool weight_ok(const void* w, int32_t type) { return w == nullptr || (is_dtype(type) && is_aligned(w, dtype_bytes(type))); }
 
 }  // namespace
@@ -531,11 +533,17 @@ int mgwfbp_norm(const void* d_x, int64_t x_stride, int32_t dtype, const void* d_
     if (keep != (d_rstd != nullptr) || keep != (d_scale != nullptr) || keep != (d_linear_scale != nullptr)) return MGWFBP_EINVAL;
     if (!side_ok(d_x, n_tokens, n_channels, x_stride, dtype) || !side_ok(d_y, n_tokens, n_channels, y_stride, dtype)) return MGWFBP_EINVAL;
     if (d_residual != nullptr && (!side_ok(d_residual, n_tokens, n_channels, residual_stride, stream_dtype) ||
-                                  !side_ok(d_h, n_tokens, n_channels, h_stride, stream_dtype) ||
-                                  (d_h == d_residual && n_tokens > 1 && h_stride != residual_stride)))
+                                  !side_ok(d_h, n_tokens, n_channels, h_stride, stream_dtype)))
         return MGWFBP_EINVAL;
-    if (d_h != nullptr ? d_y == d_h : keep && d_y == d_x) return MGWFBP_EINVAL;         // the codes are made of h, behind y
     if (keep && (!kept_ok(d_q, d_scale, d_rstd, n_tokens, n_channels, ld) || !is_aligned(d_linear_scale, 16))) return MGWFBP_EINVAL;
+    const int64_t bytes = dtype_bytes(dtype), stream_bytes = dtype_bytes(stream_dtype), own = own_columns(n_channels), groups = ceil_div(n_tokens, GROUP);
+    const uint32_t H = 1, Y = 2, made_of_x = d_residual == nullptr && keep;             // the codes are made of h, behind y
+    if (tangled({matrix_span(d_h, n_tokens, n_channels, h_stride, stream_bytes), matrix_span(d_y, n_tokens, n_channels, y_stride, bytes), vector_span(d_rstd, n_tokens, 4),
+                 matrix_span(d_q, n_tokens, own, ld, 1), matrix_span(d_scale, groups, own, ld, 4), matrix_span(d_linear_scale, groups, own, ld, 4)},
+                {{matrix_span(d_x, n_tokens, n_channels, x_stride, bytes), made_of_x ? 0 : H | Y},
+                 {matrix_span(d_residual, n_tokens, n_channels, residual_stride, stream_bytes), H | Y},
+                 {vector_span(d_weight, n_channels, weight_bytes(d_weight, weight_dtype)), 0}}))
+        return MGWFBP_EINVAL;
     CodeArgs c{};
     const bool narrow = ceil_div(n_channels, 128) * ceil_div(n_tokens, GROUP) < NARROW_BELOW;
     c.col_blocks = static_cast<uint32_t>(ceil_div(n_channels, narrow ? 64 : 128));
@@ -610,16 +618,26 @@ int mgwfbp_norm_backward(const int8_t* d_q, const float* d_scale, int64_t ld, co
     if (n_tokens == 0) return d_dw == nullptr || accumulate ? static_cast<int>(MGWFBP_OK) : launch(join_kernel, j, join_grid, dim3(JOIN_COLS * JOIN_ROWS), hip_stream);
     if (!kept_ok(d_q, d_scale, d_rstd, n_tokens, n_channels, ld) || !side_ok(d_dy, n_tokens, n_channels, dy_stride, dtype) ||
         !side_ok(d_dh, n_tokens, n_channels, dh_stride, stream_dtype) ||
-        (d_dresidual != nullptr && (!side_ok(d_dresidual, n_tokens, n_channels, dresidual_stride, stream_dtype) ||
-                                    (d_dh == d_dresidual && n_tokens > 1 && dh_stride != dresidual_stride))) ||
+        (d_dresidual != nullptr && !side_ok(d_dresidual, n_tokens, n_channels, dresidual_stride, stream_dtype)) ||
         (d_dx != nullptr && !side_ok(d_dx, n_tokens, n_channels, dx_stride, dtype)))
         return MGWFBP_EINVAL;
     const Cut cut = cut_of(n_tokens, n_channels);
+    uint64_t needed = 0;
     if (d_dw != nullptr || cut.wide) {
-        uint64_t bytes = 0;
-        mgwfbp_norm_backward_workspace(n_tokens, n_channels, &bytes);
-        if (d_workspace == nullptr || !is_aligned(d_workspace, 256) || workspace_bytes < bytes) return MGWFBP_EINVAL;
+        mgwfbp_norm_backward_workspace(n_tokens, n_channels, &needed);
+        if (d_workspace == nullptr || !is_aligned(d_workspace, 256) || workspace_bytes < needed) return MGWFBP_EINVAL;
     }
+    const int64_t bytes = dtype_bytes(dtype), stream_bytes = dtype_bytes(stream_dtype), own = own_columns(n_channels);
+    const uint32_t DH = 1, DX = 2;
+    if (tangled({matrix_span(d_dh, n_tokens, n_channels, dh_stride, stream_bytes), matrix_span(d_dx, n_tokens, n_channels, dx_stride, bytes),
+                 vector_span(d_dw, n_channels, weight_bytes(d_dw, grad_dtype)), vector_span(d_workspace, static_cast<int64_t>(needed), 1)},
+                {{matrix_span(d_dy, n_tokens, n_channels, dy_stride, bytes), DH | DX},
+                 {matrix_span(d_dresidual, n_tokens, n_channels, dresidual_stride, stream_bytes), DH | DX},
+                 {matrix_span(d_q, n_tokens, own, ld, 1), 0},
+                 {matrix_span(d_scale, ceil_div(n_tokens, GROUP), own, ld, 4), 0},
+                 {vector_span(d_rstd, n_tokens, 4), 0},
+                 {vector_span(d_weight, n_channels, weight_bytes(d_weight, weight_dtype)), 0}}))
+        return MGWFBP_EINVAL;
     BackArgs a{};
     a.q = d_q;
     a.scale = d_scale;

@@ -32,6 +32,7 @@
 
 #include "device_types.h"
 #include "mgwfbp_layers.h"
+#include "spans.h"
 
 namespace {
 
@@ -874,6 +875,12 @@ uint64_t workspace_of(const mgwfbp_sequences& s, int64_t channels, int32_t dtype
     return bytes;
 }
 
+Span ends_span(const float* p, const mgwfbp_sequences& s, int64_t channels) { return vector_span(p, s.n_sequences * channels, 4); }
+Span states_span(const float* p, const mgwfbp_sequences& s, int64_t channels) {
+    return vector_span(p, (s.d_offsets != nullptr ? 1 : s.n_sequences) * ceil_div(unit_tokens(s), BLOCK) * channels, 4);
+}
+Span offsets_span(const mgwfbp_sequences& s) { return vector_span(s.d_offsets, s.n_sequences + 1, s.offset_type == MGWFBP_I64 ? 8 : 4); }
+
 template <int K> struct Kind { static constexpr int value = K; };
 template <typename F> int with_kind(int32_t kind, F&& f) {
     switch (kind) {
@@ -960,7 +967,15 @@ int mgwfbp_recur(const mgwfbp_sequences* sequences, int64_t n_channels, int32_t 
         !side_ok(d_y, tokens, n_channels, y_stride, dtype) || !states_ok(d_first) || !states_ok(d_last) || !states_ok(d_states) ||
         !is_matrix(sequences->n_sequences, n_channels, n_channels, 4))
         return MGWFBP_EINVAL;
-    if (sequences->d_offsets != nullptr && d_first != nullptr && d_first == d_last) return MGWFBP_EINVAL;
+    const int64_t bytes = dtype_bytes(dtype);
+    const uint32_t Y = 1, LAST = 2;
+    if (tangled({matrix_span(d_y, tokens, n_channels, y_stride, bytes), ends_span(d_last, *sequences, n_channels), states_span(d_states, *sequences, n_channels),
+                 vector_span(d_workspace, static_cast<int64_t>(workspace_of(*sequences, n_channels, dtype)), 1)},
+                {{matrix_span(d_gate, tokens, n_channels, gate_stride, bytes), Y},
+                 {matrix_span(d_x, tokens, n_channels, x_stride, bytes), Y},
+                 {ends_span(d_first, *sequences, n_channels), sequences->d_offsets == nullptr ? LAST : 0},
+                 {offsets_span(*sequences), 0}}))
+        return MGWFBP_EINVAL;
     RecurArgs a{};
     a.gate = d_gate;
     a.x = d_x;
@@ -985,7 +1000,19 @@ int mgwfbp_recur_backward(const mgwfbp_sequences* sequences, int64_t n_channels,
     if (!side_ok(d_gate, tokens, n_channels, gate_stride, dtype) || !side_ok(d_x, tokens, n_channels, x_stride, dtype) ||
         !side_ok(d_dy, tokens, n_channels, dy_stride, dtype) || !side_ok(d_dgate, tokens, n_channels, dgate_stride, dtype) ||
         !side_ok(d_dx, tokens, n_channels, dx_stride, dtype) || !states_ok(d_first) || !states_ok(d_states) || !states_ok(d_dlast) || !states_ok(d_dfirst) ||
-        (tokens > 0 && !is_short(*sequences) && d_states == nullptr) || (d_dlast != nullptr && d_dlast == d_dfirst) || !is_matrix(sequences->n_sequences, n_channels, n_channels, 4))
+        (tokens > 0 && !is_short(*sequences) && d_states == nullptr) || !is_matrix(sequences->n_sequences, n_channels, n_channels, 4))
+        return MGWFBP_EINVAL;
+    const int64_t bytes = dtype_bytes(dtype);
+    const uint32_t DGATE = 1, DX = 2;
+    if (tangled({matrix_span(d_dgate, tokens, n_channels, dgate_stride, bytes), matrix_span(d_dx, tokens, n_channels, dx_stride, bytes),
+                 ends_span(d_dfirst, *sequences, n_channels), vector_span(d_workspace, static_cast<int64_t>(workspace_of(*sequences, n_channels, dtype)), 1)},
+                {{matrix_span(d_gate, tokens, n_channels, gate_stride, bytes), DGATE | DX},
+                 {matrix_span(d_x, tokens, n_channels, x_stride, bytes), DGATE | DX},
+                 {matrix_span(d_dy, tokens, n_channels, dy_stride, bytes), DGATE | DX},
+                 {ends_span(d_first, *sequences, n_channels), 0},
+                 {ends_span(d_dlast, *sequences, n_channels), 0},
+                 {states_span(d_states, *sequences, n_channels), 0},
+                 {offsets_span(*sequences), 0}}))
         return MGWFBP_EINVAL;
     RecurArgs a{};
     a.gate = d_gate;

@@ -10,6 +10,9 @@ The operators are the backward pass, and autograd knows nothing of them: results
 a word, tensors that require grad are refused in grad mode; under torch.no_grad(), in an autograd.Function and detached they are
 taken.  Tensors that a call has written count as changed: autograd refuses to go on with one that it has saved before.
 
+An output of norm, recur, their ways back and distill may lie over an input as a whole where a line says so; every other overlap of what a call
+writes with its other tensors is refused.
+
     h = layers.embed([word, position, token_type], [ids, places, types])          # bf16, from binary32 weights
     u = torch.empty_like(z)
     kept = layers.act_store(z, kind="gelu", y=u)                                  # z in 8 bits, u = gelu(z)
@@ -105,12 +108,48 @@ def _written(*tensors) -> None:
             torch.autograd.graph.increment_version(t)
 
 
-class _on:
-    """The device's current stream as a handle, with the device current: free of charge where it is already."""
-    __slots__ = ("device", "guard")
+def _span(t: torch.Tensor):
+    """A tensor's memory: address, rows, bytes of a row, bytes from one row to the next."""
+    size, width = t.element_size(), t.shape[-1]
+    rows = t.numel() // width
+    step = next((stride for n, stride in zip(t.shape[-2::-1], t.stride()[-2::-1]) if n > 1), width)
+    return t.data_ptr(), rows, width * size, step * size
 
-    def __init__(self, device: torch.device):
-        self.device, self.guard = device, None
+
+def _share(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether matrices share memory, as the library sees it (csrc/spans.h)."""
+    if a.numel() == 0 or b.numel() == 0:
+        return False
+    (p, rows, width, step), (q, q_rows, q_width, q_step) = _span(a), _span(b)
+    behind = q - p
+    if behind >= (rows - 1) * step + width or -behind >= (q_rows - 1) * q_step + q_width:
+        return False
+    if rows > 1 and q_rows > 1 and step != q_step:
+        return True
+    step = step if rows > 1 else q_step if q_rows > 1 else 1
+    return max(1 - rows, (-q_width - behind) // step + 1) <= min(q_rows - 1, -((behind - width) // step) - 1)
+
+
+def _why(writes: dict, reads: dict) -> None:
+    """Behind a call that the library refuses: a ValueError that names tensors over each other, where that is the reason."""
+    writes, reads = ({name: t for name, t in of.items() if t is not None} for of in (writes, reads))
+    names = list(writes)
+    for i, name in enumerate(names):
+        for other in names[i + 1:]:
+            if _share(writes[name], writes[other]):
+                _fail(f"{name} and {other} are written and share memory")
+        for other, t in reads.items():
+            if _share(writes[name], t) and _span(writes[name]) != _span(t):
+                _fail(f"{name} is written and shares memory with {other}")
+
+
+class _on:
+    """The device's current stream as a handle, with the device current: free of charge where it is already.  A refusal of the library is
+    explained where tensors that the call writes lie over others."""
+    __slots__ = ("device", "guard", "writes", "reads")
+
+    def __init__(self, device: torch.device, writes: dict = {}, reads: dict = {}):
+        self.device, self.guard, self.writes, self.reads = device, None, writes, reads
 
     def __enter__(self) -> int:
         if torch.cuda.current_device() != self.device.index:
@@ -121,6 +160,8 @@ class _on:
     def __exit__(self, *exc):
         if self.guard is not None:
             self.guard.__exit__(*exc)
+        if isinstance(exc[1], B.MgwfbpError) and exc[1].status == -1:
+            _why(self.writes, self.reads)
 
 
 def _workspace(given: Optional[torch.Tensor], nbytes: int, device: torch.device) -> torch.Tensor:
@@ -313,6 +354,10 @@ def _kept(kept: Norm8):
     return tokens, ld
 
 
+def _kept_names(kept: Optional[Norm8]) -> dict:
+    return {} if kept is None else {"kept.rstd": kept.rstd, "kept.act.q": kept.act.q, "kept.act.scale": kept.act.scale, "kept.linear.scale": kept.linear.scale}
+
+
 def _vector(t: Optional[torch.Tensor], name: str, n: int, dtypes=_DTYPES) -> int:
     """Checks a contiguous vector, which may be left out, and returns its address."""
     if t is None:
@@ -334,8 +379,8 @@ def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optio
          h: Optional[torch.Tensor] = None, kept: Optional[Norm8] = None, eps: float = 1e-6):
     """h = x + residual and y = h / sqrt(mean(h^2) + eps) * weight over the channels of x [tokens, channels]; returns (y, h).
 
-    weight [channels] (None: 1).  residual, and h with it, are of x's type or float32; h may be residual, None makes a new tensor; without a residual
-    h is x.  y is of x's type; it is other memory than h.  `kept` (norm_empty) takes what norm_backward and the next layer's act_linear_grad need."""
+    weight [channels] (None: 1).  residual, and h with it, are of x's type or float32; None for h makes a new tensor; without a residual h is x.  y is of x's type.
+    h and y may each lie over residual or x (y not over an x that is kept).  `kept` (norm_empty) takes what norm_backward and the next layer's act_linear_grad need."""
     if y is not None and (residual is None) == (h is None) and isinstance(eps, float):
         act, rstd, linear = (None, None, None) if kept is None else kept
         if kept is None or (linear.q is act.q and linear.channels == act.channels):
@@ -367,7 +412,7 @@ def norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optio
         rows, ld = _kept(kept)
         if rows != tokens or kept.act.channels != channels:
             _fail(f"x has shape {tuple(x.shape)}, what is kept is of {(rows, kept.act.channels)}")
-    with _on(device) as stream:
+    with _on(device, dict(h=h, y=y, **_kept_names(kept)), dict(x=x, residual=residual, weight=weight)) as stream:
         B.norm(x.data_ptr(), x_stride, _DTYPES[x.dtype], _address(residual), res_stride, _DTYPES[stream_type], tokens, channels, w, _code(weight), float(eps),
                _address(h), h_stride, y.data_ptr(), y_stride, *((m.data_ptr() for m in (kept.rstd, kept.act.q, kept.act.scale, kept.linear.scale)) if kept else (0, 0, 0, 0)),
                ld, stream)
@@ -380,7 +425,7 @@ def norm_backward(kept: Norm8, dy: torch.Tensor, weight: Optional[torch.Tensor] 
                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The gradient of norm's h, from the gradient dy [tokens, channels] of its y and what it has kept, plus `dres`, what flows into h by itself;
     that is the gradient of x and of residual.  Where given, `dx` gets it in dy's type, too, and `dw` [channels] the weight's gradient (added to
-    what is there where `accumulate`).  dres and dh are of dy's type or float32, dh may be dres, None makes a new tensor.
+    what is there where `accumulate`).  dres and dh are of dy's type or float32, None makes a new tensor; dh and dx may each lie over dres or dy.
     `workspace`: device memory of layers_binding.norm_backward_workspace(tokens, channels) bytes; None takes torch's.  Returns dh."""
     if dh is not None and kept.linear.q is kept.act.q:
         if _native.norm_backward(kept.act.q, kept.act.scale, kept.act.channels, kept.rstd, dy, weight, dres, dh, dx, dw, accumulate, workspace) is None:
@@ -397,7 +442,7 @@ def norm_backward(kept: Norm8, dy: torch.Tensor, weight: Optional[torch.Tensor] 
     if _same_place(dh, dres) and dh_stride != dres_stride:
         _fail("dh over dres must have its strides")
     w, to = _vector(weight, "weight", channels), _vector(dw, "dw", channels)
-    with _on(device) as stream:
+    with _on(device, dict(dh=dh, dx=dx, dw=dw, workspace=workspace), dict(dy=dy, dres=dres, weight=weight, **_kept_names(kept))) as stream:
         space = _workspace(workspace, B.norm_backward_workspace(tokens, channels), device)
         B.norm_backward(kept.act.q.data_ptr(), kept.act.scale.data_ptr(), ld, kept.rstd.data_ptr(), tokens, channels, w, _code(weight), dy.data_ptr(), dy_stride,
                         _DTYPES[dy.dtype], _address(dres), dres_stride, dh.data_ptr(), dh_stride, _DTYPES[dh.dtype], _address(dx), dx_stride, accumulate, to,
@@ -461,6 +506,7 @@ def recur(gate: torch.Tensor, x: torch.Tensor, kind: str = "convex", first: Opti
 
     gate, x and y are of one type: [length, channels], [sequences, length, channels], or with `offsets` [sequences + 1] sequences one behind the other
     in [tokens, channels], offsets[s] .. offsets[s+1]-1 being sequence s (rows behind the last one are left as they are; a new y has zeros there).
+    y may lie over gate or x.
     h is float32: `first` [sequences, channels] goes in (None: 0) and `last`, which may be first where there are no offsets, comes out.  `states`
     (recur_empty) takes what recur_backward needs.  `workspace`: device memory of layers_binding.recur_workspace bytes; None takes torch's."""
     if y is not None and _native.recur(gate, x, RECUR_KINDS.get(kind), first, offsets, y, last, states, workspace) is None:
@@ -476,7 +522,7 @@ def recur(gate: torch.Tensor, x: torch.Tensor, kind: str = "convex", first: Opti
     if offsets is not None and first_at and first_at == last_at:
         _fail("last over first takes sequences of one length")
     states_at = _states(states, "states", B.recur_states(sequences), channels)
-    with _on(device) as stream:
+    with _on(device, dict(y=y, last=last, states=states, workspace=workspace), dict(gate=gate, x=x, first=first, offsets=offsets)) as stream:
         space = _workspace(workspace, B.recur_workspace(sequences, channels, _DTYPES[gate.dtype]), device)
         B.recur(sequences, channels, _recur_kind(kind), _DTYPES[gate.dtype], *sides[0], *sides[1], first_at, *sides[2], last_at, states_at, space.data_ptr(),
                 space.numel() * space.element_size(), stream)
@@ -488,7 +534,8 @@ def recur_backward(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, dy
                    offsets: Optional[torch.Tensor] = None, dlast: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
                    dx: Optional[torch.Tensor] = None, dfirst: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Gradients of recur's gate and x, and of `first` where `dfirst` is given, from those of its y and, where given, of `last`; gate, x, kind, first and offsets as
-    they were, `states` as recur has written them.  Returns (dgate, dx); rows behind the last sequence are left as they are (new tensors have zeros there)."""
+    they were, `states` as recur has written them.  Returns (dgate, dx); rows behind the last sequence are left as they are (new tensors have zeros there).
+    dgate and dx may each lie over gate, x or dy."""
     if dgate is not None and dx is not None and _native.recur_backward(gate, x, states, dy, RECUR_KINDS.get(kind), first, offsets, dlast, dgate, dx, dfirst, workspace) is None:
         return dgate, dx
     sequences, tokens, channels = _sequences(gate, offsets)
@@ -503,7 +550,8 @@ def recur_backward(gate: torch.Tensor, x: torch.Tensor, states: torch.Tensor, dy
     if dlast_at and dlast_at == dfirst_at:
         _fail("dfirst must be other memory than dlast")
     states_at = _states(states, "states", B.recur_states(sequences), channels)
-    with _on(device) as stream:
+    with _on(device, dict(dgate=dgate, dx=dx, dfirst=dfirst, workspace=workspace),
+             dict(gate=gate, x=x, dy=dy, first=first, dlast=dlast, states=states, offsets=offsets)) as stream:
         space = _workspace(workspace, B.recur_workspace(sequences, channels, _DTYPES[gate.dtype]), device)
         B.recur_backward(sequences, channels, _recur_kind(kind), _DTYPES[gate.dtype], *sides[0], *sides[1], first_at, states_at, *sides[2], dlast_at, *sides[3],
                          *sides[4], dfirst_at, space.data_ptr(), space.numel() * space.element_size(), stream)
@@ -546,7 +594,9 @@ def distill(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, teacher: O
         dz_stride = _matrix(dlogits, "dlogits", tokens, vocabulary, (logits.dtype,))
         if _same_place(dlogits, logits) and dz_stride != stride:
             _fail("dlogits over logits must have its strides")
-    with _on(device) as stream:
+    if tokens and row_weight is not None and _same_place(loss, row_weight):
+        _fail("loss must be other memory than row_weight")
+    with _on(device, dict(loss=loss, dlogits=dlogits, workspace=workspace), dict(logits=logits, labels=labels, ids=ids, teacher=teacher, row_weight=row_weight)) as stream:
         space = _workspace(workspace, B.distill_workspace(tokens, vocabulary, top), device)
         B.distill(logits.data_ptr(), stride, _DTYPES[logits.dtype], tokens, vocabulary, labels_at, _code(labels, _ID_TYPES), _address(ids), ids_stride,
                   _code(ids, _ID_TYPES), _address(teacher), teacher_stride, _code(teacher), top, temperature, label_weight, teacher_weight, weight_at, loss_at,
