@@ -104,8 +104,10 @@ template <int THREADS> struct Entries {
         id[end] = label;
         p[end] = 0.f;
     }
-    // After a barrier: whether an entry's index is another one's, too.  Nearly none is.
+    // After a barrier: whether an entry's index is another one's, too.  Nearly none is.  A workgroup of one wavefront has had none yet (its reductions
+    // need no LDS), and what other lanes have put into LDS is seen behind one only.
     __device__ __forceinline__ void find_again(int top) {
+        if constexpr (THREADS == 64) __syncthreads();
         const int end = label_place(top);
         for (int j = threadIdx.x; j <= end; j += THREADS) {
             const int32_t mine = id[j];
