@@ -243,7 +243,7 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, scale: f
 def act_empty(tokens: int, channels: int, device="cuda") -> Act8:
     """Memory for the checkpoint of a [tokens, channels] activation."""
     ld, groups = B.act_dims(tokens, channels)
-    return Act8(torch.empty(tokens, ld, dtype=torch.int8, device=device), torch.empty(groups, ld, device=device), channels)
+    return Act8(torch.empty(tokens, ld, dtype=torch.int8, device=device), torch.empty(groups, ld, dtype=torch.float32, device=device), channels)
 
 
 def _act(act: Act8):
@@ -341,7 +341,7 @@ class Norm8(NamedTuple):
 def norm_empty(tokens: int, channels: int, device="cuda") -> Norm8:
     """Memory for what norm keeps of [tokens, channels]."""
     act = act_empty(tokens, channels, device)
-    return Norm8(act, torch.empty(tokens, device=device), Act8(act.q, torch.empty_like(act.scale), channels))
+    return Norm8(act, torch.empty(tokens, dtype=torch.float32, device=device), Act8(act.q, torch.empty_like(act.scale), channels))
 
 
 def _kept(kept: Norm8):
@@ -495,7 +495,7 @@ def _recur_kind(kind: str) -> int:
 def recur_empty(gate: torch.Tensor, offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Memory for the states that recur keeps for recur_backward: one for every 128 tokens of a sequence, or of all where there are offsets."""
     sequences, _, channels = _sequences(gate, offsets)
-    return torch.empty(B.recur_states(sequences), channels, device=gate.device)
+    return torch.empty(B.recur_states(sequences), channels, dtype=torch.float32, device=gate.device)
 
 
 def recur(gate: torch.Tensor, x: torch.Tensor, kind: str = "convex", first: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
@@ -576,7 +576,7 @@ def distill(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, teacher: O
     stride = _matrix(logits, "logits", None, None)
     tokens, vocabulary = logits.shape
     if loss is None:
-        loss = torch.empty(tokens, device=logits.device)
+        loss = torch.empty(tokens, dtype=torch.float32, device=logits.device)
     device = _device(logits, ids, teacher, labels, row_weight, loss, dlogits, workspace)
     if vocabulary < 1 or (ids is None) != (teacher is None):
         _fail("a vocabulary of one logit or more, and ids and teacher together")
