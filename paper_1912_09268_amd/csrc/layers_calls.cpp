@@ -9,11 +9,13 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/forward_grad.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -51,6 +53,8 @@ int id_type_of(const at::Tensor& t) { return t.scalar_type() == at::kLong ? MGWF
 struct Call {
     bool ok = true;
     int device = -1;
+    // Within a level of forward-mode autograd (there is one at a time, number 0) tensors may have tangents.
+    const bool dual = c10::AutogradState::get_tls_state().get_fw_grad_mode() && torch::autograd::ForwardADLevel::try_get_by_idx(0) != nullptr;
 
     // A tensor, or null for None where `optional`.
     const at::Tensor* tensor(PyObject* o, bool optional = false) {
@@ -59,6 +63,7 @@ struct Call {
         const at::Tensor& t = THPVariable_Unpack(o);
         if (t.layout() != at::kStrided || !t.is_cuda() || t.is_neg()) return fail();      // a negated view's memory is not its values
         if (t.requires_grad() && c10::GradMode::is_enabled()) return fail();
+        if (dual && t._fw_grad(0).defined()) return fail();
         if (device < 0) {
             device = t.get_device();
             if (device != c10::hip::current_device()) return fail();

@@ -8,7 +8,8 @@ needs that stream's work to be waited for, and Tensor.record_stream where it is 
 
 The operators are the backward pass, and autograd knows nothing of them: results have no graph.  So that no gradient is lost without
 a word, tensors that require grad are refused in grad mode; under torch.no_grad(), in an autograd.Function and detached they are
-taken.  Tensors that a call has written count as changed: autograd refuses to go on with one that it has saved before.
+taken.  Dual tensors of forward-mode autograd are refused, too: their tangents would be lost.  Tensors that a call has written count as changed:
+autograd refuses to go on with one that it has saved before.
 
 An output of norm, recur, their ways back and distill may lie over an input as a whole where a line says so; every other overlap of what a call
 writes with its other tensors is refused.
@@ -35,6 +36,7 @@ from __future__ import annotations
 from typing import NamedTuple, Optional, Sequence, Union
 
 import torch
+from torch.autograd import forward_ad
 
 from . import layers_binding as B
 
@@ -90,6 +92,8 @@ def _flat(t: torch.Tensor, name: str, tokens: int, dim: int) -> torch.Tensor:
 def _device(*tensors) -> torch.device:
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         _fail("autograd follows a tensor, and the operators have no graph: call them without grad mode, or detach it")
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        _fail("forward-mode autograd follows a tensor, and the operators have no tangents: take its primal")
     if any(t is not None and t.is_neg() for t in tensors):
         _fail("the memory of a tensor holds its values negated: take its resolve_neg()")
     device = tensors[0].device
