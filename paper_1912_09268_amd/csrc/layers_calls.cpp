@@ -49,12 +49,16 @@ int dtype_of(const at::Tensor& t) {
 }
 int id_type_of(const at::Tensor& t) { return t.scalar_type() == at::kLong ? MGWFBP_I64 : t.scalar_type() == at::kInt ? MGWFBP_I32 : -1; }
 
+// Whether forward-mode autograd follows a tensor: only within its level (there is one at a time, number 0) do tensors have tangents.  Most have no memory for
+// autograd at all, and are not asked.
+bool has_tangent(const at::Tensor& t) {
+    return c10::AutogradState::get_tls_state().get_fw_grad_mode() && torch::autograd::ForwardADLevel::try_get_by_idx(0) != nullptr && t._fw_grad(0).defined();
+}
+
 // What the tensors of a call have in common: the current device, found with the first of them.
 struct Call {
     bool ok = true;
     int device = -1;
-    // Within a level of forward-mode autograd (there is one at a time, number 0) tensors may have tangents.
-    const bool dual = c10::AutogradState::get_tls_state().get_fw_grad_mode() && torch::autograd::ForwardADLevel::try_get_by_idx(0) != nullptr;
 
     // A tensor, or null for None where `optional`.
     const at::Tensor* tensor(PyObject* o, bool optional = false) {
@@ -63,7 +67,7 @@ struct Call {
         const at::Tensor& t = THPVariable_Unpack(o);
         if (t.layout() != at::kStrided || !t.is_cuda() || t.is_neg()) return fail();      // a negated view's memory is not its values
         if (t.requires_grad() && c10::GradMode::is_enabled()) return fail();
-        if (dual && t._fw_grad(0).defined()) return fail();
+        if (t.unsafeGetTensorImpl()->autograd_meta() != nullptr && has_tangent(t)) return fail();
         if (device < 0) {
             device = t.get_device();
             if (device != c10::hip::current_device()) return fail();

@@ -45,7 +45,7 @@ int main() {
     const bool lies[] = {ops::tangled({whole}, {{whole, 1}}),         ops::tangled({none, whole}, {{whole, 2}}), ops::tangled({half, other}, {{half, 1}, {other, 2}}),
                          ops::tangled({none, empty}, {{whole, 0}}),   ops::tangled({half}, {{other, 0}, {none, 0}})};
     const bool tangles[] = {ops::tangled({whole}, {{whole, 0}}),      ops::tangled({none, whole}, {{whole, 1}}), ops::tangled({half}, {{whole, 1}}),
-                            ops::tangled({whole, other}, {}),         ops::tangled({half, half}, {}),            ops::tangled({half, other}, {{half, 2}})};
+                            ops::tangled({whole, other}, {{none, 0}}),       ops::tangled({half, half}, {{none, 0}}),            ops::tangled({half, other}, {{half, 2}})};
     for (bool t : lies)
         if (t) return std::puts("what lies well is refused"), 1;
     for (bool t : tangles)
