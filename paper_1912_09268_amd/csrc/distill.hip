@@ -222,7 +222,7 @@ template <typename T> __device__ __forceinline__ void add(const Raw8<T>& r, int 
 constexpr int AHEAD = 4;                 // vectors of a lane on their way where a row does not stay in registers
 
 // V vectors of eight elements a lane hold a row of eight elements or more; V = 0: they do not.  Bound by memory, and by the exponentials where there are two
-// softmaxes: 4096 rows of 30522 bfloat16 logits, 500 MB, with labels alone 94 us, 5.3 TB/s, with labels and 64 entries at another temperature 106; 129 rows of 100003
+// softmaxes: 4096 rows of 30522 bfloat16 logits, 500 MB, with labels alone 94 us, 5.3 TB/s, with labels and 64 entries at another temperature 104; 129 rows of 100003
 // binary32 logits, too long for registers, 31 us, 3.3 TB/s (4.9 counting both readings), as long as the last of them.
 //
 // The last vector of a row that is no multiple of eight begins before its place, so that it ends with the row; lanes behind it take it, too.

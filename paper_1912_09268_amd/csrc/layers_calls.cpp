@@ -1,7 +1,7 @@
 // CPython extension module: the calls of layers.py with their tensors taken apart in native code.
 //
 // A call of an operator is a check of a handful of tensors and a launch or two.  In Python the checks and the marshalling take
-// 12 to 18 us, more than the kernels of small calls; here about 1.  A function returns NotImplemented for whatever it does
+// 12 to 24 us, more than the kernels of small calls; here about 1.  A function returns NotImplemented for whatever it does
 // not take as it stands -- tensors that are to be refused (those that autograd follows among them), on another device than the
 // current one, subclasses of tensors, the library not loaded yet -- and layers.py goes the plain way, which refuses with the reason.
 // The module has no link to the library: layers_binding.py loads that through ctypes and hands over the addresses of its entry points.

@@ -278,7 +278,7 @@ template <typename T, typename S> __device__ __forceinline__ void finish(const B
 
 // A team of TEAM lanes goes through `rows` consecutive rows, V vectors of eight columns a lane, the next row on its way while one is
 // worked on; the lanes' columns stay the same, so their share of dw stays in registers.  Bound by memory: 32775 tokens of 4096 binary16 channels on
-// a binary32 stream 291 us, 1.5 GB at 5.1 TB/s; 4096 tokens of 1024 bfloat16 channels 12 us, of which joining dw is a launch of 4.
+// a binary32 stream 291 us, 1.5 GB at 5.1 TB/s, four wavefronts a SIMD that wait for 60 % of their time; 4096 tokens of 1024 bfloat16 channels 12 us, of which joining dw is a launch of 4.
 // Small teams share a workgroup, so that there are few sums of dw to join.
 constexpr int back_threads(int team, int vecs) { return team >= 256 ? team : vecs == 1 ? 1024 : 512; }
 
@@ -458,8 +458,9 @@ __global__ __launch_bounds__(JOIN_COLS * JOIN_ROWS) void join_kernel(JoinArgs A)
 
 constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_CHANNELS = int64_t(1) << 23, TEAM_CHANNELS = 16384, BACK_TEAM_CHANNELS = 8192;
 
-// Pieces of 128 channels and 128 tokens below which a workgroup takes half of one: 1003 tokens of 1001 binary32 channels 5.9 and 4.8 us; beyond, whole lines of
-// q are better: 32775 tokens of 4096 channels 412 and 435 us for norm and codes.
+// Pieces of 128 channels and 128 tokens below which a workgroup takes half of one: 1003 tokens of 1001 binary32 channels 5.9 and 4.8 us.  Norm and codes of 1024 bfloat16
+// channels, whole pieces and halves: 1024 tokens (64 pieces) 8.0 and 7.5 us, 2048 (128) 8.9 and 8.5, 4096 (256) 11.4 both, as are 192 to 512 pieces of other shapes within 1 %;
+// 8192 tokens of 2048 (1024) 25.9 and 26.7 (binary32 44.6 and 43.6).  Beyond, whole lines of q are better: 32775 tokens of 4096 channels, binary16 on a binary32 stream, 400 and 424.
 constexpr int64_t NARROW_BELOW = 256;
 
 // Calls f with the team and the vectors of a lane for rows of `channels` columns, up to BACK_TEAM_CHANNELS.  Us forward and back, bfloat16, the other shape

@@ -13,8 +13,8 @@
 // workgroup goes through the blocks of a sequence one after the other.  Where there are too few sequences and channels to fill the
 // chip, sequences are cut into segments, whose maps a launch before finds (fold_kernel): gate and x (or dy) are read twice then.
 //
-// The way back needs h[t-1].  It is made again from gate and x and a kept state before each block, 1/32 of a byte an element
-// for each byte of a channel's state, instead of kept for every token: y may be thrown away, and h is not rounded.
+// The way back needs h[t-1].  It is made again from gate and x and a kept state before each block of 128 tokens, 1/32 of a byte
+// an element, instead of kept for every token: y may be thrown away, and h is not rounded.
 //
 // Sequences lie side by side, all of one length, or one behind the other between offsets.  In the latter form a sequence's first token
 // drops what came before it wherever in a block it falls: its map has A = -0, which no product of gates is, and does not look at h, so
@@ -434,8 +434,9 @@ template <int N, int CH, typename T, typename P, typename F> __device__ __forcei
 // forward
 // ---------------------------------------------------------------------------------------------
 
-// Bound by memory: with the chip full the data passes once at 5.1 TB/s, what a large copy reaches (65543 tokens of 1024 binary16 channels, 403 MB, 83 us; with the
-// segments' maps before it 154).  32 x 128 tokens of 512 channels, in one block each, 5.7 us.
+// 65543 tokens of 1024 binary16 channels, 403 MB: 83 to 87 us, 4.7 to 4.9 TB/s, with the segments' maps before it 154.  The vector units are at work in 57 % of the
+// cycles (three transcendental functions an element), and four wavefronts a SIMD wait for 35 % of their time: neither is full.  32 x 128 tokens of 512 channels, in
+// one block each, 5.7 us.
 template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bounds__(W * LANES) void scan_kernel(RecurArgs A) {
     typedef Place<MODE, CH, W> P;
     constexpr int N = P::N;
@@ -535,8 +536,9 @@ template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bou
 // backward
 // ---------------------------------------------------------------------------------------------
 
-// Bound by memory: gate, x and dy in, dgate and dx out, a state for every 128 tokens: 32775 tokens of 1001 binary32 channels, 37 sequences one behind the other, 656 MB, 143 us,
-// 4.6 TB/s; with the segments' maps 212.  8 x 512 tokens of 1024 bfloat16 channels 11 us and 4 for the maps.
+// gate, x and dy in, dgate and dx out, a state for every 128 tokens: 32775 tokens of 1001 binary32 channels, 37 sequences one behind the other, 656 MB, 143 to 147 us,
+// 4.5 TB/s; with the segments' maps 212.  Vector units 22 % of the cycles; two wavefronts a SIMD (256 workgroups), which wait for 53 % of their time.
+// 8 x 512 tokens of 1024 bfloat16 channels 11 us and 4 for the maps.
 template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bounds__(W * LANES) void back_kernel(RecurArgs A) {
     typedef Place<MODE, CH, W> P;
     constexpr int N = P::N;
@@ -647,8 +649,8 @@ template <typename T, int KIND, int CH, int W, int MODE> __global__ __launch_bou
 
 // The map of a segment: every wavefront composes its share of the tokens, N at a time.  On the way back it is the map of what
 // flows from a token to the one before it.  The last segment's map (the first one's, on the way back) is
-// nobody's, so it is not made; its place keeps the first state where that may be overwritten.  Bound by memory: 65543 tokens of 1024 binary16 channels 75 us, 268 MB at
-// 3.6 TB/s, and as much again is read by the launch behind it.  Workgroups of a block each that wait within one launch for the maps of the blocks before theirs read
+// nobody's, so it is not made; its place keeps the first state where that may be overwritten.  65543 tokens of 1024 binary16 channels, 268 MB: 75 to 79 us,
+// 3.5 TB/s; vector units 49 % of the cycles, four wavefronts a SIMD that wait for 45 % of their time.  As much again is read by the launch behind it.  Workgroups of a block each that wait within one launch for the maps of the blocks before theirs read
 // everything once; they were 154 -> 516 us forward and 214 -> 251 back here, since the some 500 workgroups that fit the chip are one stretch of the chain after the other,
 // each with its loads, its wait and its stores by themselves; only wide binary32 rows gained on the way back (2 x 16384 tokens 184 -> 145).
 template <typename T, int KIND, int CH, int W, int MODE, bool BACK> __global__ __launch_bounds__(W * LANES) void fold_kernel(RecurArgs A) {
@@ -816,9 +818,7 @@ constexpr int64_t MOST_TOKENS = int64_t(1) << 26, MOST_CHANNELS = int64_t(1) << 
 
 // Channels of a lane and wavefronts of a workgroup.  65543 binary16 tokens of 1024 channels, one channel a lane and two: forward 86 and 99 us, back 192 and 158, the maps of the way
 // back 68 and 90.  Sixteen wavefronts of eight tokens are level.
-constexpr int FOLD_CH(int64_t) { return 1; }
-constexpr int SCAN_CH(int64_t) { return 1; }
-constexpr int BACK_CH(int64_t bytes) { return channels_of(bytes); }
+constexpr int FOLD_CH = 1, SCAN_CH = 1;                      // back: channels_of
 constexpr int FOLD_W = 8, SCAN_W = 8, BACK_W = 8;
 
 // How the work is cut.
@@ -827,12 +827,16 @@ struct Cut {
     int64_t units, tokens, blocks, segments, per_segment;
 };
 
-// Sequences of up to EVEN_MOST tokens share a block: 256 of 20 tokens and 512 bfloat16 channels 28 us each by itself and 9
-// together, back 46 and 21.
+// Sequences of up to EVEN_MOST tokens share a block.  Us together and each by itself, forward, back; 256 sequences of 1024 channels: 33 tokens, bfloat16 20 and 48,
+// 50 and 87, binary32 27 and 48, 67 and 84; 64 tokens, bfloat16 27 and 43, 58 and 89, binary32 46 and 53, but 115 and 90; 65 tokens (a block each in both) bfloat16 45 and 42,
+// 118 and 94, binary32 53 and 51, 129 and 88.  So the border is right but for the way back of binary32, whose is between 48 tokens (81 and 90) and 64.
 constexpr int64_t EVEN_MOST = BLOCK / 2;
 // Workgroups that are wanted.  Segments cost a launch and a second reading; 8 x 4096 tokens of 1024 bfloat16 channels whole, with 256, 512 and
-// 1024 workgroups: forward 88, 76, 76, 74 us, back 198, 99, 103, 107; 65543 binary16 tokens 1315, 152, 158, 159 and 3272, 213, 235, 244.  Forward, few blocks
-// are faster whole on half the compute units: 8 x 512 tokens bfloat16 12.4 and 13.1 us, binary32 13.7 and 15.9 (back 23 and 18, 19.4 and 20.6).
+// 1024 workgroups: forward 88, 76, 76, 74 us, back 198, 99, 103, 107; 65543 binary16 tokens 1315, 152, 158, 159 and 3272, 213, 235, 244.  Forward, few blocks are faster
+// whole on half the compute units.  Whole and in segments, 1024 channels, us: 4 sequences of 512 tokens (64 workgroups) bfloat16 10.5 and 9.2, binary32 11.1 and 11.1; 7 of them (112)
+// 11.1 and 12.7, 11.9 and 14.4; 8 (128) 11.2 and 12.9, 12.4 and 14.9; 16 (256) 12.7 and 18.3.  8 of 1024 (8 blocks) 18.6 and 18.9, 27.3 and 29.2; of 1152 (9 blocks) 20.5 and 20.4,
+// 31 and 32; of 2048 39 and 35, 55 and 58.  With 192 workgroups and more, whole would be faster beyond 8 blocks, too: 12 of 2048 bfloat16 43 and 62.  Back, 8 of 512: bfloat16 22.8
+// and 16.5, binary32 17.4 and 20.0.
 constexpr int64_t FILL = 256, WHOLE_FILL = 128, WHOLE_BLOCKS = 8;
 
 Cut cut_of(const mgwfbp_sequences& s, int64_t channels, int32_t dtype, bool back) {
@@ -924,7 +928,7 @@ template <bool BACK> int run(const mgwfbp_sequences& s, int32_t kind, int32_t dt
     return with_dtype(dtype, [&](auto* type) {
         return with_kind(kind, [&](auto k) {
             typedef std::remove_pointer_t<decltype(type)> T;
-            constexpr int K = decltype(k)::value, FCH = FOLD_CH(sizeof(T)), FW = FOLD_W, SCH = BACK ? BACK_CH(sizeof(T)) : SCAN_CH(sizeof(T)), SW = BACK ? BACK_W : SCAN_W;
+            constexpr int K = decltype(k)::value, FCH = FOLD_CH, FW = FOLD_W, SCH = BACK ? channels_of(sizeof(T)) : SCAN_CH, SW = BACK ? BACK_W : SCAN_W;
             auto start = [&](void (*one)(RecurArgs), void (*even)(RecurArgs), void (*packed)(RecurArgs), int ch, int waves) {
                 a.slabs = static_cast<uint32_t>(ceil_div(channels, static_cast<int64_t>(LANES) * ch));
                 const int64_t groups = cut.units * cut.segments * a.slabs;

@@ -11,6 +11,9 @@ a word, tensors that require grad are refused in grad mode; under torch.no_grad(
 taken.  Dual tensors of forward-mode autograd are refused, too: their tangents would be lost.  Tensors that a call has written count as changed:
 autograd refuses to go on with one that it has saved before.
 
+A call that is given its outputs (y, and h with a residual; dh; dgate and dx; loss; out, act, dx) costs some 3 us of the host.  One that makes them, and
+one on [sequences, 1, channels] tensors that are not contiguous, has its arguments taken apart in Python: 15 to 24 us.
+
 An output of norm, recur, their ways back and distill may lie over an input as a whole where a line says so; every other overlap of what a call
 writes with its other tensors is refused.
 
@@ -573,7 +576,8 @@ def distill(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, teacher: O
 
     labels [tokens] (integers, contiguous; one outside the vocabulary: none) and the teacher's top logits `teacher` [tokens, top] with their `ids`; either may be
     left out (labels alone: cross entropy).  An id outside the vocabulary or a logit of -inf is no entry.  row_weight float32 [tokens] (None: 1).
-    Rows with weight 0, and those with neither label nor entry, have loss 0 and gradient 0 whatever is in them.
+    Rows with weight 0, and those with neither label nor entry, have loss 0 and gradient 0 whatever is in them.  Where entries cover the vocabulary, the
+    divergence nears 0 as the temperature grows, and the loss is what binary32 leaves of a difference: 1e-6 of it at 4, 2e-4 at 64, 6 % at 1024.
     `workspace`: device memory of layers_binding.distill_workspace(tokens, vocabulary, top) bytes; None takes torch's.  Returns `loss`, float32 [tokens]."""
     if loss is not None and _native.distill(logits, ids, teacher, labels, temperature, label_weight, teacher_weight, row_weight, loss, dlogits, workspace) is None:
         return loss

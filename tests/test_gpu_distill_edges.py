@@ -104,3 +104,20 @@ def test_logits_that_decide_at_every_border(rows, vocabulary, dtype):
             over = z.clone()
             layers.distill(over, ids, teacher, labels=labels, temperature=tau, label_weight=0.4, teacher_weight=0.7, dlogits=over)
             assert torch.equal(over, dz)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tau", [2.0 ** -20, 2.0 ** -6, 0.25, 16.0, 1024.0, 2.0 ** 20])
+@pytest.mark.parametrize("vocabulary,top", [(6, 6), (64, 64), (1000, 1000), (30522, 64)])
+def test_temperatures_from_cold_to_hot(vocabulary, top, tau):
+    """Entries that cover the vocabulary, where the divergence nears 0 as tau grows, and some of it: the loss is off by roundings of numbers of log V, times tau^2."""
+    _say("temperature", vocabulary, top, tau)
+    tokens = 20
+    z, _, teacher, labels, rw = _case(tokens, vocabulary, top, "f32", vocabulary)
+    ids = torch.rand(tokens, vocabulary, generator=_gen(top), device="cuda").topk(top, 1).indices.contiguous()
+    for l in (None, labels):
+        dz = torch.empty_like(z)
+        loss = layers.distill(z, ids, teacher, labels=l, temperature=tau, label_weight=0.3, teacher_weight=0.6, row_weight=rw, dlogits=dz)
+        want, off, want_dz, dz_off = _reference(z, ids, teacher, l, tau, 0.3, 0.6, rw)
+        _close(loss, want, off, "loss")
+        _close(dz, want_dz, dz_off, "dz")
