@@ -16,8 +16,9 @@ struct Span {
     int64_t bytes() const { return rows > 1 ? (rows - 1) * stride + width : width; }
 };
 inline Span vector_span(const void* p, int64_t n, int64_t elem_bytes) { return {p, 1, n * elem_bytes, 0}; }
+// In elements; of a matrix that is left out the stride may be any number.
 inline Span matrix_span(const void* p, int64_t rows, int64_t width, int64_t stride, int64_t elem_bytes) {
-    return {p, rows, width * elem_bytes, rows > 1 ? stride * elem_bytes : 0};
+    return {p, rows, width * elem_bytes, p != nullptr && width > 0 && rows > 1 ? stride * elem_bytes : 0};
 }
 
 // Whether a byte is in a row of both.  Matrices whose rows are at one distance may lie beside each other in the same rows (parts of one product);

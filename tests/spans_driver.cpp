@@ -53,6 +53,9 @@ int main() {
     // far apart and far wide: nothing overflows
     const Span low{reinterpret_cast<const void*>(uintptr_t(1) << 12), int64_t(1) << 20, 4, int64_t(1) << 41}, high{reinterpret_cast<const void*>((uintptr_t(1) << 12) + 4), int64_t(1) << 20, 4, int64_t(1) << 41};
     if (ops::share(low, high) || !ops::share(low, low)) return std::puts("wide"), 1;
+    // what is left out may come with any stride
+    const Span out = ops::matrix_span(nullptr, 5, 4, INT64_MAX, 4), no_width = ops::matrix_span(memory, 5, 0, INT64_MAX, 8), one = ops::matrix_span(memory, 1, 4, INT64_MAX, 4);
+    if (ops::share(out, whole) || ops::share(no_width, whole) || !ops::share(one, whole) || one.bytes() != 16) return std::puts("left out"), 1;
     if (shared < 1000 || apart < 1000) return std::puts("too few of one kind"), 1;
     std::puts("ok");
 }
